@@ -68,7 +68,12 @@ def listed():
 
 
 def _log(rng, lo, hi):
-    return max(lo, min(hi, int(math.exp(rng.uniform(math.log(lo), math.log(hi + 1))))))
+    """A size spread over its logarithm; large ones are odd or an odd multiple of 64, half of each."""
+    n = max(lo, min(hi, int(math.exp(rng.uniform(math.log(lo), math.log(hi + 1))))))
+    if n < 256:
+        return n
+    n = n | 1 if rng.random() < 0.5 else (n // 64 | 1) * 64
+    return n if n <= hi else n - 64
 
 
 def draw(rng):
