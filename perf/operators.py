@@ -98,9 +98,8 @@ def draw(rng):
             c["B"] = _log(rng, 1, 2048)
         else:
             c["T"] = _log(rng, 1, 65536)
-            c["B"] = _log(rng, 1, max(1, min(8192, (1 << 26) // (c["T"] * c["D"]))))
-            if c["B"] * c["T"] * c["D"] > 1 << 26:
-                c["D"] = max(1, (1 << 26) // c["T"])
+            c["D"] = min(c["D"], max(1, (1 << 25) // c["T"]))
+            c["B"] = _log(rng, 1, max(1, min(8192, (1 << 25) // (c["T"] * c["D"]))))
             c["ragged"], c["packed"] = rng.random() < 0.4, rng.random() < 0.5
     return c
 
