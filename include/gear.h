@@ -563,6 +563,180 @@ int gear_table_column(const gear_table *t, int32_t c, void **base, void **host_p
  * [capacity].  Reading it is safe after the stream work that wrote it. */
 int gear_table_priorities(const gear_table *t, uint32_t **d_priority);
 
+/*
+ * The learner's operators on collected windows: the gated linear recurrence
+ * of a sequence model, the advantages of its rewards, and the clipped policy
+ * loss.  They need no table, run on the current HIP device, keep nothing
+ * between calls and allocate nothing: what they need beside their inputs and
+ * outputs is the caller's workspace.  Captures of them replay correctly.
+ * Every pointer but a descriptor is device memory; inputs are not written.
+ * No content of an input (flags, lengths, actions) makes a kernel read or
+ * write outside buffers of the stated sizes.
+ */
+
+/* Gate forms of the recurrence. */
+#define GEAR_GATE_VALUE    0  /* h_t = gate_t h_{t-1} + x_t */
+#define GEAR_GATE_SIGMOID  1  /* f_t = 1/(1 + exp(-gate_t)), h_t = f_t h_{t-1} + (1 - f_t) x_t */
+
+#define GEAR_RECURRENCE_STEPS 16  /* steps between the states that a forward call saves */
+
+/* Sizes and layouts of a recurrence over B windows of T steps of D channels.
+ * Strides are in elements; channels lie next to each other. */
+typedef struct gear_recurrence_desc {
+    int32_t dtype;             /* of gate, x, y, dy, dgate, dx: GEAR_DTYPE_F16, _BF16 or _F32 */
+    int32_t form;              /* GEAR_GATE_* */
+    int64_t B, T, D;           /* each 0 or more */
+    int64_t gate_b, gate_t;    /* strides of gate from window to window and from step to step */
+    int64_t x_b, x_t;
+    int64_t dy_b, dy_t;        /* read by the backward call only */
+    const uint8_t *d_reset;    /* device uint8[B][T] or NULL: where not 0, h_{t-1} counts as 0 at step t */
+    int64_t reset_b;           /* its stride from window to window */
+    const int32_t *d_lengths;  /* device int32[B] or NULL: steps of each window, clamped to [0, T] */
+} gear_recurrence_desc;
+
+/*
+ * gear_recurrence_sizes - bytes of d_saved and of d_work that gear_recurrence
+ * and gear_recurrence_backward of this descriptor need.  Either pointer may
+ * be NULL.  Host only; reads no device memory.
+ */
+int gear_recurrence_sizes(const gear_recurrence_desc *d, int64_t *saved_bytes, int64_t *work_bytes);
+
+/*
+ * gear_recurrence - the recurrence over whole windows, or over one step
+ * (T = 1) as an actor calls it.  States are held in 32 bits throughout and
+ * rounded once into y.
+ *
+ *   d_gate, d_x  inputs as the descriptor lays them out, of any alignment
+ *   d_state      float[B][D]: the states before the first step; NULL for zeros
+ *   d_y          [B][T][D], contiguous: the states after every step; 0 past a
+ *                window's length.  NULL: not written
+ *   d_final      float[B][D]: the state after the last step (after a window of
+ *                length 0: its first state).  NULL: not written.  It may be
+ *                d_state itself when T is 0 or 1; otherwise they must not meet
+ *   d_saved      what gear_recurrence_backward needs of this call, or NULL
+ *   d_work       workspace; its contents do not matter.  May be NULL when
+ *                gear_recurrence_sizes states 0
+ *
+ * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
+ */
+int gear_recurrence(const gear_recurrence_desc *d, const void *d_gate, const void *d_x, const float *d_state,
+                    void *d_y, float *d_final, float *d_saved, void *d_work, int64_t work_bytes, void *stream);
+
+/*
+ * gear_recurrence_backward - gradients of a gear_recurrence call with the
+ * same descriptor, gate, x and state, for the gradients d_dy of its y and
+ * d_dfinal of its final state.
+ *
+ *   d_saved   as that call wrote it
+ *   d_dy      as the descriptor lays it out; NULL for zeros
+ *   d_dfinal  float[B][D]; NULL for zeros
+ *   d_dgate, d_dx  [B][T][D], contiguous; 0 past a window's length
+ *   d_dstate  float[B][D] or NULL: not written
+ *
+ * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
+ */
+int gear_recurrence_backward(const gear_recurrence_desc *d, const void *d_gate, const void *d_x,
+                             const float *d_state, const float *d_saved, const void *d_dy, const float *d_dfinal,
+                             void *d_dgate, void *d_dx, float *d_dstate, void *d_work, int64_t work_bytes,
+                             void *stream);
+
+/* Sizes, layouts and constants of gear_advantages: B windows of L steps. */
+typedef struct gear_advantages_desc {
+    int32_t reward_dtype, value_dtype;  /* GEAR_DTYPE_F16, _BF16 or _F32 */
+    int64_t B, L;                       /* 0 or more */
+    int64_t reward_b, value_b, done_b;  /* strides from window to window, in elements; steps lie next to each other */
+    const uint8_t *d_done;              /* uint8[B][L] or NULL: not 0 where the episode ended with step t */
+    const int32_t *d_lengths;           /* int32[B] or NULL: steps of each window, clamped to [0, L] */
+    float gamma, lambda;
+} gear_advantages_desc;
+
+/* gear_advantages_sizes - bytes of d_work that gear_advantages needs.  Host only. */
+int gear_advantages_sizes(const gear_advantages_desc *d, int64_t *work_bytes);
+
+/*
+ * gear_advantages - generalised advantage estimates of windows and the
+ * returns they imply, from the last step back:
+ *
+ *   delta_t = r_t + gamma V_{t+1} - V_t,  A_t = delta_t + gamma lambda A_{t+1},  R_t = A_t + V_t
+ *
+ * where V_{t+1} and A_{t+1} count as 0 after a step that ended its episode
+ * (and A after a window's last step).
+ *
+ *   d_reward  [B][L]
+ *   d_value   [B][L + 1]: the critic's value before every step and after the last;
+ *             a window of length n ends with value n
+ *   d_adv, d_ret  float[B][L], contiguous; 0 past a window's length.  d_ret may be NULL
+ *
+ * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
+ */
+int gear_advantages(const gear_advantages_desc *d, const void *d_reward, const void *d_value, float *d_adv,
+                    float *d_ret, void *d_work, int64_t work_bytes, void *stream);
+
+/* Sizes, layouts and constants of the policy calls: n rows of V logits. */
+typedef struct gear_policy_desc {
+    int32_t dtype;         /* of logits and grad: GEAR_DTYPE_F16, _BF16 or _F32 */
+    int32_t action_dtype;  /* GEAR_DTYPE_U8, _I32 or _I64 */
+    int64_t n, V;          /* n 0 or more, V 1 or more, below 2^31 */
+    int64_t row_stride;    /* of logits from row to row, in elements */
+    const void *d_action;  /* [n]: the action taken; a row whose action is outside [0, V) takes no part */
+    const uint8_t *d_mask; /* [ceil(n / mask_group)] or NULL: rows with 0 take no part, nor is any logit of theirs used */
+    int64_t mask_group;    /* consecutive rows that share a mask value, 1 or more; likewise below */
+    int64_t adv_group, weight_group;
+    float clip_low, clip_high;  /* the ratio is clipped to [1 - clip_low, 1 + clip_high]; each 0 or more */
+    float kl, entropy;     /* coefficients of the KL and entropy terms */
+    float denom;           /* what the sum over rows is divided by; 0 for the number of rows that take part */
+    float grad_scale;      /* the gradient is that of grad_scale * loss (a loss scale) */
+} gear_policy_desc;
+
+/* gear_policy_sizes - bytes of d_work that gear_policy_loss needs.  Host only. */
+int gear_policy_sizes(const gear_policy_desc *d, int64_t *work_bytes);
+
+/*
+ * gear_policy_loss - the clipped policy loss of rows of logits z, with a KL
+ * term towards a reference policy and an entropy term, and its gradient.
+ * With log p = z - log sum exp z, lp = log p[action], H = -sum p log p, ratio
+ * r = exp(lp - old), advantage A and window weight w, a row's loss is
+ *
+ *   w (-min(r A, clip(r) A) + kl (exp(ref - lp) - (ref - lp) - 1) - entropy H)
+ *
+ * and the loss is their sum over the rows that take part, over denom.
+ *
+ *   d_old_logp   float[n]: log-probabilities under the policy that acted
+ *   d_ref_logp   float[n]: ... under the reference policy.  NULL: no KL term
+ *   d_adv        float[ceil(n / adv_group)]
+ *   d_weight     float[ceil(n / weight_group)] (importance-sampling weights of
+ *                gear_select, say) or NULL for ones
+ *   d_grad_loss  one float that multiplies the gradient, read on the device, or NULL for 1
+ *   d_loss       one float
+ *   d_stats      float[4] or NULL: sums over the rows that take part, over
+ *                denom, of the unweighted clipped term, KL term, H, and of the rows
+ *                whose policy gradient the clip took away
+ *   d_logp, d_entropy  float[n] or NULL: lp and H; 0 for rows that take no part
+ *   d_grad       [n][V], contiguous, or NULL: the gradient for the logits; 0 for rows that
+ *                take no part.  It may be the logits' own memory when row_stride is V
+ *   d_work       workspace of gear_policy_sizes bytes; its contents do not matter
+ *
+ * Logits of -inf, or of the type's lowest value, have probability 0 beside
+ * larger ones.  A row whose logits are all -inf has no distribution: it
+ * counts among the rows, with lp = -inf, and adds nothing to loss, stats or
+ * gradient.  Sums over rows have an order that depends on n and V alone, so
+ * results repeat bit for bit.
+ * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
+ */
+int gear_policy_loss(const gear_policy_desc *d, const void *d_logits, const float *d_old_logp,
+                     const float *d_ref_logp, const float *d_adv, const float *d_weight, const float *d_grad_loss,
+                     float *d_loss, float *d_stats, float *d_logp, float *d_entropy, void *d_grad, void *d_work,
+                     int64_t work_bytes, void *stream);
+
+/*
+ * gear_action_logp - lp and H of gear_policy_loss alone: the old and the
+ * reference policy's log-probabilities of the actions taken.  Reads the
+ * descriptor's dtype, sizes, actions and mask.  Either output may be NULL.
+ * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
+ */
+int gear_action_logp(const gear_policy_desc *d, const void *d_logits, float *d_logp, float *d_entropy,
+                     void *stream);
+
 /* gear_last_error - message describing the last failed call on this
  * thread ("" if none).  Valid until the next call on the same thread. */
 const char *gear_last_error(void);

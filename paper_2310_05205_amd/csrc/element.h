@@ -1,0 +1,65 @@
+// Elements of the learner's tensors on the device: fp16, bf16 and fp32 values
+// in short vectors, loaded and stored whatever their alignment, computed in
+// 32 bits and rounded to nearest even once, when they are stored.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gear.h"
+
+namespace gear {
+
+template <typename E, int N>
+struct Vec {
+    typedef E raw __attribute__((ext_vector_type(N)));
+    typedef float wide __attribute__((ext_vector_type(N)));
+    static_assert(sizeof(raw) == sizeof(E) * N, "no padding");
+
+    // N elements at p, which need no alignment beyond the element's own.
+    static __device__ __forceinline__ raw load(const E* p) {
+        raw v;
+        __builtin_memcpy(&v, p, sizeof(v));
+        return v;
+    }
+    static __device__ __forceinline__ void unpack(raw v, float (&f)[N]) {
+        const wide w = __builtin_convertvector(v, wide);
+#pragma unroll
+        for (int j = 0; j < N; j++) f[j] = w[j];
+    }
+    static __device__ __forceinline__ void store(E* p, const float (&f)[N]) {
+        wide w;
+#pragma unroll
+        for (int j = 0; j < N; j++) w[j] = f[j];
+        const raw v = __builtin_convertvector(w, raw);
+        __builtin_memcpy(p, &v, sizeof(v));
+    }
+};
+template <typename E>
+struct Vec<E, 1> {
+    typedef E raw;
+    static __device__ __forceinline__ raw load(const E* p) { return *p; }
+    static __device__ __forceinline__ void unpack(raw v, float (&f)[1]) { f[0] = (float)v; }
+    static __device__ __forceinline__ void store(E* p, const float (&f)[1]) { *p = (E)f[0]; }
+};
+
+// Element i of an array whose type is known at run time.
+__device__ __forceinline__ float load_float(const void* p, int32_t dtype, int64_t i) {
+    if (dtype == GEAR_DTYPE_F32) return static_cast<const float*>(p)[i];
+    if (dtype == GEAR_DTYPE_BF16) return (float)static_cast<const __bf16*>(p)[i];
+    return (float)static_cast<const _Float16*>(p)[i];
+}
+
+// Natural exp and log by the hardware's base-2 instructions.  exp's relative
+// error grows as |x| 2^-24 (the product's rounding), log's absolute error is
+// that of its result's last bit.
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+__device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ __forceinline__ float fast_log(float x) { return __builtin_amdgcn_logf(x) * kLn2; }
+
+// Whether the library's float operators take tensors of this type, and its size.
+inline int float_bytes(int32_t dtype) {
+    return dtype == GEAR_DTYPE_F32 ? 4 : dtype == GEAR_DTYPE_F16 || dtype == GEAR_DTYPE_BF16 ? 2 : 0;
+}
+
+}  // namespace gear

@@ -8,7 +8,9 @@ the HIP library; a failing call raises ``GearError``.  ``Table`` is a
 convenience wrapper that takes torch tensors and uses torch only to allocate
 device memory and to name the current stream.  Its calls of every step go
 through the native module ``_binding`` (built beside libgear.so), which
-allocates the outputs and makes the C call in one go.
+allocates the outputs and makes the C call in one go; so do the learner's
+operators on collected windows (``recurrence``, ``advantages``,
+``policy_loss``, ``action_logp``), which take and return torch tensors.
 """
 import ctypes
 import os
@@ -46,6 +48,8 @@ GEAR_OPT_GATHER_SHARE_CU = 4
 GEAR_DTYPE_U8, GEAR_DTYPE_I8, GEAR_DTYPE_U16, GEAR_DTYPE_I16, GEAR_DTYPE_F16, GEAR_DTYPE_BF16 = 0, 1, 2, 3, 4, 5
 GEAR_DTYPE_U32, GEAR_DTYPE_I32, GEAR_DTYPE_F32, GEAR_DTYPE_U64, GEAR_DTYPE_I64, GEAR_DTYPE_F64 = 6, 7, 8, 9, 10, 11
 GEAR_MAX_NAME = 63
+GEAR_GATE_VALUE, GEAR_GATE_SIGMOID = 0, 1
+GEAR_RECURRENCE_STEPS = 16
 # torch dtype name of each GEAR_DTYPE_* (the library only moves bytes).
 DTYPE_NAMES = {GEAR_DTYPE_U8: "uint8", GEAR_DTYPE_I8: "int8", GEAR_DTYPE_U16: "uint16", GEAR_DTYPE_I16: "int16",
                GEAR_DTYPE_F16: "float16", GEAR_DTYPE_BF16: "bfloat16", GEAR_DTYPE_U32: "uint32",
@@ -59,6 +63,30 @@ DTYPE_BYTES = {GEAR_DTYPE_U8: 1, GEAR_DTYPE_I8: 1, GEAR_DTYPE_U16: 2, GEAR_DTYPE
 class gear_column(ctypes.Structure):
     """Mirror of the C descriptor gear_column."""
     _fields_ = [("name", ctypes.c_char_p), ("dtype", ctypes.c_int32), ("elems_per_step", ctypes.c_int32)]
+
+
+class gear_recurrence_desc(ctypes.Structure):
+    """Mirror of the C descriptor gear_recurrence_desc."""
+    _fields_ = ([("dtype", ctypes.c_int32), ("form", ctypes.c_int32)]
+                + [(n, ctypes.c_int64) for n in ("B", "T", "D", "gate_b", "gate_t", "x_b", "x_t", "dy_b", "dy_t")]
+                + [("d_reset", ctypes.c_void_p), ("reset_b", ctypes.c_int64), ("d_lengths", ctypes.c_void_p)])
+
+
+class gear_advantages_desc(ctypes.Structure):
+    """Mirror of the C descriptor gear_advantages_desc."""
+    _fields_ = ([("reward_dtype", ctypes.c_int32), ("value_dtype", ctypes.c_int32)]
+                + [(n, ctypes.c_int64) for n in ("B", "L", "reward_b", "value_b", "done_b")]
+                + [("d_done", ctypes.c_void_p), ("d_lengths", ctypes.c_void_p), ("gamma", ctypes.c_float),
+                   ("lambda", ctypes.c_float)])
+
+
+class gear_policy_desc(ctypes.Structure):
+    """Mirror of the C descriptor gear_policy_desc."""
+    _fields_ = ([("dtype", ctypes.c_int32), ("action_dtype", ctypes.c_int32)]
+                + [(n, ctypes.c_int64) for n in ("n", "V", "row_stride")]
+                + [("d_action", ctypes.c_void_p), ("d_mask", ctypes.c_void_p)]
+                + [(n, ctypes.c_int64) for n in ("mask_group", "adv_group", "weight_group")]
+                + [(n, ctypes.c_float) for n in ("clip_low", "clip_high", "kl", "entropy", "denom", "grad_scale")])
 
 
 class GearError(RuntimeError):
@@ -84,7 +112,9 @@ def native():
         L = lib()
         _binding.bind(*[ctypes.cast(f, ctypes.c_void_p).value for f in
                         (L.gear_select, L.gear_collect, L.gear_select_collect, L.gear_update_priorities,
-                         L.gear_select_shard, L.gear_is_weights, L.gear_topk_merge)])
+                         L.gear_select_shard, L.gear_is_weights, L.gear_topk_merge, L.gear_recurrence_sizes,
+                         L.gear_recurrence, L.gear_recurrence_backward, L.gear_advantages_sizes, L.gear_advantages,
+                         L.gear_policy_sizes, L.gear_policy_loss, L.gear_action_logp)])
         _native = _binding
     return _native
 
@@ -133,6 +163,15 @@ def lib():
         L.gear_table_column_info.argtypes = [vp, i32, ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(i32),
                                              ctypes.POINTER(i32)]
         L.gear_table_find_column.argtypes = [vp, ctypes.c_char_p, ctypes.POINTER(i32)]
+        rec, adv, pol = (ctypes.POINTER(t) for t in (gear_recurrence_desc, gear_advantages_desc, gear_policy_desc))
+        L.gear_recurrence_sizes.argtypes = [rec, pi64, pi64]
+        L.gear_recurrence.argtypes = [rec, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.gear_recurrence_backward.argtypes = [rec, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.gear_advantages_sizes.argtypes = [adv, pi64]
+        L.gear_advantages.argtypes = [adv, vp, vp, vp, vp, vp, i64, vp]
+        L.gear_policy_sizes.argtypes = [pol, pi64]
+        L.gear_policy_loss.argtypes = [pol, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.gear_action_logp.argtypes = [pol, vp, vp, vp, vp]
         for name in ["gear_table_create", "gear_table_destroy", "gear_insert", "gear_select", "gear_collect",
                      "gear_select_collect",
                      "gear_update_priorities", "gear_table_sync", "gear_table_info", "gear_table_column",
@@ -140,7 +179,9 @@ def lib():
                      "gear_allocate", "gear_commit", "gear_allocator_info", "gear_write_rows", "gear_shard_total",
                      "gear_select_shard", "gear_is_weights", "gear_topk_merge",
                      "gear_select_prioritized_noalloc", "gear_table_create_columns", "gear_table_column_info",
-                     "gear_table_find_column"]:
+                     "gear_table_find_column", "gear_recurrence_sizes", "gear_recurrence",
+                     "gear_recurrence_backward", "gear_advantages_sizes", "gear_advantages", "gear_policy_sizes",
+                     "gear_policy_loss", "gear_action_logp"]:
             getattr(L, name).restype = ctypes.c_int
         L.gear_last_error.argtypes = []
         L.gear_last_error.restype = ctypes.c_char_p
@@ -327,6 +368,76 @@ def topk_merge(prio, gidx, K, T, L, seed, device=0):
     import torch
     return _result(native().topk_merge(prio.contiguous(), gidx.contiguous(), int(gidx.shape[0]), K, int(T), int(L),
                                        int(seed), device, torch._C._cuda_getCurrentRawStream(device)))
+
+
+def _on_stream(call, x, stream, *args):
+    """call(*args, stream handle) on `stream` or the current stream of x's
+    device; outputs and workspace are allocated for that stream."""
+    import torch
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise ValueError("tensors must be torch tensors on the GPU")
+    if stream is None:
+        return _result(call(*args, torch._C._cuda_getCurrentRawStream(x.device.index)))
+    with torch.cuda.stream(stream):
+        return _result(call(*args, stream.cuda_stream))
+
+
+def recurrence(gate, x, state=None, *, form=GEAR_GATE_VALUE, reset=None, lengths=None, save=False, stream=None):
+    """The gated linear recurrence over windows (gear_recurrence).
+
+    gate, x [B, T, D] of one dtype (float32, bfloat16 or float16), any strides
+    with the channels next to each other (two halves of one projection, say);
+    state float32 [B, D] or None for zeros; reset uint8 or bool [B, T]: the
+    state counts as 0 before those steps; lengths int32 [B].  Returns (y,
+    final state float32 [B, D], saved), saved being what recurrence_backward
+    needs when `save` is set, else None.  No gradient is recorded: see
+    ``learn.recurrence`` for that.
+    """
+    return _on_stream(native().recurrence, x, stream, gate, x, state, form, reset, lengths, save)
+
+
+def recurrence_backward(gate, x, saved, dy, dfinal=None, state=None, *, form=GEAR_GATE_VALUE, reset=None,
+                        lengths=None, stream=None):
+    """Gradients (dgate, dx, dstate) of recurrence(gate, x, state, ..., save=True)
+    for the gradients dy of its y and dfinal of its final state (None: zeros)."""
+    return _on_stream(native().recurrence_backward, x, stream, gate, x, state, form, reset, lengths, saved, dy, dfinal)
+
+
+def recurrence_step(gate, x, state, *, form=GEAR_GATE_VALUE, reset=None, out=None, stream=None):
+    """One step of the recurrence, as an actor takes it: gate, x [B, D], state
+    float32 [B, D] (None: zeros), reset [B].  Returns (y, state after the
+    step); `out` may be a float32 tensor for the latter, `state` itself included."""
+    return _on_stream(native().recurrence_step, x, stream, gate, x, state, form, reset, out)
+
+
+def advantages(reward, value, gamma, lam, *, done=None, lengths=None, stream=None):
+    """Generalised advantage estimates and returns of windows (gear_advantages):
+    reward [B, L], value [B, L + 1] (float32, bfloat16 or float16), done uint8
+    or bool [B, L], lengths int32 [B].  Returns float32 (adv, ret), [B, L]."""
+    return _on_stream(native().advantages, reward, stream, reward, value, gamma, lam, done, lengths)
+
+
+def policy_loss(logits, action, old_logp, adv, *, ref_logp=None, weight=None, mask=None, clip=(0.2, 0.2), kl=0.0,
+                entropy=0.0, denom=None, grad=True, grad_scale=1.0, grad_loss=None, in_place=False, stream=None):
+    """The clipped policy loss with KL and entropy terms (gear_policy_loss).
+
+    logits [..., V]; action uint8, int32 or int64, old_logp and ref_logp
+    float32, all of the leading shape; adv, weight (float32) and mask (uint8 or
+    bool) of that shape or of its first dimensions, each value then serving
+    every row below it.  Returns (loss, logp, entropy, stats, grad): float32
+    scalars and rows, stats the means of the clipped, KL and entropy terms and
+    of the rows clipped, grad the gradient of grad_scale * grad_loss * loss for
+    the logits, of their dtype, or None without `grad`.  With `in_place` it
+    takes the logits' memory.
+    """
+    return _on_stream(native().policy_loss, logits, stream, logits, action, old_logp, adv, ref_logp, weight, mask,
+                      clip[0], clip[1], kl, entropy, denom, grad, grad_scale, grad_loss, in_place)
+
+
+def action_logp(logits, action, *, mask=None, stream=None):
+    """Log-probabilities of the actions taken and entropies, float32 (gear_action_logp);
+    arguments as for policy_loss."""
+    return _on_stream(native().action_logp, logits, stream, logits, action, mask)
 
 
 class _DeviceBytes:
