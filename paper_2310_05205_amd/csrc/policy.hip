@@ -14,11 +14,39 @@
 namespace gear {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kSums = 5;              // loss, clipped term, KL term, entropy, clipped rows
-constexpr int kCountBlocks = 256;     // workgroups that count the rows that take part
-constexpr int kMaxBlocks = 4096;      // workgroups of the row kernel
+constexpr int kThreads = 256;
+constexpr int kSums = 5;               // loss, clipped term, KL term, entropy, clipped rows
+constexpr int kCountBlocks = 256;      // workgroups that count the rows that take part
+constexpr int kMaxBlocks = 2048;       // workgroups of the row kernels
+constexpr int kSoloThreads = 1024;     // calls of one workgroup
+constexpr int64_t kSoloLogits = 1 << 15;
 constexpr int64_t kCountOff = 0, kSumOff = kCountBlocks * (int64_t)sizeof(int64_t);
+// A masked logit's d, and where it stops mattering: e^d is 0 well above it,
+// and a multiple of it stays finite.
+constexpr float kFloor = -1e4f;
+
+// Quotients by a number fixed for the launch: for dividends below 2^31, the
+// high part of a product with ceil(2^(31 + l) / d), 2^l >= d, which is exact.
+struct Divisor {
+    int64_t d;
+    uint32_t mul, shift;  // mul 0: divide
+};
+Divisor divisor(int64_t d, int64_t dividends) {
+    Divisor r{d, 0, 0};
+    if (dividends >= (1ll << 31) || d > dividends) {
+        // Nothing below d: the quotient is 0, which mul 0 would compute too.
+        return r;
+    }
+    uint32_t l = 0;
+    while ((1ll << l) < d) l++;
+    r.mul = (uint32_t)(((1ull << (31 + l)) + (uint64_t)d - 1) / (uint64_t)d);
+    r.shift = 31 + l;
+    return r;
+}
+__device__ __forceinline__ int64_t quotient(int64_t x, const Divisor& d) {
+    if (d.mul) return (int64_t)(((uint64_t)(uint32_t)x * d.mul) >> d.shift);
+    return x / d.d;
+}
 
 struct Args {
     const void* logits;
@@ -28,9 +56,11 @@ struct Args {
     const float *old_logp, *ref_logp, *adv, *weight, *grad_loss;
     float *loss, *stats, *logp, *entropy;
     int64_t* counts;  // [kCountBlocks]
-    float* sums;      // [blocks][kSums]
-    int64_t n, V, row_stride, mask_group, adv_group, weight_group;
+    float* sums;      // [kSums][kMaxBlocks]
+    int64_t n, V, row_stride;
+    Divisor mask_group, adv_group, weight_group;
     int32_t action_dtype, count_blocks;
+    bool solo;        // one workgroup counts, runs all rows and adds up
     float lo, hi, kl, ent, denom, grad_scale;
 };
 
@@ -40,34 +70,46 @@ __device__ __forceinline__ int64_t action_of(const Args& a, int64_t row) {
     return static_cast<const uint8_t*>(a.action)[row];
 }
 __device__ __forceinline__ bool takes_part(const Args& a, int64_t row, int64_t action) {
-    return action >= 0 && action < a.V && (a.mask == nullptr || a.mask[row / a.mask_group] != 0);
+    return (action >= 0) & (action < a.V) && (a.mask == nullptr || a.mask[quotient(row, a.mask_group)] != 0);
 }
 
-__device__ __forceinline__ float wave_max(float v) {
+template <int G>
+__device__ __forceinline__ float group_max(float v) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
+    for (int off = G / 2; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
     return v;
 }
-template <typename T>
-__device__ __forceinline__ T wave_add(T v) {
+template <int G, typename T>
+__device__ __forceinline__ T group_add(T v) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+    for (int off = G / 2; off > 0; off >>= 1) v += __shfl_xor(v, off);
     return v;
+}
+
+// Sum of one value per lane over the workgroup, in thread 0; `s` holds a value per wave.
+template <int THREADS, typename T>
+__device__ __forceinline__ T block_add(T v, T* s) {
+    v = group_add<64>(v);
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        for (int k = 1; k < THREADS / 64; k++) v += s[k];
+    return v;
+}
+
+template <int THREADS>
+__device__ __forceinline__ int64_t count_rows(const Args& a, int64_t* s) {
+    int64_t c = 0;
+    for (int64_t r = (int64_t)blockIdx.x * THREADS + threadIdx.x; r < a.n; r += (int64_t)gridDim.x * THREADS)
+        c += takes_part(a, r, action_of(a, r)) ? 1 : 0;
+    return block_add<THREADS>(c, s);
 }
 
 // Rows that take part, per workgroup.
 __global__ __launch_bounds__(kThreads) void count_kernel(const Args a) {
-    __shared__ int64_t s[kWaves];
-    int64_t c = 0;
-    for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < a.n; r += (int64_t)gridDim.x * kThreads)
-        c += takes_part(a, r, action_of(a, r)) ? 1 : 0;
-    c = wave_add(c);
-    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = c;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int k = 1; k < kWaves; k++) c += s[k];
-        a.counts[blockIdx.x] = c;
-    }
+    __shared__ int64_t s[kThreads / 64];
+    const int64_t c = count_rows<kThreads>(a, s);
+    if (threadIdx.x == 0) a.counts[blockIdx.x] = c;
 }
 
 // What the sums are divided by, in every lane of the wave.
@@ -75,19 +117,21 @@ __device__ __forceinline__ float denominator(const Args& a) {
     if (a.denom > 0.0f) return a.denom;
     int64_t c = 0;
     for (int k = threadIdx.x & 63; k < a.count_blocks; k += 64) c += a.counts[k];
-    c = wave_add(c);
+    c = group_add<64>(c);
     return c > 0 ? (float)c : 1.0f;
 }
 
 struct Row {
-    float lp, H;   // log-probability of the action, entropy
-    float c, s;    // derivative of the loss for lp, factor of the gradient
+    float lp, H;  // log-probability of the action, entropy
+    float c, s;   // derivative of the loss for lp, factor of the gradient
     float sums[kSums];
 };
 
-// A row's terms from its largest logit, its sums and the action's logit.
+// A row's terms from its largest logit, its sums and the action's logit.  The
+// operations are spelled out, so that lp and H come out the same in every kernel.
 template <bool LOSS>
 __device__ __forceinline__ Row row_terms(const Args& a, int64_t row, float m, float S, float dS, float za, float denom) {
+#pragma clang fp contract(off)
     Row r{};
     if (m == -INFINITY) {  // no distribution
         r.lp = -INFINITY;
@@ -95,9 +139,10 @@ __device__ __forceinline__ Row row_terms(const Args& a, int64_t row, float m, fl
     }
     const float log_S = fast_log(S);
     r.lp = (za - m) - log_S;
-    r.H = log_S - dS / S;
+    r.H = log_S - dS * __builtin_amdgcn_rcpf(S);
     if (!LOSS) return r;
-    const float A = a.adv[row / a.adv_group], w = a.weight ? a.weight[row / a.weight_group] : 1.0f;
+    const float A = a.adv[quotient(row, a.adv_group)];
+    const float w = a.weight ? a.weight[quotient(row, a.weight_group)] : 1.0f;
     const float ratio = expf(r.lp - a.old_logp[row]);
     const float free = ratio * A, held = fminf(fmaxf(ratio, a.lo), a.hi) * A;
     const bool clipped = held < free;
@@ -122,16 +167,254 @@ __device__ __forceinline__ Row row_terms(const Args& a, int64_t row, float m, fl
     return r;
 }
 
-// Gradient of one logit that is not the action's: d = z - m.
-__device__ __forceinline__ float slope(const Args& a, const Row& r, float d, float inv_S, float log_S) {
-    const float p = fast_exp(d) * inv_S;
-    return r.s * p * (a.ent * (fmaxf(d, -3e38f) - log_S + r.H) - r.c);
+// dz_j = e^d_j (k1 d_j + k0), and k2 more for the action.
+struct Slope {
+    float k0, k1, k2;
+};
+__device__ __forceinline__ Slope slope_of(const Args& a, const Row& r, float S) {
+    const float f = r.s / S;
+    return Slope{f * (a.ent * (r.H - fast_log(S)) - r.c), f * a.ent, r.s * r.c};
+}
+__device__ __forceinline__ float slope(const Slope& k, float d) { return fast_exp(d) * fmaf(k.k1, fmaxf(d, kFloor), k.k0); }
+
+// The sums of a call that one workgroup ran, or this workgroup's share of them.
+template <int THREADS>
+__device__ __forceinline__ void leave_sums(const Args& a, const float (&total)[kSums], float denom, double* s) {
+#pragma unroll
+    for (int k = 0; k < kSums; k++) {
+        __syncthreads();
+        const double v = block_add<THREADS>((double)total[k], s);
+        if (threadIdx.x == 0) {
+            if (!a.solo) a.sums[k * kMaxBlocks + blockIdx.x] = (float)v;
+            else if (k == 0) *a.loss = (float)(v / (double)denom);
+            else if (a.stats) a.stats[k - 1] = (float)(v / (double)denom);
+        }
+    }
 }
 
-// A workgroup per row, which reads it three times.
+// 16 bytes of a row as four words: the vectors of 16-bit elements that the
+// language offers are taken apart into a register per element as soon as one is replaced.
+template <typename E>
+struct Piece {
+    static constexpr int VE = 16 / sizeof(E), kPerWord = 4 / sizeof(E);
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    words w;
+
+    static __device__ __forceinline__ uint32_t lowest() {  // a word of -inf
+        const E e[kPerWord] = {};
+        E f[kPerWord];
+#pragma unroll
+        for (int k = 0; k < kPerWord; k++) f[k] = e[k] - (E)INFINITY;
+        return __builtin_bit_cast(uint32_t, f);
+    }
+    __device__ __forceinline__ void load(const E* p) { __builtin_memcpy(&w, p, sizeof(w)); }
+    __device__ __forceinline__ void fill() { w = words{lowest(), lowest(), lowest(), lowest()}; }
+    // The first n elements become -inf.
+    __device__ __forceinline__ void drop(int n) {
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            if (kPerWord == 2 && n == 2 * k + 1) w[k] = (w[k] & 0xFFFF0000u) | (lowest() & 0xFFFFu);
+            if (n >= kPerWord * (k + 1)) w[k] = lowest();
+        }
+    }
+    // A row of V < VE elements, the rest -inf.
+    __device__ __forceinline__ void gather(const E* p, int V) {
+        fill();
+#pragma unroll
+        for (int j = 0; j < VE; j++)
+            if (j < V) {
+                if constexpr (sizeof(E) == 4) {
+                    w[j] = __builtin_bit_cast(uint32_t, p[j]);
+                } else {
+                    uint16_t h16;
+                    __builtin_memcpy(&h16, p + j, 2);
+                    const uint32_t h = h16;
+                    w[j / 2] = j % 2 ? (w[j / 2] & 0xFFFFu) | (h << 16) : (w[j / 2] & 0xFFFF0000u) | h;
+                }
+            }
+    }
+    __device__ __forceinline__ void unpack(float (&f)[VE]) const {
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            E e[kPerWord];
+            const uint32_t u = w[k];
+            __builtin_memcpy(e, &u, 4);
+#pragma unroll
+            for (int h = 0; h < kPerWord; h++) f[kPerWord * k + h] = (float)e[h];
+        }
+    }
+    // Keeps the compiler from holding on to what it computed from the piece:
+    // unpacked values kept from one pass to the next take several times its registers.
+    __device__ __forceinline__ void forget() { asm volatile("" : "+v"(w)); }
+};
+
+// Rows held in registers: G lanes share a row, each with NV pieces of 16 bytes
+// every G pieces, so that a row is read once and its gradient written once.
+// A lane past the end of its row reads the row's last piece and keeps of it
+// what no other lane has; with TINY, rows are shorter than a piece.
+template <typename E, int G, int NV, int THREADS, bool TINY, bool LOSS>
+__global__ __launch_bounds__(THREADS) void held_kernel(const Args a) {
+    constexpr int VE = 16 / sizeof(E), kGroups = THREADS / G, kWaves = THREADS / 64;
+    constexpr bool kBlock = G > 64;  // the whole workgroup shares a row
+    static_assert(!kBlock || G == THREADS, "one row at a time");
+    __shared__ float s_max[kWaves], s_sum[kWaves], s_dsum[kWaves], s_za;
+    __shared__ double s_add[kWaves];
+    __shared__ int64_t s_count;
+    const int lane = threadIdx.x % G, V = (int)a.V;  // at most 2^17 elements are held
+    float denom = 1.0f;
+    if (LOSS) {
+        if (a.solo && !(a.denom > 0.0f)) {
+            const int64_t c = count_rows<THREADS>(a, reinterpret_cast<int64_t*>(s_add));
+            if (threadIdx.x == 0) s_count = c;
+            __syncthreads();
+            denom = s_count > 0 ? (float)s_count : 1.0f;
+        } else {
+            denom = denominator(a);
+        }
+    }
+    float total[kSums] = {};
+    for (int64_t first = (int64_t)blockIdx.x * kGroups; first < a.n; first += (int64_t)gridDim.x * kGroups) {
+        const int64_t row = first + (kBlock ? 0 : threadIdx.x / G);
+        const bool used = row < a.n;
+        const int64_t action = used ? action_of(a, row) : -1;
+        const bool on = used && takes_part(a, row, action);
+        if (kBlock && !on) {  // the same in every lane
+            if (threadIdx.x == 0) {
+                if (a.logp) a.logp[row] = 0.0f;
+                if (a.entropy) a.entropy[row] = 0.0f;
+            }
+            if (LOSS && a.grad) {
+                E* g = static_cast<E*>(a.grad) + row * a.V;
+                const float zero[VE] = {};
+                for (int j = lane * VE; j < V; j += G * VE) {
+                    if (j + VE <= V) Vec<E, VE>::store(g + j, zero);
+                    else
+                        for (int k = j; k < V; k++) g[k] = (E)0.0f;
+                }
+            }
+            continue;
+        }
+        const E* z = static_cast<const E*>(a.logits) + row * a.row_stride;
+        Piece<E> v[NV];
+        float za = 0.0f;
+        // The lane's number, hidden so that what follows from it for each piece is not kept from row to row.
+        int mine = lane;
+        asm volatile("" : "+v"(mine));
+        if (on) {
+#pragma unroll
+            for (int i = 0; i < NV; i++) {
+                if (TINY) {
+                    v[i].gather(z, V);
+                } else if ((i + 1) * G * VE <= V) {
+                    v[i].load(z + i * G * VE + mine * VE);
+                } else if (i * G * VE < V) {
+                    const int base = (i * G + mine) * VE, over = base + VE - V;
+                    v[i].load(z + (over < 0 ? base : V - VE));
+                    if (over > 0) v[i].drop(over);
+                } else {
+                    v[i].fill();
+                }
+            }
+            if (!kBlock || threadIdx.x == 0) za = (float)z[action];
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; i++) v[i].fill();
+        }
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            float f[VE];
+            v[i].unpack(f);
+#pragma unroll
+            for (int j = 0; j < VE; j++) m = fmaxf(m, f[j]);
+            v[i].forget();
+        }
+        m = group_max<kBlock ? 64 : G>(m);
+        if (kBlock) {
+            if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = m;
+            if (threadIdx.x == 0) s_za = za;
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < kWaves; k++) m = fmaxf(m, s_max[k]);
+            za = s_za;
+        }
+        const float ref = m == -INFINITY ? 0.0f : m;  // a row of -inf sums to 0
+        float S = 0.0f, dS = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            float f[VE];
+            v[i].unpack(f);
+#pragma unroll
+            for (int j = 0; j < VE; j++) {
+                const float d = f[j] - ref, e = fast_exp(d);
+                S += e;
+                dS = fmaf(e, fmaxf(d, kFloor), dS);
+            }
+            v[i].forget();
+        }
+        S = group_add<kBlock ? 64 : G>(S);
+        dS = group_add<kBlock ? 64 : G>(dS);
+        if (kBlock) {
+            if ((threadIdx.x & 63) == 0) {
+                s_sum[threadIdx.x >> 6] = S;
+                s_dsum[threadIdx.x >> 6] = dS;
+            }
+            __syncthreads();
+            S = dS = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kWaves; k++) {
+                S += s_sum[k];
+                dS += s_dsum[k];
+            }
+        }
+        Row r{};
+        if (on) r = row_terms<LOSS>(a, row, m, S, dS, za, denom);
+        if (used && lane == 0) {
+            if (a.logp) a.logp[row] = r.lp;
+            if (a.entropy) a.entropy[row] = r.H;
+#pragma unroll
+            for (int k = 0; k < kSums; k++) total[k] += r.sums[k];
+        }
+        if (LOSS && a.grad && used) {
+            E* g = static_cast<E*>(a.grad) + row * a.V;
+            const bool some = on && m != -INFINITY;
+            const Slope k = some ? slope_of(a, r, S) : Slope{};
+            asm volatile("" : "+v"(mine));
+#pragma unroll
+            for (int i = 0; i < NV; i++) {
+                if (i * G * VE < V) {
+                    const int base = (i * G + mine) * VE;
+                    // A lane at the end of its row holds the last piece, of which it has the last elements.
+                    const bool whole = !TINY && ((i + 1) * G * VE <= V || base + VE <= V);
+                    const int at = TINY || whole ? base : V - VE;
+                    float f[VE], o[VE];
+                    v[i].unpack(f);
+                    const int hit = (int)action - at;
+#pragma unroll
+                    for (int j = 0; j < VE; j++) {
+                        o[j] = some ? slope(k, f[j] - ref) : 0.0f;
+                        if (some && j == hit) o[j] += k.k2;
+                    }
+                    if (whole) {
+                        Vec<E, VE>::store(g + base, o);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < VE; j++)
+                            if (at + j >= base && at + j < V) g[at + j] = (E)o[j];
+                    }
+                }
+            }
+        }
+    }
+    if (LOSS) leave_sums<THREADS>(a, total, denom, s_add);
+}
+
+// Rows longer than registers hold: a workgroup per row, which reads it three times.
 template <typename E, bool LOSS>
-__global__ __launch_bounds__(kThreads) void row_kernel(const Args a) {
+__global__ __launch_bounds__(kSoloThreads) void long_kernel(const Args a) {
+    constexpr int kWaves = kSoloThreads / 64;
     __shared__ float s_max[kWaves], s_sum[kWaves], s_dsum[kWaves];
+    __shared__ double s_add[kWaves];
     const int wave = threadIdx.x >> 6;
     const float denom = LOSS ? denominator(a) : 1.0f;
     float total[kSums] = {};
@@ -144,28 +427,27 @@ __global__ __launch_bounds__(kThreads) void row_kernel(const Args a) {
                 if (a.entropy) a.entropy[row] = 0.0f;
             }
             if (g)
-                for (int64_t j = threadIdx.x; j < a.V; j += kThreads) g[j] = (E)0.0f;
+                for (int64_t j = threadIdx.x; j < a.V; j += kSoloThreads) g[j] = (E)0.0f;
             continue;
         }
         const E* z = static_cast<const E*>(a.logits) + row * a.row_stride;
         const float za = (float)z[action];
         float m = -INFINITY;
-        for (int64_t j = threadIdx.x; j < a.V; j += kThreads) m = fmaxf(m, (float)z[j]);
-        m = wave_max(m);
+        for (int64_t j = threadIdx.x; j < a.V; j += kSoloThreads) m = fmaxf(m, (float)z[j]);
+        m = group_max<64>(m);
         if ((threadIdx.x & 63) == 0) s_max[wave] = m;
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kWaves; k++) m = fmaxf(m, s_max[k]);
+        const float ref = m == -INFINITY ? 0.0f : m;
         float S = 0.0f, dS = 0.0f;
-        if (m != -INFINITY) {
-            for (int64_t j = threadIdx.x; j < a.V; j += kThreads) {
-                const float d = (float)z[j] - m, e = fast_exp(d);
-                S += e;
-                dS += e * fmaxf(d, -3e38f);
-            }
+        for (int64_t j = threadIdx.x; j < a.V; j += kSoloThreads) {
+            const float d = (float)z[j] - ref, e = fast_exp(d);
+            S += e;
+            dS = fmaf(e, fmaxf(d, kFloor), dS);
         }
-        S = wave_add(S);
-        dS = wave_add(dS);
+        S = group_add<64>(S);
+        dS = group_add<64>(dS);
         if ((threadIdx.x & 63) == 0) {
             s_sum[wave] = S;
             s_dsum[wave] = dS;
@@ -185,38 +467,73 @@ __global__ __launch_bounds__(kThreads) void row_kernel(const Args a) {
             for (int k = 0; k < kSums; k++) total[k] += r.sums[k];
         }
         if (g) {
-            const float inv_S = 1.0f / S, log_S = fast_log(S);
-            for (int64_t j = threadIdx.x; j < a.V; j += kThreads) {
-                float v = 0.0f;
-                if (m != -INFINITY) {
-                    v = slope(a, r, (float)z[j] - m, inv_S, log_S);
-                    if (j == action) v += r.s * r.c;
-                }
-                g[j] = (E)v;
+            const bool some = m != -INFINITY;
+            const Slope k = some ? slope_of(a, r, S) : Slope{};
+            for (int64_t j = threadIdx.x; j < a.V; j += kSoloThreads) {
+                float o = some ? slope(k, (float)z[j] - ref) : 0.0f;
+                if (some && j == action) o += k.k2;
+                g[j] = (E)o;
             }
         }
     }
-    if (LOSS && threadIdx.x == 0) {
-#pragma unroll
-        for (int k = 0; k < kSums; k++) a.sums[(int64_t)blockIdx.x * kSums + k] = total[k];
-    }
+    if (LOSS) leave_sums<kSoloThreads>(a, total, denom, s_add);
 }
 
-// Adds the workgroups' sums, in 64 bits and always in the same order.
-__global__ __launch_bounds__(64) void finish_kernel(const Args a, int32_t blocks) {
+// Adds the workgroups' sums, a wave for each, in 64 bits and always in the same order.
+__global__ __launch_bounds__(64 * kSums) void finish_kernel(const Args a, int32_t blocks) {
     const float denom = denominator(a);
-    for (int k = 0; k < kSums; k++) {
-        double v = 0.0;
-        for (int b = threadIdx.x; b < blocks; b += 64) v += (double)a.sums[(int64_t)b * kSums + k];
-        v = wave_add(v) / (double)denom;
-        if (threadIdx.x == 0) {
-            if (k == 0) *a.loss = (float)v;
-            else if (a.stats) a.stats[k - 1] = (float)v;
-        }
+    const int k = threadIdx.x >> 6;
+    double v = 0.0;
+#pragma unroll 8
+    for (int b = threadIdx.x & 63; b < blocks; b += 64) v += (double)a.sums[k * kMaxBlocks + b];
+    v = group_add<64>(v) / (double)denom;
+    if ((threadIdx.x & 63) == 0) {
+        if (k == 0) *a.loss = (float)v;
+        else if (a.stats) a.stats[k - 1] = (float)v;
     }
 }
 
-int64_t work_bytes_of(const gear_policy_desc&) { return kSumOff + (int64_t)kMaxBlocks * kSums * (int64_t)sizeof(float); }
+typedef void (*Kernel)(const Args);
+struct Choice {
+    Kernel kernel;
+    int threads, rows;  // rows that a workgroup runs at a time
+};
+template <typename E, int G, int NV, int THREADS, bool LOSS, bool TINY = false>
+Choice held() {
+    return {held_kernel<E, G, NV, THREADS, TINY, LOSS>, THREADS, THREADS / G};
+}
+
+// The kernel for rows of V: as few lanes as hold a row in one piece each up to a
+// wave, then more pieces, then a workgroup.
+template <typename E, bool LOSS>
+Choice choose(int64_t V, bool solo) {
+    constexpr int VE = 16 / sizeof(E);
+    const int64_t pieces = (V + VE - 1) / VE;
+    if (solo) {
+        if (V < VE) return held<E, 1, 1, kSoloThreads, LOSS, true>();
+        if (pieces <= 4) return held<E, 4, 1, kSoloThreads, LOSS>();
+        if (pieces <= 16) return held<E, 16, 1, kSoloThreads, LOSS>();
+        if (pieces <= 64) return held<E, 64, 1, kSoloThreads, LOSS>();
+        if (pieces <= 256) return held<E, 64, 4, kSoloThreads, LOSS>();
+    }
+    if (V < VE) return held<E, 1, 1, kThreads, LOSS, true>();
+    if (pieces <= 1) return held<E, 1, 1, kThreads, LOSS>();
+    if (pieces <= 2) return held<E, 2, 1, kThreads, LOSS>();
+    if (pieces <= 4) return held<E, 4, 1, kThreads, LOSS>();
+    if (pieces <= 8) return held<E, 8, 1, kThreads, LOSS>();
+    if (pieces <= 16) return held<E, 16, 1, kThreads, LOSS>();
+    if (pieces <= 64) return held<E, 64, 1, kThreads, LOSS>();
+    if (pieces <= 128) return held<E, 64, 2, kThreads, LOSS>();
+    if (pieces <= 256) return held<E, 64, 4, kThreads, LOSS>();
+    if (pieces <= 512) return held<E, 64, 8, kThreads, LOSS>();
+    if (pieces <= 1024) return held<E, 256, 4, 256, LOSS>();
+    if (pieces <= 4096) return held<E, 1024, 4, 1024, LOSS>();
+    if (pieces <= 8192) return held<E, 1024, 8, 1024, LOSS>();
+    if (pieces <= 16384) return held<E, 1024, 16, 1024, LOSS>();
+    return {long_kernel<E, LOSS>, kSoloThreads, 1};
+}
+
+int64_t work_bytes_of(const gear_policy_desc&) { return kSumOff + (int64_t)kSums * kMaxBlocks * (int64_t)sizeof(float); }
 
 const char* flaw(const gear_policy_desc* d) {
     if (d == nullptr) return "NULL descriptor";
@@ -245,18 +562,20 @@ Args args_of(const gear_policy_desc& d, const void* logits) {
     a.n = d.n;
     a.V = d.V;
     a.row_stride = d.row_stride;
-    a.mask_group = d.mask_group;
-    a.adv_group = d.adv_group;
-    a.weight_group = d.weight_group;
+    a.mask_group = divisor(d.mask_group, d.n);
+    a.adv_group = divisor(d.adv_group, d.n);
+    a.weight_group = divisor(d.weight_group, d.n);
     a.action_dtype = d.action_dtype;
     return a;
 }
 
 template <bool LOSS>
-hipError_t launch_rows(const Args& a, int32_t dtype, int blocks, hipStream_t s) {
-    void (*k)(const Args) = dtype == GEAR_DTYPE_F32 ? row_kernel<float, LOSS>
-                            : dtype == GEAR_DTYPE_BF16 ? row_kernel<__bf16, LOSS> : row_kernel<_Float16, LOSS>;
-    hipLaunchKernelGGL(k, dim3(blocks), dim3(kThreads), 0, s, a);
+hipError_t launch_rows(const Args& a, int32_t dtype, int* blocks, hipStream_t s) {
+    const Choice c = dtype == GEAR_DTYPE_F32 ? choose<float, LOSS>(a.V, a.solo)
+                     : dtype == GEAR_DTYPE_BF16 ? choose<__bf16, LOSS>(a.V, a.solo) : choose<_Float16, LOSS>(a.V, a.solo);
+    const int64_t want = (a.n + c.rows - 1) / c.rows;
+    *blocks = a.solo ? 1 : (int)(want < kMaxBlocks ? want : kMaxBlocks);
+    hipLaunchKernelGGL(c.kernel, dim3(*blocks), dim3(c.threads), 0, s, a);
     return hipGetLastError();
 }
 
@@ -304,20 +623,24 @@ extern "C" int gear_policy_loss(const gear_policy_desc* d, const void* d_logits,
     a.grad_scale = d->grad_scale;
     hipStream_t s = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();  // an error pending from an earlier HIP call is not this call's
+    // Few logits: one workgroup does it all, and the launches saved are worth
+    // more than the others would bring.
+    a.solo = a.n > 0 && a.n <= kSoloLogits / a.V;
     hipError_t e = hipSuccess;
-    if (!(a.denom > 0.0f)) {
+    int blocks = 0;
+    if (!a.solo && !(a.denom > 0.0f)) {
         const int64_t want = (a.n + kThreads - 1) / kThreads;
         a.count_blocks = (int32_t)(want < 1 ? 1 : want < kCountBlocks ? want : kCountBlocks);
         hipLaunchKernelGGL(count_kernel, dim3(a.count_blocks), dim3(kThreads), 0, s, a);
         e = hipGetLastError();
         if (e != hipSuccess) return hip_fail(e, "gear_policy_loss: count launch");
     }
-    const int blocks = (int)(a.n < kMaxBlocks ? a.n : kMaxBlocks);
-    if (blocks > 0) {
-        e = launch_rows<true>(a, d->dtype, blocks, s);
+    if (a.n > 0) {
+        e = launch_rows<true>(a, d->dtype, &blocks, s);
         if (e != hipSuccess) return hip_fail(e, "gear_policy_loss: row launch");
+        if (a.solo) return GEAR_OK;
     }
-    hipLaunchKernelGGL(finish_kernel, dim3(1), dim3(64), 0, s, a, blocks);
+    hipLaunchKernelGGL(finish_kernel, dim3(1), dim3(64 * kSums), 0, s, a, blocks);
     e = hipGetLastError();
     return e == hipSuccess ? GEAR_OK : hip_fail(e, "gear_policy_loss: sum launch");
 }
@@ -332,7 +655,7 @@ extern "C" int gear_action_logp(const gear_policy_desc* d, const void* d_logits,
     a.logp = d_logp;
     a.entropy = d_entropy;
     (void)hipGetLastError();  // an error pending from an earlier HIP call is not this call's
-    const int blocks = (int)(a.n < kMaxBlocks ? a.n : kMaxBlocks);
-    const hipError_t e = launch_rows<false>(a, d->dtype, blocks, static_cast<hipStream_t>(stream));
+    int blocks = 0;
+    const hipError_t e = launch_rows<false>(a, d->dtype, &blocks, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? GEAR_OK : hip_fail(e, "gear_action_logp: launch");
 }
