@@ -16,13 +16,13 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kSums = 5;               // loss, clipped term, KL term, entropy, clipped rows
-constexpr int kCountBlocks = 256;      // workgroups that count the rows that take part
+constexpr int kCountBlocks = 512;      // workgroups that count the rows that take part
 constexpr int kMaxBlocks = 2048;       // workgroups of the row kernels
 constexpr int kSoloThreads = 1024;     // calls of one workgroup
-constexpr int64_t kSoloLogits = 1 << 15;
+constexpr int64_t kSoloLogits = 1 << 15, kSoloActions = 1024;
 constexpr int64_t kCountOff = 0, kSumOff = kCountBlocks * (int64_t)sizeof(int64_t);
-// A masked logit's d, and where it stops mattering: e^d is 0 well above it,
-// and a multiple of it stays finite.
+// Where a logit's distance stops mattering: 2^d is 0 well above it, and a
+// multiple of it stays finite.
 constexpr float kFloor = -1e4f;
 
 // Quotients by a number fixed for the launch: for dividends below 2^31, the
@@ -60,7 +60,6 @@ struct Args {
     int64_t n, V, row_stride;
     Divisor mask_group, adv_group, weight_group;
     int32_t action_dtype, count_blocks;
-    bool solo;        // one workgroup counts, runs all rows and adds up
     float lo, hi, kl, ent, denom, grad_scale;
 };
 
@@ -100,6 +99,7 @@ __device__ __forceinline__ T block_add(T v, T* s) {
 template <int THREADS>
 __device__ __forceinline__ int64_t count_rows(const Args& a, int64_t* s) {
     int64_t c = 0;
+#pragma unroll 8
     for (int64_t r = (int64_t)blockIdx.x * THREADS + threadIdx.x; r < a.n; r += (int64_t)gridDim.x * THREADS)
         c += takes_part(a, r, action_of(a, r)) ? 1 : 0;
     return block_add<THREADS>(c, s);
@@ -121,45 +121,83 @@ __device__ __forceinline__ float denominator(const Args& a) {
     return c > 0 ? (float)c : 1.0f;
 }
 
+// Distances from a row's largest logit m, in powers of two: 0 for m itself, so
+// that a row's only possible action has log-probability 0.
+struct Scale {
+    float m;
+    __device__ __forceinline__ float operator()(float z) const { return (z - m) * kLog2e; }
+};
+__device__ __forceinline__ Scale scale_of(float m) { return Scale{m == -INFINITY ? 0.0f : m}; }  // a row of -inf sums to 0
+
+// What a row has beside its logits, read while they are on their way.
+struct Inputs {
+    float old, ref, A, w;
+};
+__device__ __forceinline__ Inputs inputs_of(const Args& a, int64_t row) {
+    Inputs in;
+    in.old = a.old_logp[row];
+    in.ref = a.ref_logp ? a.ref_logp[row] : 0.0f;
+    in.A = a.adv[quotient(row, a.adv_group)];
+    in.w = a.weight ? a.weight[quotient(row, a.weight_group)] : 1.0f;
+    return in;
+}
+
+// exp(q) - 1 and exp(q) - 1 - q, the latter without cancellation near 0: there by
+// the exponential's series, whose first omitted term is below 2^-30 of the result.
+__device__ __forceinline__ void exp_less_one(float q, float& e, float& k) {
+#pragma clang fp contract(off)
+    float p = 1.0f / 40320.0f;
+    p = fmaf(p, q, 1.0f / 5040.0f);
+    p = fmaf(p, q, 1.0f / 720.0f);
+    p = fmaf(p, q, 1.0f / 120.0f);
+    p = fmaf(p, q, 1.0f / 24.0f);
+    p = fmaf(p, q, 1.0f / 6.0f);
+    p = fmaf(p, q, 0.5f);
+    const float near_k = p * q * q, far_e = fast_exp(q) - 1.0f;
+    const bool near = fabsf(q) < 0.25f;
+    k = near ? near_k : far_e - q;
+    e = near ? q + near_k : far_e;
+}
+
 struct Row {
     float lp, H;  // log-probability of the action, entropy
     float c, s;   // derivative of the loss for lp, factor of the gradient
     float sums[kSums];
 };
 
-// A row's terms from its largest logit, its sums and the action's logit.  The
-// operations are spelled out, so that lp and H come out the same in every kernel.
+// A row's terms from its largest logit, the sums of 2^d and of d 2^d, and the
+// action's d.  The operations are spelled out, so that lp and H come out the
+// same in every kernel.
 template <bool LOSS>
-__device__ __forceinline__ Row row_terms(const Args& a, int64_t row, float m, float S, float dS, float za, float denom) {
+__device__ __forceinline__ Row row_terms(const Args& a, const Inputs& in, float m, float S, float dS, float da,
+                                         float scale) {
 #pragma clang fp contract(off)
     Row r{};
     if (m == -INFINITY) {  // no distribution
         r.lp = -INFINITY;
         return r;
     }
-    const float log_S = fast_log(S);
-    r.lp = (za - m) - log_S;
-    r.H = log_S - dS * __builtin_amdgcn_rcpf(S);
+    const float log_S = __builtin_amdgcn_logf(S);
+    r.lp = (da - log_S) * kLn2;
+    r.H = (log_S - dS * __builtin_amdgcn_rcpf(S)) * kLn2;
     if (!LOSS) return r;
-    const float A = a.adv[quotient(row, a.adv_group)];
-    const float w = a.weight ? a.weight[quotient(row, a.weight_group)] : 1.0f;
-    const float ratio = expf(r.lp - a.old_logp[row]);
-    const float free = ratio * A, held = fminf(fmaxf(ratio, a.lo), a.hi) * A;
+    const float ratio = fast_exp(r.lp - in.old);
+    const float free = ratio * in.A, held = fminf(fmaxf(ratio, a.lo), a.hi) * in.A;
     const bool clipped = held < free;
     const float pg = clipped ? -held : -free;
     r.c = clipped ? 0.0f : -free;
     float kl = 0.0f, row_loss = pg;
     if (a.ref_logp) {
-        const float q = a.ref_logp[row] - r.lp, e = expm1f(q);
-        kl = e - q;
+        float e;
+        exp_less_one(in.ref - r.lp, e, kl);
         if (a.kl != 0.0f) {
             row_loss += a.kl * kl;
             r.c -= a.kl * e;
         }
     }
     if (a.ent != 0.0f) row_loss -= a.ent * r.H;
-    r.s = w * a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / denom;
-    r.sums[0] = w * row_loss;
+    r.s = in.w * scale;
+    r.sums[0] = in.w * row_loss;
     r.sums[1] = pg;
     r.sums[2] = kl;
     r.sums[3] = r.H;
@@ -167,25 +205,27 @@ __device__ __forceinline__ Row row_terms(const Args& a, int64_t row, float m, fl
     return r;
 }
 
-// dz_j = e^d_j (k1 d_j + k0), and k2 more for the action.
+// dz_j = 2^d_j (k1 d_j + k0), and k2 more for the action.
 struct Slope {
     float k0, k1, k2;
+    __device__ __forceinline__ float operator()(float d) const {
+        return __builtin_amdgcn_exp2f(d) * fmaf(k1, fmaxf(d, kFloor), k0);
+    }
 };
 __device__ __forceinline__ Slope slope_of(const Args& a, const Row& r, float S) {
-    const float f = r.s / S;
-    return Slope{f * (a.ent * (r.H - fast_log(S)) - r.c), f * a.ent, r.s * r.c};
+    const float f = r.s * __builtin_amdgcn_rcpf(S), g = a.ent * kLn2;
+    return Slope{f * (a.ent * r.H - g * __builtin_amdgcn_logf(S) - r.c), f * g, r.s * r.c};
 }
-__device__ __forceinline__ float slope(const Slope& k, float d) { return fast_exp(d) * fmaf(k.k1, fmaxf(d, kFloor), k.k0); }
 
 // The sums of a call that one workgroup ran, or this workgroup's share of them.
-template <int THREADS>
+template <int THREADS, bool SOLO>
 __device__ __forceinline__ void leave_sums(const Args& a, const float (&total)[kSums], float denom, double* s) {
 #pragma unroll
     for (int k = 0; k < kSums; k++) {
         __syncthreads();
         const double v = block_add<THREADS>((double)total[k], s);
         if (threadIdx.x == 0) {
-            if (!a.solo) a.sums[k * kMaxBlocks + blockIdx.x] = (float)v;
+            if (!SOLO) a.sums[k * kMaxBlocks + blockIdx.x] = (float)v;
             else if (k == 0) *a.loss = (float)(v / (double)denom);
             else if (a.stats) a.stats[k - 1] = (float)(v / (double)denom);
         }
@@ -248,22 +288,24 @@ struct Piece {
     __device__ __forceinline__ void forget() { asm volatile("" : "+v"(w)); }
 };
 
-// Rows held in registers: G lanes share a row, each with NV pieces of 16 bytes
-// every G pieces, so that a row is read once and its gradient written once.
-// A lane past the end of its row reads the row's last piece and keeps of it
-// what no other lane has; with TINY, rows are shorter than a piece.
+// Rows held in registers: G lanes share a row, each with up to NV pieces of 16
+// bytes every G pieces, so that a row is read once and its gradient written
+// once.  A lane past the end of its row reads the row's last piece and keeps of
+// it what no other lane has; with TINY, rows are shorter than a piece.
 template <typename E, int G, int NV, int THREADS, bool TINY, bool LOSS>
 __global__ __launch_bounds__(THREADS) void held_kernel(const Args a) {
     constexpr int VE = 16 / sizeof(E), kGroups = THREADS / G, kWaves = THREADS / 64;
     constexpr bool kBlock = G > 64;  // the whole workgroup shares a row
+    constexpr bool kSolo = THREADS == kSoloThreads && !kBlock;  // the one workgroup of its call
     static_assert(!kBlock || G == THREADS, "one row at a time");
     __shared__ float s_max[kWaves], s_sum[kWaves], s_dsum[kWaves], s_za;
     __shared__ double s_add[kWaves];
     __shared__ int64_t s_count;
+    __shared__ Inputs s_in[2];  // in turn: read after the row's last barrier
     const int lane = threadIdx.x % G, V = (int)a.V;  // at most 2^17 elements are held
-    float denom = 1.0f;
+    float denom = 1.0f, scale = 1.0f;
     if (LOSS) {
-        if (a.solo && !(a.denom > 0.0f)) {
+        if (kSolo && !(a.denom > 0.0f)) {
             const int64_t c = count_rows<THREADS>(a, reinterpret_cast<int64_t*>(s_add));
             if (threadIdx.x == 0) s_count = c;
             __syncthreads();
@@ -271,8 +313,10 @@ __global__ __launch_bounds__(THREADS) void held_kernel(const Args a) {
         } else {
             denom = denominator(a);
         }
+        scale = a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / denom;
     }
     float total[kSums] = {};
+    int turn = 0;
     for (int64_t first = (int64_t)blockIdx.x * kGroups; first < a.n; first += (int64_t)gridDim.x * kGroups) {
         const int64_t row = first + (kBlock ? 0 : threadIdx.x / G);
         const bool used = row < a.n;
@@ -297,6 +341,7 @@ __global__ __launch_bounds__(THREADS) void held_kernel(const Args a) {
         const E* z = static_cast<const E*>(a.logits) + row * a.row_stride;
         Piece<E> v[NV];
         float za = 0.0f;
+        Inputs in{};
         // The lane's number, hidden so that what follows from it for each piece is not kept from row to row.
         int mine = lane;
         asm volatile("" : "+v"(mine));
@@ -315,7 +360,10 @@ __global__ __launch_bounds__(THREADS) void held_kernel(const Args a) {
                     v[i].fill();
                 }
             }
-            if (!kBlock || threadIdx.x == 0) za = (float)z[action];
+            if (!kBlock || threadIdx.x == 0) {
+                za = (float)z[action];
+                if (LOSS) in = inputs_of(a, row);
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < NV; i++) v[i].fill();
@@ -332,13 +380,16 @@ __global__ __launch_bounds__(THREADS) void held_kernel(const Args a) {
         m = group_max<kBlock ? 64 : G>(m);
         if (kBlock) {
             if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = m;
-            if (threadIdx.x == 0) s_za = za;
+            if (threadIdx.x == 0) {
+                s_za = za;
+                s_in[turn] = in;
+            }
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < kWaves; k++) m = fmaxf(m, s_max[k]);
             za = s_za;
         }
-        const float ref = m == -INFINITY ? 0.0f : m;  // a row of -inf sums to 0
+        const Scale dist = scale_of(m);
         float S = 0.0f, dS = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; i++) {
@@ -346,7 +397,7 @@ __global__ __launch_bounds__(THREADS) void held_kernel(const Args a) {
             v[i].unpack(f);
 #pragma unroll
             for (int j = 0; j < VE; j++) {
-                const float d = f[j] - ref, e = fast_exp(d);
+                const float d = dist(f[j]), e = __builtin_amdgcn_exp2f(d);
                 S += e;
                 dS = fmaf(e, fmaxf(d, kFloor), dS);
             }
@@ -366,9 +417,11 @@ __global__ __launch_bounds__(THREADS) void held_kernel(const Args a) {
                 S += s_sum[k];
                 dS += s_dsum[k];
             }
+            in = s_in[turn];
+            turn ^= 1;
         }
         Row r{};
-        if (on) r = row_terms<LOSS>(a, row, m, S, dS, za, denom);
+        if (on) r = row_terms<LOSS>(a, in, m, S, dS, dist(za), scale);
         if (used && lane == 0) {
             if (a.logp) a.logp[row] = r.lp;
             if (a.entropy) a.entropy[row] = r.H;
@@ -376,37 +429,35 @@ __global__ __launch_bounds__(THREADS) void held_kernel(const Args a) {
             for (int k = 0; k < kSums; k++) total[k] += r.sums[k];
         }
         if (LOSS && a.grad && used) {
+            // Rows without part or distribution hold only -inf, and get zeros.
             E* g = static_cast<E*>(a.grad) + row * a.V;
             const bool some = on && m != -INFINITY;
-            const Slope k = some ? slope_of(a, r, S) : Slope{};
+            const Slope slope = some ? slope_of(a, r, S) : Slope{};
             asm volatile("" : "+v"(mine));
 #pragma unroll
             for (int i = 0; i < NV; i++) {
                 if (i * G * VE < V) {
-                    const int base = (i * G + mine) * VE;
-                    // A lane at the end of its row holds the last piece, of which it has the last elements.
-                    const bool whole = !TINY && ((i + 1) * G * VE <= V || base + VE <= V);
-                    const int at = TINY || whole ? base : V - VE;
                     float f[VE], o[VE];
                     v[i].unpack(f);
-                    const int hit = (int)action - at;
 #pragma unroll
-                    for (int j = 0; j < VE; j++) {
-                        o[j] = some ? slope(k, f[j] - ref) : 0.0f;
-                        if (some && j == hit) o[j] += k.k2;
-                    }
-                    if (whole) {
+                    for (int j = 0; j < VE; j++) o[j] = slope(dist(f[j]));
+                    const int base = (i * G + mine) * VE;
+                    if (!TINY && ((i + 1) * G * VE <= V || base + VE <= V)) {
                         Vec<E, VE>::store(g + base, o);
                     } else {
+                        // The row's last piece, of which this lane has the last elements, or none.
+                        const int at = TINY ? 0 : V - VE;
 #pragma unroll
                         for (int j = 0; j < VE; j++)
                             if (at + j >= base && at + j < V) g[at + j] = (E)o[j];
                     }
                 }
             }
+            // The action's, over the value just written by the same lane.
+            if (some && lane == (TINY ? 0 : (int)action / VE % G)) g[action] = (E)(slope(dist(za)) + slope.k2);
         }
     }
-    if (LOSS) leave_sums<THREADS>(a, total, denom, s_add);
+    if (LOSS) leave_sums<THREADS, kSolo>(a, total, denom, s_add);
 }
 
 // Rows longer than registers hold: a workgroup per row, which reads it three times.
@@ -417,6 +468,7 @@ __global__ __launch_bounds__(kSoloThreads) void long_kernel(const Args a) {
     __shared__ double s_add[kWaves];
     const int wave = threadIdx.x >> 6;
     const float denom = LOSS ? denominator(a) : 1.0f;
+    const float scale = LOSS ? a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / denom : 1.0f;
     float total[kSums] = {};
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const int64_t action = action_of(a, row);
@@ -432,6 +484,8 @@ __global__ __launch_bounds__(kSoloThreads) void long_kernel(const Args a) {
         }
         const E* z = static_cast<const E*>(a.logits) + row * a.row_stride;
         const float za = (float)z[action];
+        Inputs in{};
+        if (LOSS) in = inputs_of(a, row);
         float m = -INFINITY;
         for (int64_t j = threadIdx.x; j < a.V; j += kSoloThreads) m = fmaxf(m, (float)z[j]);
         m = group_max<64>(m);
@@ -439,10 +493,10 @@ __global__ __launch_bounds__(kSoloThreads) void long_kernel(const Args a) {
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kWaves; k++) m = fmaxf(m, s_max[k]);
-        const float ref = m == -INFINITY ? 0.0f : m;
+        const Scale dist = scale_of(m);
         float S = 0.0f, dS = 0.0f;
         for (int64_t j = threadIdx.x; j < a.V; j += kSoloThreads) {
-            const float d = (float)z[j] - ref, e = fast_exp(d);
+            const float d = dist((float)z[j]), e = __builtin_amdgcn_exp2f(d);
             S += e;
             dS = fmaf(e, fmaxf(d, kFloor), dS);
         }
@@ -459,7 +513,7 @@ __global__ __launch_bounds__(kSoloThreads) void long_kernel(const Args a) {
             S += s_sum[k];
             dS += s_dsum[k];
         }
-        const Row r = row_terms<LOSS>(a, row, m, S, dS, za, denom);
+        const Row r = row_terms<LOSS>(a, in, m, S, dS, dist(za), scale);
         if (threadIdx.x == 0) {
             if (a.logp) a.logp[row] = r.lp;
             if (a.entropy) a.entropy[row] = r.H;
@@ -467,16 +521,14 @@ __global__ __launch_bounds__(kSoloThreads) void long_kernel(const Args a) {
             for (int k = 0; k < kSums; k++) total[k] += r.sums[k];
         }
         if (g) {
-            const bool some = m != -INFINITY;
-            const Slope k = some ? slope_of(a, r, S) : Slope{};
+            const Slope slope = m != -INFINITY ? slope_of(a, r, S) : Slope{};
             for (int64_t j = threadIdx.x; j < a.V; j += kSoloThreads) {
-                float o = some ? slope(k, (float)z[j] - ref) : 0.0f;
-                if (some && j == action) o += k.k2;
-                g[j] = (E)o;
+                const float o = slope(dist((float)z[j]));
+                g[j] = (E)(j == action ? o + slope.k2 : o);
             }
         }
     }
-    if (LOSS) leave_sums<kSoloThreads>(a, total, denom, s_add);
+    if (LOSS) leave_sums<kSoloThreads, false>(a, total, denom, s_add);
 }
 
 // Adds the workgroups' sums, a wave for each, in 64 bits and always in the same order.
@@ -503,32 +555,35 @@ Choice held() {
     return {held_kernel<E, G, NV, THREADS, TINY, LOSS>, THREADS, THREADS / G};
 }
 
-// The kernel for rows of V: as few lanes as hold a row in one piece each up to a
-// wave, then more pieces, then a workgroup.
+// The kernel for rows of V: as few lanes as hold a row in four pieces each, so
+// that what is done once per row is done by few, then up to 16 pieces.  How many
+// lanes share a row, and so the order of its sums, depends on V alone.
 template <typename E, bool LOSS>
 Choice choose(int64_t V, bool solo) {
     constexpr int VE = 16 / sizeof(E);
     const int64_t pieces = (V + VE - 1) / VE;
-    if (solo) {
-        if (V < VE) return held<E, 1, 1, kSoloThreads, LOSS, true>();
-        if (pieces <= 4) return held<E, 4, 1, kSoloThreads, LOSS>();
-        if (pieces <= 16) return held<E, 16, 1, kSoloThreads, LOSS>();
-        if (pieces <= 64) return held<E, 64, 1, kSoloThreads, LOSS>();
-        if (pieces <= 256) return held<E, 64, 4, kSoloThreads, LOSS>();
+    if constexpr (LOSS) {
+        if (solo && V < VE) return held<E, 1, 1, kSoloThreads, LOSS, true>();
+        if (solo && pieces <= 4) return held<E, 1, 4, kSoloThreads, LOSS>();
+        if (solo && pieces <= 8) return held<E, 2, 4, kSoloThreads, LOSS>();
+        if (solo && pieces <= 16) return held<E, 4, 4, kSoloThreads, LOSS>();
+        if (solo && pieces <= 32) return held<E, 8, 4, kSoloThreads, LOSS>();
+        if (solo && pieces <= 64) return held<E, 16, 4, kSoloThreads, LOSS>();
+        if (solo) return held<E, 64, 4, kSoloThreads, LOSS>();
     }
     if (V < VE) return held<E, 1, 1, kThreads, LOSS, true>();
     if (pieces <= 1) return held<E, 1, 1, kThreads, LOSS>();
-    if (pieces <= 2) return held<E, 2, 1, kThreads, LOSS>();
-    if (pieces <= 4) return held<E, 4, 1, kThreads, LOSS>();
-    if (pieces <= 8) return held<E, 8, 1, kThreads, LOSS>();
-    if (pieces <= 16) return held<E, 16, 1, kThreads, LOSS>();
-    if (pieces <= 64) return held<E, 64, 1, kThreads, LOSS>();
-    if (pieces <= 128) return held<E, 64, 2, kThreads, LOSS>();
+    if (pieces <= 2) return held<E, 1, 2, kThreads, LOSS>();
+    if (pieces <= 4) return held<E, 1, 4, kThreads, LOSS>();
+    if (pieces <= 8) return held<E, 2, 4, kThreads, LOSS>();
+    if (pieces <= 16) return held<E, 4, 4, kThreads, LOSS>();
+    if (pieces <= 32) return held<E, 8, 4, kThreads, LOSS>();
+    if (pieces <= 64) return held<E, 16, 4, kThreads, LOSS>();
     if (pieces <= 256) return held<E, 64, 4, kThreads, LOSS>();
     if (pieces <= 512) return held<E, 64, 8, kThreads, LOSS>();
     if (pieces <= 1024) return held<E, 256, 4, 256, LOSS>();
-    if (pieces <= 4096) return held<E, 1024, 4, 1024, LOSS>();
-    if (pieces <= 8192) return held<E, 1024, 8, 1024, LOSS>();
+    if (pieces <= 4096) return held<E, 256, 16, 256, LOSS>();
+    if (pieces <= 8192) return held<E, 512, 16, 512, LOSS>();
     if (pieces <= 16384) return held<E, 1024, 16, 1024, LOSS>();
     return {long_kernel<E, LOSS>, kSoloThreads, 1};
 }
@@ -570,11 +625,11 @@ Args args_of(const gear_policy_desc& d, const void* logits) {
 }
 
 template <bool LOSS>
-hipError_t launch_rows(const Args& a, int32_t dtype, int* blocks, hipStream_t s) {
-    const Choice c = dtype == GEAR_DTYPE_F32 ? choose<float, LOSS>(a.V, a.solo)
-                     : dtype == GEAR_DTYPE_BF16 ? choose<__bf16, LOSS>(a.V, a.solo) : choose<_Float16, LOSS>(a.V, a.solo);
+hipError_t launch_rows(const Args& a, int32_t dtype, bool solo, int* blocks, hipStream_t s) {
+    const Choice c = dtype == GEAR_DTYPE_F32 ? choose<float, LOSS>(a.V, solo)
+                     : dtype == GEAR_DTYPE_BF16 ? choose<__bf16, LOSS>(a.V, solo) : choose<_Float16, LOSS>(a.V, solo);
     const int64_t want = (a.n + c.rows - 1) / c.rows;
-    *blocks = a.solo ? 1 : (int)(want < kMaxBlocks ? want : kMaxBlocks);
+    *blocks = solo ? 1 : (int)(want < kMaxBlocks ? want : kMaxBlocks);
     hipLaunchKernelGGL(c.kernel, dim3(*blocks), dim3(c.threads), 0, s, a);
     return hipGetLastError();
 }
@@ -625,10 +680,10 @@ extern "C" int gear_policy_loss(const gear_policy_desc* d, const void* d_logits,
     (void)hipGetLastError();  // an error pending from an earlier HIP call is not this call's
     // Few logits: one workgroup does it all, and the launches saved are worth
     // more than the others would bring.
-    a.solo = a.n > 0 && a.n <= kSoloLogits / a.V;
+    const bool solo = a.n > 0 && a.n <= kSoloLogits / a.V && a.V <= kSoloActions;
     hipError_t e = hipSuccess;
     int blocks = 0;
-    if (!a.solo && !(a.denom > 0.0f)) {
+    if (!solo && !(a.denom > 0.0f)) {
         const int64_t want = (a.n + kThreads - 1) / kThreads;
         a.count_blocks = (int32_t)(want < 1 ? 1 : want < kCountBlocks ? want : kCountBlocks);
         hipLaunchKernelGGL(count_kernel, dim3(a.count_blocks), dim3(kThreads), 0, s, a);
@@ -636,9 +691,9 @@ extern "C" int gear_policy_loss(const gear_policy_desc* d, const void* d_logits,
         if (e != hipSuccess) return hip_fail(e, "gear_policy_loss: count launch");
     }
     if (a.n > 0) {
-        e = launch_rows<true>(a, d->dtype, &blocks, s);
+        e = launch_rows<true>(a, d->dtype, solo, &blocks, s);
         if (e != hipSuccess) return hip_fail(e, "gear_policy_loss: row launch");
-        if (a.solo) return GEAR_OK;
+        if (solo) return GEAR_OK;
     }
     hipLaunchKernelGGL(finish_kernel, dim3(1), dim3(64 * kSums), 0, s, a, blocks);
     e = hipGetLastError();
@@ -656,6 +711,6 @@ extern "C" int gear_action_logp(const gear_policy_desc* d, const void* d_logits,
     a.entropy = d_entropy;
     (void)hipGetLastError();  // an error pending from an earlier HIP call is not this call's
     int blocks = 0;
-    const hipError_t e = launch_rows<false>(a, d->dtype, &blocks, static_cast<hipStream_t>(stream));
+    const hipError_t e = launch_rows<false>(a, d->dtype, false, &blocks, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? GEAR_OK : hip_fail(e, "gear_action_logp: launch");
 }

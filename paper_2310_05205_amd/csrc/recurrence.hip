@@ -20,6 +20,7 @@ namespace gear {
 namespace {
 
 constexpr int kSteps = GEAR_RECURRENCE_STEPS;  // steps of a tile
+constexpr int kForwardBytes = 8, kBackwardBytes = 4;  // neighbouring channels of a lane
 constexpr int kThreads = 256;
 constexpr int kWantLanes = 2048 * 64;  // lanes that fill the GPU
 constexpr int64_t kMaxBlocks = 1 << 22;
@@ -33,6 +34,12 @@ struct Map {
 };
 __device__ __forceinline__ float apply(Map m, float c) {
     return __float_as_uint(m.P) == kCutBits ? m.Z : fmaf(m.P, c, m.Z);
+}
+
+// `early` first, then `late`.
+__device__ __forceinline__ Map compose(Map late, Map early) {
+    const bool cut = __float_as_uint(late.P) == kCutBits || __float_as_uint(early.P) == kCutBits;
+    return Map{cut ? __uint_as_float(kCutBits) : late.P * early.P, apply(late, early.Z)};
 }
 
 struct Args {
@@ -86,36 +93,92 @@ __device__ __forceinline__ uint32_t resets(const Args& a, int64_t b, int64_t t0,
     return bits;
 }
 
-// Decay and input weight of a gate; neither form's weight cancels, whatever the gate's size.
+// Decay and input weight of a gate.  With e = exp(-g) they are 1 / (1 + e) and
+// e / (1 + e), neither of which cancels; where e is large the latter is 1,
+// and its product would fail as the decay underflows.  A NaN stays one.
 template <int FORM>
 __device__ __forceinline__ void gates(float g, float& f, float& w) {
     if (FORM == GEAR_GATE_VALUE) {
         f = g;
         w = 1.0f;
     } else {
-        const float e = fast_exp(-fabsf(g));  // in [0, 1]
-        const float big = __builtin_amdgcn_rcpf(1.0f + e), small = e * big;
-        f = g >= 0.0f ? big : small;
-        w = g >= 0.0f ? small : big;
+        const float e = fast_exp(-g);
+        f = __builtin_amdgcn_rcpf(1.0f + e);
+        w = e > 0x1p30f ? 1.0f : e * f;
     }
+}
+
+// What the lanes of a wave have in common at a tile: every step of it and no
+// reset, every step, or anything else.  The first two run without a branch
+// per step, so that the steps' gates are computed side by side.
+enum { kPlain = 0, kCuts = 1, kAny = 2 };
+__device__ __forceinline__ int mode_of(int count, uint32_t r) {
+    if (!__all(count == kSteps)) return kAny;
+    return __any(r != 0) ? kCuts : kPlain;
 }
 
 template <typename E, int VE>
 struct Tile {
     typename Vec<E, VE>::raw v[kSteps];
+    template <int MODE>
     __device__ __forceinline__ void load(const E* p, int64_t stride, int count) {
-        if (count == kSteps) {
 #pragma unroll
-            for (int i = 0; i < kSteps; i++) v[i] = Vec<E, VE>::load(p + i * stride);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kSteps; i++)
-                if (i < count) v[i] = Vec<E, VE>::load(p + i * stride);
-        }
+        for (int i = 0; i < kSteps; i++)
+            if (MODE != kAny || i < count) v[i] = Vec<E, VE>::load(p + i * stride);
     }
 };
 
 __device__ __forceinline__ int clamp_count(int64_t n) { return n < 0 ? 0 : n < kSteps ? (int)n : kSteps; }
+
+// A lane's pointers at its window and channels.
+template <typename E>
+struct Rows {
+    const E *gate, *x, *dy;
+    E *y, *dgate, *dx;
+};
+template <typename E>
+__device__ __forceinline__ Rows<E> rows_of(const Args& a, const Place& p) {
+    Rows<E> r;
+    r.gate = static_cast<const E*>(a.gate) + p.b * a.gate_b + p.c;
+    r.x = static_cast<const E*>(a.x) + p.b * a.x_b + p.c;
+    r.dy = a.dy ? static_cast<const E*>(a.dy) + p.b * a.dy_b + p.c : nullptr;
+    r.y = static_cast<E*>(a.y) + p.b * a.T * a.D + p.c;
+    r.dgate = static_cast<E*>(a.dgate) + p.b * a.T * a.D + p.c;
+    r.dx = static_cast<E*>(a.dx) + p.b * a.T * a.D + p.c;
+    return r;
+}
+
+// `count` steps of the recurrence from step t0 on; zeros up to `room`.
+template <typename E, int VE, int FORM, bool MAPS, int MODE>
+__device__ __forceinline__ void forward_tile(const Args& a, const Rows<E>& rows, int64_t t0, int count, int room,
+                                             uint32_t r, float (&h)[VE], float (&P)[VE]) {
+#pragma clang fp contract(off)  // the modes round alike: lanes that share channels may run different ones
+    Tile<E, VE> g, x;
+    g.template load<MODE>(rows.gate + t0 * a.gate_t, a.gate_t, count);
+    x.template load<MODE>(rows.x + t0 * a.x_t, a.x_t, count);
+    E* y = rows.y + t0 * a.D;
+#pragma unroll
+    for (int s = 0; s < kSteps; s++) {
+        if (MODE != kAny || s < count) {
+            float gv[VE], xv[VE];
+            Vec<E, VE>::unpack(g.v[s], gv);
+            Vec<E, VE>::unpack(x.v[s], xv);
+            const bool z = MODE != kPlain && ((r >> s) & 1u);
+#pragma unroll
+            for (int j = 0; j < VE; j++) {
+                float f, w;
+                gates<FORM>(gv[j], f, w);
+                const float u = FORM == GEAR_GATE_VALUE ? xv[j] : w * xv[j];
+                h[j] = z ? u : fmaf(f, h[j], u);
+                if (MAPS) P[j] *= f;
+            }
+            if (!MAPS && a.y) Vec<E, VE>::store(y + s * a.D, h);
+        } else if (!MAPS && s < room && a.y) {
+            const float zero[VE] = {};
+            Vec<E, VE>::store(y + s * a.D, zero);
+        }
+    }
+}
 
 // Segments forward: with MAPS, reduces each to its map; else the whole recurrence.
 template <typename E, int VE, int FORM, bool MAPS>
@@ -125,6 +188,7 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(const Args a) {
          i += (int64_t)gridDim.x * kThreads) {
         const int64_t seg = i / a.lanes;
         const Place p = place_of<VE>(a, i - seg * a.lanes);
+        const Rows<E> rows = rows_of<E>(a, p);
         const int64_t at = p.b * a.D + p.c;
         float h[VE], P[VE];
         bool cut = false;
@@ -139,33 +203,12 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(const Args a) {
             const int64_t t0 = k * kSteps;
             const int count = clamp_count(p.n - t0), room = clamp_count(a.T - t0);
             if (!MAPS && a.out_saved && k > 0) Vec<float, VE>::store(a.out_saved + (k - 1) * BD + at, h);
-            Tile<E, VE> g, x;
-            g.load(static_cast<const E*>(a.gate) + p.b * a.gate_b + t0 * a.gate_t + p.c, a.gate_t, count);
-            x.load(static_cast<const E*>(a.x) + p.b * a.x_b + t0 * a.x_t + p.c, a.x_t, count);
             const uint32_t r = resets(a, p.b, t0, count);
-            E* y = static_cast<E*>(a.y) + (p.b * a.T + t0) * a.D + p.c;
-#pragma unroll
-            for (int s = 0; s < kSteps; s++) {
-                if (s < count) {
-                    float gv[VE], xv[VE];
-                    Vec<E, VE>::unpack(g.v[s], gv);
-                    Vec<E, VE>::unpack(x.v[s], xv);
-                    const bool z = (r >> s) & 1u;
-                    cut |= z;
-#pragma unroll
-                    for (int j = 0; j < VE; j++) {
-                        float f, w;
-                        gates<FORM>(gv[j], f, w);
-                        const float u = FORM == GEAR_GATE_VALUE ? xv[j] : w * xv[j];
-                        h[j] = z ? u : fmaf(f, h[j], u);
-                        if (MAPS) P[j] *= f;
-                    }
-                    if (!MAPS && a.y) Vec<E, VE>::store(y + s * a.D, h);
-                } else if (!MAPS && s < room && a.y) {
-                    const float zero[VE] = {};
-                    Vec<E, VE>::store(y + s * a.D, zero);
-                }
-            }
+            cut |= r != 0;
+            const int mode = mode_of(count, r);
+            if (mode == kPlain) forward_tile<E, VE, FORM, MAPS, kPlain>(a, rows, t0, count, room, r, h, P);
+            else if (mode == kCuts) forward_tile<E, VE, FORM, MAPS, kCuts>(a, rows, t0, count, room, r, h, P);
+            else forward_tile<E, VE, FORM, MAPS, kAny>(a, rows, t0, count, room, r, h, P);
         }
         if (MAPS) {
 #pragma unroll
@@ -178,25 +221,117 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(const Args a) {
 }
 
 // Applies every channel's maps in order (the last segment first when
-// BACKWARD) and leaves the value each segment starts from in its map.
+// BACKWARD) and leaves the value each segment starts from in its map.  A
+// workgroup takes 64 channels; its waves compose a run of segments each, the
+// runs' maps lead to every run's first value, and the waves go through their
+// runs again.  (A thread per channel took 261 us for 1024 segments of 512.)
+constexpr int kCarryWaves = 16, kCarryAhead = 8;
 template <bool BACKWARD>
-__global__ __launch_bounds__(kThreads) void carry_kernel(Map* __restrict__ maps, const float* __restrict__ first,
-                                                         int64_t channels, int32_t S) {
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < channels; i += (int64_t)gridDim.x * kThreads) {
-        float c = first ? first[i] : 0.0f;
-        for (int32_t s = 0; s < S; s++) {
-            Map* m = maps + (BACKWARD ? S - 1 - s : s) * channels + i;
-            const Map v = *m;
-            m->P = c;
-            c = apply(v, c);
+__global__ __launch_bounds__(64 * kCarryWaves) void carry_kernel(Map* __restrict__ maps, const float* __restrict__ first,
+                                                                int64_t channels, int32_t S) {
+    __shared__ Map s_run[kCarryWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t i = (int64_t)blockIdx.x * 64 + lane;
+    const bool used = i < channels;
+    const int32_t run = (S + kCarryWaves - 1) / kCarryWaves;
+    const int32_t s0 = wave * run < S ? wave * run : S, s1 = s0 + run < S ? s0 + run : S;
+    Map whole = {1.0f, 0.0f};
+    if (used) {
+        for (int32_t s = s0; s < s1; s += kCarryAhead) {
+            Map m[kCarryAhead];
+#pragma unroll
+            for (int k = 0; k < kCarryAhead; k++)
+                if (s + k < s1) m[k] = maps[(BACKWARD ? S - 1 - (s + k) : s + k) * channels + i];
+#pragma unroll
+            for (int k = 0; k < kCarryAhead; k++)
+                if (s + k < s1) whole = compose(m[k], whole);
+        }
+    }
+    s_run[wave][lane] = whole;
+    __syncthreads();
+    if (!used) return;
+    float c = first ? first[i] : 0.0f;
+    for (int k = 0; k < wave; k++) c = apply(s_run[k][lane], c);
+    for (int32_t s = s0; s < s1; s += kCarryAhead) {
+        Map m[kCarryAhead];
+#pragma unroll
+        for (int k = 0; k < kCarryAhead; k++)
+            if (s + k < s1) m[k] = maps[(BACKWARD ? S - 1 - (s + k) : s + k) * channels + i];
+#pragma unroll
+        for (int k = 0; k < kCarryAhead; k++) {
+            if (s + k < s1) {
+                maps[(BACKWARD ? S - 1 - (s + k) : s + k) * channels + i].P = c;
+                c = apply(m[k], c);
+            }
+        }
+    }
+}
+
+// A tile backward: G comes in as the gradient of the state after it and goes
+// out as that of the state before it.  h is the state before it, from which
+// the states inside are recomputed in 32 bits: read back from y they would carry
+// its rounding into h_{t-1} - x_t.
+template <typename E, int VE, int FORM, bool MAPS, int MODE>
+__device__ __forceinline__ void backward_tile(const Args& a, const Rows<E>& rows, int64_t t0, int count, int room,
+                                              uint32_t r, float (&h)[VE], float (&G)[VE], float (&P)[VE]) {
+#pragma clang fp contract(off)  // as forward_tile
+    Tile<E, VE> g, x, d;
+    g.template load<MODE>(rows.gate + t0 * a.gate_t, a.gate_t, count);
+    if (!MAPS) x.template load<MODE>(rows.x + t0 * a.x_t, a.x_t, count);
+    if (rows.dy) d.template load<MODE>(rows.dy + t0 * a.dy_t, a.dy_t, count);
+    // Per step: decay, input weight, and what the gate's gradient is a multiple of.
+    float F[kSteps][VE], W[kSteps][VE], Q[kSteps][VE];
+#pragma unroll
+    for (int s = 0; s < kSteps; s++) {
+        if (MODE != kAny || s < count) {
+            float gv[VE], xv[VE];
+            Vec<E, VE>::unpack(g.v[s], gv);
+            if (!MAPS) Vec<E, VE>::unpack(x.v[s], xv);
+            const bool z = MODE != kPlain && ((r >> s) & 1u);
+#pragma unroll
+            for (int j = 0; j < VE; j++) {
+                gates<FORM>(gv[j], F[s][j], W[s][j]);
+                if (!MAPS) {
+                    const float before = z ? 0.0f : h[j];
+                    const float u = FORM == GEAR_GATE_VALUE ? xv[j] : W[s][j] * xv[j];
+                    Q[s][j] = FORM == GEAR_GATE_VALUE ? before : before - xv[j];
+                    h[j] = z ? u : fmaf(F[s][j], h[j], u);
+                }
+            }
+        }
+    }
+    E* dgate = rows.dgate + t0 * a.D;
+    E* dx = rows.dx + t0 * a.D;
+#pragma unroll
+    for (int s = kSteps - 1; s >= 0; s--) {
+        if (MODE != kAny || s < count) {
+            float dv[VE] = {}, og[VE], ox[VE];
+            if (rows.dy) Vec<E, VE>::unpack(d.v[s], dv);
+            const bool z = MODE != kPlain && ((r >> s) & 1u);
+#pragma unroll
+            for (int j = 0; j < VE; j++) {
+                const float f = F[s][j], t = G[j] + dv[j];
+                if (!MAPS) {
+                    ox[j] = FORM == GEAR_GATE_VALUE ? t : t * W[s][j];
+                    og[j] = FORM == GEAR_GATE_VALUE ? t * Q[s][j] : ox[j] * Q[s][j] * f;
+                }
+                G[j] = z ? 0.0f : f * t;
+                if (MAPS) P[j] *= f;
+            }
+            if (!MAPS) {
+                Vec<E, VE>::store(dgate + s * a.D, og);
+                Vec<E, VE>::store(dx + s * a.D, ox);
+            }
+        } else if (!MAPS && s < room) {
+            const float zero[VE] = {};
+            Vec<E, VE>::store(dgate + s * a.D, zero);
+            Vec<E, VE>::store(dx + s * a.D, zero);
         }
     }
 }
 
 // Segments backward: with MAPS, reduces each to what it does to the gradient
-// that comes in at its end; else the gradients.  The states inside a tile are
-// recomputed in 32 bits from the state saved before it: read back from y they
-// would carry its rounding into h_{t-1} - x_t.
+// that comes in at its end; else the gradients.
 template <typename E, int VE, int FORM, bool MAPS>
 __global__ __launch_bounds__(kThreads) void backward_kernel(const Args a) {
     const int64_t BD = a.B * a.D, tiles = (a.T + kSteps - 1) / kSteps;
@@ -204,6 +339,7 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(const Args a) {
          i += (int64_t)gridDim.x * kThreads) {
         const int64_t seg = i / a.lanes;
         const Place p = place_of<VE>(a, i - seg * a.lanes);
+        const Rows<E> rows = rows_of<E>(a, p);
         const int64_t at = p.b * a.D + p.c;
         float G[VE], P[VE];
         bool cut = false;
@@ -218,75 +354,19 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(const Args a) {
             const int64_t t0 = k * kSteps;
             const int count = clamp_count(p.n - t0), room = clamp_count(a.T - t0);
             const uint32_t r = resets(a, p.b, t0, count);
-            Tile<E, VE> g, x, d;
-            g.load(static_cast<const E*>(a.gate) + p.b * a.gate_b + t0 * a.gate_t + p.c, a.gate_t, count);
-            if (a.dy) d.load(static_cast<const E*>(a.dy) + p.b * a.dy_b + t0 * a.dy_t + p.c, a.dy_t, count);
-            float before[MAPS ? 1 : kSteps][VE];
-            if (!MAPS) {
-                x.load(static_cast<const E*>(a.x) + p.b * a.x_b + t0 * a.x_t + p.c, a.x_t, count);
-                float h[VE] = {};
-                if (k > 0) {
-                    if (count > 0) {
+            cut |= r != 0;
+            float h[VE] = {};
+            if (!MAPS && count > 0) {
+                const float* from = k > 0 ? a.saved + (k - 1) * BD + at : a.state ? a.state + at : nullptr;
+                if (from) {
 #pragma unroll
-                        for (int j = 0; j < VE; j++) h[j] = a.saved[(k - 1) * BD + at + j];
-                    }
-                } else if (a.state) {
-#pragma unroll
-                    for (int j = 0; j < VE; j++) h[j] = a.state[at + j];
-                }
-#pragma unroll
-                for (int s = 0; s < kSteps; s++) {
-                    if (s < count) {
-                        float gv[VE], xv[VE];
-                        Vec<E, VE>::unpack(g.v[s], gv);
-                        Vec<E, VE>::unpack(x.v[s], xv);
-                        const bool z = (r >> s) & 1u;
-#pragma unroll
-                        for (int j = 0; j < VE; j++) {
-                            float f, w;
-                            gates<FORM>(gv[j], f, w);
-                            before[MAPS ? 0 : s][j] = z ? 0.0f : h[j];
-                            const float u = FORM == GEAR_GATE_VALUE ? xv[j] : w * xv[j];
-                            h[j] = z ? u : fmaf(f, h[j], u);
-                        }
-                    }
+                    for (int j = 0; j < VE; j++) h[j] = from[j];
                 }
             }
-            E* dgate = static_cast<E*>(a.dgate) + (p.b * a.T + t0) * a.D + p.c;
-            E* dx = static_cast<E*>(a.dx) + (p.b * a.T + t0) * a.D + p.c;
-#pragma unroll
-            for (int s = kSteps - 1; s >= 0; s--) {
-                if (s < count) {
-                    float gv[VE], dv[VE] = {}, og[VE], ox[VE];
-                    Vec<E, VE>::unpack(g.v[s], gv);
-                    if (a.dy) Vec<E, VE>::unpack(d.v[s], dv);
-                    float xv[VE] = {};
-                    if (!MAPS) Vec<E, VE>::unpack(x.v[s], xv);
-                    const bool z = (r >> s) & 1u;
-                    cut |= z;
-#pragma unroll
-                    for (int j = 0; j < VE; j++) {
-                        float f, w;
-                        gates<FORM>(gv[j], f, w);
-                        const float t = G[j] + dv[j];
-                        if (!MAPS) {
-                            const float hp = before[MAPS ? 0 : s][j];
-                            og[j] = FORM == GEAR_GATE_VALUE ? t * hp : t * (hp - xv[j]) * f * w;
-                            ox[j] = FORM == GEAR_GATE_VALUE ? t : t * w;
-                        }
-                        G[j] = z ? 0.0f : f * t;
-                        if (MAPS) P[j] *= f;
-                    }
-                    if (!MAPS) {
-                        Vec<E, VE>::store(dgate + s * a.D, og);
-                        Vec<E, VE>::store(dx + s * a.D, ox);
-                    }
-                } else if (!MAPS && s < room) {
-                    const float zero[VE] = {};
-                    Vec<E, VE>::store(dgate + s * a.D, zero);
-                    Vec<E, VE>::store(dx + s * a.D, zero);
-                }
-            }
+            const int mode = mode_of(count, r);
+            if (mode == kPlain) backward_tile<E, VE, FORM, MAPS, kPlain>(a, rows, t0, count, room, r, h, G, P);
+            else if (mode == kCuts) backward_tile<E, VE, FORM, MAPS, kCuts>(a, rows, t0, count, room, r, h, G, P);
+            else backward_tile<E, VE, FORM, MAPS, kAny>(a, rows, t0, count, room, r, h, G, P);
         }
         if (MAPS) {
 #pragma unroll
@@ -300,18 +380,19 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(const Args a) {
 
 typedef void (*Kernel)(const Args);
 struct Kernels {
-    Kernel fwd_maps, fwd, bwd_maps, bwd;
+    Kernel maps, whole;
 };
-template <typename E, int VE, int FORM>
+template <typename E, int VE, int FORM, bool BACKWARD>
 Kernels kernels_of() {
-    return {forward_kernel<E, VE, FORM, true>, forward_kernel<E, VE, FORM, false>,
-            backward_kernel<E, VE, FORM, true>, backward_kernel<E, VE, FORM, false>};
+    if constexpr (BACKWARD) return {backward_kernel<E, VE, FORM, true>, backward_kernel<E, VE, FORM, false>};
+    else return {forward_kernel<E, VE, FORM, true>, forward_kernel<E, VE, FORM, false>};
 }
-template <typename E>
+template <typename E, bool BACKWARD>
 Kernels kernels_for(int32_t form, bool wide) {
-    constexpr int VE = 8 / sizeof(E);
-    if (form == GEAR_GATE_VALUE) return wide ? kernels_of<E, VE, GEAR_GATE_VALUE>() : kernels_of<E, 1, GEAR_GATE_VALUE>();
-    return wide ? kernels_of<E, VE, GEAR_GATE_SIGMOID>() : kernels_of<E, 1, GEAR_GATE_SIGMOID>();
+    constexpr int VE = (BACKWARD ? kBackwardBytes : kForwardBytes) / sizeof(E);
+    if (form == GEAR_GATE_VALUE)
+        return wide ? kernels_of<E, VE, GEAR_GATE_VALUE, BACKWARD>() : kernels_of<E, 1, GEAR_GATE_VALUE, BACKWARD>();
+    return wide ? kernels_of<E, VE, GEAR_GATE_SIGMOID, BACKWARD>() : kernels_of<E, 1, GEAR_GATE_SIGMOID, BACKWARD>();
 }
 
 // How a call is cut: channels per lane, lanes, segments.
@@ -320,9 +401,9 @@ struct Plan {
     int64_t groups, lanes, tiles, seg_tiles;
     int32_t S;
 };
-Plan plan_of(const gear_recurrence_desc& d, bool in_place) {
+Plan plan_of(const gear_recurrence_desc& d, bool backward, bool in_place) {
     Plan p;
-    const int full = 8 / float_bytes(d.dtype);
+    const int full = (backward ? kBackwardBytes : kForwardBytes) / float_bytes(d.dtype);
     // Widths below a lane's are taken channel by channel, as are odd ones
     // whose states are updated in place: lanes that share channels must not
     // read what another has written.
@@ -338,8 +419,8 @@ Plan plan_of(const gear_recurrence_desc& d, bool in_place) {
     return p;
 }
 int64_t work_bytes_of(const gear_recurrence_desc& d) {
-    const Plan p = plan_of(d, false);
-    return p.S > 1 ? (int64_t)p.S * d.B * d.D * (int64_t)sizeof(Map) : 0;
+    const int32_t f = plan_of(d, false, false).S, b = plan_of(d, true, false).S, S = f > b ? f : b;
+    return S > 1 ? (int64_t)S * d.B * d.D * (int64_t)sizeof(Map) : 0;
 }
 int64_t saved_bytes_of(const gear_recurrence_desc& d) {
     const int64_t tiles = (d.T + kSteps - 1) / kSteps;
@@ -367,18 +448,18 @@ const char* flaw(const gear_recurrence_desc* d) {
 
 template <typename E>
 int run(const Args& base, const Plan& p, int32_t form, bool backward, const char* what, hipStream_t s) {
-    const Kernels k = kernels_for<E>(form, p.ve > 1);
+    const Kernels k = backward ? kernels_for<E, true>(form, p.ve > 1) : kernels_for<E, false>(form, p.ve > 1);
     const int64_t BD = base.B * base.D;
     if (p.S > 1) {
-        hipLaunchKernelGGL(backward ? k.bwd_maps : k.fwd_maps, dim3(blocks_for(p.lanes * p.S)), dim3(kThreads), 0, s, base);
+        hipLaunchKernelGGL(k.maps, dim3(blocks_for(p.lanes * p.S)), dim3(kThreads), 0, s, base);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return hip_fail(e, what);
-        hipLaunchKernelGGL(backward ? carry_kernel<true> : carry_kernel<false>, dim3(blocks_for(BD)), dim3(kThreads), 0,
-                           s, base.maps, backward ? base.dfinal : base.state, BD, p.S);
+        hipLaunchKernelGGL(backward ? carry_kernel<true> : carry_kernel<false>, dim3((unsigned)((BD + 63) / 64)),
+                           dim3(64 * kCarryWaves), 0, s, base.maps, backward ? base.dfinal : base.state, BD, p.S);
         e = hipGetLastError();
         if (e != hipSuccess) return hip_fail(e, what);
     }
-    hipLaunchKernelGGL(backward ? k.bwd : k.fwd, dim3(blocks_for(p.lanes * p.S)), dim3(kThreads), 0, s, base);
+    hipLaunchKernelGGL(k.whole, dim3(blocks_for(p.lanes * p.S)), dim3(kThreads), 0, s, base);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? GEAR_OK : hip_fail(e, what);
 }
@@ -437,7 +518,7 @@ extern "C" int gear_recurrence(const gear_recurrence_desc* d, const void* d_gate
     const int64_t need = work_bytes_of(*d);
     if (need > 0 && (d_work == nullptr || work_bytes < need))
         return fail(GEAR_E_INVAL, "gear_recurrence: workspace smaller than gear_recurrence_sizes states");
-    const Plan p = plan_of(*d, in_place);
+    const Plan p = plan_of(*d, false, in_place);
     Args a = args_of(*d, p, d_work);
     a.gate = d_gate;
     a.x = d_x;
@@ -462,7 +543,7 @@ extern "C" int gear_recurrence_backward(const gear_recurrence_desc* d, const voi
     const int64_t need = work_bytes_of(*d);
     if (need > 0 && (d_work == nullptr || work_bytes < need))
         return fail(GEAR_E_INVAL, "gear_recurrence_backward: workspace smaller than gear_recurrence_sizes states");
-    const Plan p = plan_of(*d, false);
+    const Plan p = plan_of(*d, true, false);
     Args a = args_of(*d, p, d_work);
     a.gate = d_gate;
     a.x = d_x;
