@@ -27,11 +27,14 @@ struct Vec {
 #pragma unroll
         for (int j = 0; j < N; j++) f[j] = w[j];
     }
-    static __device__ __forceinline__ void store(E* p, const float (&f)[N]) {
+    static __device__ __forceinline__ raw round(const float (&f)[N]) {
         wide w;
 #pragma unroll
         for (int j = 0; j < N; j++) w[j] = f[j];
-        const raw v = __builtin_convertvector(w, raw);
+        return __builtin_convertvector(w, raw);
+    }
+    static __device__ __forceinline__ void store(E* p, const float (&f)[N]) {
+        const raw v = round(f);
         __builtin_memcpy(p, &v, sizeof(v));
     }
 };

@@ -17,7 +17,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kSums = 5;               // loss, clipped term, KL term, entropy, clipped rows
 constexpr int kCountBlocks = 512;      // workgroups that count the rows that take part
-constexpr int kMaxBlocks = 2048;       // workgroups of the row kernels
+constexpr int kMaxBlocks = 1024;       // workgroups of the row kernels
 constexpr int kSoloThreads = 1024;     // calls of one workgroup
 constexpr int64_t kSoloLogits = 1 << 15, kSoloActions = 1024;
 constexpr int64_t kCountOff = 0, kSumOff = kCountBlocks * (int64_t)sizeof(int64_t);
@@ -85,23 +85,37 @@ __device__ __forceinline__ T group_add(T v) {
     return v;
 }
 
-// Sum of one value per lane over the workgroup, in thread 0; `s` holds a value per wave.
+// Sum of one value per lane over the workgroup, in the first wave's lanes; `s` holds a value per wave.
 template <int THREADS, typename T>
 __device__ __forceinline__ T block_add(T v, T* s) {
     v = group_add<64>(v);
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
     __syncthreads();
-    if (threadIdx.x == 0)
-        for (int k = 1; k < THREADS / 64; k++) v += s[k];
-    return v;
+    return group_add<THREADS / 64>(s[threadIdx.x % (THREADS / 64)]);
 }
 
+// Rows that take part, of which a thread takes 16 neighbouring ones at a time.
+constexpr int kCountRows = 16;
 template <int THREADS>
 __device__ __forceinline__ int64_t count_rows(const Args& a, int64_t* s) {
     int64_t c = 0;
-#pragma unroll 8
-    for (int64_t r = (int64_t)blockIdx.x * THREADS + threadIdx.x; r < a.n; r += (int64_t)gridDim.x * THREADS)
-        c += takes_part(a, r, action_of(a, r)) ? 1 : 0;
+    for (int64_t r = ((int64_t)blockIdx.x * THREADS + threadIdx.x) * kCountRows; r < a.n;
+         r += (int64_t)gridDim.x * THREADS * kCountRows) {
+        if (a.action_dtype == GEAR_DTYPE_I32 && a.mask_group.d == 1 && r + kCountRows <= a.n) {
+            int32_t act[kCountRows];
+            uint32_t mask[kCountRows / 4];
+            __builtin_memcpy(act, static_cast<const int32_t*>(a.action) + r, sizeof(act));
+            if (a.mask) __builtin_memcpy(mask, a.mask + r, sizeof(mask));
+#pragma unroll
+            for (int k = 0; k < kCountRows; k++) {
+                const bool on = a.mask == nullptr || ((mask[k / 4] >> (8 * (k % 4))) & 0xFFu) != 0;
+                c += on && (uint32_t)act[k] < (uint32_t)a.V ? 1 : 0;
+            }
+        } else {
+            const int64_t end = r + kCountRows < a.n ? r + kCountRows : a.n;
+            for (int64_t k = r; k < end; k++) c += takes_part(a, k, action_of(a, k)) ? 1 : 0;
+        }
+    }
     return block_add<THREADS>(c, s);
 }
 
@@ -116,6 +130,7 @@ __global__ __launch_bounds__(kThreads) void count_kernel(const Args a) {
 __device__ __forceinline__ float denominator(const Args& a) {
     if (a.denom > 0.0f) return a.denom;
     int64_t c = 0;
+#pragma unroll 8
     for (int k = threadIdx.x & 63; k < a.count_blocks; k += 64) c += a.counts[k];
     c = group_add<64>(c);
     return c > 0 ? (float)c : 1.0f;
@@ -128,6 +143,27 @@ struct Scale {
     __device__ __forceinline__ float operator()(float z) const { return (z - m) * kLog2e; }
 };
 __device__ __forceinline__ Scale scale_of(float m) { return Scale{m == -INFINITY ? 0.0f : m}; }  // a row of -inf sums to 0
+
+// Adds a piece's 2^d and d 2^d.
+template <int VE>
+__device__ __forceinline__ void add_piece(const float (&f)[VE], const Scale& dist, float& S, float& dS) {
+#pragma unroll
+    for (int j = 0; j < VE; j++) {
+        const float d = dist(f[j]), e = __builtin_amdgcn_exp2f(d);
+        S += e;
+        dS = fmaf(e, fmaxf(d, kFloor), dS);
+    }
+}
+
+// Sums against logit m become sums against logit `top`, which is no smaller.
+struct Sums {
+    float m, S, dS;
+};
+__device__ __forceinline__ void rescale(float m, float top, float& S, float& dS) {
+    const float d = fmaxf((m - scale_of(top).m) * kLog2e, kFloor), e = __builtin_amdgcn_exp2f(d);
+    dS = e * fmaf(d, S, dS);
+    S *= e;
+}
 
 // What a row has beside its logits, read while they are on their way.
 struct Inputs {
@@ -219,11 +255,19 @@ __device__ __forceinline__ Slope slope_of(const Args& a, const Row& r, float S) 
 
 // The sums of a call that one workgroup ran, or this workgroup's share of them.
 template <int THREADS, bool SOLO>
-__device__ __forceinline__ void leave_sums(const Args& a, const float (&total)[kSums], float denom, double* s) {
+__device__ __forceinline__ void leave_sums(const Args& a, const float (&total)[kSums], float denom,
+                                           double (*s)[THREADS / 64]) {
+    constexpr int kWaves = THREADS / 64;
 #pragma unroll
     for (int k = 0; k < kSums; k++) {
-        __syncthreads();
-        const double v = block_add<THREADS>((double)total[k], s);
+        const double v = group_add<64>((double)total[k]);
+        if ((threadIdx.x & 63) == 0) s[k][threadIdx.x >> 6] = v;
+    }
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+#pragma unroll
+    for (int k = 0; k < kSums; k++) {
+        const double v = group_add<kWaves>(s[k][threadIdx.x % kWaves]);
         if (threadIdx.x == 0) {
             if (!SOLO) a.sums[k * kMaxBlocks + blockIdx.x] = (float)v;
             else if (k == 0) *a.loss = (float)(v / (double)denom);
@@ -247,7 +291,14 @@ struct Piece {
         for (int k = 0; k < kPerWord; k++) f[k] = e[k] - (E)INFINITY;
         return __builtin_bit_cast(uint32_t, f);
     }
-    __device__ __forceinline__ void load(const E* p) { __builtin_memcpy(&w, p, sizeof(w)); }
+    typedef words loose __attribute__((aligned(2)));
+    // Streaming loads where a wave takes whole lines of a row: 8% of the time at
+    // 32768 actions.  Where it takes parts of many rows' lines, the rest has to stay in the cache.
+    template <bool STREAM>
+    __device__ __forceinline__ void load(const E* p) {
+        if (STREAM) w = __builtin_nontemporal_load(reinterpret_cast<const loose*>(p));
+        else w = *reinterpret_cast<const loose*>(p);
+    }
     __device__ __forceinline__ void fill() { w = words{lowest(), lowest(), lowest(), lowest()}; }
     // The first n elements become -inf.
     __device__ __forceinline__ void drop(int n) {
@@ -288,34 +339,60 @@ struct Piece {
     __device__ __forceinline__ void forget() { asm volatile("" : "+v"(w)); }
 };
 
+// Lane `mine`'s pieces i0 .. i0 + N - 1 of a row, one in G: past the row's end, the
+// rest of its last piece that no other lane has, or -inf.
+template <typename E, int G, int N>
+__device__ __forceinline__ void load_row(Piece<E> (&v)[N], const E* z, int V, int mine, int i0) {
+    constexpr int VE = Piece<E>::VE;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const int first = (i0 + i) * G * VE;
+        if (first + G * VE <= V) {
+            v[i].template load<(G >= 64)>(z + first + mine * VE);
+        } else if (first < V) {
+            const int base = first + mine * VE, over = base + VE - V;
+            v[i].template load<(G >= 64)>(z + (over < 0 ? base : V - VE));
+            if (over > 0) v[i].drop(over);
+        } else {
+            v[i].fill();
+        }
+    }
+}
+
 // Rows held in registers: G lanes share a row, each with up to NV pieces of 16
 // bytes every G pieces, so that a row is read once and its gradient written
 // once.  A lane past the end of its row reads the row's last piece and keeps of
 // it what no other lane has; with TINY, rows are shorter than a piece.
 template <typename E, int G, int NV, int THREADS, bool TINY, bool LOSS>
-__global__ __launch_bounds__(THREADS) void held_kernel(const Args a) {
+__global__ __launch_bounds__(THREADS, LOSS ? 4 : 8) void held_kernel(const Args a) {
     constexpr int VE = 16 / sizeof(E), kGroups = THREADS / G, kWaves = THREADS / 64;
     constexpr bool kBlock = G > 64;  // the whole workgroup shares a row
+    // Without a gradient nothing need be held, and few registers let two long rows share a CU.
+    constexpr int kHeld = LOSS || !kBlock ? NV : 4;
     constexpr bool kSolo = THREADS == kSoloThreads && !kBlock;  // the one workgroup of its call
     static_assert(!kBlock || G == THREADS, "one row at a time");
-    __shared__ float s_max[kWaves], s_sum[kWaves], s_dsum[kWaves], s_za;
-    __shared__ double s_add[kWaves];
-    __shared__ int64_t s_count;
-    __shared__ Inputs s_in[2];  // in turn: read after the row's last barrier
+    __shared__ double s_add[kSums][kWaves];
+    __shared__ int64_t s_count[kWaves];
+    // Rows take these in turn: a row's are read after its only barrier.
+    __shared__ Sums s_wave[2][kBlock ? kWaves : 1];
+    __shared__ Inputs s_in[2];
+    __shared__ float s_za[2];
     const int lane = threadIdx.x % G, V = (int)a.V;  // at most 2^17 elements are held
     float denom = 1.0f, scale = 1.0f;
     if (LOSS) {
         if (kSolo && !(a.denom > 0.0f)) {
-            const int64_t c = count_rows<THREADS>(a, reinterpret_cast<int64_t*>(s_add));
-            if (threadIdx.x == 0) s_count = c;
-            __syncthreads();
-            denom = s_count > 0 ? (float)s_count : 1.0f;
+            const int64_t c = count_rows<THREADS>(a, s_count);
+            denom = c > 0 ? (float)c : 1.0f;
         } else {
             denom = denominator(a);
         }
         scale = a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / denom;
     }
+    // Lane 0 of every group adds its rows' terms; a workgroup's only one keeps them in LDS, where they take no registers.
+    __shared__ float s_total[kSums];
     float total[kSums] = {};
+    if (kBlock && LOSS && threadIdx.x < kSums) s_total[threadIdx.x] = 0.0f;
+    __syncthreads();
     int turn = 0;
     for (int64_t first = (int64_t)blockIdx.x * kGroups; first < a.n; first += (int64_t)gridDim.x * kGroups) {
         const int64_t row = first + (kBlock ? 0 : threadIdx.x / G);
@@ -339,94 +416,99 @@ __global__ __launch_bounds__(THREADS) void held_kernel(const Args a) {
             continue;
         }
         const E* z = static_cast<const E*>(a.logits) + row * a.row_stride;
-        Piece<E> v[NV];
+        Piece<E> v[kHeld];
         float za = 0.0f;
         Inputs in{};
         // The lane's number, hidden so that what follows from it for each piece is not kept from row to row.
         int mine = lane;
         asm volatile("" : "+v"(mine));
         if (on) {
-#pragma unroll
-            for (int i = 0; i < NV; i++) {
-                if (TINY) {
-                    v[i].gather(z, V);
-                } else if ((i + 1) * G * VE <= V) {
-                    v[i].load(z + i * G * VE + mine * VE);
-                } else if (i * G * VE < V) {
-                    const int base = (i * G + mine) * VE, over = base + VE - V;
-                    v[i].load(z + (over < 0 ? base : V - VE));
-                    if (over > 0) v[i].drop(over);
-                } else {
-                    v[i].fill();
-                }
-            }
+            if (TINY) v[0].gather(z, V);
+            else if (kHeld == NV) load_row<E, G>(v, z, V, mine, 0);
             if (!kBlock || threadIdx.x == 0) {
                 za = (float)z[action];
                 if (LOSS) in = inputs_of(a, row);
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < NV; i++) v[i].fill();
+            for (int i = 0; i < kHeld; i++) v[i].fill();
         }
-        float m = -INFINITY;
+        float m = -INFINITY, S = 0.0f, dS = 0.0f;
+        if (!kBlock) {
 #pragma unroll
-        for (int i = 0; i < NV; i++) {
-            float f[VE];
-            v[i].unpack(f);
+            for (int i = 0; i < NV; i++) {
+                float f[VE];
+                v[i].unpack(f);
 #pragma unroll
-            for (int j = 0; j < VE; j++) m = fmaxf(m, f[j]);
-            v[i].forget();
-        }
-        m = group_max<kBlock ? 64 : G>(m);
-        if (kBlock) {
-            if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = m;
+                for (int j = 0; j < VE; j++) m = fmaxf(m, f[j]);
+                v[i].forget();
+            }
+            m = group_max<G < 64 ? G : 64>(m);
+            const Scale dist = scale_of(m);
+#pragma unroll
+            for (int i = 0; i < NV; i++) {
+                float f[VE];
+                v[i].unpack(f);
+                add_piece(f, dist, S, dS);
+                v[i].forget();
+            }
+            S = group_add<G < 64 ? G : 64>(S);
+            dS = group_add<G < 64 ? G : 64>(dS);
+        } else {
+            // Each lane sums its pieces two at a time as they arrive, against the largest logit it has seen.
+#pragma unroll 1
+            for (int i0 = 0; i0 < NV; i0 += kHeld) {
+                if (kHeld < NV) load_row<E, G>(v, z, V, mine, i0);
+#pragma unroll
+                for (int i = 0; i < kHeld; i += 2) {
+                    if ((i0 + i) * G * VE < V) {
+                        float f[VE], h[VE];
+                        v[i].unpack(f);
+                        v[i + 1].unpack(h);
+                        float top = m;
+#pragma unroll
+                        for (int j = 0; j < VE; j++) top = fmaxf(fmaxf(top, f[j]), h[j]);
+                        rescale(m, top, S, dS);
+                        m = top;
+                        add_piece(f, scale_of(m), S, dS);
+                        add_piece(h, scale_of(m), S, dS);
+                        v[i].forget();
+                        v[i + 1].forget();
+                    }
+                }
+            }
+            const float top = group_max<64>(m);
+            rescale(m, top, S, dS);
+            S = group_add<64>(S);
+            dS = group_add<64>(dS);
+            if ((threadIdx.x & 63) == 0) s_wave[turn][threadIdx.x >> 6] = Sums{top, S, dS};
             if (threadIdx.x == 0) {
-                s_za = za;
+                s_za[turn] = za;
                 s_in[turn] = in;
             }
             __syncthreads();
-#pragma unroll
-            for (int k = 0; k < kWaves; k++) m = fmaxf(m, s_max[k]);
-            za = s_za;
-        }
-        const Scale dist = scale_of(m);
-        float S = 0.0f, dS = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NV; i++) {
-            float f[VE];
-            v[i].unpack(f);
-#pragma unroll
-            for (int j = 0; j < VE; j++) {
-                const float d = dist(f[j]), e = __builtin_amdgcn_exp2f(d);
-                S += e;
-                dS = fmaf(e, fmaxf(d, kFloor), dS);
-            }
-            v[i].forget();
-        }
-        S = group_add<kBlock ? 64 : G>(S);
-        dS = group_add<kBlock ? 64 : G>(dS);
-        if (kBlock) {
-            if ((threadIdx.x & 63) == 0) {
-                s_sum[threadIdx.x >> 6] = S;
-                s_dsum[threadIdx.x >> 6] = dS;
-            }
-            __syncthreads();
-            S = dS = 0.0f;
-#pragma unroll
-            for (int k = 0; k < kWaves; k++) {
-                S += s_sum[k];
-                dS += s_dsum[k];
-            }
+            const Sums w = s_wave[turn][threadIdx.x % kWaves];
+            m = group_max<kWaves>(w.m);
+            S = w.S;
+            dS = w.dS;
+            rescale(w.m, m, S, dS);
+            S = group_add<kWaves>(S);
+            dS = group_add<kWaves>(dS);
+            za = s_za[turn];
             in = s_in[turn];
             turn ^= 1;
         }
+        const Scale dist = scale_of(m);
         Row r{};
         if (on) r = row_terms<LOSS>(a, in, m, S, dS, dist(za), scale);
         if (used && lane == 0) {
             if (a.logp) a.logp[row] = r.lp;
             if (a.entropy) a.entropy[row] = r.H;
 #pragma unroll
-            for (int k = 0; k < kSums; k++) total[k] += r.sums[k];
+            for (int k = 0; k < kSums; k++) {
+                if (kBlock && LOSS) s_total[k] += r.sums[k];
+                else total[k] += r.sums[k];
+            }
         }
         if (LOSS && a.grad && used) {
             // Rows without part or distribution hold only -inf, and get zeros.
@@ -435,7 +517,7 @@ __global__ __launch_bounds__(THREADS) void held_kernel(const Args a) {
             const Slope slope = some ? slope_of(a, r, S) : Slope{};
             asm volatile("" : "+v"(mine));
 #pragma unroll
-            for (int i = 0; i < NV; i++) {
+            for (int i = 0; i < kHeld; i++) {
                 if (i * G * VE < V) {
                     float f[VE], o[VE];
                     v[i].unpack(f);
@@ -457,6 +539,10 @@ __global__ __launch_bounds__(THREADS) void held_kernel(const Args a) {
             if (some && lane == (TINY ? 0 : (int)action / VE % G)) g[action] = (E)(slope(dist(za)) + slope.k2);
         }
     }
+    if (kBlock && LOSS && threadIdx.x == 0) {
+#pragma unroll
+        for (int k = 0; k < kSums; k++) total[k] = s_total[k];
+    }
     if (LOSS) leave_sums<THREADS, kSolo>(a, total, denom, s_add);
 }
 
@@ -465,7 +551,7 @@ template <typename E, bool LOSS>
 __global__ __launch_bounds__(kSoloThreads) void long_kernel(const Args a) {
     constexpr int kWaves = kSoloThreads / 64;
     __shared__ float s_max[kWaves], s_sum[kWaves], s_dsum[kWaves];
-    __shared__ double s_add[kWaves];
+    __shared__ double s_add[kSums][kWaves];
     const int wave = threadIdx.x >> 6;
     const float denom = LOSS ? denominator(a) : 1.0f;
     const float scale = LOSS ? a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / denom : 1.0f;
@@ -684,7 +770,7 @@ extern "C" int gear_policy_loss(const gear_policy_desc* d, const void* d_logits,
     hipError_t e = hipSuccess;
     int blocks = 0;
     if (!solo && !(a.denom > 0.0f)) {
-        const int64_t want = (a.n + kThreads - 1) / kThreads;
+        const int64_t want = (a.n + kThreads * kCountRows - 1) / (kThreads * kCountRows);
         a.count_blocks = (int32_t)(want < 1 ? 1 : want < kCountBlocks ? want : kCountBlocks);
         hipLaunchKernelGGL(count_kernel, dim3(a.count_blocks), dim3(kThreads), 0, s, a);
         e = hipGetLastError();
