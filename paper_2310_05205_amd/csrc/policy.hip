@@ -17,9 +17,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kSums = 5;               // loss, clipped term, KL term, entropy, clipped rows
 constexpr int kCountBlocks = 512;      // workgroups that count the rows that take part
-constexpr int kMaxBlocks = 1024;       // workgroups of the row kernels
+constexpr int kMaxBlocks = 2048;       // workgroups of the row kernels
 constexpr int kSoloThreads = 1024;     // calls of one workgroup
-constexpr int64_t kSoloLogits = 1 << 15, kSoloActions = 1024;
+constexpr int64_t kSoloLogits = 1 << 15, kSoloActions = 1024;  // at most 256 pieces a row
 constexpr int64_t kCountOff = 0, kSumOff = kCountBlocks * (int64_t)sizeof(int64_t);
 // Where a logit's distance stops mattering: 2^d is 0 well above it, and a
 // multiple of it stays finite.
@@ -339,45 +339,58 @@ struct Piece {
     __device__ __forceinline__ void forget() { asm volatile("" : "+v"(w)); }
 };
 
-// Lane `mine`'s pieces i0 .. i0 + N - 1 of a row, one in G: past the row's end, the
-// rest of its last piece that no other lane has, or -inf.
-template <typename E, int G, int N>
-__device__ __forceinline__ void load_row(Piece<E> (&v)[N], const E* z, int V, int mine, int i0) {
+// Lane `mine`'s piece number i of a row shared by G lanes, which take its pieces
+// in turn: past the row's end, the rest of its last piece that no other lane has, or -inf.
+template <typename E, int G>
+__device__ __forceinline__ void load_piece(Piece<E>& v, const E* z, int V, int mine, int i) {
     constexpr int VE = Piece<E>::VE;
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-        const int first = (i0 + i) * G * VE;
-        if (first + G * VE <= V) {
-            v[i].template load<(G >= 64)>(z + first + mine * VE);
-        } else if (first < V) {
-            const int base = first + mine * VE, over = base + VE - V;
-            v[i].template load<(G >= 64)>(z + (over < 0 ? base : V - VE));
-            if (over > 0) v[i].drop(over);
-        } else {
-            v[i].fill();
-        }
+    const int first = i * G * VE;
+    if (first + G * VE <= V) {
+        v.template load<(G >= 64)>(z + first + mine * VE);
+    } else if (first < V) {
+        const int base = first + mine * VE, over = base + VE - V;
+        v.template load<(G >= 64)>(z + (over < 0 ? base : V - VE));
+        if (over > 0) v.drop(over);
+    } else {
+        v.fill();
     }
 }
 
+// Writes the gradient of the elements that load_piece gave to this lane.
+template <typename E, int G, bool TINY>
+__device__ __forceinline__ void store_piece(E* g, const Piece<E>& v, int V, int mine, int i, const Slope& slope,
+                                            const Scale& dist) {
+    constexpr int VE = Piece<E>::VE;
+    const int base = (i * G + mine) * VE;
+    float f[VE], o[VE];
+    v.unpack(f);
+#pragma unroll
+    for (int j = 0; j < VE; j++) o[j] = slope(dist(f[j]));
+    if (!TINY && ((i + 1) * G * VE <= V || base + VE <= V)) {
+        Vec<E, VE>::store(g + base, o);
+    } else {
+        const int at = TINY ? 0 : V - VE;
+#pragma unroll
+        for (int j = 0; j < VE; j++)
+            if (at + j >= base && at + j < V) g[at + j] = (E)o[j];
+    }
+}
+
+// The gradient's factor beside denom, grad_scale's, and the loss's own gradient.
+__device__ __forceinline__ float scale_by(const Args& a, float denom) {
+    return a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / denom;
+}
+
 // Rows held in registers: G lanes share a row, each with up to NV pieces of 16
-// bytes every G pieces, so that a row is read once and its gradient written
-// once.  A lane past the end of its row reads the row's last piece and keeps of
-// it what no other lane has; with TINY, rows are shorter than a piece.
-template <typename E, int G, int NV, int THREADS, bool TINY, bool LOSS>
-__global__ __launch_bounds__(THREADS, LOSS ? 4 : 8) void held_kernel(const Args a) {
-    constexpr int VE = 16 / sizeof(E), kGroups = THREADS / G, kWaves = THREADS / 64;
-    constexpr bool kBlock = G > 64;  // the whole workgroup shares a row
-    // Without a gradient nothing need be held, and few registers let two long rows share a CU.
-    constexpr int kHeld = LOSS || !kBlock ? NV : 4;
-    constexpr bool kSolo = THREADS == kSoloThreads && !kBlock;  // the one workgroup of its call
-    static_assert(!kBlock || G == THREADS, "one row at a time");
+// bytes, so that a row is read once and its gradient written once.  With TINY,
+// rows are shorter than a piece.
+template <typename E, int G, int NV, int THREADS, int WAVES, bool TINY, bool LOSS>
+__global__ __launch_bounds__(THREADS, WAVES) void held_kernel(const Args a) {
+    constexpr int VE = Piece<E>::VE, kGroups = THREADS / G, kWaves = THREADS / 64;
+    constexpr bool kSolo = THREADS == kSoloThreads;  // the one workgroup of its call
     __shared__ double s_add[kSums][kWaves];
     __shared__ int64_t s_count[kWaves];
-    // Rows take these in turn: a row's are read after its only barrier.
-    __shared__ Sums s_wave[2][kBlock ? kWaves : 1];
-    __shared__ Inputs s_in[2];
-    __shared__ float s_za[2];
-    const int lane = threadIdx.x % G, V = (int)a.V;  // at most 2^17 elements are held
+    const int lane = threadIdx.x % G, V = (int)a.V;
     float denom = 1.0f, scale = 1.0f;
     if (LOSS) {
         if (kSolo && !(a.denom > 0.0f)) {
@@ -386,79 +399,120 @@ __global__ __launch_bounds__(THREADS, LOSS ? 4 : 8) void held_kernel(const Args 
         } else {
             denom = denominator(a);
         }
-        scale = a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / denom;
+        scale = scale_by(a, denom);
     }
-    // Lane 0 of every group adds its rows' terms; a workgroup's only one keeps them in LDS, where they take no registers.
-    __shared__ float s_total[kSums];
-    float total[kSums] = {};
-    if (kBlock && LOSS && threadIdx.x < kSums) s_total[threadIdx.x] = 0.0f;
-    __syncthreads();
-    int turn = 0;
+    float total[kSums] = {};  // of the group's rows, in its lane 0
     for (int64_t first = (int64_t)blockIdx.x * kGroups; first < a.n; first += (int64_t)gridDim.x * kGroups) {
-        const int64_t row = first + (kBlock ? 0 : threadIdx.x / G);
+        const int64_t row = first + threadIdx.x / G;
         const bool used = row < a.n;
         const int64_t action = used ? action_of(a, row) : -1;
         const bool on = used && takes_part(a, row, action);
-        if (kBlock && !on) {  // the same in every lane
-            if (threadIdx.x == 0) {
-                if (a.logp) a.logp[row] = 0.0f;
-                if (a.entropy) a.entropy[row] = 0.0f;
-            }
-            if (LOSS && a.grad) {
-                E* g = static_cast<E*>(a.grad) + row * a.V;
-                const float zero[VE] = {};
-                for (int j = lane * VE; j < V; j += G * VE) {
-                    if (j + VE <= V) Vec<E, VE>::store(g + j, zero);
-                    else
-                        for (int k = j; k < V; k++) g[k] = (E)0.0f;
-                }
-            }
-            continue;
-        }
         const E* z = static_cast<const E*>(a.logits) + row * a.row_stride;
-        Piece<E> v[kHeld];
+        Piece<E> v[NV];
         float za = 0.0f;
         Inputs in{};
         // The lane's number, hidden so that what follows from it for each piece is not kept from row to row.
         int mine = lane;
         asm volatile("" : "+v"(mine));
         if (on) {
-            if (TINY) v[0].gather(z, V);
-            else if (kHeld == NV) load_row<E, G>(v, z, V, mine, 0);
-            if (!kBlock || threadIdx.x == 0) {
+#pragma unroll
+            for (int i = 0; i < NV; i++) {
+                if (TINY) v[i].gather(z, V);
+                else load_piece<E, G>(v[i], z, V, mine, i);
+            }
+            za = (float)z[action];
+            if (LOSS) in = inputs_of(a, row);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; i++) v[i].fill();
+        }
+        float m = -INFINITY, S = 0.0f, dS = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            float f[VE];
+            v[i].unpack(f);
+#pragma unroll
+            for (int j = 0; j < VE; j++) m = fmaxf(m, f[j]);
+            v[i].forget();
+        }
+        m = group_max<G>(m);
+        const Scale dist = scale_of(m);
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            float f[VE];
+            v[i].unpack(f);
+            add_piece(f, dist, S, dS);
+            v[i].forget();
+        }
+        S = group_add<G>(S);
+        dS = group_add<G>(dS);
+        Row r{};
+        if (on) r = row_terms<LOSS>(a, in, m, S, dS, dist(za), scale);
+        if (used && lane == 0) {
+            if (a.logp) a.logp[row] = r.lp;
+            if (a.entropy) a.entropy[row] = r.H;
+#pragma unroll
+            for (int k = 0; k < kSums; k++) total[k] += r.sums[k];
+        }
+        if (LOSS && a.grad && used) {
+            // Rows without part or distribution hold only -inf, and get zeros.
+            E* g = static_cast<E*>(a.grad) + row * a.V;
+            const bool some = on && m != -INFINITY;
+            const Slope slope = some ? slope_of(a, r, S) : Slope{};
+            asm volatile("" : "+v"(mine));
+#pragma unroll
+            for (int i = 0; i < NV; i++)
+                if (i * G * VE < V) store_piece<E, G, TINY>(g, v[i], V, mine, i, slope, dist);
+            // The action's, over the value just written by the same lane.
+            if (some && lane == (TINY ? 0 : (int)action / VE % G)) g[action] = (E)(slope(dist(za)) + slope.k2);
+        }
+    }
+    if (LOSS) leave_sums<THREADS, kSolo>(a, total, denom, s_add);
+}
+
+// Rows that a workgroup shares.  Each lane sums its pieces two at a time as they
+// arrive, against the largest logit it has seen so far, so one barrier a row
+// is enough.  For the gradient a lane holds all its pieces; without one nothing
+// is held, and few registers let two of the longest rows share a CU.
+template <typename E, int NV, int THREADS, bool LOSS>
+__global__ __launch_bounds__(THREADS, LOSS ? 4 : 8) void block_kernel(const Args a) {
+    constexpr int VE = Piece<E>::VE, G = THREADS, kWaves = THREADS / 64, kHeld = LOSS ? NV : 4;
+    // Rows take these in turn: a row's are read after its only barrier.
+    __shared__ Sums s_wave[2][kWaves];
+    __shared__ Inputs s_in[2];
+    __shared__ float s_za[2];
+    __shared__ float s_total[kSums];  // thread 0's
+    __shared__ double s_add[kSums][kWaves];
+    const int V = (int)a.V;  // at most 2^17
+    const float denom = LOSS ? denominator(a) : 1.0f, scale = LOSS ? scale_by(a, denom) : 1.0f;
+    if (threadIdx.x < kSums) s_total[threadIdx.x] = 0.0f;
+    __syncthreads();
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        const int64_t action = action_of(a, row);
+        const E* z = static_cast<const E*>(a.logits) + row * a.row_stride;
+        E* g = static_cast<E*>(a.grad) + row * a.V;
+        // The lane's number, hidden so that what follows from it for each piece is not kept from row to row.
+        int mine = threadIdx.x;
+        asm volatile("" : "+v"(mine));
+        if (takes_part(a, row, action)) {
+            Piece<E> v[kHeld];
+            if (LOSS) {
+#pragma unroll
+                for (int i = 0; i < kHeld; i++) load_piece<E, G>(v[i], z, V, mine, i);
+            }
+            float za = 0.0f, m = -INFINITY, S = 0.0f, dS = 0.0f;
+            Inputs in{};
+            if (threadIdx.x == 0) {
                 za = (float)z[action];
                 if (LOSS) in = inputs_of(a, row);
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < kHeld; i++) v[i].fill();
-        }
-        float m = -INFINITY, S = 0.0f, dS = 0.0f;
-        if (!kBlock) {
-#pragma unroll
-            for (int i = 0; i < NV; i++) {
-                float f[VE];
-                v[i].unpack(f);
-#pragma unroll
-                for (int j = 0; j < VE; j++) m = fmaxf(m, f[j]);
-                v[i].forget();
-            }
-            m = group_max<G < 64 ? G : 64>(m);
-            const Scale dist = scale_of(m);
-#pragma unroll
-            for (int i = 0; i < NV; i++) {
-                float f[VE];
-                v[i].unpack(f);
-                add_piece(f, dist, S, dS);
-                v[i].forget();
-            }
-            S = group_add<G < 64 ? G : 64>(S);
-            dS = group_add<G < 64 ? G : 64>(dS);
-        } else {
-            // Each lane sums its pieces two at a time as they arrive, against the largest logit it has seen.
 #pragma unroll 1
             for (int i0 = 0; i0 < NV; i0 += kHeld) {
-                if (kHeld < NV) load_row<E, G>(v, z, V, mine, i0);
+                if (!LOSS) {
+#pragma unroll
+                    for (int i = 0; i < kHeld; i++) load_piece<E, G>(v[i], z, V, mine, i0 + i);
+                }
 #pragma unroll
                 for (int i = 0; i < kHeld; i += 2) {
                     if ((i0 + i) * G * VE < V) {
@@ -497,53 +551,50 @@ __global__ __launch_bounds__(THREADS, LOSS ? 4 : 8) void held_kernel(const Args 
             za = s_za[turn];
             in = s_in[turn];
             turn ^= 1;
-        }
-        const Scale dist = scale_of(m);
-        Row r{};
-        if (on) r = row_terms<LOSS>(a, in, m, S, dS, dist(za), scale);
-        if (used && lane == 0) {
-            if (a.logp) a.logp[row] = r.lp;
-            if (a.entropy) a.entropy[row] = r.H;
+            const Scale dist = scale_of(m);
+            const Row r = row_terms<LOSS>(a, in, m, S, dS, dist(za), scale);
+            if (threadIdx.x == 0) {
+                if (a.logp) a.logp[row] = r.lp;
+                if (a.entropy) a.entropy[row] = r.H;
 #pragma unroll
-            for (int k = 0; k < kSums; k++) {
-                if (kBlock && LOSS) s_total[k] += r.sums[k];
-                else total[k] += r.sums[k];
+                for (int k = 0; k < kSums; k++)
+                    if (LOSS) s_total[k] += r.sums[k];
             }
-        }
-        if (LOSS && a.grad && used) {
-            // Rows without part or distribution hold only -inf, and get zeros.
-            E* g = static_cast<E*>(a.grad) + row * a.V;
-            const bool some = on && m != -INFINITY;
-            const Slope slope = some ? slope_of(a, r, S) : Slope{};
-            asm volatile("" : "+v"(mine));
+            if (LOSS) {
+                const bool some = m != -INFINITY;
+                const Slope slope = some ? slope_of(a, r, S) : Slope{};
+                asm volatile("" : "+v"(mine));
+                if (a.grad) {
 #pragma unroll
-            for (int i = 0; i < kHeld; i++) {
-                if (i * G * VE < V) {
-                    float f[VE], o[VE];
-                    v[i].unpack(f);
-#pragma unroll
-                    for (int j = 0; j < VE; j++) o[j] = slope(dist(f[j]));
-                    const int base = (i * G + mine) * VE;
-                    if (!TINY && ((i + 1) * G * VE <= V || base + VE <= V)) {
-                        Vec<E, VE>::store(g + base, o);
-                    } else {
-                        // The row's last piece, of which this lane has the last elements, or none.
-                        const int at = TINY ? 0 : V - VE;
-#pragma unroll
-                        for (int j = 0; j < VE; j++)
-                            if (at + j >= base && at + j < V) g[at + j] = (E)o[j];
-                    }
+                    for (int i = 0; i < kHeld; i++)
+                        if (i * G * VE < V) store_piece<E, G, false>(g, v[i], V, mine, i, slope, dist);
+                }
+                // The action's, over the value just written by the same lane.
+                if (a.grad && some && mine == (int)action / VE % G) g[action] = (E)(slope(dist(za)) + slope.k2);
+            }
+        } else {
+            if (threadIdx.x == 0) {
+                if (a.logp) a.logp[row] = 0.0f;
+                if (a.entropy) a.entropy[row] = 0.0f;
+            }
+            if (LOSS && a.grad) {
+                const float zero[VE] = {};
+                for (int j = mine * VE; j < V; j += G * VE) {
+                    if (j + VE <= V) Vec<E, VE>::store(g + j, zero);
+                    else
+                        for (int k = j; k < V; k++) g[k] = (E)0.0f;
                 }
             }
-            // The action's, over the value just written by the same lane.
-            if (some && lane == (TINY ? 0 : (int)action / VE % G)) g[action] = (E)(slope(dist(za)) + slope.k2);
         }
     }
-    if (kBlock && LOSS && threadIdx.x == 0) {
+    if (LOSS) {
+        float total[kSums] = {};
+        if (threadIdx.x == 0) {
 #pragma unroll
-        for (int k = 0; k < kSums; k++) total[k] = s_total[k];
+            for (int k = 0; k < kSums; k++) total[k] = s_total[k];
+        }
+        leave_sums<THREADS, false>(a, total, denom, s_add);
     }
-    if (LOSS) leave_sums<THREADS, kSolo>(a, total, denom, s_add);
 }
 
 // Rows longer than registers hold: a workgroup per row, which reads it three times.
@@ -554,7 +605,7 @@ __global__ __launch_bounds__(kSoloThreads) void long_kernel(const Args a) {
     __shared__ double s_add[kSums][kWaves];
     const int wave = threadIdx.x >> 6;
     const float denom = LOSS ? denominator(a) : 1.0f;
-    const float scale = LOSS ? a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / denom : 1.0f;
+    const float scale = LOSS ? scale_by(a, denom) : 1.0f;
     float total[kSums] = {};
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const int64_t action = action_of(a, row);
@@ -635,10 +686,21 @@ typedef void (*Kernel)(const Args);
 struct Choice {
     Kernel kernel;
     int threads, rows;  // rows that a workgroup runs at a time
+    int blocks;         // workgroups that the GPU runs at a time
 };
-template <typename E, int G, int NV, int THREADS, bool LOSS, bool TINY = false>
-Choice held() {
-    return {held_kernel<E, G, NV, THREADS, TINY, LOSS>, THREADS, THREADS / G};
+constexpr int kCUs = 256;
+constexpr int resident(int threads, int waves) { return kCUs * waves * 4 / (threads / 64); }
+template <typename E, int G, int NV, int WAVES, bool LOSS, bool TINY = false>
+Choice held(bool solo) {
+    if constexpr (LOSS) {
+        if (solo) return {held_kernel<E, G, NV, kSoloThreads, 4, TINY, true>, kSoloThreads, kSoloThreads / G, 1};
+    }
+    constexpr int W = LOSS ? WAVES : 8;
+    return {held_kernel<E, G, NV, kThreads, W, TINY, LOSS>, kThreads, kThreads / G, resident(kThreads, W)};
+}
+template <typename E, int NV, int THREADS, bool LOSS>
+Choice block() {
+    return {block_kernel<E, NV, THREADS, LOSS>, THREADS, 1, resident(THREADS, LOSS ? 4 : 8)};
 }
 
 // The kernel for rows of V: as few lanes as hold a row in four pieces each, so
@@ -648,30 +710,22 @@ template <typename E, bool LOSS>
 Choice choose(int64_t V, bool solo) {
     constexpr int VE = 16 / sizeof(E);
     const int64_t pieces = (V + VE - 1) / VE;
-    if constexpr (LOSS) {
-        if (solo && V < VE) return held<E, 1, 1, kSoloThreads, LOSS, true>();
-        if (solo && pieces <= 4) return held<E, 1, 4, kSoloThreads, LOSS>();
-        if (solo && pieces <= 8) return held<E, 2, 4, kSoloThreads, LOSS>();
-        if (solo && pieces <= 16) return held<E, 4, 4, kSoloThreads, LOSS>();
-        if (solo && pieces <= 32) return held<E, 8, 4, kSoloThreads, LOSS>();
-        if (solo && pieces <= 64) return held<E, 16, 4, kSoloThreads, LOSS>();
-        if (solo) return held<E, 64, 4, kSoloThreads, LOSS>();
-    }
-    if (V < VE) return held<E, 1, 1, kThreads, LOSS, true>();
-    if (pieces <= 1) return held<E, 1, 1, kThreads, LOSS>();
-    if (pieces <= 2) return held<E, 1, 2, kThreads, LOSS>();
-    if (pieces <= 4) return held<E, 1, 4, kThreads, LOSS>();
-    if (pieces <= 8) return held<E, 2, 4, kThreads, LOSS>();
-    if (pieces <= 16) return held<E, 4, 4, kThreads, LOSS>();
-    if (pieces <= 32) return held<E, 8, 4, kThreads, LOSS>();
-    if (pieces <= 64) return held<E, 16, 4, kThreads, LOSS>();
-    if (pieces <= 256) return held<E, 64, 4, kThreads, LOSS>();
-    if (pieces <= 512) return held<E, 64, 8, kThreads, LOSS>();
-    if (pieces <= 1024) return held<E, 256, 4, 256, LOSS>();
-    if (pieces <= 4096) return held<E, 256, 16, 256, LOSS>();
-    if (pieces <= 8192) return held<E, 512, 16, 512, LOSS>();
-    if (pieces <= 16384) return held<E, 1024, 16, 1024, LOSS>();
-    return {long_kernel<E, LOSS>, kSoloThreads, 1};
+    static_assert(resident(kThreads, 8) <= kMaxBlocks, "the sums have a place per workgroup");
+    if (V < VE) return held<E, 1, 1, 8, LOSS, true>(solo);
+    if (pieces <= 1) return held<E, 1, 1, 8, LOSS>(solo);
+    if (pieces <= 2) return held<E, 1, 2, 6, LOSS>(solo);
+    if (pieces <= 4) return held<E, 1, 4, 4, LOSS>(solo);
+    if (pieces <= 8) return held<E, 2, 4, 6, LOSS>(solo);
+    if (pieces <= 16) return held<E, 4, 4, 6, LOSS>(solo);
+    if (pieces <= 32) return held<E, 8, 4, 6, LOSS>(solo);
+    if (pieces <= 64) return held<E, 16, 4, 6, LOSS>(solo);
+    if (pieces <= 256) return held<E, 64, 4, 6, LOSS>(solo);
+    if (pieces <= 512) return held<E, 64, 8, 4, LOSS>(false);
+    if (pieces <= 1024) return block<E, 4, 256, LOSS>();
+    if (pieces <= 4096) return block<E, 16, 256, LOSS>();
+    if (pieces <= 8192) return block<E, 16, 512, LOSS>();
+    if (pieces <= 16384) return block<E, 16, 1024, LOSS>();
+    return {long_kernel<E, LOSS>, kSoloThreads, 1, resident(kSoloThreads, 4)};
 }
 
 int64_t work_bytes_of(const gear_policy_desc&) { return kSumOff + (int64_t)kSums * kMaxBlocks * (int64_t)sizeof(float); }
@@ -715,7 +769,7 @@ hipError_t launch_rows(const Args& a, int32_t dtype, bool solo, int* blocks, hip
     const Choice c = dtype == GEAR_DTYPE_F32 ? choose<float, LOSS>(a.V, solo)
                      : dtype == GEAR_DTYPE_BF16 ? choose<__bf16, LOSS>(a.V, solo) : choose<_Float16, LOSS>(a.V, solo);
     const int64_t want = (a.n + c.rows - 1) / c.rows;
-    *blocks = solo ? 1 : (int)(want < kMaxBlocks ? want : kMaxBlocks);
+    *blocks = (int)(want < c.blocks ? want : c.blocks);
     hipLaunchKernelGGL(c.kernel, dim3(*blocks), dim3(c.threads), 0, s, a);
     return hipGetLastError();
 }
