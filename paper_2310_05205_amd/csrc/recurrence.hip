@@ -6,13 +6,14 @@
 // where a reset makes h_{t-1} count as 0 and cuts the chain in both directions.
 //
 // Both directions read and write every element once and do a few operations
-// on it, so memory bounds them.  A lane owns the 8 bytes of neighbouring
+// on it, so memory bounds them.  A lane owns 8 (backward 4) bytes of neighbouring
 // channels of one window and walks its steps in tiles of 16, whose loads are
 // all issued before the first is used.  Windows and channels give the
 // parallelism; where they are too few to fill the GPU, the steps are split
-// into segments: one launch reduces every segment to what it does to a state
-// carried through it (an affine map), one applies the maps in order, and the
-// last runs every segment from its own first state.
+// into segments, one to a wave: one launch reduces every segment, and every
+// workgroup's run of segments, to what it does to a value carried through it
+// (an affine map), one applies the runs' maps in order, and the last goes
+// through every segment from its own first value.
 #include "element.h"
 #include "gear_internal.h"
 
@@ -20,10 +21,17 @@ namespace gear {
 namespace {
 
 constexpr int kSteps = GEAR_RECURRENCE_STEPS;  // steps of a tile
-constexpr int kForwardBytes = 8, kBackwardBytes = 4;  // neighbouring channels of a lane
+// Neighbouring channels of a lane: 8 bytes of them forward; two backward, which
+// holds three fp32 values for every step of each.  Of 16-bit types four took 473 us
+// for forward and backward of 8192 x 32 x 512, two 423; of fp32 one took 332 us for 4 x 16384 x
+// 512, two 305.
+constexpr int kForwardBytes = 8, kBackwardChannels = 2;
 constexpr int kThreads = 256;
-constexpr int kWantLanes = 2048 * 64;  // lanes that fill the GPU
+constexpr int kWholeLanes = 1024 * 64;  // calls of more lanes are not split
+constexpr int kWantLanes = 8192 * 64;   // lanes that a split call is cut into, at most:
+constexpr int kMostSegments = 1024;     // more segments of long windows cost more in maps than they gain
 constexpr int64_t kMaxBlocks = 1 << 22;
+constexpr int kRun = 8;  // segments of a workgroup of a split call, a wave each
 
 // A map c -> P c + Z of a carried value; a reset inside it cuts the value
 // off, which P holds as these bits (a NaN that no operation makes), because
@@ -49,12 +57,15 @@ struct Args {
     float *final_state, *out_saved, *dstate;
     const uint8_t* reset;
     const int32_t* lengths;
-    Map* maps;            // [S][B][D] when S > 1; their first states after carry_kernel
+    Map* maps;            // of split calls: [runs * kRun][B][D], one per segment ...
+    Map* run_maps;        // ... and [runs][B][D], one per run; their first values after carry_kernel
     int64_t B, T, D, gate_b, gate_t, x_b, x_t, dy_b, dy_t, reset_b;
     int64_t groups;       // of VE channels in a window
     int64_t lanes;        // B * groups
     int64_t seg_tiles;    // tiles of a segment
-    int32_t S;
+    int64_t columns;      // of 64 lanes
+    int32_t runs;         // of kRun segments; 0 for a call that is not split
+    bool stream;          // write past the caches
 };
 
 // A lane's place: window b, first channel c, and the steps of its window.
@@ -77,21 +88,24 @@ __device__ __forceinline__ Place place_of(const Args& a, int64_t q) {
     return p;
 }
 
-// Resets of steps [t0, t0 + count), one bit each.
-__device__ __forceinline__ uint32_t resets(const Args& a, int64_t b, int64_t t0, int count) {
-    if (a.reset == nullptr) return 0;
-    const uint8_t* r = a.reset + b * a.reset_b + t0;
-    uint32_t bits = 0;
-    if (count == kSteps) {
-        uint32_t w[kSteps / 4];
-        __builtin_memcpy(w, r, sizeof(w));
+// Reset flags of the steps of a tile: read before the tile, so that they need
+// not be waited for, and looked at after its loads are on their way.
+struct Flags {
+    uint32_t w[kSteps / 4];
+    __device__ __forceinline__ void load(const Args& a, int64_t b, int64_t t0, int count) {
 #pragma unroll
-        for (int i = 0; i < kSteps; i++) bits |= ((w[i / 4] >> (8 * (i % 4))) & 0xFFu) != 0 ? 1u << i : 0u;
-    } else {
-        for (int i = 0; i < count; i++) bits |= r[i] != 0 ? 1u << i : 0u;
+        for (int i = 0; i < kSteps / 4; i++) w[i] = 0;
+        const uint8_t* r = a.reset + b * a.reset_b + t0;
+        if (count == kSteps) __builtin_memcpy(w, r, sizeof(w));
+        else
+#pragma unroll
+            for (int i = 0; i < kSteps; i++)
+                if (i < count) w[i / 4] |= (uint32_t)r[i] << (8 * (i % 4));
     }
-    return bits;
-}
+    __device__ __forceinline__ bool any() const { return (w[0] | w[1] | w[2] | w[3]) != 0; }
+    __device__ __forceinline__ bool at(int s) const { return (w[s / 4] & (0xFFu << (8 * (s % 4)))) != 0; }
+};
+static_assert(kSteps == 16, "four words of flags");
 
 // Decay and input weight of a gate.  With e = exp(-g) they are 1 / (1 + e) and
 // e / (1 + e), neither of which cancels; where e is large the latter is 1,
@@ -108,23 +122,26 @@ __device__ __forceinline__ void gates(float g, float& f, float& w) {
     }
 }
 
-// What the lanes of a wave have in common at a tile: every step of it and no
-// reset, every step, or anything else.  The first two run without a branch
-// per step, so that the steps' gates are computed side by side.
-enum { kPlain = 0, kCuts = 1, kAny = 2 };
-__device__ __forceinline__ int mode_of(int count, uint32_t r) {
-    if (!__all(count == kSteps)) return kAny;
-    return __any(r != 0) ? kCuts : kPlain;
+// Hides where a pointer comes from.  A tile's addresses follow from its first;
+// left to itself the compiler keeps a pointer per step from tile to tile, 96 registers.
+template <typename P>
+__device__ __forceinline__ void hide(P*& p) {
+    asm volatile("" : "+v"(p));
 }
 
 template <typename E, int VE>
 struct Tile {
     typename Vec<E, VE>::raw v[kSteps];
-    template <int MODE>
+    // With FULL every lane of the wave has all steps, and no step takes a branch:
+    // their gates are computed side by side.
+    template <bool FULL>
     __device__ __forceinline__ void load(const E* p, int64_t stride, int count) {
+        hide(p);
 #pragma unroll
-        for (int i = 0; i < kSteps; i++)
-            if (MODE != kAny || i < count) v[i] = Vec<E, VE>::load(p + i * stride);
+        for (int i = 0; i < kSteps; i++) {
+            if (FULL || i < count) v[i] = Vec<E, VE>::load(p);
+            p += stride;
+        }
     }
 };
 
@@ -149,21 +166,22 @@ __device__ __forceinline__ Rows<E> rows_of(const Args& a, const Place& p) {
 }
 
 // `count` steps of the recurrence from step t0 on; zeros up to `room`.
-template <typename E, int VE, int FORM, bool MAPS, int MODE>
+template <typename E, int VE, int FORM, bool RESET, bool MAPS, bool FULL, bool STREAM>
 __device__ __forceinline__ void forward_tile(const Args& a, const Rows<E>& rows, int64_t t0, int count, int room,
-                                             uint32_t r, float (&h)[VE], float (&P)[VE]) {
-#pragma clang fp contract(off)  // the modes round alike: lanes that share channels may run different ones
+                                             const Flags& flags, float (&h)[VE], float (&P)[VE]) {
+#pragma clang fp contract(off)  // full and other tiles round alike: lanes that share channels may have either
     Tile<E, VE> g, x;
-    g.template load<MODE>(rows.gate + t0 * a.gate_t, a.gate_t, count);
-    x.template load<MODE>(rows.x + t0 * a.x_t, a.x_t, count);
+    g.template load<FULL>(rows.gate + t0 * a.gate_t, a.gate_t, count);
+    x.template load<FULL>(rows.x + t0 * a.x_t, a.x_t, count);
     E* y = rows.y + t0 * a.D;
+    hide(y);
 #pragma unroll
     for (int s = 0; s < kSteps; s++) {
-        if (MODE != kAny || s < count) {
+        if (FULL || s < count) {
             float gv[VE], xv[VE];
             Vec<E, VE>::unpack(g.v[s], gv);
             Vec<E, VE>::unpack(x.v[s], xv);
-            const bool z = MODE != kPlain && ((r >> s) & 1u);
+            const bool z = RESET && flags.at(s);
 #pragma unroll
             for (int j = 0; j < VE; j++) {
                 float f, w;
@@ -172,95 +190,168 @@ __device__ __forceinline__ void forward_tile(const Args& a, const Rows<E>& rows,
                 h[j] = z ? u : fmaf(f, h[j], u);
                 if (MAPS) P[j] *= f;
             }
-            if (!MAPS && a.y) Vec<E, VE>::store(y + s * a.D, h);
+            if (!MAPS && a.y) Vec<E, VE>::template store<STREAM>(y, h);
         } else if (!MAPS && s < room && a.y) {
             const float zero[VE] = {};
-            Vec<E, VE>::store(y + s * a.D, zero);
+            Vec<E, VE>::store(y, zero);
         }
+        y += a.D;
     }
 }
 
-// Segments forward: with MAPS, reduces each to its map; else the whole recurrence.
-template <typename E, int VE, int FORM, bool MAPS>
+// A wave's part of a split call: 64 lanes' channels, one segment of their
+// steps.  A workgroup has neighbouring segments of the same lanes.
+struct Part {
+    int64_t q, seg;  // lane among the call's; segment from the start, or for the backward pass from the end
+    int32_t run;
+    bool used;
+};
+__device__ __forceinline__ Part part_of(const Args& a) {
+    Part w;
+    w.run = (int32_t)(blockIdx.x / a.columns);
+    w.q = ((int64_t)blockIdx.x - w.run * a.columns) * 64 + (threadIdx.x & 63);
+    w.used = w.q < a.lanes;
+    if (!w.used) w.q = 0;
+    w.seg = (int64_t)w.run * kRun + (threadIdx.x >> 6);
+    return w;
+}
+
+// Leaves a wave's map, and the first wave its workgroup's.
+template <int VE>
+__device__ __forceinline__ void leave_maps(const Args& a, const Part& w, int64_t at, const Map (&m)[VE],
+                                           Map (*s)[VE][64]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t BD = a.B * a.D;
+#pragma unroll
+    for (int j = 0; j < VE; j++) {
+        s[wave][j][lane] = m[j];
+        if (w.used) a.maps[w.seg * BD + at + j] = m[j];
+    }
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int j = 0; j < VE; j++) {
+        Map all = m[j];
+#pragma unroll
+        for (int k = 1; k < kRun; k++) all = compose(s[k][j][lane], all);
+        if (w.used) a.run_maps[w.run * BD + at + j] = all;
+    }
+}
+
+// The value a wave's segment starts from: its run's, through the run's earlier segments.
+template <int VE>
+__device__ __forceinline__ void first_of(const Args& a, const Part& w, int64_t at, float (&c)[VE]) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t BD = a.B * a.D;
+#pragma unroll
+    for (int j = 0; j < VE; j++) c[j] = a.run_maps[w.run * BD + at + j].P;
+    for (int k = 0; k < wave; k++) {
+#pragma unroll
+        for (int j = 0; j < VE; j++) c[j] = apply(a.maps[((int64_t)w.run * kRun + k) * BD + at + j], c[j]);
+    }
+}
+
+// The steps of lane q from tile k0 to tile k1, from state h.
+template <typename E, int VE, int FORM, bool RESET, bool MAPS>
+__device__ __forceinline__ bool forward_tiles(const Args& a, const Place& p, int64_t at, bool used, int64_t k0, int64_t k1,
+                                              float (&h)[VE], float (&P)[VE]) {
+    const Rows<E> rows = rows_of<E>(a, p);
+    const int64_t BD = a.B * a.D;
+    bool cut = false;
+    for (int64_t k = k0; k < k1; k++) {
+        const int64_t t0 = k * kSteps;
+        const int count = used ? clamp_count(p.n - t0) : 0, room = used ? clamp_count(a.T - t0) : 0;
+        if (!MAPS && used && a.out_saved && k > 0) Vec<float, VE>::store(a.out_saved + (k - 1) * BD + at, h);
+        Flags flags;
+        if (RESET) flags.load(a, p.b, t0, count);
+        if (!__all(count == kSteps))
+            forward_tile<E, VE, FORM, RESET, MAPS, false, false>(a, rows, t0, count, room, flags, h, P);
+        else if (!MAPS && a.stream)
+            forward_tile<E, VE, FORM, RESET, MAPS, true, true>(a, rows, t0, count, room, flags, h, P);
+        else forward_tile<E, VE, FORM, RESET, MAPS, true, false>(a, rows, t0, count, room, flags, h, P);
+        if (RESET) cut |= flags.any();
+    }
+    return cut;
+}
+
+// Windows that are not split.
+template <typename E, int VE, int FORM, bool RESET>
 __global__ __launch_bounds__(kThreads) void forward_kernel(const Args a) {
-    const int64_t BD = a.B * a.D, tiles = (a.T + kSteps - 1) / kSteps;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < a.lanes * a.S;
-         i += (int64_t)gridDim.x * kThreads) {
-        const int64_t seg = i / a.lanes;
-        const Place p = place_of<VE>(a, i - seg * a.lanes);
-        const Rows<E> rows = rows_of<E>(a, p);
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < a.lanes; i += (int64_t)gridDim.x * kThreads) {
+        const Place p = place_of<VE>(a, i);
         const int64_t at = p.b * a.D + p.c;
         float h[VE], P[VE];
-        bool cut = false;
 #pragma unroll
-        for (int j = 0; j < VE; j++) {
-            P[j] = 1.0f;
-            h[j] = MAPS || !a.state ? 0.0f : a.state[at + j];
-            if (!MAPS && a.S > 1) h[j] = a.maps[seg * BD + at + j].P;
-        }
-        const int64_t k1 = (seg + 1) * a.seg_tiles < tiles ? (seg + 1) * a.seg_tiles : tiles;
-        for (int64_t k = seg * a.seg_tiles; k < k1; k++) {
-            const int64_t t0 = k * kSteps;
-            const int count = clamp_count(p.n - t0), room = clamp_count(a.T - t0);
-            if (!MAPS && a.out_saved && k > 0) Vec<float, VE>::store(a.out_saved + (k - 1) * BD + at, h);
-            const uint32_t r = resets(a, p.b, t0, count);
-            cut |= r != 0;
-            const int mode = mode_of(count, r);
-            if (mode == kPlain) forward_tile<E, VE, FORM, MAPS, kPlain>(a, rows, t0, count, room, r, h, P);
-            else if (mode == kCuts) forward_tile<E, VE, FORM, MAPS, kCuts>(a, rows, t0, count, room, r, h, P);
-            else forward_tile<E, VE, FORM, MAPS, kAny>(a, rows, t0, count, room, r, h, P);
-        }
-        if (MAPS) {
-#pragma unroll
-            for (int j = 0; j < VE; j++)
-                a.maps[seg * BD + at + j] = Map{cut ? __uint_as_float(kCutBits) : P[j], h[j]};
-        } else if (a.final_state && seg == a.S - 1) {
-            Vec<float, VE>::store(a.final_state + at, h);
-        }
+        for (int j = 0; j < VE; j++) h[j] = a.state ? a.state[at + j] : 0.0f;
+        forward_tiles<E, VE, FORM, RESET, false>(a, p, at, true, 0, (a.T + kSteps - 1) / kSteps, h, P);
+        if (a.final_state) Vec<float, VE>::store(a.final_state + at, h);
     }
 }
 
-// Applies every channel's maps in order (the last segment first when
-// BACKWARD) and leaves the value each segment starts from in its map.  A
-// workgroup takes 64 channels; its waves compose a run of segments each, the
-// runs' maps lead to every run's first value, and the waves go through their
-// runs again.  (A thread per channel took 261 us for 1024 segments of 512.)
-constexpr int kCarryWaves = 16, kCarryAhead = 8;
-template <bool BACKWARD>
-__global__ __launch_bounds__(64 * kCarryWaves) void carry_kernel(Map* __restrict__ maps, const float* __restrict__ first,
-                                                                int64_t channels, int32_t S) {
-    __shared__ Map s_run[kCarryWaves][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t i = (int64_t)blockIdx.x * 64 + lane;
-    const bool used = i < channels;
-    const int32_t run = (S + kCarryWaves - 1) / kCarryWaves;
-    const int32_t s0 = wave * run < S ? wave * run : S, s1 = s0 + run < S ? s0 + run : S;
-    Map whole = {1.0f, 0.0f};
-    if (used) {
-        for (int32_t s = s0; s < s1; s += kCarryAhead) {
-            Map m[kCarryAhead];
+// Segments: with MAPS, reduces each to its map; else goes through it.
+template <typename E, int VE, int FORM, bool RESET, bool MAPS>
+__global__ __launch_bounds__(64 * kRun) void forward_split_kernel(const Args a) {
+    __shared__ Map s[MAPS ? kRun : 1][VE][64];
+    const Part w = part_of(a);
+    const Place p = place_of<VE>(a, w.q);
+    const int64_t at = p.b * a.D + p.c, tiles = (a.T + kSteps - 1) / kSteps;
+    const int64_t k0 = w.seg * a.seg_tiles < tiles ? w.seg * a.seg_tiles : tiles;
+    const int64_t k1 = k0 + a.seg_tiles < tiles ? k0 + a.seg_tiles : tiles;
+    float h[VE], P[VE];
 #pragma unroll
-            for (int k = 0; k < kCarryAhead; k++)
-                if (s + k < s1) m[k] = maps[(BACKWARD ? S - 1 - (s + k) : s + k) * channels + i];
-#pragma unroll
-            for (int k = 0; k < kCarryAhead; k++)
-                if (s + k < s1) whole = compose(m[k], whole);
-        }
+    for (int j = 0; j < VE; j++) {
+        P[j] = 1.0f;
+        h[j] = 0.0f;
     }
-    s_run[wave][lane] = whole;
+    if (!MAPS) first_of<VE>(a, w, at, h);
+    const bool cut = forward_tiles<E, VE, FORM, RESET, MAPS>(a, p, at, w.used, k0, k1, h, P);
+    if (MAPS) {
+        Map m[VE];
+#pragma unroll
+        for (int j = 0; j < VE; j++) m[j] = Map{cut ? __uint_as_float(kCutBits) : P[j], h[j]};
+        leave_maps<VE>(a, w, at, m, s);
+    } else if (w.used && a.final_state && k0 < k1 && k1 == tiles) {
+        Vec<float, VE>::store(a.final_state + at, h);
+    }
+}
+
+// Applies every channel's run maps in order and leaves the value each run
+// starts from in its map.  A workgroup takes 64 channels; each of its waves
+// composes a share of the runs, the shares' maps lead to every share's first
+// value, and the waves go through their shares again.
+constexpr int kCarryWaves = 16, kCarryAhead = 16;
+__global__ __launch_bounds__(64 * kCarryWaves) void carry_kernel(Map* __restrict__ maps, const float* __restrict__ first,
+                                                                int64_t channels, int32_t runs) {
+    __shared__ Map s_share[kCarryWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t i = (int64_t)blockIdx.x * 64 + lane;
+    const bool used = i < channels;
+    if (!used) i = channels - 1;
+    const int32_t share = (runs + kCarryWaves - 1) / kCarryWaves;
+    const int32_t s0 = wave * share < runs ? wave * share : runs, s1 = s0 + share < runs ? s0 + share : runs;
+    Map whole = {1.0f, 0.0f}, m[kCarryAhead];
+    for (int32_t s = s0; s < s1; s += kCarryAhead) {
+        // Places past the share read its last map again and are not used.
+#pragma unroll
+        for (int k = 0; k < kCarryAhead; k++) m[k] = maps[(s + k < s1 ? s + k : s1 - 1) * channels + i];
+#pragma unroll
+        for (int k = 0; k < kCarryAhead; k++)
+            if (s + k < s1) whole = compose(m[k], whole);
+    }
+    s_share[wave][lane] = whole;
     __syncthreads();
     if (!used) return;
     float c = first ? first[i] : 0.0f;
-    for (int k = 0; k < wave; k++) c = apply(s_run[k][lane], c);
+    for (int k = 0; k < wave; k++) c = apply(s_share[k][lane], c);
     for (int32_t s = s0; s < s1; s += kCarryAhead) {
-        Map m[kCarryAhead];
+        if (share > kCarryAhead) {
 #pragma unroll
-        for (int k = 0; k < kCarryAhead; k++)
-            if (s + k < s1) m[k] = maps[(BACKWARD ? S - 1 - (s + k) : s + k) * channels + i];
+            for (int k = 0; k < kCarryAhead; k++) m[k] = maps[(s + k < s1 ? s + k : s1 - 1) * channels + i];
+        }
 #pragma unroll
         for (int k = 0; k < kCarryAhead; k++) {
             if (s + k < s1) {
-                maps[(BACKWARD ? S - 1 - (s + k) : s + k) * channels + i].P = c;
+                maps[(s + k) * channels + i].P = c;
                 c = apply(m[k], c);
             }
         }
@@ -271,23 +362,23 @@ __global__ __launch_bounds__(64 * kCarryWaves) void carry_kernel(Map* __restrict
 // out as that of the state before it.  h is the state before it, from which
 // the states inside are recomputed in 32 bits: read back from y they would carry
 // its rounding into h_{t-1} - x_t.
-template <typename E, int VE, int FORM, bool MAPS, int MODE>
+template <typename E, int VE, int FORM, bool RESET, bool MAPS, bool FULL, bool STREAM>
 __device__ __forceinline__ void backward_tile(const Args& a, const Rows<E>& rows, int64_t t0, int count, int room,
-                                              uint32_t r, float (&h)[VE], float (&G)[VE], float (&P)[VE]) {
+                                              const Flags& flags, float (&h)[VE], float (&G)[VE], float (&P)[VE]) {
 #pragma clang fp contract(off)  // as forward_tile
     Tile<E, VE> g, x, d;
-    g.template load<MODE>(rows.gate + t0 * a.gate_t, a.gate_t, count);
-    if (!MAPS) x.template load<MODE>(rows.x + t0 * a.x_t, a.x_t, count);
-    if (rows.dy) d.template load<MODE>(rows.dy + t0 * a.dy_t, a.dy_t, count);
+    g.template load<FULL>(rows.gate + t0 * a.gate_t, a.gate_t, count);
+    if (!MAPS) x.template load<FULL>(rows.x + t0 * a.x_t, a.x_t, count);
+    if (rows.dy) d.template load<FULL>(rows.dy + t0 * a.dy_t, a.dy_t, count);
     // Per step: decay, input weight, and what the gate's gradient is a multiple of.
     float F[kSteps][VE], W[kSteps][VE], Q[kSteps][VE];
 #pragma unroll
     for (int s = 0; s < kSteps; s++) {
-        if (MODE != kAny || s < count) {
+        if (FULL || s < count) {
             float gv[VE], xv[VE];
             Vec<E, VE>::unpack(g.v[s], gv);
             if (!MAPS) Vec<E, VE>::unpack(x.v[s], xv);
-            const bool z = MODE != kPlain && ((r >> s) & 1u);
+            const bool z = RESET && flags.at(s);
 #pragma unroll
             for (int j = 0; j < VE; j++) {
                 gates<FORM>(gv[j], F[s][j], W[s][j]);
@@ -300,14 +391,16 @@ __device__ __forceinline__ void backward_tile(const Args& a, const Rows<E>& rows
             }
         }
     }
-    E* dgate = rows.dgate + t0 * a.D;
-    E* dx = rows.dx + t0 * a.D;
+    E* dgate = rows.dgate + (t0 + kSteps - 1) * a.D;
+    E* dx = rows.dx + (t0 + kSteps - 1) * a.D;
+    hide(dgate);
+    hide(dx);
 #pragma unroll
     for (int s = kSteps - 1; s >= 0; s--) {
-        if (MODE != kAny || s < count) {
+        if (FULL || s < count) {
             float dv[VE] = {}, og[VE], ox[VE];
             if (rows.dy) Vec<E, VE>::unpack(d.v[s], dv);
-            const bool z = MODE != kPlain && ((r >> s) & 1u);
+            const bool z = RESET && flags.at(s);
 #pragma unroll
             for (int j = 0; j < VE; j++) {
                 const float f = F[s][j], t = G[j] + dv[j];
@@ -319,112 +412,161 @@ __device__ __forceinline__ void backward_tile(const Args& a, const Rows<E>& rows
                 if (MAPS) P[j] *= f;
             }
             if (!MAPS) {
-                Vec<E, VE>::store(dgate + s * a.D, og);
-                Vec<E, VE>::store(dx + s * a.D, ox);
+                Vec<E, VE>::template store<STREAM>(dgate, og);
+                Vec<E, VE>::template store<STREAM>(dx, ox);
             }
         } else if (!MAPS && s < room) {
             const float zero[VE] = {};
-            Vec<E, VE>::store(dgate + s * a.D, zero);
-            Vec<E, VE>::store(dx + s * a.D, zero);
+            Vec<E, VE>::store(dgate, zero);
+            Vec<E, VE>::store(dx, zero);
         }
+        dgate -= a.D;
+        dx -= a.D;
     }
 }
 
-// Segments backward: with MAPS, reduces each to what it does to the gradient
-// that comes in at its end; else the gradients.
-template <typename E, int VE, int FORM, bool MAPS>
+// The steps of lane q back from tile k1 to tile k0.
+template <typename E, int VE, int FORM, bool RESET, bool MAPS>
+__device__ __forceinline__ bool backward_tiles(const Args& a, const Place& p, int64_t at, bool used, int64_t k0, int64_t k1,
+                                               float (&G)[VE], float (&P)[VE]) {
+    const Rows<E> rows = rows_of<E>(a, p);
+    const int64_t BD = a.B * a.D;
+    bool cut = false;
+    for (int64_t k = k1 - 1; k >= k0; k--) {
+        const int64_t t0 = k * kSteps;
+        const int count = used ? clamp_count(p.n - t0) : 0, room = used ? clamp_count(a.T - t0) : 0;
+        Flags flags;
+        if (RESET) flags.load(a, p.b, t0, count);
+        float h[VE] = {};
+        if (!MAPS && count > 0) {
+            const float* from = k > 0 ? a.saved + (k - 1) * BD + at : a.state ? a.state + at : nullptr;
+            if (from) {
+#pragma unroll
+                for (int j = 0; j < VE; j++) h[j] = from[j];
+            }
+        }
+        if (!__all(count == kSteps))
+            backward_tile<E, VE, FORM, RESET, MAPS, false, false>(a, rows, t0, count, room, flags, h, G, P);
+        else if (!MAPS && a.stream)
+            backward_tile<E, VE, FORM, RESET, MAPS, true, true>(a, rows, t0, count, room, flags, h, G, P);
+        else backward_tile<E, VE, FORM, RESET, MAPS, true, false>(a, rows, t0, count, room, flags, h, G, P);
+        if (RESET) cut |= flags.any();
+    }
+    return cut;
+}
+
+template <typename E, int VE, int FORM, bool RESET>
 __global__ __launch_bounds__(kThreads) void backward_kernel(const Args a) {
-    const int64_t BD = a.B * a.D, tiles = (a.T + kSteps - 1) / kSteps;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < a.lanes * a.S;
-         i += (int64_t)gridDim.x * kThreads) {
-        const int64_t seg = i / a.lanes;
-        const Place p = place_of<VE>(a, i - seg * a.lanes);
-        const Rows<E> rows = rows_of<E>(a, p);
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < a.lanes; i += (int64_t)gridDim.x * kThreads) {
+        const Place p = place_of<VE>(a, i);
         const int64_t at = p.b * a.D + p.c;
         float G[VE], P[VE];
-        bool cut = false;
 #pragma unroll
-        for (int j = 0; j < VE; j++) {
-            P[j] = 1.0f;
-            G[j] = MAPS || !a.dfinal ? 0.0f : a.dfinal[at + j];
-            if (!MAPS && a.S > 1) G[j] = a.maps[seg * BD + at + j].P;
-        }
-        const int64_t k1 = (seg + 1) * a.seg_tiles < tiles ? (seg + 1) * a.seg_tiles : tiles;
-        for (int64_t k = k1 - 1; k >= seg * a.seg_tiles; k--) {
-            const int64_t t0 = k * kSteps;
-            const int count = clamp_count(p.n - t0), room = clamp_count(a.T - t0);
-            const uint32_t r = resets(a, p.b, t0, count);
-            cut |= r != 0;
-            float h[VE] = {};
-            if (!MAPS && count > 0) {
-                const float* from = k > 0 ? a.saved + (k - 1) * BD + at : a.state ? a.state + at : nullptr;
-                if (from) {
+        for (int j = 0; j < VE; j++) G[j] = a.dfinal ? a.dfinal[at + j] : 0.0f;
+        backward_tiles<E, VE, FORM, RESET, false>(a, p, at, true, 0, (a.T + kSteps - 1) / kSteps, G, P);
+        if (a.dstate) Vec<float, VE>::store(a.dstate + at, G);
+    }
+}
+
+// Segments are numbered from the end here: the gradient is carried from there.
+template <typename E, int VE, int FORM, bool RESET, bool MAPS>
+__global__ __launch_bounds__(64 * kRun) void backward_split_kernel(const Args a) {
+    __shared__ Map s[MAPS ? kRun : 1][VE][64];
+    const Part w = part_of(a);
+    const Place p = place_of<VE>(a, w.q);
+    const int64_t at = p.b * a.D + p.c, tiles = (a.T + kSteps - 1) / kSteps;
+    const int64_t k1 = tiles - w.seg * a.seg_tiles > 0 ? tiles - w.seg * a.seg_tiles : 0;
+    const int64_t k0 = k1 - a.seg_tiles > 0 ? k1 - a.seg_tiles : 0;
+    float G[VE], P[VE];
 #pragma unroll
-                    for (int j = 0; j < VE; j++) h[j] = from[j];
-                }
-            }
-            const int mode = mode_of(count, r);
-            if (mode == kPlain) backward_tile<E, VE, FORM, MAPS, kPlain>(a, rows, t0, count, room, r, h, G, P);
-            else if (mode == kCuts) backward_tile<E, VE, FORM, MAPS, kCuts>(a, rows, t0, count, room, r, h, G, P);
-            else backward_tile<E, VE, FORM, MAPS, kAny>(a, rows, t0, count, room, r, h, G, P);
-        }
-        if (MAPS) {
+    for (int j = 0; j < VE; j++) {
+        P[j] = 1.0f;
+        G[j] = 0.0f;
+    }
+    if (!MAPS) first_of<VE>(a, w, at, G);
+    const bool cut = backward_tiles<E, VE, FORM, RESET, MAPS>(a, p, at, w.used, k0, k1, G, P);
+    if (MAPS) {
+        Map m[VE];
 #pragma unroll
-            for (int j = 0; j < VE; j++)
-                a.maps[seg * BD + at + j] = Map{cut ? __uint_as_float(kCutBits) : P[j], G[j]};
-        } else if (a.dstate && seg == 0) {
-            Vec<float, VE>::store(a.dstate + at, G);
-        }
+        for (int j = 0; j < VE; j++) m[j] = Map{cut ? __uint_as_float(kCutBits) : P[j], G[j]};
+        leave_maps<VE>(a, w, at, m, s);
+    } else if (w.used && a.dstate && k0 < k1 && k0 == 0) {
+        Vec<float, VE>::store(a.dstate + at, G);
     }
 }
 
 typedef void (*Kernel)(const Args);
 struct Kernels {
-    Kernel maps, whole;
+    Kernel whole, maps, split;
 };
-template <typename E, int VE, int FORM, bool BACKWARD>
+template <typename E, int VE, int FORM, bool RESET, bool BACKWARD>
 Kernels kernels_of() {
-    if constexpr (BACKWARD) return {backward_kernel<E, VE, FORM, true>, backward_kernel<E, VE, FORM, false>};
-    else return {forward_kernel<E, VE, FORM, true>, forward_kernel<E, VE, FORM, false>};
+    if constexpr (BACKWARD)
+        return {backward_kernel<E, VE, FORM, RESET>, backward_split_kernel<E, VE, FORM, RESET, true>,
+                backward_split_kernel<E, VE, FORM, RESET, false>};
+    else
+        return {forward_kernel<E, VE, FORM, RESET>, forward_split_kernel<E, VE, FORM, RESET, true>,
+                forward_split_kernel<E, VE, FORM, RESET, false>};
+}
+template <typename E, int VE, bool BACKWARD>
+Kernels kernels_for(int32_t form, bool reset) {
+    if (form == GEAR_GATE_VALUE)
+        return reset ? kernels_of<E, VE, GEAR_GATE_VALUE, true, BACKWARD>() : kernels_of<E, VE, GEAR_GATE_VALUE, false, BACKWARD>();
+    return reset ? kernels_of<E, VE, GEAR_GATE_SIGMOID, true, BACKWARD>() : kernels_of<E, VE, GEAR_GATE_SIGMOID, false, BACKWARD>();
 }
 template <typename E, bool BACKWARD>
-Kernels kernels_for(int32_t form, bool wide) {
-    constexpr int VE = (BACKWARD ? kBackwardBytes : kForwardBytes) / sizeof(E);
-    if (form == GEAR_GATE_VALUE)
-        return wide ? kernels_of<E, VE, GEAR_GATE_VALUE, BACKWARD>() : kernels_of<E, 1, GEAR_GATE_VALUE, BACKWARD>();
-    return wide ? kernels_of<E, VE, GEAR_GATE_SIGMOID, BACKWARD>() : kernels_of<E, 1, GEAR_GATE_SIGMOID, BACKWARD>();
+Kernels kernels_for(int32_t form, bool reset, bool wide) {
+    constexpr int VE = BACKWARD ? kBackwardChannels : kForwardBytes / (int)sizeof(E);
+    return wide ? kernels_for<E, VE, BACKWARD>(form, reset) : kernels_for<E, 1, BACKWARD>(form, reset);
 }
 
-// How a call is cut: channels per lane, lanes, segments.
+// How a call is cut: channels per lane; for a split one, segments of tiles and runs of them.
 struct Plan {
     int ve;
-    int64_t groups, lanes, tiles, seg_tiles;
-    int32_t S;
+    int64_t groups, lanes, columns, seg_tiles;
+    int32_t runs;
 };
 Plan plan_of(const gear_recurrence_desc& d, bool backward, bool in_place) {
     Plan p;
-    const int full = (backward ? kBackwardBytes : kForwardBytes) / float_bytes(d.dtype);
+    const int full = backward ? kBackwardChannels : kForwardBytes / float_bytes(d.dtype);
     // Widths below a lane's are taken channel by channel, as are odd ones
     // whose states are updated in place: lanes that share channels must not
     // read what another has written.
     p.ve = d.D < full || (in_place && d.D % full != 0) ? 1 : full;
     p.groups = (d.D + p.ve - 1) / p.ve;
     p.lanes = d.B * p.groups;
-    p.tiles = (d.T + kSteps - 1) / kSteps;
-    int64_t S = p.lanes > 0 ? kWantLanes / p.lanes : 1;
-    if (S > p.tiles) S = p.tiles;
-    if (S < 1) S = 1;
-    p.seg_tiles = (p.tiles + S - 1) / S;
-    p.S = p.seg_tiles > 0 ? (int32_t)((p.tiles + p.seg_tiles - 1) / p.seg_tiles) : 1;
+    p.columns = (p.lanes + 63) / 64;
+    p.seg_tiles = 0;
+    p.runs = 0;
+    const int64_t tiles = (d.T + kSteps - 1) / kSteps;
+    if (tiles < 2 || p.lanes == 0 || p.lanes > kWholeLanes) return p;
+    int64_t S = kWantLanes / p.lanes;
+    if (S > kMostSegments) S = kMostSegments;
+    if (S > tiles) S = tiles;
+    p.seg_tiles = (tiles + S - 1) / S;
+    S = (tiles + p.seg_tiles - 1) / p.seg_tiles;
+    p.runs = (int32_t)((S + kRun - 1) / kRun);
     return p;
 }
 int64_t work_bytes_of(const gear_recurrence_desc& d) {
-    const int32_t f = plan_of(d, false, false).S, b = plan_of(d, true, false).S, S = f > b ? f : b;
-    return S > 1 ? (int64_t)S * d.B * d.D * (int64_t)sizeof(Map) : 0;
+    const int32_t f = plan_of(d, false, false).runs, b = plan_of(d, true, false).runs;
+    return (int64_t)(f > b ? f : b) * (kRun + 1) * d.B * d.D * (int64_t)sizeof(Map);
 }
 int64_t saved_bytes_of(const gear_recurrence_desc& d) {
     const int64_t tiles = (d.T + kSteps - 1) / kSteps;
     return tiles > 1 ? (tiles - 1) * d.B * d.D * (int64_t)sizeof(float) : 0;
+}
+
+// Outputs that the last-level cache cannot hold are written past it, where a
+// wave writes whole lines of 128 bytes: forward and backward of 8192 x 32 x 512 in
+// bf16 took 422 us without and 369 with.  Rows that share lines want the cache:
+// 37 x 1000 x 1003 in fp16 took 192 us with it and 252 without; so do outputs that
+// it holds for the next reader (1 x 131072 x 512 in bf16: 124 and 129 us).
+constexpr int64_t kCacheBytes = 192ll << 20;  // of 256 MB, beside what else is in use
+bool streams(const gear_recurrence_desc& d, const void* out, const void* other, int outputs) {
+    const int64_t row = d.D * float_bytes(d.dtype);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(other);
+    return row % 128 == 0 && at % 128 == 0 && outputs * d.B * d.T * row > kCacheBytes;
 }
 
 unsigned blocks_for(int64_t items) {
@@ -448,19 +590,24 @@ const char* flaw(const gear_recurrence_desc* d) {
 
 template <typename E>
 int run(const Args& base, const Plan& p, int32_t form, bool backward, const char* what, hipStream_t s) {
-    const Kernels k = backward ? kernels_for<E, true>(form, p.ve > 1) : kernels_for<E, false>(form, p.ve > 1);
+    const Kernels k = backward ? kernels_for<E, true>(form, base.reset != nullptr, p.ve > 1)
+                               : kernels_for<E, false>(form, base.reset != nullptr, p.ve > 1);
     const int64_t BD = base.B * base.D;
-    if (p.S > 1) {
-        hipLaunchKernelGGL(k.maps, dim3(blocks_for(p.lanes * p.S)), dim3(kThreads), 0, s, base);
-        hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return hip_fail(e, what);
-        hipLaunchKernelGGL(backward ? carry_kernel<true> : carry_kernel<false>, dim3((unsigned)((BD + 63) / 64)),
-                           dim3(64 * kCarryWaves), 0, s, base.maps, backward ? base.dfinal : base.state, BD, p.S);
-        e = hipGetLastError();
-        if (e != hipSuccess) return hip_fail(e, what);
+    if (p.runs == 0) {
+        hipLaunchKernelGGL(k.whole, dim3(blocks_for(p.lanes)), dim3(kThreads), 0, s, base);
+        const hipError_t e = hipGetLastError();
+        return e == hipSuccess ? GEAR_OK : hip_fail(e, what);
     }
-    hipLaunchKernelGGL(k.whole, dim3(blocks_for(p.lanes * p.S)), dim3(kThreads), 0, s, base);
-    const hipError_t e = hipGetLastError();
+    const dim3 grid((unsigned)(p.columns * p.runs)), block(64 * kRun);
+    hipLaunchKernelGGL(k.maps, grid, block, 0, s, base);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return hip_fail(e, what);
+    hipLaunchKernelGGL(carry_kernel, dim3((unsigned)((BD + 63) / 64)), dim3(64 * kCarryWaves), 0, s, base.run_maps,
+                       backward ? base.dfinal : base.state, BD, p.runs);
+    e = hipGetLastError();
+    if (e != hipSuccess) return hip_fail(e, what);
+    hipLaunchKernelGGL(k.split, grid, block, 0, s, base);
+    e = hipGetLastError();
     return e == hipSuccess ? GEAR_OK : hip_fail(e, what);
 }
 
@@ -477,7 +624,8 @@ Args args_of(const gear_recurrence_desc& d, const Plan& p, void* work) {
     Args a{};
     a.reset = d.d_reset;
     a.lengths = d.d_lengths;
-    a.maps = static_cast<Map*>(work);
+    a.run_maps = static_cast<Map*>(work);
+    a.maps = a.run_maps + (int64_t)p.runs * d.B * d.D;
     a.B = d.B;
     a.T = d.T;
     a.D = d.D;
@@ -491,7 +639,8 @@ Args args_of(const gear_recurrence_desc& d, const Plan& p, void* work) {
     a.groups = p.groups;
     a.lanes = p.lanes;
     a.seg_tiles = p.seg_tiles;
-    a.S = p.S;
+    a.columns = p.columns;
+    a.runs = p.runs;
     return a;
 }
 
@@ -526,6 +675,7 @@ extern "C" int gear_recurrence(const gear_recurrence_desc* d, const void* d_gate
     a.y = d_y;
     a.final_state = d_final;
     a.out_saved = d_saved;
+    a.stream = streams(*d, d_y, nullptr, 1);
     return dispatch(a, p, *d, false, "gear_recurrence: launch", static_cast<hipStream_t>(stream));
 }
 
@@ -554,5 +704,6 @@ extern "C" int gear_recurrence_backward(const gear_recurrence_desc* d, const voi
     a.dgate = d_dgate;
     a.dx = d_dx;
     a.dstate = d_dstate;
+    a.stream = streams(*d, d_dgate, d_dx, 2);
     return dispatch(a, p, *d, true, "gear_recurrence_backward: launch", static_cast<hipStream_t>(stream));
 }
