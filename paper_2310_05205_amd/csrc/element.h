@@ -19,10 +19,12 @@ struct Vec {
     typedef uint32_t words __attribute__((ext_vector_type(sizeof(raw) / 4)));
     typedef words loose __attribute__((aligned(sizeof(E))));
 
-    // N elements at p, which need no alignment beyond the element's own, read
-    // past the caches: 5 to 15% faster where tensors exceed them.
+    // N elements at p, which need no alignment beyond the element's own; with
+    // STREAM past the caches, 5 to 15% faster where tensors exceed them.
+    template <bool STREAM = false>
     static __device__ __forceinline__ raw load(const E* p) {
-        return __builtin_bit_cast(raw, __builtin_nontemporal_load(reinterpret_cast<const loose*>(p)));
+        if (STREAM) return __builtin_bit_cast(raw, __builtin_nontemporal_load(reinterpret_cast<const loose*>(p)));
+        return __builtin_bit_cast(raw, *reinterpret_cast<const loose*>(p));
     }
     static __device__ __forceinline__ void unpack(raw v, float (&f)[N]) {
         const wide w = __builtin_convertvector(v, wide);
@@ -46,25 +48,17 @@ struct Vec {
 template <typename E>
 struct Vec<E, 1> {
     typedef E raw;
+    template <bool STREAM = false>
     static __device__ __forceinline__ raw load(const E* p) { return *p; }
     static __device__ __forceinline__ void unpack(raw v, float (&f)[1]) { f[0] = (float)v; }
     template <bool STREAM = false>
     static __device__ __forceinline__ void store(E* p, const float (&f)[1]) { *p = (E)f[0]; }
 };
 
-// Element i of an array whose type is known at run time.
-__device__ __forceinline__ float load_float(const void* p, int32_t dtype, int64_t i) {
-    if (dtype == GEAR_DTYPE_F32) return static_cast<const float*>(p)[i];
-    if (dtype == GEAR_DTYPE_BF16) return (float)static_cast<const __bf16*>(p)[i];
-    return (float)static_cast<const _Float16*>(p)[i];
-}
-
-// Natural exp and log by the hardware's base-2 instructions.  exp's relative
-// error grows as |x| 2^-24 (the product's rounding), log's absolute error is
-// that of its result's last bit.
+// Natural exp by the hardware's base-2 instruction: its relative error grows as
+// |x| 2^-24 (the product's rounding).
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
-__device__ __forceinline__ float fast_log(float x) { return __builtin_amdgcn_logf(x) * kLn2; }
 
 // Whether the library's float operators take tensors of this type, and its size.
 inline int float_bytes(int32_t dtype) {

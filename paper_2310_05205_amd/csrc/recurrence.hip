@@ -139,7 +139,7 @@ struct Tile {
         hide(p);
 #pragma unroll
         for (int i = 0; i < kSteps; i++) {
-            if (FULL || i < count) v[i] = Vec<E, VE>::load(p);
+            if (FULL || i < count) v[i] = Vec<E, VE>::template load<true>(p);
             p += stride;
         }
     }

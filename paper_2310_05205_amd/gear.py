@@ -373,11 +373,15 @@ def topk_merge(prio, gidx, K, T, L, seed, device=0):
 def _on_stream(call, x, stream, *args):
     """call(*args, stream handle) on `stream` or the current stream of x's
     device; outputs and workspace are allocated for that stream."""
-    import torch
-    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+    try:
+        device = x.get_device()  # -1 on the CPU
+    except AttributeError:
+        device = -1
+    if device < 0:
         raise ValueError("tensors must be torch tensors on the GPU")
+    import torch
     if stream is None:
-        return _result(call(*args, torch._C._cuda_getCurrentRawStream(x.device.index)))
+        return _result(call(*args, torch._C._cuda_getCurrentRawStream(device)))
     with torch.cuda.stream(stream):
         return _result(call(*args, stream.cuda_stream))
 
