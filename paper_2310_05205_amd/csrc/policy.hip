@@ -144,16 +144,18 @@ struct Scale {
 };
 __device__ __forceinline__ Scale scale_of(float m) { return Scale{m == -INFINITY ? 0.0f : m}; }  // a row of -inf sums to 0
 
-// Adds a piece's 2^d and d 2^d.
-template <int VE>
+// Adds a piece's 2^d and d 2^d.  With TAME no logit is far enough out for its d,
+// or a multiple of it, to be infinite, and need not be kept from it.
+template <bool TAME, int VE>
 __device__ __forceinline__ void add_piece(const float (&f)[VE], const Scale& dist, float& S, float& dS) {
 #pragma unroll
     for (int j = 0; j < VE; j++) {
         const float d = dist(f[j]), e = __builtin_amdgcn_exp2f(d);
         S += e;
-        dS = fmaf(e, fmaxf(d, kFloor), dS);
+        dS = fmaf(e, TAME ? d : fmaxf(d, kFloor), dS);
     }
 }
+constexpr float kTame = 1e9f;
 
 // Sums against logit m become sums against logit `top`, which is no smaller.
 struct Sums {
@@ -244,9 +246,11 @@ __device__ __forceinline__ Row row_terms(const Args& a, const Inputs& in, float 
 // dz_j = 2^d_j (k1 d_j + k0), and k2 more for the action.
 struct Slope {
     float k0, k1, k2;
-    __device__ __forceinline__ float operator()(float d) const {
-        return __builtin_amdgcn_exp2f(d) * fmaf(k1, fmaxf(d, kFloor), k0);
+    template <bool TAME>
+    __device__ __forceinline__ float at(float d) const {
+        return __builtin_amdgcn_exp2f(d) * fmaf(k1, TAME ? d : fmaxf(d, kFloor), k0);
     }
+    __device__ __forceinline__ float operator()(float d) const { return at<false>(d); }
 };
 __device__ __forceinline__ Slope slope_of(const Args& a, const Row& r, float S) {
     const float f = r.s * __builtin_amdgcn_rcpf(S), g = a.ent * kLn2;
@@ -357,7 +361,7 @@ __device__ __forceinline__ void load_piece(Piece<E>& v, const E* z, int V, int m
 }
 
 // Writes the gradient of the elements that load_piece gave to this lane.
-template <typename E, int G, bool TINY>
+template <typename E, int G, bool TINY, bool TAME>
 __device__ __forceinline__ void store_piece(E* g, const Piece<E>& v, int V, int mine, int i, const Slope& slope,
                                             const Scale& dist) {
     constexpr int VE = Piece<E>::VE;
@@ -365,7 +369,7 @@ __device__ __forceinline__ void store_piece(E* g, const Piece<E>& v, int V, int 
     float f[VE], o[VE];
     v.unpack(f);
 #pragma unroll
-    for (int j = 0; j < VE; j++) o[j] = slope(dist(f[j]));
+    for (int j = 0; j < VE; j++) o[j] = slope.template at<TAME>(dist(f[j]));
     if (!TINY && ((i + 1) * G * VE <= V || base + VE <= V)) {
         Vec<E, VE>::store(g + base, o);
     } else {
@@ -441,7 +445,7 @@ __global__ __launch_bounds__(THREADS, WAVES) void held_kernel(const Args a) {
         for (int i = 0; i < NV; i++) {
             float f[VE];
             v[i].unpack(f);
-            add_piece(f, dist, S, dS);
+            add_piece<false>(f, dist, S, dS);
             v[i].forget();
         }
         S = group_add<G>(S);
@@ -462,7 +466,7 @@ __global__ __launch_bounds__(THREADS, WAVES) void held_kernel(const Args a) {
             asm volatile("" : "+v"(mine));
 #pragma unroll
             for (int i = 0; i < NV; i++)
-                if (i * G * VE < V) store_piece<E, G, TINY>(g, v[i], V, mine, i, slope, dist);
+                if (i * G * VE < V) store_piece<E, G, TINY, false>(g, v[i], V, mine, i, slope, dist);
             // The action's, over the value just written by the same lane.
             if (some && lane == (TINY ? 0 : (int)action / VE % G)) g[action] = (E)(slope(dist(za)) + slope.k2);
         }
@@ -502,6 +506,7 @@ __global__ __launch_bounds__(THREADS, LOSS ? 4 : 8) void block_kernel(const Args
                 for (int i = 0; i < kHeld; i++) load_piece<E, G>(v[i], z, V, mine, i);
             }
             float za = 0.0f, m = -INFINITY, S = 0.0f, dS = 0.0f;
+            bool tame = true;  // the wave's pieces; the row's largest logit is looked at below
             Inputs in{};
             if (threadIdx.x == 0) {
                 za = (float)z[action];
@@ -519,13 +524,22 @@ __global__ __launch_bounds__(THREADS, LOSS ? 4 : 8) void block_kernel(const Args
                         float f[VE], h[VE];
                         v[i].unpack(f);
                         v[i + 1].unpack(h);
-                        float top = m;
+                        float top = m, low = kTame;
 #pragma unroll
-                        for (int j = 0; j < VE; j++) top = fmaxf(fmaxf(top, f[j]), h[j]);
+                        for (int j = 0; j < VE; j++) {
+                            top = fmaxf(fmaxf(top, f[j]), h[j]);
+                            low = fminf(fminf(low, f[j]), h[j]);
+                        }
                         rescale(m, top, S, dS);
                         m = top;
-                        add_piece(f, scale_of(m), S, dS);
-                        add_piece(h, scale_of(m), S, dS);
+                        if (__all(low > -kTame && top < kTame)) {
+                            add_piece<true>(f, scale_of(m), S, dS);
+                            add_piece<true>(h, scale_of(m), S, dS);
+                        } else {
+                            tame = false;
+                            add_piece<false>(f, scale_of(m), S, dS);
+                            add_piece<false>(h, scale_of(m), S, dS);
+                        }
                         v[i].forget();
                         v[i + 1].forget();
                     }
@@ -564,10 +578,14 @@ __global__ __launch_bounds__(THREADS, LOSS ? 4 : 8) void block_kernel(const Args
                 const bool some = m != -INFINITY;
                 const Slope slope = some ? slope_of(a, r, S) : Slope{};
                 asm volatile("" : "+v"(mine));
-                if (a.grad) {
+                if (a.grad && tame && m < kTame) {
 #pragma unroll
                     for (int i = 0; i < kHeld; i++)
-                        if (i * G * VE < V) store_piece<E, G, false>(g, v[i], V, mine, i, slope, dist);
+                        if (i * G * VE < V) store_piece<E, G, false, true>(g, v[i], V, mine, i, slope, dist);
+                } else if (a.grad) {
+#pragma unroll
+                    for (int i = 0; i < kHeld; i++)
+                        if (i * G * VE < V) store_piece<E, G, false, false>(g, v[i], V, mine, i, slope, dist);
                 }
                 // The action's, over the value just written by the same lane.
                 if (a.grad && some && mine == (int)action / VE % G) g[action] = (E)(slope(dist(za)) + slope.k2);
@@ -692,7 +710,8 @@ constexpr int kCUs = 256;
 constexpr int resident(int threads, int waves) { return kCUs * waves * 4 / (threads / 64); }
 template <typename E, int G, int NV, int WAVES, bool LOSS, bool TINY = false>
 Choice held(bool solo) {
-    if constexpr (LOSS) {
+    // 64 lanes with more than 4 pieces each have more actions than one workgroup takes on.
+    if constexpr (LOSS && NV <= 4) {
         if (solo) return {held_kernel<E, G, NV, kSoloThreads, 4, TINY, true>, kSoloThreads, kSoloThreads / G, 1};
     }
     constexpr int W = LOSS ? WAVES : 8;
@@ -720,7 +739,7 @@ Choice choose(int64_t V, bool solo) {
     if (pieces <= 32) return held<E, 8, 4, 6, LOSS>(solo);
     if (pieces <= 64) return held<E, 16, 4, 6, LOSS>(solo);
     if (pieces <= 256) return held<E, 64, 4, 6, LOSS>(solo);
-    if (pieces <= 512) return held<E, 64, 8, 4, LOSS>(false);
+    if (pieces <= 512) return held<E, 64, 8, 4, LOSS>(solo);
     if (pieces <= 1024) return block<E, 4, 256, LOSS>();
     if (pieces <= 4096) return block<E, 16, 256, LOSS>();
     if (pieces <= 8192) return block<E, 16, 512, LOSS>();
