@@ -23,6 +23,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kFew = 4, kMany = 8;     // steps of a lane in a tile
 constexpr int64_t kWantGroups = 8192;  // waves that fill the GPU
+// Calls of fewer windows, of at least so many tiles each, are split.  In fp32, split
+// and not: 1 window of 2100 steps (5 tiles) 10.4 and 9.2 us, 1 of 4200 11 and 15, 256
+// of 4200 11 and 14, 256 of 16400 22 and 43, 1024 of 4200 21 and 17, 4096 of 600 18 and 10.
+constexpr int64_t kWholeWindows = 1024, kSplitTiles = 6;
 constexpr int64_t kMaxBlocks = 1 << 22;
 
 // c -> P c + Z with P in [0, 1], or Z whatever c (P = -1): a step that ended
@@ -109,7 +113,10 @@ __device__ __forceinline__ Map suffix(Map m, int lane) {
     return m;
 }
 
-// G lanes share a window or, with S > 1, a segment of one.
+// G lanes share a window or, with S > 1, a segment of one.  8192 windows of 32
+// fp32 steps take 3.4 us, a launch and two dependent loads; 19 of 262147 bf16
+// steps 9 us for the maps and 15 for the results, 40 MB written and 25 read
+// in each: latency and instructions, with memory's share about 10.
 template <typename ER, typename EV, int G, int PER, bool MAPS>
 __global__ __launch_bounds__(kThreads) void advantage_kernel(const Args a) {
     const int lane = threadIdx.x % G;
@@ -207,7 +214,7 @@ Plan plan_of(const gear_advantages_desc& d) {
     while (p.G < 64 && (int64_t)p.G * kFew < d.L) p.G *= 2;
     p.per = (int64_t)p.G * kFew < d.L ? kMany : kFew;
     const int64_t tile = (int64_t)p.G * p.per, tiles = (d.L + tile - 1) / tile;
-    int64_t S = d.B > 0 ? kWantGroups / d.B : 1;
+    int64_t S = d.B > 0 && d.B < kWholeWindows && tiles >= kSplitTiles ? kWantGroups / d.B : 1;
     if (S > tiles) S = tiles;
     if (S < 1) S = 1;
     p.seg_tiles = (tiles + S - 1) / S;

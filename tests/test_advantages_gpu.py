@@ -45,6 +45,14 @@ def test_against_definition(B, L, done, ragged, rt, vt):
     check(*make(B, L, rt, vt, B + L, done, ragged)[:2], 0.99, 0.95, *make(B, L, rt, vt, B + L, done, ragged)[2:])
 
 
+@pytest.mark.parametrize("B,L", [(2, 513), (2, 2560), (2, 2561), (1023, 2600), (1024, 2600), (1030, 600)])
+def test_around_the_split(B, L):
+    """Windows just too short and just long enough for segments, and calls of nearly too many and too many windows."""
+    r, v, d, n = make(B, L, "bfloat16", "float32", B + L, 0.01, True)
+    say("advantages around the split B=%d L=%d" % (B, L))
+    check(r, v, 0.99, 0.95, d, n)
+
+
 @pytest.mark.parametrize("gamma,lam", [(0.0, 0.95), (1.0, 0.0), (1.0, 1.0), (0.5, 1.0)])
 def test_limits_of_the_discounts(gamma, lam):
     r, v, d, n = make(4, 900, "float32", "float32", 1, 0.01, True)

@@ -69,6 +69,14 @@ def test_against_definition(B, T, D, packed, reset, ragged, dtype, sigmoid):
     check(*make(B, T, D, dtype, 7 * B + T + D, sigmoid, packed, reset, ragged), dtype, sigmoid)
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("B,T,D", [(2, 80, 9), (2, 81, 9), (3, 96, 66), (3, 97, 66), (270, 97, 256), (505, 83, 260)])
+def test_around_the_split(B, T, D, dtype):
+    """Windows just too short and just long enough for segments, and calls of nearly too many and too many channels."""
+    say("recurrence around the split B=%d T=%d D=%d %s" % (B, T, D, dtype))
+    check(*make(B, T, D, dtype, B + T, True, True, 0.05, True), dtype, True)
+
+
 @pytest.mark.parametrize("T", [5, 40, 2000])
 def test_without_states_and_gradients(T):
     gate, x, dy, _, _, r, n = make(2, T, 9, "float32", 3, True, reset=0.1)
