@@ -9,7 +9,10 @@
  *                importance-sampling weights, priority-update scatter;
  *   collection - gather of fixed-length windows of selected trajectories
  *                into contiguous per-column batches, from a table held in
- *                HBM or in pinned host memory read zero-copy by the kernel.
+ *                HBM or in pinned host memory read zero-copy by the kernel;
+ *   learning   - what a learner computes on the collected windows: a gated
+ *                linear recurrence with its gradients, advantages, and the
+ *                clipped policy loss with its gradient.
  *
  * Conventions for every call:
  *   - Return value: GEAR_OK (0) or a negative GEAR_E_* code, with a message
@@ -55,8 +58,9 @@
  *         GEAR_SMALL_SELECT_MAX_N slots, for batches of at most
  *         GEAR_SMALL_SELECT_MAX_B and without GEAR_OPT_INCREMENTAL_TREE
  *         (one launch, no sum tree);
- *       gear_update_priorities without GEAR_OPT_INCREMENTAL_TREE.
- *     They read the table's ring position, live count and options when
+ *       gear_update_priorities without GEAR_OPT_INCREMENTAL_TREE;
+ *       the learner's operators, which choose by their arguments alone.
+ *     The calls on a table read its ring position, live count and options when
  *     captured, so no insertion, allocation, commit or option change may
  *     come between a capture and its replays.  Prioritized selection on
  *     larger tables decides at each call whether to rebuild the sum tree,

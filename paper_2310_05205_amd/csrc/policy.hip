@@ -627,8 +627,8 @@ __global__ __launch_bounds__(THREADS, LOSS ? 4 : 8) void block_kernel(const Args
 }
 
 // Rows longer than registers hold: a workgroup per row, which reads it three
-// times, twice from the last-level cache: such rows are many megabytes together
-// but a launch's are less than it holds.
+// times, the second and third from the last-level cache as long as it holds the
+// 256 rows at work together (512 K logits each in 16 bits).
 template <typename E, bool LOSS>
 __global__ __launch_bounds__(kSoloThreads) void long_kernel(const Args a) {
     constexpr int kWaves = kSoloThreads / 64;
