@@ -728,7 +728,7 @@ Choice held(bool solo) {
     if constexpr (LOSS && NV <= 4) {
         if (solo) return {held_kernel<E, G, NV, kSoloThreads, 4, TINY, true>, kSoloThreads, kSoloThreads / G, 1};
     }
-    constexpr int W = LOSS ? WAVES : 8;
+    constexpr int W = LOSS ? WAVES : NV > 8 ? 5 : 8;
     return {held_kernel<E, G, NV, kThreads, W, TINY, LOSS>, kThreads, kThreads / G, resident(kThreads, W)};
 }
 template <typename E, int NV, int THREADS, bool LOSS>
@@ -740,8 +740,11 @@ Choice block() {
 // that what is done once per row is done by few (2097152 rows of 16 bf16: 116 us
 // with two lanes a row, 78 with one, everything else as it then was), then up to 16
 // pieces, which leaves more workgroups to hide one's barrier (4096 rows of 32768
-// bf16: 115 us with 256 lanes of 16, 127 with 512 of 8).  How many lanes share a
-// row, and so the order of its sums, depends on V alone.
+// bf16: 115 us with 256 lanes of 16, 127 with 512 of 8).  A wave keeps rows of up to
+// 12 pieces a lane to itself: 16384 rows of 2047, 2304, 4096, 5000 and 7000 bf16
+// take it 45, 61, 70, 94 and (16 pieces) 116 us, and a workgroup 87, 96, 90, 117
+// and 127, but 120 and 117 at 8192; log-probabilities likewise, 50 and 50 there.
+// How many lanes share a row, and so the order of its sums, depends on V alone.
 template <typename E, bool LOSS>
 Choice choose(int64_t V, bool solo) {
     constexpr int VE = 16 / sizeof(E);
@@ -757,6 +760,7 @@ Choice choose(int64_t V, bool solo) {
     if (pieces <= 64) return held<E, 16, 4, 6, LOSS>(solo);
     if (pieces <= 256) return held<E, 64, 4, 6, LOSS>(solo);
     if (pieces <= 512) return held<E, 64, 8, 4, LOSS>(solo);
+    if (pieces <= 768) return held<E, 64, 12, 4, LOSS>(solo);
     if (pieces <= 1024) return block<E, 4, 256, LOSS>();
     if (pieces <= 4096) return block<E, 16, 256, LOSS>();
     if (pieces <= 8192) return block<E, 16, 512, LOSS>();

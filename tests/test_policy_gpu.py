@@ -85,6 +85,13 @@ def test_against_definition(lead, V, mask, dtype):
     check(*make(lead, V, dtype, V, mask), scale=64.0)
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("V", [2500, 3071, 3073, 5000, 6143, 6144, 6145])
+def test_longest_rows_of_a_wave(V, dtype):
+    say("policy V=%d %s" % (V, dtype))
+    check(*make((2100 if V == 5000 else 6,), V, dtype, V, True), scale=64.0)
+
+
 @pytest.mark.parametrize("action", list(ACTIONS))
 @pytest.mark.parametrize("case", ["plain", "no-kl", "no-ref", "no-entropy", "denom", "wide-clip", "negative"])
 def test_terms(case, action):
