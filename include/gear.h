@@ -621,6 +621,12 @@ int gear_recurrence_sizes(const gear_recurrence_desc *d, int64_t *saved_bytes, i
  *   d_work       workspace; its contents do not matter.  May be NULL when
  *                gear_recurrence_sizes states 0
  *
+ * Long windows of few channels are worked on in segments, side by side.  Where
+ * a value that one segment hands to the next is not below 2^40 (states that grow
+ * under gates beyond 1, an infinity, a NaN), the call goes through the steps
+ * one after the other instead: results as by the definition's steps, for
+ * many times the time.  The same holds for the gradients.
+ *
  * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
  */
 int gear_recurrence(const gear_recurrence_desc *d, const void *d_gate, const void *d_x, const float *d_state,

@@ -14,6 +14,8 @@
 // workgroup's run of segments, to what it does to a value carried through it
 // (an affine map), one applies the runs' maps in order, and the last goes
 // through every segment from its own first value.
+#include <type_traits>
+
 #include "element.h"
 #include "gear_internal.h"
 
@@ -39,23 +41,66 @@ constexpr int kWantLanes = 8192 * 64;   // lanes that a split call is cut into, 
 constexpr int kMostSegments = 1024;     // more segments of long windows cost more in maps than they gain
 constexpr int64_t kMaxBlocks = 1 << 22;
 constexpr int kRun = 8;  // segments of a workgroup of a split call, a wave each
+constexpr int32_t kMostExponent = 1 << 20;  // of a segment's decays: those of all segments together fit 31 bits
 
-// A map c -> P c + Z of a carried value; a reset inside it cuts the value
-// off, which P holds as these bits (a NaN that no operation makes), because
-// 0 c would be NaN for an infinite c.
-constexpr uint32_t kCutBits = 0x7FC0DEADu;
-struct Map {
+// What a segment does to the value c carried through it: c -> P c + Z, with a P of
+// 0 from a reset on.  A sigmoid's decays are 1 at most: what their product loses
+// below 2^-149 no later step raises again.
+struct DecayMap {
     float P, Z;
+    __device__ __forceinline__ float apply(float c) const { return fmaf(P, c, Z); }
+    // `early` before this one.
+    __device__ __forceinline__ DecayMap after(DecayMap early) const { return {P * early.P, apply(early.Z)}; }
 };
-__device__ __forceinline__ float apply(Map m, float c) {
-    return __float_as_uint(m.P) == kCutBits ? m.Z : fmaf(m.P, c, m.Z);
-}
+// Gates as given may exceed 1, and their product P 2^n has an exponent of its own:
+// fp32 alone would pass into an infinity, or into a 0, which loses what later
+// steps raise again.  A P of 0 leaves nothing of any c, which may have grown to an
+// infinity before a reset.
+struct GrowthMap {
+    float P, Z;
+    int32_t n;
+    __device__ __forceinline__ float apply(float c) const {
+        const int32_t e = n < -1024 ? -1024 : n > 1024 ? 1024 : n;
+        return __builtin_amdgcn_ldexpf(P == 0.0f ? 0.0f : P * c, e) + Z;
+    }
+    __device__ __forceinline__ GrowthMap after(GrowthMap early) const {
+        const float p = P * early.P;
+        return {__builtin_amdgcn_frexp_mantf(p), apply(early.Z), n + early.n + __builtin_amdgcn_frexp_expf(p)};
+    }
+};
+template <int FORM>
+using Map = std::conditional_t<FORM == GEAR_GATE_VALUE, GrowthMap, DecayMap>;
 
-// `early` first, then `late`.
-__device__ __forceinline__ Map compose(Map late, Map early) {
-    const bool cut = __float_as_uint(late.P) == kCutBits || __float_as_uint(early.P) == kCutBits;
-    return Map{cut ? __uint_as_float(kCutBits) : late.P * early.P, apply(late, early.Z)};
-}
+// The product of a segment's decays so far.
+template <int FORM>
+struct Product {
+    float P = 1.0f;
+    __device__ __forceinline__ void multiply(float f) { P *= f; }
+    __device__ __forceinline__ void end_tile() {}
+    __device__ __forceinline__ DecayMap map(float Z, bool cut) const { return {cut ? 0.0f : P, Z}; }
+};
+template <>
+struct Product<GEAR_GATE_VALUE> {
+    float P = 1.0f;
+    int32_t n = 0;
+    __device__ __forceinline__ void multiply(float f) {  // 16 factors of at least 0.5 stay in range
+        P *= __builtin_amdgcn_frexp_mantf(f);
+        n += __builtin_amdgcn_frexp_expf(f);
+    }
+    __device__ __forceinline__ void end_tile() {
+        n += __builtin_amdgcn_frexp_expf(P);
+        P = __builtin_amdgcn_frexp_mantf(P);
+        n = n < -kMostExponent ? -kMostExponent : n > kMostExponent ? kMostExponent : n;
+    }
+    __device__ __forceinline__ GrowthMap map(float Z, bool cut) const { return {cut ? 0.0f : P, Z, n}; }
+};
+
+// A map gives the value of the steps as long as its two parts do not cancel and
+// none of them overflows.  Where a Z, or a value carried from run to run, is
+// this large (growth, an infinity, a NaN), the call is not trusted to maps: its
+// lanes go through all their steps, as in calls that are not split.
+constexpr float kTrusted = 0x1p40f;
+__device__ __forceinline__ bool trusted(float v) { return fabsf(v) < kTrusted; }
 
 struct Args {
     const void *gate, *x, *dy;
@@ -64,8 +109,9 @@ struct Args {
     float *final_state, *out_saved, *dstate;
     const uint8_t* reset;
     const int32_t* lengths;
-    Map* maps;            // of split calls: [runs * kRun][B][D], one per segment ...
-    Map* run_maps;        // ... and [runs][B][D], one per run; their first values after carry_kernel
+    void* maps;           // of split calls: Map<FORM>[runs * kRun][B][D], one per segment, and [runs][B][D], one per
+                          // run, whose first value carry_kernel leaves in P
+    int32_t* doubt;       // whether carry_kernel found one that is not trusted
     int64_t B, T, D, gate_b, gate_t, x_b, x_t, dy_b, dy_t, reset_b;
     int64_t groups;       // of VE channels in a window
     int64_t lanes;        // B * groups
@@ -175,7 +221,7 @@ __device__ __forceinline__ Rows<E> rows_of(const Args& a, const Place& p) {
 // `count` steps of the recurrence from step t0 on; zeros up to `room`.
 template <typename E, int VE, int FORM, bool RESET, bool MAPS, bool FULL, bool STREAM>
 __device__ __forceinline__ void forward_tile(const Args& a, const Rows<E>& rows, int64_t t0, int count, int room,
-                                             const Flags& flags, float (&h)[VE], float (&P)[VE]) {
+                                             const Flags& flags, float (&h)[VE], Product<FORM> (&P)[VE]) {
 #pragma clang fp contract(off)  // full and other tiles round alike: lanes that share channels may have either
     Tile<E, VE> g, x;
     g.template load<FULL>(rows.gate + t0 * a.gate_t, a.gate_t, count);
@@ -195,7 +241,7 @@ __device__ __forceinline__ void forward_tile(const Args& a, const Rows<E>& rows,
                 gates<FORM>(gv[j], f, w);
                 const float u = FORM == GEAR_GATE_VALUE ? xv[j] : w * xv[j];
                 h[j] = z ? u : fmaf(f, h[j], u);
-                if (MAPS) P[j] *= f;
+                if (MAPS) P[j].multiply(f);
             }
             if (!MAPS && a.y) Vec<E, VE>::template store<STREAM>(y, h);
         } else if (!MAPS && s < room && a.y) {
@@ -223,45 +269,55 @@ __device__ __forceinline__ Part part_of(const Args& a) {
     return w;
 }
 
-// Leaves a wave's map, and the first wave its workgroup's.
-template <int VE>
-__device__ __forceinline__ void leave_maps(const Args& a, const Part& w, int64_t at, const Map (&m)[VE],
-                                           Map (*s)[VE][64]) {
+// Leaves a wave's map, and the first wave its workgroup's, with a Z of NaN where
+// that of a segment, or of the segments so far, is not trusted.
+template <int FORM, int VE>
+__device__ __forceinline__ void leave_maps(const Args& a, const Part& w, int64_t at, const Map<FORM> (&m)[VE],
+                                           Map<FORM> (*s)[VE][64]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t BD = a.B * a.D;
+    Map<FORM>* const maps = static_cast<Map<FORM>*>(a.maps);
+    const int64_t BD = a.B * a.D, run_maps = (int64_t)a.runs * kRun * BD;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.doubt = 0;  // for the next launch
 #pragma unroll
     for (int j = 0; j < VE; j++) {
         s[wave][j][lane] = m[j];
-        if (w.used) a.maps[w.seg * BD + at + j] = m[j];
+        if (w.used) maps[w.seg * BD + at + j] = m[j];
     }
     __syncthreads();
     if (wave > 0) return;
 #pragma unroll
     for (int j = 0; j < VE; j++) {
-        Map all = m[j];
+        Map<FORM> all = m[j];
+        bool sound = trusted(all.Z);
 #pragma unroll
-        for (int k = 1; k < kRun; k++) all = compose(s[k][j][lane], all);
-        if (w.used) a.run_maps[w.run * BD + at + j] = all;
+        for (int k = 1; k < kRun; k++) {
+            const Map<FORM> next = s[k][j][lane];
+            all = next.after(all);
+            sound = sound && trusted(next.Z) && trusted(all.Z);
+        }
+        if (!sound) all.Z = NAN;
+        if (w.used) maps[run_maps + w.run * BD + at + j] = all;
     }
 }
 
 // The value a wave's segment starts from: its run's, through the run's earlier segments.
-template <int VE>
+template <int FORM, int VE>
 __device__ __forceinline__ void first_of(const Args& a, const Part& w, int64_t at, float (&c)[VE]) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t BD = a.B * a.D;
+    const Map<FORM>* const maps = static_cast<const Map<FORM>*>(a.maps);
+    const int64_t BD = a.B * a.D, run_maps = (int64_t)a.runs * kRun * BD;
 #pragma unroll
-    for (int j = 0; j < VE; j++) c[j] = a.run_maps[w.run * BD + at + j].P;
+    for (int j = 0; j < VE; j++) c[j] = maps[run_maps + w.run * BD + at + j].P;
     for (int k = 0; k < wave; k++) {
 #pragma unroll
-        for (int j = 0; j < VE; j++) c[j] = apply(a.maps[((int64_t)w.run * kRun + k) * BD + at + j], c[j]);
+        for (int j = 0; j < VE; j++) c[j] = maps[((int64_t)w.run * kRun + k) * BD + at + j].apply(c[j]);
     }
 }
 
 // The steps of lane q from tile k0 to tile k1, from state h.
 template <typename E, int VE, int FORM, bool RESET, bool MAPS>
 __device__ __forceinline__ bool forward_tiles(const Args& a, const Place& p, int64_t at, bool used, int64_t k0, int64_t k1,
-                                              float (&h)[VE], float (&P)[VE]) {
+                                              float (&h)[VE], Product<FORM> (&P)[VE]) {
     const Rows<E> rows = rows_of<E>(a, p);
     const int64_t BD = a.B * a.D;
     bool cut = false;
@@ -277,6 +333,10 @@ __device__ __forceinline__ bool forward_tiles(const Args& a, const Place& p, int
             forward_tile<E, VE, FORM, RESET, MAPS, true, true>(a, rows, t0, count, room, flags, h, P);
         else forward_tile<E, VE, FORM, RESET, MAPS, true, false>(a, rows, t0, count, room, flags, h, P);
         if (RESET) cut |= flags.any();
+        if (MAPS) {
+#pragma unroll
+            for (int j = 0; j < VE; j++) P[j].end_tile();
+        }
     }
     return cut;
 }
@@ -289,7 +349,8 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(const Args a) {
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < a.lanes; i += (int64_t)gridDim.x * kThreads) {
         const Place p = place_of<VE>(a, i);
         const int64_t at = p.b * a.D + p.c;
-        float h[VE], P[VE];
+        float h[VE];
+        Product<FORM> P[VE];
 #pragma unroll
         for (int j = 0; j < VE; j++) h[j] = a.state ? a.state[at + j] : 0.0f;
         forward_tiles<E, VE, FORM, RESET, false>(a, p, at, true, 0, (a.T + kSteps - 1) / kSteps, h, P);
@@ -303,27 +364,27 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(const Args a) {
 // them 5.5; at 1 x 131072 x 512 bf16 49, 69 and 5.5.
 template <typename E, int VE, int FORM, bool RESET, bool MAPS>
 __global__ __launch_bounds__(64 * kRun) void forward_split_kernel(const Args a) {
-    __shared__ Map s[MAPS ? kRun : 1][VE][64];
+    __shared__ Map<FORM> s[MAPS ? kRun : 1][VE][64];
     const Part w = part_of(a);
     const Place p = place_of<VE>(a, w.q);
     const int64_t at = p.b * a.D + p.c, tiles = (a.T + kSteps - 1) / kSteps;
     const int64_t k0 = w.seg * a.seg_tiles < tiles ? w.seg * a.seg_tiles : tiles;
-    const int64_t k1 = k0 + a.seg_tiles < tiles ? k0 + a.seg_tiles : tiles;
-    float h[VE], P[VE];
-#pragma unroll
-    for (int j = 0; j < VE; j++) {
-        P[j] = 1.0f;
-        h[j] = 0.0f;
-    }
-    if (!MAPS) first_of<VE>(a, w, at, h);
-    const bool cut = forward_tiles<E, VE, FORM, RESET, MAPS>(a, p, at, w.used, k0, k1, h, P);
+    int64_t k1 = k0 + a.seg_tiles < tiles ? k0 + a.seg_tiles : tiles;
+    float h[VE] = {};
+    Product<FORM> P[VE];
     if (MAPS) {
-        Map m[VE];
+        const bool cut = forward_tiles<E, VE, FORM, RESET, MAPS>(a, p, at, w.used, k0, k1, h, P);
+        Map<FORM> m[VE];
 #pragma unroll
-        for (int j = 0; j < VE; j++) m[j] = Map{cut ? __uint_as_float(kCutBits) : P[j], h[j]};
-        leave_maps<VE>(a, w, at, m, s);
-    } else if (w.used && a.final_state && k0 < k1 && k1 == tiles) {
-        Vec<float, VE>::store(a.final_state + at, h);
+        for (int j = 0; j < VE; j++) m[j] = P[j].map(h[j], cut);
+        leave_maps<FORM, VE>(a, w, at, m, s);
+    } else {
+        const int32_t doubt = *a.doubt;
+        first_of<FORM, VE>(a, w, at, h);
+        // In doubt the first segment's wave takes all tiles.
+        if (doubt) k1 = w.seg == 0 ? tiles : k0;
+        forward_tiles<E, VE, FORM, RESET, MAPS>(a, p, at, w.used, k0, k1, h, P);
+        if (w.used && a.final_state && k0 < k1 && k1 == tiles) Vec<float, VE>::store(a.final_state + at, h);
     }
 }
 
@@ -332,29 +393,37 @@ __global__ __launch_bounds__(64 * kRun) void forward_split_kernel(const Args a) 
 // composes a share of the runs, the shares' maps lead to every share's first
 // value, and the waves go through their shares again.
 constexpr int kCarryWaves = 16, kCarryAhead = 16;
-__global__ __launch_bounds__(64 * kCarryWaves) void carry_kernel(Map* __restrict__ maps, const float* __restrict__ first,
-                                                                int64_t channels, int32_t runs) {
-    __shared__ Map s_share[kCarryWaves][64];
+template <int FORM>
+__global__ __launch_bounds__(64 * kCarryWaves) void carry_kernel(const Args a, const float* __restrict__ first) {
+    const int64_t channels = a.B * a.D;
+    const int32_t runs = a.runs;
+    Map<FORM>* __restrict__ const maps = static_cast<Map<FORM>*>(a.maps) + (int64_t)runs * kRun * channels;
+    __shared__ Map<FORM> s_share[kCarryWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int64_t i = (int64_t)blockIdx.x * 64 + lane;
     const bool used = i < channels;
     if (!used) i = channels - 1;
     const int32_t share = (runs + kCarryWaves - 1) / kCarryWaves;
     const int32_t s0 = wave * share < runs ? wave * share : runs, s1 = s0 + share < runs ? s0 + share : runs;
-    Map whole = {1.0f, 0.0f}, m[kCarryAhead];
+    Map<FORM> whole = Product<FORM>().map(0.0f, false), m[kCarryAhead];
+    bool sound = true;
     for (int32_t s = s0; s < s1; s += kCarryAhead) {
         // Places past the share read its last map again and are not used.
 #pragma unroll
         for (int k = 0; k < kCarryAhead; k++) m[k] = maps[(s + k < s1 ? s + k : s1 - 1) * channels + i];
 #pragma unroll
-        for (int k = 0; k < kCarryAhead; k++)
-            if (s + k < s1) whole = compose(m[k], whole);
+        for (int k = 0; k < kCarryAhead; k++) {
+            if (s + k < s1) {
+                whole = m[k].after(whole);
+                sound = sound && trusted(m[k].Z) && trusted(whole.Z);
+            }
+        }
     }
     s_share[wave][lane] = whole;
     __syncthreads();
     if (!used) return;
     float c = first ? first[i] : 0.0f;
-    for (int k = 0; k < wave; k++) c = apply(s_share[k][lane], c);
+    for (int k = 0; k < wave; k++) c = s_share[k][lane].apply(c);
     for (int32_t s = s0; s < s1; s += kCarryAhead) {
         if (share > kCarryAhead) {
 #pragma unroll
@@ -363,11 +432,13 @@ __global__ __launch_bounds__(64 * kCarryWaves) void carry_kernel(Map* __restrict
 #pragma unroll
         for (int k = 0; k < kCarryAhead; k++) {
             if (s + k < s1) {
+                sound = sound && trusted(c);
                 maps[(s + k) * channels + i].P = c;
-                c = apply(m[k], c);
+                c = m[k].apply(c);
             }
         }
     }
+    if (!sound) *a.doubt = 1;
 }
 
 // A tile backward: G comes in as the gradient of the state after it and goes
@@ -376,7 +447,8 @@ __global__ __launch_bounds__(64 * kCarryWaves) void carry_kernel(Map* __restrict
 // its rounding into h_{t-1} - x_t.
 template <typename E, int VE, int FORM, bool RESET, bool MAPS, bool FULL, bool STREAM>
 __device__ __forceinline__ void backward_tile(const Args& a, const Rows<E>& rows, int64_t t0, int count, int room,
-                                              const Flags& flags, float (&h)[VE], float (&G)[VE], float (&P)[VE]) {
+                                              const Flags& flags, float (&h)[VE], float (&G)[VE],
+                                              Product<FORM> (&P)[VE]) {
 #pragma clang fp contract(off)  // as forward_tile
     Tile<E, VE> g, x, d;
     g.template load<FULL>(rows.gate + t0 * a.gate_t, a.gate_t, count);
@@ -421,7 +493,7 @@ __device__ __forceinline__ void backward_tile(const Args& a, const Rows<E>& rows
                     og[j] = FORM == GEAR_GATE_VALUE ? t * Q[s][j] : ox[j] * Q[s][j] * f;
                 }
                 G[j] = z ? 0.0f : f * t;
-                if (MAPS) P[j] *= f;
+                if (MAPS) P[j].multiply(f);
             }
             if (!MAPS) {
                 Vec<E, VE>::template store<STREAM>(dgate, og);
@@ -440,7 +512,7 @@ __device__ __forceinline__ void backward_tile(const Args& a, const Rows<E>& rows
 // The steps of lane q back from tile k1 to tile k0.
 template <typename E, int VE, int FORM, bool RESET, bool MAPS>
 __device__ __forceinline__ bool backward_tiles(const Args& a, const Place& p, int64_t at, bool used, int64_t k0, int64_t k1,
-                                               float (&G)[VE], float (&P)[VE]) {
+                                               float (&G)[VE], Product<FORM> (&P)[VE]) {
     const Rows<E> rows = rows_of<E>(a, p);
     const int64_t BD = a.B * a.D;
     bool cut = false;
@@ -463,6 +535,10 @@ __device__ __forceinline__ bool backward_tiles(const Args& a, const Place& p, in
             backward_tile<E, VE, FORM, RESET, MAPS, true, true>(a, rows, t0, count, room, flags, h, G, P);
         else backward_tile<E, VE, FORM, RESET, MAPS, true, false>(a, rows, t0, count, room, flags, h, G, P);
         if (RESET) cut |= flags.any();
+        if (MAPS) {
+#pragma unroll
+            for (int j = 0; j < VE; j++) P[j].end_tile();
+        }
     }
     return cut;
 }
@@ -474,7 +550,8 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(const Args a) {
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < a.lanes; i += (int64_t)gridDim.x * kThreads) {
         const Place p = place_of<VE>(a, i);
         const int64_t at = p.b * a.D + p.c;
-        float G[VE], P[VE];
+        float G[VE];
+        Product<FORM> P[VE];
 #pragma unroll
         for (int j = 0; j < VE; j++) G[j] = a.dfinal ? a.dfinal[at + j] : 0.0f;
         backward_tiles<E, VE, FORM, RESET, false>(a, p, at, true, 0, (a.T + kSteps - 1) / kSteps, G, P);
@@ -486,27 +563,26 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(const Args a) {
 // At 4 x 16384 x 512 fp32 the maps take 45 us and the gradients 121 (679 MB, 5.6 TB/s).
 template <typename E, int VE, int FORM, bool RESET, bool MAPS>
 __global__ __launch_bounds__(64 * kRun) void backward_split_kernel(const Args a) {
-    __shared__ Map s[MAPS ? kRun : 1][VE][64];
+    __shared__ Map<FORM> s[MAPS ? kRun : 1][VE][64];
     const Part w = part_of(a);
     const Place p = place_of<VE>(a, w.q);
     const int64_t at = p.b * a.D + p.c, tiles = (a.T + kSteps - 1) / kSteps;
     const int64_t k1 = tiles - w.seg * a.seg_tiles > 0 ? tiles - w.seg * a.seg_tiles : 0;
-    const int64_t k0 = k1 - a.seg_tiles > 0 ? k1 - a.seg_tiles : 0;
-    float G[VE], P[VE];
-#pragma unroll
-    for (int j = 0; j < VE; j++) {
-        P[j] = 1.0f;
-        G[j] = 0.0f;
-    }
-    if (!MAPS) first_of<VE>(a, w, at, G);
-    const bool cut = backward_tiles<E, VE, FORM, RESET, MAPS>(a, p, at, w.used, k0, k1, G, P);
+    int64_t k0 = k1 - a.seg_tiles > 0 ? k1 - a.seg_tiles : 0;
+    float G[VE] = {};
+    Product<FORM> P[VE];
     if (MAPS) {
-        Map m[VE];
+        const bool cut = backward_tiles<E, VE, FORM, RESET, MAPS>(a, p, at, w.used, k0, k1, G, P);
+        Map<FORM> m[VE];
 #pragma unroll
-        for (int j = 0; j < VE; j++) m[j] = Map{cut ? __uint_as_float(kCutBits) : P[j], G[j]};
-        leave_maps<VE>(a, w, at, m, s);
-    } else if (w.used && a.dstate && k0 < k1 && k0 == 0) {
-        Vec<float, VE>::store(a.dstate + at, G);
+        for (int j = 0; j < VE; j++) m[j] = P[j].map(G[j], cut);
+        leave_maps<FORM, VE>(a, w, at, m, s);
+    } else {
+        const int32_t doubt = *a.doubt;
+        first_of<FORM, VE>(a, w, at, G);
+        if (doubt) k0 = w.seg == 0 ? 0 : k1;  // as forward
+        backward_tiles<E, VE, FORM, RESET, MAPS>(a, p, at, w.used, k0, k1, G, P);
+        if (w.used && a.dstate && k0 < k1 && k0 == 0) Vec<float, VE>::store(a.dstate + at, G);
     }
 }
 
@@ -563,9 +639,11 @@ Plan plan_of(const gear_recurrence_desc& d, bool backward, bool in_place) {
     p.runs = (int32_t)((S + kRun - 1) / kRun);
     return p;
 }
+int64_t map_bytes(const gear_recurrence_desc& d) { return d.form == GEAR_GATE_VALUE ? sizeof(GrowthMap) : sizeof(DecayMap); }
 int64_t work_bytes_of(const gear_recurrence_desc& d) {
     const int32_t f = plan_of(d, false, false).runs, b = plan_of(d, true, false).runs;
-    return (int64_t)(f > b ? f : b) * (kRun + 1) * d.B * d.D * (int64_t)sizeof(Map);
+    const int64_t runs = f > b ? f : b;
+    return runs ? runs * (kRun + 1) * d.B * d.D * map_bytes(d) + (int64_t)sizeof(int32_t) : 0;
 }
 int64_t saved_bytes_of(const gear_recurrence_desc& d) {
     const int64_t tiles = (d.T + kSteps - 1) / kSteps;
@@ -617,8 +695,9 @@ int run(const Args& base, const Plan& p, int32_t form, bool backward, const char
     hipLaunchKernelGGL(k.maps, grid, block, 0, s, base);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, what);
-    hipLaunchKernelGGL(carry_kernel, dim3((unsigned)((BD + 63) / 64)), dim3(64 * kCarryWaves), 0, s, base.run_maps,
-                       backward ? base.dfinal : base.state, BD, p.runs);
+    hipLaunchKernelGGL(form == GEAR_GATE_VALUE ? carry_kernel<GEAR_GATE_VALUE> : carry_kernel<GEAR_GATE_SIGMOID>,
+                       dim3((unsigned)((BD + 63) / 64)), dim3(64 * kCarryWaves), 0, s, base,
+                       backward ? base.dfinal : base.state);
     e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, what);
     hipLaunchKernelGGL(k.split, grid, block, 0, s, base);
@@ -639,8 +718,8 @@ Args args_of(const gear_recurrence_desc& d, const Plan& p, void* work) {
     Args a{};
     a.reset = d.d_reset;
     a.lengths = d.d_lengths;
-    a.run_maps = static_cast<Map*>(work);
-    a.maps = a.run_maps + (int64_t)p.runs * d.B * d.D;
+    a.maps = work;
+    a.doubt = reinterpret_cast<int32_t*>(static_cast<char*>(work) + (int64_t)p.runs * (kRun + 1) * d.B * d.D * map_bytes(d));
     a.B = d.B;
     a.T = d.T;
     a.D = d.D;

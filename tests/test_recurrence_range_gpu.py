@@ -1,0 +1,144 @@
+"""The recurrence over windows that are split into segments, where the product of
+a segment's decays or the values carried between segments pass what 32 bits
+hold: the definition's steps give finite values there, or keep an infinity (GPU)."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2310_05205_amd import gear
+from tests import learner_reference as ref
+from tests.helpers import cuda, say
+from tests.test_recurrence_gpu import DTYPES, check, make, wide
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("B,T,D", [(1, 2048, 64), (1, 96, 64), (2, 300, 7), (3, 20000, 5)])
+@pytest.mark.parametrize("gate", [2.0, -2.0, 1.25])
+def test_nothing_carried_stays_nothing(B, T, D, dtype, gate):
+    """Zero inputs, no state: zeros, however large the decays' product."""
+    dt = DTYPES[dtype]
+    g, x = torch.full((B, T, D), gate, dtype=dt, device=cuda()), torch.zeros(B, T, D, dtype=dt, device=cuda())
+    say("recurrence of zeros B=%d T=%d D=%d gate=%s %s" % (B, T, D, gate, dtype))
+    y, final, saved = gear.recurrence(g, x, save=True)
+    assert not bool(y.any()) and not bool(final.any()) and not bool(saved.any())
+    dgate, dx, dstate = gear.recurrence_backward(g, x, saved, torch.zeros_like(x))
+    assert not bool(dgate.any()) and not bool(dx.any()) and not bool(dstate.any())
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("B,T,D,reset,ragged", [(1, 1024, 33, False, False), (2, 3000, 6, False, False),
+                                                (3, 2500, 66, True, False), (4, 1500, 9, True, True)])
+def test_growth_before_the_first_input(B, T, D, reset, ragged, dtype):
+    """Gates of 1.25, inputs in the last 24 steps and gradients in the first 24 alone; every other channel decays as usual."""
+    gate, x, dy, _, _, r, n = make(B, T, D, dtype, T + D, False, reset=0.002 if reset else 0, ragged=ragged)
+    gate[:, :, ::2] = 1.25
+    x[:, :-24, ::2] = 0
+    dy[:, 24:, ::2] = 0
+    say("recurrence with growing gates B=%d T=%d D=%d %s" % (B, T, D, dtype))
+    check(gate, x, dy, None, None, r, n, dtype, False)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("T", [96, 1000, 5000])
+def test_a_zero_gate_ends_growth(T, dtype):
+    """Nothing before a gate of 0, growth or not, counts after it, whichever of a lane's channels it is in."""
+    gate, x, dy, state, dfinal, _, _ = make(2, T, 7, dtype, T, False)
+    k = T // 2
+    for c, at in ((0, k), (3, k - 1), (6, k + 1)):
+        gate[:, :at, c], gate[:, at, c], x[:, :at, c], dy[:, 24:, c] = 1.5, 0.0, 0.0, 0.0
+        state[:, c] = dfinal[:, c] = 0.0
+    say("recurrence with a gate of 0 after growth T=%d %s" % (T, dtype))
+    check(gate, x, dy, state, dfinal, None, None, dtype, False)
+
+
+@pytest.mark.parametrize("T", [400, 3000])
+def test_growth_and_decay_in_turn(T):
+    """Decays of 2^20 and 2^-20 in turn, runs of either 7 to 40 steps: products of runs pass 2^127 both ways.  The
+    state is a power of two that stays in range, so every step is exact."""
+    rng = np.random.default_rng(T)
+    e, at = [], 0
+    while len(e) < T:  # exponents of a walk between 2^-100 and 2^100
+        to = int(rng.integers(-5, 6)) * 20
+        e += [20 * int(np.sign(to - at))] * (abs(to - at) // 20) + [0] * int(rng.integers(1, 30))
+        at = to
+    gate = torch.tensor(np.exp2(np.array(e[:T], np.float64)), dtype=torch.float32, device=cuda()).view(1, T, 1).repeat(1, 1, 3)
+    x = torch.zeros(1, T, 3, device=cuda())
+    state = torch.tensor([[1.0, -2.0, 0.0]], device=cuda())
+    want = np.exp2(np.cumsum(e[:T]))[:, None] * np.array([1.0, -2.0, 0.0])
+    say("recurrence that grows and decays in turn T=%d" % T)
+    y, final, _ = gear.recurrence(gate, x, state)
+    np.testing.assert_array_equal(wide(y)[0], want)
+    np.testing.assert_array_equal(wide(final)[0], want[-1])
+
+
+@pytest.mark.parametrize("T", [90, 96, 2000])
+def test_a_balance_of_growth_and_input(T):
+    """h = 2 h + 1 rests at -1, which no sum of a part from the state and a part from the inputs shows."""
+    gate, x = torch.full((1, T, 4), 2.0, device=cuda()), torch.ones(1, T, 4, device=cuda())
+    state = torch.tensor([[-1.0, 0.0, -1.0, -2.0]], device=cuda())
+    say("recurrence at rest T=%d" % T)
+    y, final, _ = gear.recurrence(gate, x, state)
+    assert bool((y[:, :, ::2] == -1).all()) and bool((final[:, ::2] == -1).all())
+    t = np.arange(1, T + 1)
+    with np.errstate(over="ignore"):
+        up = (np.exp2(np.minimum(t, 1000)) - 1).astype(np.float32)  # from 0: 2^t - 1, at last beyond fp32
+    got = wide(y)[0]
+    np.testing.assert_allclose(got[:, 1], up, rtol=1e-6)
+    np.testing.assert_allclose(got[:, 3], -up - 2, rtol=1e-6)
+
+
+@pytest.mark.parametrize("T", [300, 4000])
+@pytest.mark.parametrize("D", [4, 5])
+def test_an_infinite_state_stays(T, D):
+    """An infinity carried through decays that multiply to nothing stays one; so does a state near the type's end."""
+    gate, x, dy, state, dfinal, _, _ = make(2, T, D, "float32", 3, False)
+    gate.abs_()
+    gate.clamp_(0.3, 0.9)
+    state[0, 1], state[1, 3], dfinal[0, 2], dfinal[1, 1] = float("inf"), float("-inf"), float("inf"), float("-inf")
+    say("recurrence with an infinite state T=%d D=%d" % (T, D))
+    y, final, saved = gear.recurrence(gate, x, state, save=True)
+    dgate, dx, dstate = gear.recurrence_backward(gate, x, saved, dy, dfinal, state)
+    for t, v in ((y[0, :, 1], 1), (y[1, :, 3], -1), (final[0, 1], 1), (final[1, 3], -1), (dx[0, :, 2], 1),
+                 (dx[1, :, 1], -1), (dstate[0, 2], 1), (dstate[1, 1], -1)):
+        assert bool((t == v * float("inf")).all())
+    others = torch.ones(2, D, dtype=torch.bool, device=cuda())
+    others[0, 1] = others[1, 3] = False
+    assert bool(torch.isfinite(y.transpose(1, 2)[others]).all()) and bool(torch.isfinite(final[others]).all())
+    big = torch.full((1, 900, 3), 0.5, device=cuda())
+    y, _, _ = gear.recurrence(big, torch.zeros_like(big), torch.full((1, 3), 2.0 ** 127, device=cuda()))
+    np.testing.assert_array_equal(wide(y)[0, :276, 0], np.exp2(127.0 - np.arange(1, 277)))
+
+
+def test_channels_that_lanes_share():
+    """A width that a lane's channels do not divide, growth in a channel that two lanes compute or beside one: both
+    write the same, every time."""
+    for dtype, D in (("float32", 5), ("bfloat16", 9), ("bfloat16", 11), ("float32", 67)):
+        for grow in range(max(0, D - 5), D):
+            gate, x, dy, _, _, _, _ = make(3, 1300, D, dtype, D + grow, False)
+            gate[1, :, grow] = 1.25
+            x[1, :-24, grow] = 0
+            dy[1, 24:, grow] = 0
+            say("recurrence with growth in channel %d of %d %s" % (grow, D, dtype))
+            check(gate, x, dy, None, None, None, None, dtype, False)
+
+
+def test_not_a_number_stays_in_its_channel():
+    """A NaN anywhere reaches every later step of its channel, and no other channel."""
+    for bad in ("gate", "x", "state"):
+        gate, x, dy, state, dfinal, _, _ = make(2, 2000, 6, "float32", 9, True)
+        t = {"gate": gate, "x": x}.get(bad)
+        k = 0 if t is None else 777
+        if t is None:
+            state[1, 2] = float("nan")
+        else:
+            t[1, k, 2] = float("nan")
+        say("recurrence with NaN in %s" % bad)
+        y, final, saved = gear.recurrence(gate, x, state, form=gear.GEAR_GATE_SIGMOID, save=True)
+        hit = torch.zeros(2, 2000, 6, dtype=torch.bool, device=cuda())
+        hit[1, k:, 2] = True
+        assert torch.equal(torch.isnan(y), hit) and torch.equal(torch.isnan(final), hit[:, -1])
+        clean = [wide(torch.nan_to_num(v)) for v in (gate, x, state)]
+        (wy, ey), _, _, _ = ref.recurrence(*clean, True)
+        ref.within(np.where(wide(hit), 0, wide(y)), np.where(wide(hit), 0, wy), ey)
