@@ -729,7 +729,8 @@ int gear_policy_sizes(const gear_policy_desc *d, int64_t *work_bytes);
  * Logits of -inf, or of the type's lowest value, have probability 0 beside
  * larger ones.  A row whose logits are all -inf has no distribution: it
  * counts among the rows, with lp = -inf, and adds nothing to loss, stats or
- * gradient.  Sums over rows have an order that depends on n and V alone, so
+ * gradient.  A NaN among the logits of a row that takes part makes its lp, H and
+ * gradient, and the loss, NaN.  Sums over rows have an order that depends on n and V alone, so
  * results repeat bit for bit.
  * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
  */

@@ -209,15 +209,15 @@ struct Row {
     float sums[kSums];
 };
 
-// A row's terms from its largest logit, the sums of 2^d and of d 2^d, and the
-// action's d.  The operations are spelled out, so that lp and H come out the
+// A row's terms from the sums of 2^d and of d 2^d, and the action's d.  The operations are spelled out, so that lp and H come out the
 // same in every kernel.
 template <bool LOSS>
-__device__ __forceinline__ Row row_terms(const Args& a, const Inputs& in, float m, float S, float dS, float da,
-                                         float scale) {
+__device__ __forceinline__ Row row_terms(const Args& a, const Inputs& in, float S, float dS, float da, float scale) {
 #pragma clang fp contract(off)
     Row r{};
-    if (m == -INFINITY) {  // no distribution
+    // All -inf, no distribution.  The sum says so: it is 1 or more with any other logit and NaN with a NaN, which
+    // the maximum passes over.
+    if (S == 0.0f) {
         r.lp = -INFINITY;
         return r;
     }
@@ -459,7 +459,7 @@ __global__ __launch_bounds__(THREADS, WAVES) void held_kernel(const Args a) {
         S = group_add<G>(S);
         dS = group_add<G>(dS);
         Row r{};
-        if (on) r = row_terms<LOSS>(a, in, m, S, dS, dist(za), scale);
+        if (on) r = row_terms<LOSS>(a, in, S, dS, dist(za), scale);
         if (used && lane == 0) {
             if (a.logp) a.logp[row] = r.lp;
             if (a.entropy) a.entropy[row] = r.H;
@@ -469,7 +469,7 @@ __global__ __launch_bounds__(THREADS, WAVES) void held_kernel(const Args a) {
         if (LOSS && a.grad && used) {
             // Rows without part or distribution hold only -inf, and get zeros.
             E* g = static_cast<E*>(a.grad) + row * a.V;
-            const bool some = on && m != -INFINITY;
+            const bool some = on && S != 0.0f;
             const Slope slope = some ? slope_of(a, r, S) : Slope{};
             asm volatile("" : "+v"(mine));
 #pragma unroll
@@ -577,7 +577,7 @@ __global__ __launch_bounds__(THREADS, LOSS ? 4 : 8) void block_kernel(const Args
             in = s_in[turn];
             turn ^= 1;
             const Scale dist = scale_of(m);
-            const Row r = row_terms<LOSS>(a, in, m, S, dS, dist(za), scale);
+            const Row r = row_terms<LOSS>(a, in, S, dS, dist(za), scale);
             if (threadIdx.x == 0) {
                 if (a.logp) a.logp[row] = r.lp;
                 if (a.entropy) a.entropy[row] = r.H;
@@ -586,7 +586,7 @@ __global__ __launch_bounds__(THREADS, LOSS ? 4 : 8) void block_kernel(const Args
                     if (LOSS) s_total[k] += r.sums[k];
             }
             if (LOSS) {
-                const bool some = m != -INFINITY;
+                const bool some = S != 0.0f;
                 const Slope slope = some ? slope_of(a, r, S) : Slope{};
                 asm volatile("" : "+v"(mine));
                 if (a.grad && tame && m < kTame) {
@@ -681,7 +681,7 @@ __global__ __launch_bounds__(kSoloThreads) void long_kernel(const Args a) {
             S += s_sum[k];
             dS += s_dsum[k];
         }
-        const Row r = row_terms<LOSS>(a, in, m, S, dS, dist(za), scale);
+        const Row r = row_terms<LOSS>(a, in, S, dS, dist(za), scale);
         if (threadIdx.x == 0) {
             if (a.logp) a.logp[row] = r.lp;
             if (a.entropy) a.entropy[row] = r.H;
@@ -689,7 +689,7 @@ __global__ __launch_bounds__(kSoloThreads) void long_kernel(const Args a) {
             for (int k = 0; k < kSums; k++) total[k] += r.sums[k];
         }
         if (g) {
-            const Slope slope = m != -INFINITY ? slope_of(a, r, S) : Slope{};
+            const Slope slope = S != 0.0f ? slope_of(a, r, S) : Slope{};
             for (int64_t j = threadIdx.x; j < a.V; j += kSoloThreads) {
                 const float o = slope(dist((float)z[j]));
                 g[j] = (E)(j == action ? o + slope.k2 : o);
