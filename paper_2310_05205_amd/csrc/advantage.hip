@@ -35,9 +35,11 @@ struct Map {
     float P, Z;
 };
 __device__ __forceinline__ float apply(Map m, float c) { return m.P < 0.0f ? m.Z : fmaf(m.P, c, m.Z); }
-// `late` first, then `early`.
-__device__ __forceinline__ Map compose(Map early, Map late) {
-    return Map{early.P < 0.0f || late.P < 0.0f ? -1.0f : early.P * late.P, apply(early, late.Z)};
+// `late` first, then `early`.  A product of discounts does not fall below `least`,
+// the smallest number above 0 unless the discount itself is 0: a product of 0
+// would make a NaN of an infinity that the steps carry on.
+__device__ __forceinline__ Map compose(Map early, Map late, float least) {
+    return Map{early.P < 0.0f || late.P < 0.0f ? -1.0f : fmaxf(early.P * late.P, least), apply(early, late.Z)};
 }
 
 struct Args {
@@ -104,11 +106,11 @@ __device__ __forceinline__ int clamp_steps(int64_t n) { return n < 0 ? 0 : n < P
 
 // Inclusive scan of the G lanes' maps, each with the later ones after it.
 template <int G>
-__device__ __forceinline__ Map suffix(Map m, int lane) {
+__device__ __forceinline__ Map suffix(Map m, int lane, float least) {
 #pragma unroll
     for (int off = 1; off < G; off <<= 1) {
         const Map o = {__shfl_down(m.P, off, G), __shfl_down(m.Z, off, G)};
-        if (lane + off < G) m = compose(m, o);
+        if (lane + off < G) m = compose(m, o, least);
     }
     return m;
 }
@@ -120,6 +122,7 @@ __device__ __forceinline__ Map suffix(Map m, int lane) {
 template <typename ER, typename EV, int G, int PER, bool MAPS>
 __global__ __launch_bounds__(kThreads) void advantage_kernel(const Args a) {
     const int lane = threadIdx.x % G;
+    const float least = a.decay > 0.0f ? 0x1p-149f : 0.0f;
     const int64_t tile = (int64_t)G * PER, tiles = (a.L + tile - 1) / tile;
     const int64_t per_block = kThreads / G, units = a.B * a.S;
     // Every lane of a wave runs the same rounds, because the scan shuffles.
@@ -139,8 +142,8 @@ __global__ __launch_bounds__(kThreads) void advantage_kernel(const Args a) {
             Map m = {1.0f, 0.0f};
 #pragma unroll 4
             for (int64_t k = share - 1; k >= 0; k--)
-                if (lane * share + k < later) m = compose(maps[lane * share + k], m);
-            m = suffix<G>(m, lane);
+                if (lane * share + k < later) m = compose(maps[lane * share + k], m, least);
+            m = suffix<G>(m, lane, least);
             carry = apply(Map{__shfl(m.P, 0, G), __shfl(m.Z, 0, G)}, 0.0f);
         }
         const int64_t k1 = (seg + 1) * a.seg_tiles < tiles ? (seg + 1) * a.seg_tiles : tiles;
@@ -181,7 +184,7 @@ __global__ __launch_bounds__(kThreads) void advantage_kernel(const Args a) {
                     any |= cut[j];
                 }
             }
-            const Map mine = suffix<G>(Map{any ? -1.0f : power, z}, lane);
+            const Map mine = suffix<G>(Map{any ? -1.0f : fmaxf(power, least), z}, lane, least);
             if (!MAPS) {
                 const Map later = {__shfl_down(mine.P, 1, G), __shfl_down(mine.Z, 1, G)};
                 float c = lane + 1 < G ? apply(later, carry) : carry, A[PER], R[PER];
@@ -196,7 +199,7 @@ __global__ __launch_bounds__(kThreads) void advantage_kernel(const Args a) {
                 if (a.ret) store_steps<PER>(a.ret + b * a.L + t, R, room);
             }
             const Map head = {__shfl(mine.P, 0, G), __shfl(mine.Z, 0, G)};
-            if (MAPS) whole = compose(head, whole);
+            if (MAPS) whole = compose(head, whole, least);
             else carry = apply(head, carry);
         }
         if (MAPS && used && lane == 0) a.maps[b * a.S + seg] = whole;
