@@ -209,8 +209,8 @@ struct Row {
     float sums[kSums];
 };
 
-// A row's terms from the sums of 2^d and of d 2^d, and the action's d.  The operations are spelled out, so that lp and H come out the
-// same in every kernel.
+// A row's terms from the sums of 2^d and of d 2^d, and the action's d.  The
+// operations are spelled out, so that lp and H come out the same in every kernel.
 template <bool LOSS>
 __device__ __forceinline__ Row row_terms(const Args& a, const Inputs& in, float S, float dS, float da, float scale) {
 #pragma clang fp contract(off)
@@ -225,8 +225,11 @@ __device__ __forceinline__ Row row_terms(const Args& a, const Inputs& in, float 
     r.lp = (da - log_S) * kLn2;
     r.H = (log_S - dS * __builtin_amdgcn_rcpf(S)) * kLn2;
     if (!LOSS) return r;
-    const float ratio = fast_exp(r.lp - in.old);
-    const float free = ratio * in.A, held = fminf(fmaxf(ratio, a.lo), a.hi) * in.A;
+    // The ratio and the KL term are exponentials that may pass fp32.  Where an advantage or a weight of 0 multiplies
+    // them, 0 is left, not NaN.
+    const float lr = r.lp - in.old, ratio = fast_exp(lr);
+    const float free = in.A == 0.0f && fabsf(lr) < INFINITY ? 0.0f : ratio * in.A;
+    const float held = fminf(fmaxf(ratio, a.lo), a.hi) * in.A;
     const bool clipped = held < free;
     const float pg = clipped ? -held : -free;
     r.c = clipped ? 0.0f : -free;
@@ -240,6 +243,10 @@ __device__ __forceinline__ Row row_terms(const Args& a, const Inputs& in, float 
         }
     }
     if (a.ent != 0.0f) row_loss -= a.ent * r.H;
+    if (in.w == 0.0f) {
+        if (fabsf(row_loss) == INFINITY) row_loss = 0.0f;
+        if (fabsf(r.c) == INFINITY) r.c = 0.0f;
+    }
     r.s = in.w * scale;
     r.sums[0] = in.w * row_loss;
     r.sums[1] = pg;
