@@ -508,6 +508,12 @@ at::Tensor workspace(int64_t bytes, c10::Device dev) {
     return bytes > 0 ? make({bytes}, at::kByte, dev) : at::Tensor();
 }
 
+// Tells autograd that a call writes over a tensor of the caller's: a gradient that
+// needs what it held is then refused.  Inference tensors have no versions, and no gradient needs them.
+void overwrites(const at::Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 c10::Device gpu_of(const at::Tensor& t, const char* name) {
     TORCH_CHECK_VALUE(t.is_cuda(), name, " must be on the GPU, not on ", t.device());
     return t.device();
@@ -604,6 +610,7 @@ PyObject* py_recurrence_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
             TORCH_CHECK_VALUE(p + bytes <= q || q + bytes <= p, "out must be state itself or not overlap it");
         }
         at::Tensor y = make({r.d.B, r.d.D}, r.x.scalar_type(), r.dev);
+        if (a[5] != Py_None) overwrites(out);
         const int rc = without_gil([&] {
             return f_recurrence(&r.d, r.gate.data_ptr(), r.x.data_ptr(), data<float>(r.state), y.data_ptr(),
                                 data<float>(out), nullptr, nullptr, 0, s);
@@ -819,6 +826,7 @@ PyObject* py_policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
         at::Tensor logp = make(p.rows, at::kFloat, p.dev), entropy = make(p.rows, at::kFloat, p.dev), grad;
         if (want_grad) grad = in_place ? p.logits : make(p.logits.sizes(), p.logits.scalar_type(), p.dev);
         const at::Tensor work = workspace(work_bytes, p.dev);
+        if (want_grad && in_place) overwrites(p.logits);
         rc = without_gil([&] {
             return f_policy_loss(&p.d, p.logits.data_ptr(), data<float>(old_logp), data<float>(ref_logp), data<float>(adv),
                                  data<float>(weight), data<float>(grad_loss), data<float>(loss), data<float>(stats),
