@@ -573,7 +573,8 @@ int gear_table_priorities(const gear_table *t, uint32_t **d_priority);
  * loss.  They need no table, run on the current HIP device, keep nothing
  * between calls and allocate nothing: what they need beside their inputs and
  * outputs is the caller's workspace.  Captures of them replay correctly.
- * Every pointer but a descriptor is device memory; inputs are not written.
+ * Every pointer but a descriptor is device memory; inputs are not written, and
+ * outputs meet neither inputs nor each other but where a call allows it.
  * No content of an input (flags, lengths, actions) makes a kernel read or
  * write outside buffers of the stated sizes.
  */

@@ -514,6 +514,27 @@ void overwrites(const at::Tensor& t) {
     if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
 
+// Refuses an input that lies in the memory of `out`, which is contiguous and
+// which the call writes: other lanes may read the input afterwards.  The input is
+// contiguous, or has one or two dimensions and contiguous rows.
+void need_apart(const at::Tensor& out, const char* out_name, const at::Tensor& t, const char* name) {
+    if (!t.defined() || t.numel() == 0 || out.numel() == 0) return;
+    const char *o = data<char>(out), *o_end = o + out.nbytes(), *p = data<char>(t);
+    const int64_t item = t.element_size();
+    int64_t rows = 1, stride = 0, run = t.numel() * item;
+    if (!t.is_contiguous()) {
+        rows = t.size(0);
+        stride = t.stride(0) * item;
+        run = t.dim() == 2 ? t.size(1) * item : item;
+    }
+    bool meet = o < p + (rows - 1) * stride + run && p < o_end;
+    if (meet && rows > 1) {
+        meet = false;
+        for (int64_t r = 0; r < rows; r++) meet |= o < p + r * stride + run && p + r * stride < o_end;
+    }
+    TORCH_CHECK_VALUE(!meet, name, " must not overlap ", out_name, ", which is written");
+}
+
 c10::Device gpu_of(const at::Tensor& t, const char* name) {
     TORCH_CHECK_VALUE(t.is_cuda(), name, " must be on the GPU, not on ", t.device());
     return t.device();
@@ -608,6 +629,11 @@ PyObject* py_recurrence_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
             const char *p = data<char>(out), *q = data<char>(r.state);
             const int64_t bytes = r.d.B * r.d.D * 4;
             TORCH_CHECK_VALUE(p + bytes <= q || q + bytes <= p, "out must be state itself or not overlap it");
+        }
+        if (a[5] != Py_None) {
+            need_apart(out, "out", r.gate, "gate");
+            need_apart(out, "out", r.x, "x");
+            need_apart(out, "out", r.reset, "reset");
         }
         at::Tensor y = make({r.d.B, r.d.D}, r.x.scalar_type(), r.dev);
         if (a[5] != Py_None) overwrites(out);

@@ -410,7 +410,8 @@ def recurrence_backward(gate, x, saved, dy, dfinal=None, state=None, *, form=GEA
 def recurrence_step(gate, x, state, *, form=GEAR_GATE_VALUE, reset=None, out=None, stream=None):
     """One step of the recurrence, as an actor takes it: gate, x [B, D], state
     float32 [B, D] (None: zeros), reset [B].  Returns (y, state after the
-    step); `out` may be a float32 tensor for the latter, `state` itself included."""
+    step); `out` may be a float32 tensor for the latter, `state` itself included,
+    in memory that holds none of the other inputs."""
     return _on_stream(native().recurrence_step, x, stream, gate, x, state, form, reset, out)
 
 
