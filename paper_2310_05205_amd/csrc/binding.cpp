@@ -852,7 +852,16 @@ PyObject* py_policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
         at::Tensor logp = make(p.rows, at::kFloat, p.dev), entropy = make(p.rows, at::kFloat, p.dev), grad;
         if (want_grad) grad = in_place ? p.logits : make(p.logits.sizes(), p.logits.scalar_type(), p.dev);
         const at::Tensor work = workspace(work_bytes, p.dev);
-        if (want_grad && in_place) overwrites(p.logits);
+        if (want_grad && in_place) {
+            need_apart(p.logits, "logits", p.action, "action");
+            need_apart(p.logits, "logits", p.mask, "mask");
+            need_apart(p.logits, "logits", old_logp, "old_logp");
+            need_apart(p.logits, "logits", ref_logp, "ref_logp");
+            need_apart(p.logits, "logits", adv, "adv");
+            need_apart(p.logits, "logits", weight, "weight");
+            need_apart(p.logits, "logits", grad_loss, "grad_loss");
+            overwrites(p.logits);
+        }
         rc = without_gil([&] {
             return f_policy_loss(&p.d, p.logits.data_ptr(), data<float>(old_logp), data<float>(ref_logp), data<float>(adv),
                                  data<float>(weight), data<float>(grad_loss), data<float>(loss), data<float>(stats),

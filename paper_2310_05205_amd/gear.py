@@ -433,7 +433,8 @@ def policy_loss(logits, action, old_logp, adv, *, ref_logp=None, weight=None, ma
     scalars and rows, stats the means of the clipped, KL and entropy terms and
     of the rows clipped, grad the gradient of grad_scale * grad_loss * loss for
     the logits, of their dtype, or None without `grad`.  With `in_place` it
-    takes the logits' memory, and autograd takes them as changed in place.
+    takes the logits' memory, which must hold none of the other inputs, and
+    autograd takes them as changed in place.
     """
     return _on_stream(native().policy_loss, logits, stream, logits, action, old_logp, adv, ref_logp, weight, mask,
                       clip[0], clip[1], kl, entropy, denom, grad, grad_scale, grad_loss, in_place)

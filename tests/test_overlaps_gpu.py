@@ -40,3 +40,24 @@ def test_a_step_between_the_rows_of_its_inputs():
     assert torch.equal(gear.recurrence_step(gate, x, state, out=out)[1], want)
     with pytest.raises(ValueError, match="overlap"):
         gear.recurrence_step(gate, x, state, out=buf.view(-1)[37:49].view(2, 6))  # one element into the third row
+
+
+@pytest.mark.parametrize("which", ["action", "old_logp", "ref_logp", "adv", "weight", "mask", "grad_loss"])
+def test_a_gradient_over_the_rows_inputs(which):
+    """The gradient takes the logits' memory; what the rows' terms come from must not lie in it."""
+    n, V = 8, 6
+    z = torch.randn(n, V, device=cuda())
+    row = z.view(-1)[10:10 + n]
+    kw = {"action": torch.zeros(n, dtype=torch.int32, device=cuda()), "old_logp": torch.full((n,), -2.0, device=cuda()),
+          "adv": torch.ones(n, device=cuda())}
+    kw[which] = {"action": row.view(torch.int32), "mask": row.view(torch.uint8)[:n], "grad_loss": row[:1]}.get(which, row)
+    kept = z.clone()
+    args = [kw.pop(k) for k in ("action", "old_logp", "adv")]
+    say("policy gradient over its %s" % which)
+    with pytest.raises(ValueError, match="%s must not overlap" % which):
+        gear.policy_loss(z, *args, in_place=True, **kw)
+    torch.cuda.synchronize()
+    assert torch.equal(z, kept)
+    gear.policy_loss(z, *args, **kw)  # reads them, and writes elsewhere
+    gear.policy_loss(z, *args, grad=False, in_place=True, **kw)
+    assert torch.equal(z, kept)
