@@ -142,3 +142,33 @@ def test_not_a_number_stays_in_its_channel():
         clean = [wide(torch.nan_to_num(v)) for v in (gate, x, state)]
         (wy, ey), _, _, _ = ref.recurrence(*clean, True)
         ref.within(np.where(wide(hit), 0, wide(y)), np.where(wide(hit), 0, wy), ey)
+
+
+def test_captured_calls_follow_their_inputs():
+    """Replays decide anew whether values grow: growing, decaying and infinite inputs in turn."""
+    gate, x, dy, state, dfinal, r, _ = make(2, 1500, 9, "float32", 8, False, reset=0.002)
+    usual = gate.clone()
+
+    def both():
+        y, f, s = gear.recurrence(gate, x, state, reset=r, save=True)
+        return (y, f) + gear.recurrence_backward(gate, x, s, dy, dfinal, state, reset=r)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        both()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both()
+    for k in range(6):
+        gate.copy_(usual)
+        state.fill_(float(k))
+        if k % 3 == 1:
+            gate[1, :, 4] = 1.125
+        if k % 3 == 2:
+            state[0, 3] = float("inf")
+        say("captured recurrence, replay %d" % k)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(torch.nan_to_num(a, nan=12345.0), torch.nan_to_num(b, nan=12345.0)) for a, b in zip(out, want))
