@@ -20,7 +20,8 @@ struct Vec {
     typedef words loose __attribute__((aligned(sizeof(E))));
 
     // N elements at p, which need no alignment beyond the element's own; with
-    // STREAM past the caches, 5 to 15% faster where tensors exceed them.
+    // STREAM past the caches, 5 to 15% faster where tensors exceed them and a wave
+    // reads whole lines.
     template <bool STREAM = false>
     static __device__ __forceinline__ raw load(const E* p) {
         if (STREAM) return __builtin_bit_cast(raw, __builtin_nontemporal_load(reinterpret_cast<const loose*>(p)));

@@ -400,9 +400,9 @@ __device__ __forceinline__ float scale_by(const Args& a, float denom) {
 
 // Rows held in registers: G lanes share a row, each with up to NV pieces of 16
 // bytes, so that a row is read once and its gradient written once.  With TINY,
-// rows are shorter than a piece.  2097152 rows of 16 bf16 take 44 us, of which the
+// rows are shorter than a piece.  2097152 rows of 16 bf16 take 48 us, of which the
 // vector units' share is about 31 and memory's 28; 320 rows of 18 fp32, in one
-// workgroup without the launches before and after, 8.5 us, mostly dependent loads.
+// workgroup without the launches before and after, 8.4 us, mostly dependent loads.
 template <typename E, int G, int NV, int THREADS, int WAVES, bool TINY, bool LOSS>
 __global__ __launch_bounds__(THREADS, WAVES) void held_kernel(const Args a) {
     constexpr int VE = Piece<E>::VE, kGroups = THREADS / G, kWaves = THREADS / 64;
@@ -493,9 +493,9 @@ __global__ __launch_bounds__(THREADS, WAVES) void held_kernel(const Args a) {
 // arrive, against the largest logit it has seen so far, so one barrier a row
 // is enough.  For the gradient a lane holds all its pieces; without one nothing
 // is held, and few registers let two of the longest rows share a CU.  4096 rows of
-// 32768 bf16 take 108 us (537 MB, 4.9 TB/s; vector units busy for about 85), 1519
-// of 50001 fp16, most of them off a line's start, 80 us; log-probabilities of
-// 2048 rows of 131072 bf16 96 us (5.6 TB/s).
+// 32768 bf16 take 110 us (537 MB, 4.9 TB/s; vector units busy for about 85), 1519
+// of 50001 fp16, most of them off a line's start, 78 us; log-probabilities of
+// 2048 rows of 131072 bf16 97 us (5.5 TB/s).
 template <typename E, int NV, int THREADS, bool LOSS>
 __global__ __launch_bounds__(THREADS, LOSS ? 4 : 8) void block_kernel(const Args a) {
     constexpr int VE = Piece<E>::VE, G = THREADS, kWaves = THREADS / 64, kHeld = LOSS ? NV : 4;
@@ -633,9 +633,11 @@ __global__ __launch_bounds__(THREADS, LOSS ? 4 : 8) void block_kernel(const Args
     }
 }
 
-// Rows longer than registers hold: a workgroup per row, which reads it three
-// times, the second and third from the last-level cache as long as it holds the
-// 256 rows at work together (512 K logits each in 16 bits).
+// Rows longer than registers hold, of more than 131072 logits in 16 bits or 65536
+// in 32: a workgroup per row, which reads it three times (log-probabilities
+// twice), an element a lane and load.  Slow: 1024 rows of 151936 bf16 take 679 us,
+// log-probabilities 442, where rows of 131072 take 132 and 49; of 128256 fp32 637
+// and 397, where 65536 take 123 and 44.
 template <typename E, bool LOSS>
 __global__ __launch_bounds__(kSoloThreads) void long_kernel(const Args a) {
     constexpr int kWaves = kSoloThreads / 64;
@@ -751,6 +753,8 @@ Choice block() {
 // 12 pieces a lane to itself: 16384 rows of 2047, 2304, 4096, 5000 and 7000 bf16
 // take it 45, 61, 70, 94 and (16 pieces) 116 us, and a workgroup 87, 96, 90, 117
 // and 127, but 120 and 117 at 8192; log-probabilities likewise, 50 and 50 there.
+// Rows of 65 to 128 pieces take 64 lanes with at most two each; 32 lanes with four
+// were not tried.
 // How many lanes share a row, and so the order of its sums, depends on V alone.
 template <typename E, bool LOSS>
 Choice choose(int64_t V, bool solo) {

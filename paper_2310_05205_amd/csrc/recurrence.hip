@@ -7,8 +7,8 @@
 //
 // Both directions read and write every element once and do a few operations
 // on it, so memory bounds them.  A lane owns 8 (backward 4) bytes of neighbouring
-// channels of one window and walks its steps in tiles of 16, whose loads are
-// all issued before the first is used.  Windows and channels give the
+// channels of one window and walks its steps in tiles of 16, loading an input's
+// part of a tile as a whole.  Windows and channels give the
 // parallelism; where they are too few to fill the GPU, the steps are split
 // into segments, one to a wave: one launch reduces every segment, and every
 // workgroup's run of segments, to what it does to a value carried through it
@@ -32,10 +32,14 @@ constexpr int kThreads = 256;
 // Calls of fewer lanes and at least so many tiles are split.  Splitting reads the
 // inputs twice and takes three launches; not splitting leaves the GPU waiting for
 // one tile of each lane at a time, 2.5 to 4 us.  Forward of B x T x 512 in
-// bf16, split and not: 128 x 512 (16384 lanes) 79 and 131 us, 256 x 512 (32768) 137
-// and 137, 512 x 512 271 and 161; 1 x 64 (4 tiles) 15 and 13, 1 x 128 18 and 23,
-// 128 x 64 24 and 20, 128 x 128 30 and 37.  Backward: 64 x 512 (16384 lanes) 58 and
-// 99, 128 x 512 101 and 107, 256 x 512 198 and 130; 64 x 64 16 and 14, 64 x 128 21 and 27.
+// bf16, split and not: 128 x 512 (16384 lanes) 82 and 131 us, 256 x 512 (32768) 137
+// and 137, 512 x 512 271 and 161; 1 x 64 (4 tiles) 15 and 13, 1 x 128 20 and 23,
+// 128 x 64 24 and 20, 128 x 128 32 and 37.  Backward: 64 x 512 (16384 lanes) 59 and
+// 99, 128 x 512 106 and 107, 256 x 512 198 and 130; 64 x 64 16 and 14, 64 x 128 23 and 27.
+// The bounds were set for these.  Elsewhere, forward and backward: fp32 64 x 512 x
+// 512 69 / 93 and 77 / 125, but 96 x 512 x 512 102 / 148 and 84 / 136; bf16 64 x 512 x
+// 1003 96 / 133 and 148 / 131, but 128 x 512 x 1003 190 and 168 forward; 4096 x 256 x 8
+// 51 / 70 and 129 / 124.
 constexpr int kWholeLanes = 512 * 64, kSplitTiles = 6;
 constexpr int kWantLanes = 8192 * 64;   // lanes that a split call is cut into, at most:
 constexpr int kMostSegments = 1024;     // more segments of long windows cost more in maps than they gain
@@ -177,11 +181,19 @@ __device__ __forceinline__ void gates(float g, float& f, float& w) {
 
 // Hides where a pointer comes from.  A tile's addresses follow from its first;
 // left to itself the compiler keeps a pointer per step from tile to tile, 96 registers.
+// The pointer also loses its address space: accesses through it are flat ones, all
+// of which are waited for before any is used, in the 16-bit sigmoid forward the
+// gates before those of x go out.
 template <typename P>
 __device__ __forceinline__ void hide(P*& p) {
     asm volatile("" : "+v"(p));
 }
 
+// Loads go past the caches at every width, which suits rows of whole lines.  Where
+// rows are narrower a load touches up to a line per lane, and the next step wants
+// the same lines: forward and backward of 134 M bf16 elements in windows of 32 steps
+// take 137 and 227 us with 512 channels, 178 and 241 with 64, 294 and 482 with 20,
+// 413 and 606 with 8, 844 and 1542 with one.
 template <typename E, int VE>
 struct Tile {
     typename Vec<E, VE>::raw v[kSteps];
@@ -342,8 +354,8 @@ __device__ __forceinline__ bool forward_tiles(const Args& a, const Place& p, int
 }
 
 // Windows that are not split, a lane per piece of channels.  At 8192 x 32 x 512
-// bf16 with resets it takes 142 us for the 840 MB it reads and writes (saved
-// states included), 5.9 TB/s: memory bounds it.
+// bf16 with resets it takes 139 us for the 840 MB it reads and writes (saved
+// states included), 6.0 TB/s: memory bounds it.
 template <typename E, int VE, int FORM, bool RESET>
 __global__ __launch_bounds__(kThreads) void forward_kernel(const Args a) {
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < a.lanes; i += (int64_t)gridDim.x * kThreads) {
@@ -360,8 +372,9 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(const Args a) {
 
 // Segments: with MAPS, reduces each to its map; else goes through it.  What the
 // first launch reads the second reads again, from the last-level cache where it
-// fits: at 4 x 16384 x 512 fp32 the two take 45 and 70 us and the carry between
-// them 5.5; at 1 x 131072 x 512 bf16 49, 69 and 5.5.
+// fits: at 4 x 16384 x 512 fp32 the two take 48 and 81 us and the carry between
+// them 6.4 (a map of gates as given costs 4 us more than one of plain products);
+// at 1 x 131072 x 512 bf16 49, 69 and 6.0.
 template <typename E, int VE, int FORM, bool RESET, bool MAPS>
 __global__ __launch_bounds__(64 * kRun) void forward_split_kernel(const Args a) {
     __shared__ Map<FORM> s[MAPS ? kRun : 1][VE][64];
@@ -544,7 +557,7 @@ __device__ __forceinline__ bool backward_tiles(const Args& a, const Place& p, in
 }
 
 // Windows that are not split.  Three inputs read, two gradients written: 8192 x 32
-// x 512 bf16 with resets in 230 us, 1.36 GB with the saved states, 5.9 TB/s.
+// x 512 bf16 with resets in 227 us, 1.36 GB with the saved states, 6.0 TB/s.
 template <typename E, int VE, int FORM, bool RESET>
 __global__ __launch_bounds__(kThreads) void backward_kernel(const Args a) {
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < a.lanes; i += (int64_t)gridDim.x * kThreads) {
@@ -560,7 +573,7 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(const Args a) {
 }
 
 // Segments are numbered from the end here: the gradient is carried from there.
-// At 4 x 16384 x 512 fp32 the maps take 45 us and the gradients 121 (679 MB, 5.6 TB/s).
+// At 4 x 16384 x 512 fp32 the maps take 48 us and the gradients 120 (679 MB, 5.7 TB/s).
 template <typename E, int VE, int FORM, bool RESET, bool MAPS>
 __global__ __launch_bounds__(64 * kRun) void backward_split_kernel(const Args a) {
     __shared__ Map<FORM> s[MAPS ? kRun : 1][VE][64];
@@ -652,9 +665,11 @@ int64_t saved_bytes_of(const gear_recurrence_desc& d) {
 
 // Outputs that the last-level cache cannot hold are written past it, where a
 // wave writes whole lines of 128 bytes: forward and backward of 8192 x 32 x 512 in
-// bf16 took 422 us without and 369 with.  Rows that share lines want the cache:
-// 37 x 1000 x 1003 in fp16 took 192 us with it and 252 without; so do outputs that
-// it holds for the next reader (1 x 131072 x 512 in bf16: 124 and 129 us).
+// bf16 took 422 us without and 367 with.  Outputs that it holds for the next
+// reader stay in it (1 x 131072 x 512 in bf16: 126 and 130 us).  Rows that share
+// lines go through it, which suits outputs whose memory it already holds: 37 x 1000
+// x 1003 in fp16 took 192 us through it and 252 past it where every pass wrote the
+// same memory, but 239 and 214 where the outputs of the pass before were kept.
 constexpr int64_t kCacheBytes = 192ll << 20;  // of 256 MB, beside what else is in use
 bool streams(const gear_recurrence_desc& d, const void* out, const void* other, int outputs) {
     const int64_t row = d.D * float_bytes(d.dtype);
