@@ -65,7 +65,7 @@ struct GrowthMap {
     int32_t n;
     __device__ __forceinline__ float apply(float c) const {
         const int32_t e = n < -1024 ? -1024 : n > 1024 ? 1024 : n;
-        return __builtin_amdgcn_ldexpf(P == 0.0f ? 0.0f : P * c, e) + Z;
+        return fmaf(P, __builtin_amdgcn_ldexpf(P == 0.0f ? 0.0f : c, e), Z);
     }
     __device__ __forceinline__ GrowthMap after(GrowthMap early) const {
         const float p = P * early.P;

@@ -172,3 +172,11 @@ def test_captured_calls_follow_their_inputs():
         want = both()
         torch.cuda.synchronize()
         assert all(torch.equal(torch.nan_to_num(a, nan=12345.0), torch.nan_to_num(b, nan=12345.0)) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("B,T,D,seed", [(15, 1281, 2, 889), (40, 1281, 2, 5), (25, 1297, 3, 6)])
+def test_a_gradient_that_nearly_cancels(B, T, D, seed):
+    """A segment of one step before the window's end: dfinal and the last dy meet in its map, where they may cancel.  Its
+    product and sum round once."""
+    say("recurrence with a last tile of one step B=%d T=%d D=%d" % (B, T, D))
+    check(*make(B, T, D, "float32", seed, False, True), "float32", False)
