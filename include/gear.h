@@ -569,11 +569,11 @@ int gear_table_priorities(const gear_table *t, uint32_t **d_priority);
 
 /*
  * The learner's operators on collected windows: the gated linear recurrence
- * of a sequence model, the advantages of its rewards, and the clipped policy
- * loss.  They need no table, run on the current HIP device, keep nothing
+ * of a sequence model, the advantages of its rewards, the clipped policy
+ * loss, layer norm, the loss of a token head and the optimizer's step.  They need no table, run on the current HIP device, keep nothing
  * between calls and allocate nothing: what they need beside their inputs and
  * outputs is the caller's workspace.  Captures of them replay correctly.
- * Every pointer but a descriptor is device memory; inputs are not written, and
+ * Every pointer but a descriptor or a list of tensors is device memory; inputs are not written, and
  * outputs meet neither inputs nor each other but where a call allows it.
  * No content of an input (flags, lengths, actions) makes a kernel read or
  * write outside buffers of the stated sizes.
@@ -748,6 +748,196 @@ int gear_policy_loss(const gear_policy_desc *d, const void *d_logits, const floa
  */
 int gear_action_logp(const gear_policy_desc *d, const void *d_logits, float *d_logp, float *d_entropy,
                      void *stream);
+
+/*
+ * Layer norm of rows, with the residual sum before it:
+ *
+ *   t = x + r (rounded to the rows' type; t = x without a residual)
+ *   u = (t - mean t) / sqrt(var t + eps),  y = u weight + bias
+ *
+ * var is the mean of (t - mean t)^2.  All sums are in 32 bits.
+ */
+typedef struct gear_norm_desc {
+    int32_t dtype;        /* of x, residual, y, total, dy, dtotal, dx: GEAR_DTYPE_F16, _BF16 or _F32 */
+    int32_t param_dtype;  /* of weight, bias, dweight, dbias: dtype or GEAR_DTYPE_F32 */
+    int64_t n, D;         /* n rows (0 or more) of D values (1 .. 2^20) */
+    int64_t x_row, residual_row;  /* strides from row to row, in elements, each 0 or more */
+    int64_t dy_row, dtotal_row;   /* read by the backward call only */
+    float eps;            /* 0 or more */
+} gear_norm_desc;
+
+/* gear_layer_norm_sizes - bytes of d_work that gear_layer_norm_backward of this
+ * descriptor needs for dweight and dbias; without them it needs none.  Host only. */
+int gear_layer_norm_sizes(const gear_norm_desc *d, int64_t *work_bytes);
+
+/*
+ * gear_layer_norm - y of rows x, and the sum t where there is a residual.
+ *
+ *   d_x         rows as the descriptor lays them out, of any alignment
+ *   d_residual  likewise, or NULL
+ *   d_weight, d_bias  [D] or NULL for ones and zeros
+ *   d_y         [n][D], contiguous
+ *   d_total     [n][D], contiguous: t.  With a residual only; NULL: not written
+ *   d_saved     float[n][2] or NULL: mean and 1 / sqrt(var + eps), for the backward call
+ *
+ * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
+ */
+int gear_layer_norm(const gear_norm_desc *d, const void *d_x, const void *d_residual, const void *d_weight,
+                    const void *d_bias, void *d_y, void *d_total, float *d_saved, void *stream);
+
+/*
+ * gear_layer_norm_backward - gradients of a gear_layer_norm call for the gradient
+ * d_dy of its y and d_dtotal of its sum.  With g = dy weight:
+ *
+ *   dx = (g - mean g - u mean(g u)) / sqrt(var + eps) + dtotal,  dweight = sum_rows dy u,  dbias = sum_rows dy
+ *
+ *   d_t        the rows t that were normalised (x, or d_total where there was a
+ *              residual), at stride x_row
+ *   d_saved    as that call wrote it
+ *   d_weight   as that call had it
+ *   d_dtotal   rows or NULL for zeros
+ *   d_dx       [n][D], contiguous, or NULL: the gradient for x, and for the residual
+ *   d_dweight, d_dbias  [D], each or NULL: not written
+ *   d_work     workspace; its contents do not matter.  May be NULL without dweight and dbias
+ *
+ * Sums over rows have an order that depends on n, D and the types alone, so
+ * results repeat bit for bit.
+ * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
+ */
+int gear_layer_norm_backward(const gear_norm_desc *d, const void *d_t, const float *d_saved, const void *d_weight,
+                             const void *d_dy, const void *d_dtotal, void *d_dx, void *d_dweight, void *d_dbias,
+                             void *d_work, int64_t work_bytes, void *stream);
+
+/* The loss of a token head: n rows of D hidden values, a head of V rows of D. */
+#define GEAR_TOKEN_MAX 16777216  /* rows, and tokens, at most */
+typedef struct gear_token_desc {
+    int32_t dtype;          /* of hidden, head, dhidden, dhead: GEAR_DTYPE_F16, _BF16 or _F32 */
+    int32_t target_dtype;   /* GEAR_DTYPE_U8, _I32 or _I64 */
+    int64_t n, D, V;        /* n 0 .. GEAR_TOKEN_MAX, D 1 .. 65536, V 1 .. GEAR_TOKEN_MAX, n V at most 2^36 */
+    int64_t hidden_row, head_row;  /* strides from row to row, in elements, D or more */
+    const void *d_target;   /* [n]: a row whose target is outside [0, V) takes no part */
+    const uint8_t *d_mask;  /* [ceil(n / mask_group)] or NULL: rows with 0 take no part, nor is any value of theirs used */
+    const float *d_weight;  /* [ceil(n / weight_group)] or NULL for ones */
+    int64_t mask_group;     /* consecutive rows that share a mask value, 1 or more; likewise below */
+    int64_t weight_group;
+    float denom;            /* what the sum over rows is divided by; 0 for the number of rows that take part */
+    float grad_scale;       /* the gradients are those of grad_scale * loss (a loss scale) */
+} gear_token_desc;
+
+/* gear_token_loss_sizes - bytes of d_work that gear_token_loss and
+ * gear_token_loss_backward need.  Either pointer may be NULL.  Host only. */
+int gear_token_loss_sizes(const gear_token_desc *d, int64_t *loss_bytes, int64_t *backward_bytes);
+
+/*
+ * gear_token_loss - the cross entropy of targets under a token head, without its
+ * logits: they are formed in pieces, in 32 bits, and leave their maximum and sum.
+ * With z = hidden head^T, lse = log sum_v exp z_v and logp = z[target] - lse,
+ *
+ *   loss = -sum_rows weight logp / denom
+ *
+ *   d_hidden, d_head  rows as the descriptor lays them out
+ *   d_loss            one float
+ *   d_logp, d_lse     float[n] or NULL; 0 for rows that take no part
+ *   d_work            workspace; its contents do not matter
+ *
+ * Products of 16-bit values are exact and added in 32 bits; 32-bit values enter
+ * the products in three 16-bit parts, their six largest products: as exact as
+ * products in 32 bits, but an infinity among 32-bit values counts as NaN.  A NaN in a
+ * row that takes part, or in the head, shows in the loss.
+ * Results repeat bit for bit.
+ * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
+ */
+int gear_token_loss(const gear_token_desc *d, const void *d_hidden, const void *d_head, float *d_loss, float *d_logp,
+                    float *d_lse, void *d_work, int64_t work_bytes, void *stream);
+
+/*
+ * gear_token_loss_backward - gradients of a gear_token_loss call with the same
+ * descriptor, hidden and head.  With c = grad_scale grad_loss weight / denom and
+ * e_v = exp(z_v - lse) - [v = target]:
+ *
+ *   dhidden = c sum_v e_v head_v,  dhead_v = sum_rows c e_v hidden
+ *
+ *   d_lse        as that call wrote it
+ *   d_grad_loss  one float that multiplies the gradients, read on the device, or NULL for 1
+ *   d_dhidden    [n][D], contiguous, or NULL: not written; 0 for rows that take no part
+ *   d_dhead      [V][D], contiguous, or NULL: not written
+ *
+ * The logits are formed again, a piece of the vocabulary at a time, and e is
+ * rounded once to the products' type (three parts for 32-bit values).
+ * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
+ */
+int gear_token_loss_backward(const gear_token_desc *d, const void *d_hidden, const void *d_head, const float *d_lse,
+                             const float *d_grad_loss, void *d_dhidden, void *d_dhead, void *d_work,
+                             int64_t work_bytes, void *stream);
+
+/* One tensor of an optimizer's step: n values, contiguous. */
+typedef struct gear_step_tensor {
+    int32_t dtype;          /* of param and grad: GEAR_DTYPE_F16, _BF16 or _F32 */
+    int64_t n;              /* 0 .. 2^40 */
+    const void *d_grad;
+    void *d_param;          /* this and the following: gear_adamw only */
+    float *d_master;        /* float[n]: the parameter in 32 bits, of which d_param is the rounded copy; NULL: none */
+    void *d_exp_avg;        /* the averages: float[n], or e4m3 bytes [n] */
+    void *d_exp_avg_sq;
+    float *d_exp_avg_scale; /* 8-bit averages: float[ceil(n / GEAR_STEP_BLOCK)] each */
+    float *d_exp_avg_sq_scale;
+} gear_step_tensor;
+#define GEAR_STEP_BLOCK 256  /* values of an 8-bit average that share a scale */
+
+/* gear_step_sizes - bytes of d_work that gear_grad_norm and gear_adamw need.  Host only. */
+int gear_step_sizes(int64_t *norm_bytes, int64_t *adamw_bytes);
+
+/*
+ * gear_grad_norm - the 2-norm of all gradients together, after a factor, and what
+ * gear_adamw should multiply them by:
+ *
+ *   norm = scale ||grad||,  factor = scale min(1, max_norm / norm)
+ *
+ *   tensors    host array of `count`; dtype, n and d_grad are read
+ *   scale      above 0: 1 over a loss scale
+ *   max_norm   above 0, or infinite for no limit
+ *   d_norm     one float
+ *   d_factor   one float: NaN where the norm is not finite
+ *
+ * Squares are added in 64 bits, in an order that depends on the sizes alone.
+ * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
+ */
+int gear_grad_norm(const gear_step_tensor *tensors, int64_t count, float scale, float max_norm, float *d_norm,
+                   float *d_factor, void *d_work, int64_t work_bytes, void *stream);
+
+/* Constants of gear_adamw. */
+typedef struct gear_adamw_desc {
+    int32_t state_bits;     /* 32 or 8, of the averages */
+    double lr, beta1, beta2, eps, weight_decay;  /* lr, weight_decay 0 or more, betas in [0, 1), eps above 0 (in 32 bits) */
+    const float *d_lr;      /* one float that takes lr's place, read on the device, or NULL */
+    const float *d_factor;  /* one float that multiplies the gradients, read on the device, or NULL for 1 */
+} gear_adamw_desc;
+
+/*
+ * gear_adamw - one AdamW step of many tensors:
+ *
+ *   s <- s + 1,  g = factor grad
+ *   m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2
+ *   p <- p (1 - lr weight_decay) - lr (m / (1 - beta1^s)) / (sqrt(v / (1 - beta2^s)) + eps)
+ *
+ * in 32 bits; p is the master where there is one, and the parameter its rounded copy.
+ *
+ *   tensors  host array of `count`, read before the call returns.  What is
+ *            written (parameters, masters, averages, scales, d_step) must not overlap
+ *   d_step   one int64: s, the steps taken so far
+ *
+ * Averages of 32 bits hold m and v.  Averages of 8 bits hold e4m3 values of m
+ * and of sqrt(v), each times its block's scale, which is the block's largest
+ * magnitude over 448; they are rounded to nearest when stored, and what is not 0 is
+ * stored as no less than the least e4m3 value (an update divided by 0 would have no
+ * bound), but for blocks wholly below 2^-100, which are stored as zeros.  Zeros are
+ * zeros in both.
+ * Where the factor, or the device's lr, is not finite, the call leaves everything as
+ * it was, s too.
+ * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
+ */
+int gear_adamw(const gear_adamw_desc *d, const gear_step_tensor *tensors, int64_t count, int64_t *d_step, void *d_work,
+               int64_t work_bytes, void *stream);
 
 /* gear_last_error - message describing the last failed call on this
  * thread ("" if none).  Valid until the next call on the same thread. */

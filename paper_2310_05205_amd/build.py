@@ -15,7 +15,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libgear.so")
 BINDING = os.path.join(PKG, "_binding.so")
 SOURCES = ["table.hip", "alloc.hip", "select.hip", "topk.hip", "shard.hip", "collect.hip", "update.hip",
-           "recurrence.hip", "advantage.hip", "policy.hip"]
+           "recurrence.hip", "advantage.hip", "policy.hip", "norm.hip", "token.hip", "step.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

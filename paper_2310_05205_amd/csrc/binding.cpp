@@ -18,8 +18,11 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <exception>
+#include <utility>
 #include <vector>
 
 #include "gear.h"
@@ -41,6 +44,15 @@ decltype(&gear_advantages) f_advantages = nullptr;
 decltype(&gear_policy_sizes) f_policy_sizes = nullptr;
 decltype(&gear_policy_loss) f_policy_loss = nullptr;
 decltype(&gear_action_logp) f_action_logp = nullptr;
+decltype(&gear_layer_norm_sizes) f_layer_norm_sizes = nullptr;
+decltype(&gear_layer_norm) f_layer_norm = nullptr;
+decltype(&gear_layer_norm_backward) f_layer_norm_backward = nullptr;
+decltype(&gear_token_loss_sizes) f_token_loss_sizes = nullptr;
+decltype(&gear_token_loss) f_token_loss = nullptr;
+decltype(&gear_token_loss_backward) f_token_loss_backward = nullptr;
+decltype(&gear_step_sizes) f_step_sizes = nullptr;
+decltype(&gear_grad_norm) f_grad_norm = nullptr;
+decltype(&gear_adamw) f_adamw = nullptr;
 
 // One column of a table as its batches are handed out.
 struct Column {
@@ -81,6 +93,12 @@ float as_float(PyObject* o) {
     const double v = PyFloat_AsDouble(o);
     if (v == -1.0 && PyErr_Occurred()) throw PythonError();
     return (float)v;
+}
+
+double as_double(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw PythonError();
+    return v;
 }
 
 bool as_bool(PyObject* o) {
@@ -241,7 +259,7 @@ PyObject* entry(Py_ssize_t have, Py_ssize_t want, F body) {
 }
 
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return entry(n, 15, [&]() -> PyObject* {
+    return entry(n, 24, [&]() -> PyObject* {
         f_select = reinterpret_cast<decltype(f_select)>(as_ptr(a[0]));
         f_collect = reinterpret_cast<decltype(f_collect)>(as_ptr(a[1]));
         f_select_collect = reinterpret_cast<decltype(f_select_collect)>(as_ptr(a[2]));
@@ -257,6 +275,15 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
         f_policy_sizes = reinterpret_cast<decltype(f_policy_sizes)>(as_ptr(a[12]));
         f_policy_loss = reinterpret_cast<decltype(f_policy_loss)>(as_ptr(a[13]));
         f_action_logp = reinterpret_cast<decltype(f_action_logp)>(as_ptr(a[14]));
+        f_layer_norm_sizes = reinterpret_cast<decltype(f_layer_norm_sizes)>(as_ptr(a[15]));
+        f_layer_norm = reinterpret_cast<decltype(f_layer_norm)>(as_ptr(a[16]));
+        f_layer_norm_backward = reinterpret_cast<decltype(f_layer_norm_backward)>(as_ptr(a[17]));
+        f_token_loss_sizes = reinterpret_cast<decltype(f_token_loss_sizes)>(as_ptr(a[18]));
+        f_token_loss = reinterpret_cast<decltype(f_token_loss)>(as_ptr(a[19]));
+        f_token_loss_backward = reinterpret_cast<decltype(f_token_loss_backward)>(as_ptr(a[20]));
+        f_step_sizes = reinterpret_cast<decltype(f_step_sizes)>(as_ptr(a[21]));
+        f_grad_norm = reinterpret_cast<decltype(f_grad_norm)>(as_ptr(a[22]));
+        f_adamw = reinterpret_cast<decltype(f_adamw)>(as_ptr(a[23]));
         Py_RETURN_NONE;
     });
 }
@@ -898,6 +925,458 @@ PyObject* py_action_logp(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// Rows [..., D] at one stride.
+struct Rows {
+    Sizes lead;  // the leading sizes
+    int64_t n = 1, D = 0, stride = 0;
+
+    Rows(const at::Tensor& t, const char* name) {
+        need_rows(t, name);
+        D = t.size(-1);
+        const int64_t k = t.dim() - 1;
+        lead.assign(t.sizes().begin(), t.sizes().end() - 1);
+        stride = D;
+        bool first = true;
+        for (int64_t i = k - 1; i >= 0; i--) {
+            if (lead[i] != 1) {
+                if (first) {
+                    stride = t.stride(i);
+                } else {
+                    TORCH_CHECK_VALUE(t.stride(i) == stride * n || t.numel() == 0, "the rows of ", name,
+                                      " must lie at one stride");
+                }
+                first = false;
+            }
+            n *= lead[i];
+        }
+        if (t.numel() == 0) stride = D;
+    }
+};
+
+// A tensor or None with the shape, type and device of `like`, in rows at one stride, which is returned.
+at::Tensor rows_like(PyObject* o, const char* name, const at::Tensor& like, const char* like_name, int64_t& stride) {
+    if (o == Py_None) return at::Tensor();
+    const at::Tensor& t = tensor_of(o, name);
+    need_device(t, name, like.device());
+    TORCH_CHECK_VALUE(t.scalar_type() == like.scalar_type(), name, " and ", like_name, " must have one dtype");
+    need_sizes(t, name, like.sizes().vec());
+    stride = Rows(t, name).stride;
+    return t;
+}
+
+// A parameter [D] of a layer norm, or None.
+at::Tensor norm_param(PyObject* o, const char* name, const at::Tensor& x, int64_t D) {
+    if (o == Py_None) return at::Tensor();
+    const at::Tensor& t = tensor_of(o, name);
+    need_device(t, name, x.device());
+    TORCH_CHECK_VALUE(t.scalar_type() == at::kFloat || t.scalar_type() == x.scalar_type(), name,
+                      " must be float32 or of the rows' dtype, not ", t.scalar_type());
+    need_sizes(t, name, {D});
+    need_contiguous(t, name);
+    return t;
+}
+
+// layer_norm(x, weight, bias, eps, residual, save, stream): (y, total or None, saved or None)
+PyObject* py_layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return entry(n, 7, [&]() -> PyObject* {
+        const at::Tensor& x = tensor_of(a[0], "x");
+        const c10::Device dev = gpu_of(x, "x");
+        gear_norm_desc d{};
+        d.dtype = float_code(x, "x");
+        const Rows rows(x, "x");
+        TORCH_CHECK_VALUE(rows.D >= 1, "rows must have at least one value");
+        d.n = rows.n;
+        d.D = rows.D;
+        d.x_row = rows.stride;
+        const at::Tensor weight = norm_param(a[1], "weight", x, d.D), bias = norm_param(a[2], "bias", x, d.D);
+        TORCH_CHECK_VALUE(weight.defined() || !bias.defined(), "a bias needs a weight");
+        TORCH_CHECK_VALUE(!bias.defined() || bias.scalar_type() == weight.scalar_type(),
+                          "weight and bias must have one dtype");
+        d.param_dtype = weight.defined() ? float_code(weight, "weight") : d.dtype;
+        d.eps = as_float(a[3]);
+        const at::Tensor residual = rows_like(a[4], "residual", x, "x", d.residual_row);
+        const bool save = as_bool(a[5]);
+        void* s = as_ptr(a[6]);
+        const c10::DeviceGuard guard(dev);
+        at::Tensor y = make(x.sizes(), x.scalar_type(), dev), total, saved;
+        if (residual.defined()) total = make(x.sizes(), x.scalar_type(), dev);
+        if (save) saved = make({d.n, 2}, at::kFloat, dev);
+        const int rc = without_gil([&] {
+            return f_layer_norm(&d, x.data_ptr(), data<void>(residual), data<void>(weight), data<void>(bias), y.data_ptr(),
+                                data<void>(total), data<float>(saved), s);
+        });
+        if (rc != GEAR_OK) return PyLong_FromLong(rc);
+        Tuple t(3);
+        t.set(0, wrap(std::move(y)));
+        if (total.defined()) t.set(1, wrap(std::move(total)));
+        else t.none(1);
+        if (save) t.set(2, wrap(std::move(saved)));
+        else t.none(2);
+        return t.release();
+    });
+}
+
+// layer_norm_backward(dy, t, saved, weight, dtotal, stream): (dx, dweight or None, dbias or None)
+PyObject* py_layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return entry(n, 6, [&]() -> PyObject* {
+        const at::Tensor& x = tensor_of(a[1], "x");
+        const c10::Device dev = gpu_of(x, "x");
+        gear_norm_desc d{};
+        d.dtype = float_code(x, "x");
+        const Rows rows(x, "x");
+        TORCH_CHECK_VALUE(rows.D >= 1, "rows must have at least one value");
+        d.n = rows.n;
+        d.D = rows.D;
+        d.x_row = rows.stride;
+        const at::Tensor dy = rows_like(a[0], "dy", x, "x", d.dy_row);
+        TORCH_CHECK_VALUE(dy.defined(), "dy is missing");
+        const at::Tensor saved = optional_of(a[2], "saved", Kind::kFloat, dev);
+        TORCH_CHECK_VALUE(saved.defined(), "saved must be what layer_norm(..., save=True) returned");
+        need_sizes(saved, "saved", {d.n, 2});
+        need_contiguous(saved, "saved");
+        const at::Tensor weight = norm_param(a[3], "weight", x, d.D);
+        d.param_dtype = weight.defined() ? float_code(weight, "weight") : d.dtype;
+        const at::Tensor dtotal = rows_like(a[4], "dtotal", x, "x", d.dtotal_row);
+        void* s = as_ptr(a[5]);
+        const c10::DeviceGuard guard(dev);
+        at::Tensor dx = make(x.sizes(), x.scalar_type(), dev), dweight, dbias, work;
+        int64_t work_bytes = 0;
+        if (weight.defined()) {
+            dweight = make({d.D}, weight.scalar_type(), dev);
+            dbias = make({d.D}, weight.scalar_type(), dev);
+            const int rc = f_layer_norm_sizes(&d, &work_bytes);
+            if (rc != GEAR_OK) return PyLong_FromLong(rc);
+            work = workspace(work_bytes, dev);
+        }
+        const int rc = without_gil([&] {
+            return f_layer_norm_backward(&d, x.data_ptr(), data<float>(saved), data<void>(weight), dy.data_ptr(),
+                                         data<void>(dtotal), dx.data_ptr(), data<void>(dweight), data<void>(dbias),
+                                         data<void>(work), work_bytes, s);
+        });
+        if (rc != GEAR_OK) return PyLong_FromLong(rc);
+        Tuple t(3);
+        t.set(0, wrap(std::move(dx)));
+        if (weight.defined()) {
+            t.set(1, wrap(std::move(dweight)));
+            t.set(2, wrap(std::move(dbias)));
+        } else {
+            t.none(1);
+            t.none(2);
+        }
+        return t.release();
+    });
+}
+
+// Consecutive rows that share a value of `t`, whose shape is the first of the rows' leading sizes.
+int64_t sharing(const at::Tensor& t, const char* name, const Sizes& rows) {
+    TORCH_CHECK_VALUE(t.dim() >= 1 || rows.empty(), name, " must have at least one dimension");
+    TORCH_CHECK_VALUE((size_t)t.dim() <= rows.size(), name, " has more dimensions than target");
+    int64_t g = 1;
+    for (size_t i = 0; i < rows.size(); i++) {
+        if (i < (size_t)t.dim()) {
+            TORCH_CHECK_VALUE(t.size((int64_t)i) == rows[i], name, " must have the first sizes of ",
+                              at::IntArrayRef(rows), ", not ", t.sizes());
+        } else {
+            g *= rows[i];
+        }
+    }
+    return g < 1 ? 1 : g;
+}
+
+// Hidden rows [..., D], the head [V, D], targets, and what both directions take beside them.
+struct Token {
+    at::Tensor hidden, head, target, weight, mask;
+    gear_token_desc d{};
+    c10::Device dev = c10::Device(at::kCPU);
+    Sizes lead;
+
+    Token(PyObject* o_hidden, PyObject* o_head, PyObject* o_target, PyObject* o_weight, PyObject* o_mask, PyObject* o_denom) {
+        hidden = tensor_of(o_hidden, "hidden");
+        head = tensor_of(o_head, "head");
+        target = tensor_of(o_target, "target");
+        dev = gpu_of(hidden, "hidden");
+        need_device(head, "head", dev);
+        need_device(target, "target", dev);
+        d.dtype = float_code(hidden, "hidden");
+        TORCH_CHECK_VALUE(head.scalar_type() == hidden.scalar_type(), "head and hidden must have one dtype");
+        const Rows rows(hidden, "hidden");
+        lead = rows.lead;
+        d.n = rows.n;
+        d.D = rows.D;
+        d.hidden_row = rows.stride;
+        TORCH_CHECK_VALUE(d.n <= 1 || d.hidden_row >= d.D, "the rows of hidden must not overlap");
+        TORCH_CHECK_VALUE(head.dim() == 2 && head.size(1) == d.D && head.size(0) >= 1 && d.D >= 1,
+                          "head must have shape [V, ", d.D, "], not ", head.sizes());
+        need_rows(head, "head");
+        d.V = head.size(0);
+        d.head_row = d.V > 1 ? head.stride(0) : d.D;
+        TORCH_CHECK_VALUE(d.head_row >= d.D, "the rows of head must not overlap");
+        need_sizes(target, "target", lead);
+        need_contiguous(target, "target");
+        switch (target.scalar_type()) {
+            case at::kByte: d.target_dtype = GEAR_DTYPE_U8; break;
+            case at::kInt: d.target_dtype = GEAR_DTYPE_I32; break;
+            case at::kLong: d.target_dtype = GEAR_DTYPE_I64; break;
+            default: TORCH_CHECK_VALUE(false, "target must be uint8, int32 or int64, not ", target.scalar_type());
+        }
+        weight = optional_of(o_weight, "weight", Kind::kFloat, dev);
+        need_contiguous(weight, "weight");
+        d.weight_group = weight.defined() ? sharing(weight, "weight", lead) : 1;
+        mask = optional_of(o_mask, "mask", Kind::kFlags, dev);
+        need_contiguous(mask, "mask");
+        d.mask_group = mask.defined() ? sharing(mask, "mask", lead) : 1;
+        d.denom = o_denom == Py_None ? 0.0f : as_float(o_denom);
+        TORCH_CHECK_VALUE(o_denom == Py_None || d.denom > 0.0f, "denom must be above 0");
+        d.grad_scale = 1.0f;
+        d.d_target = target.data_ptr();
+        d.d_mask = data<uint8_t>(mask);
+        d.d_weight = data<float>(weight);
+    }
+};
+
+// token_loss(hidden, head, target, weight, mask, denom, stream): (loss, logp, lse)
+PyObject* py_token_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return entry(n, 7, [&]() -> PyObject* {
+        const Token k(a[0], a[1], a[2], a[3], a[4], a[5]);
+        void* s = as_ptr(a[6]);
+        const c10::DeviceGuard guard(k.dev);
+        int64_t bytes = 0;
+        int rc = f_token_loss_sizes(&k.d, &bytes, nullptr);
+        if (rc != GEAR_OK) return PyLong_FromLong(rc);
+        at::Tensor loss = make({}, at::kFloat, k.dev), logp = make(k.lead, at::kFloat, k.dev),
+                   lse = make(k.lead, at::kFloat, k.dev);
+        const at::Tensor work = workspace(bytes, k.dev);
+        rc = without_gil([&] {
+            return f_token_loss(&k.d, k.hidden.data_ptr(), k.head.data_ptr(), data<float>(loss), data<float>(logp),
+                                data<float>(lse), data<void>(work), bytes, s);
+        });
+        if (rc != GEAR_OK) return PyLong_FromLong(rc);
+        Tuple t(3);
+        t.set(0, wrap(std::move(loss)));
+        t.set(1, wrap(std::move(logp)));
+        t.set(2, wrap(std::move(lse)));
+        return t.release();
+    });
+}
+
+// token_loss_backward(hidden, head, target, lse, weight, mask, denom, grad_scale, grad_loss, want_dhidden, want_dhead,
+//                     stream): (dhidden or None, dhead or None)
+PyObject* py_token_loss_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return entry(n, 12, [&]() -> PyObject* {
+        Token k(a[0], a[1], a[2], a[4], a[5], a[6]);
+        const at::Tensor lse = optional_of(a[3], "lse", Kind::kFloat, k.dev);
+        TORCH_CHECK_VALUE(lse.defined(), "lse must be what token_loss returned");
+        need_sizes(lse, "lse", k.lead);
+        need_contiguous(lse, "lse");
+        k.d.grad_scale = as_float(a[7]);
+        const at::Tensor grad_loss = optional_of(a[8], "grad_loss", Kind::kFloat, k.dev);
+        TORCH_CHECK_VALUE(!grad_loss.defined() || grad_loss.numel() == 1, "grad_loss must hold one value");
+        const bool want_hidden = as_bool(a[9]), want_head = as_bool(a[10]);
+        void* s = as_ptr(a[11]);
+        const c10::DeviceGuard guard(k.dev);
+        int64_t bytes = 0;
+        int rc = f_token_loss_sizes(&k.d, nullptr, &bytes);
+        if (rc != GEAR_OK) return PyLong_FromLong(rc);
+        at::Tensor dhidden, dhead;
+        if (want_hidden) dhidden = make(k.hidden.sizes(), k.hidden.scalar_type(), k.dev);
+        if (want_head) dhead = make(k.head.sizes(), k.head.scalar_type(), k.dev);
+        const at::Tensor work = workspace(bytes, k.dev);
+        rc = without_gil([&] {
+            return f_token_loss_backward(&k.d, k.hidden.data_ptr(), k.head.data_ptr(), data<float>(lse),
+                                         data<float>(grad_loss), data<void>(dhidden), data<void>(dhead), data<void>(work),
+                                         bytes, s);
+        });
+        if (rc != GEAR_OK) return PyLong_FromLong(rc);
+        Tuple t(2);
+        if (want_hidden) t.set(0, wrap(std::move(dhidden)));
+        else t.none(0);
+        if (want_head) t.set(1, wrap(std::move(dhead)));
+        else t.none(1);
+        return t.release();
+    });
+}
+
+// The tensors of a list or tuple; undefined ones for None where `holes`.
+std::vector<at::Tensor> tensors_of(PyObject* o, const char* name, bool holes = false) {
+    TORCH_CHECK_TYPE(PyList_Check(o) || PyTuple_Check(o), name, " must be a list or tuple of tensors");
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+    std::vector<at::Tensor> out;
+    out.reserve((size_t)n);
+    for (Py_ssize_t i = 0; i < n; i++) {
+        PyObject* item = PySequence_Fast_GET_ITEM(o, i);
+        if (holes && item == Py_None) out.emplace_back();
+        else out.push_back(tensor_of(item, name));
+    }
+    return out;
+}
+void need_count(const std::vector<at::Tensor>& v, const char* name, size_t want) {
+    TORCH_CHECK_VALUE(v.size() == want, name, " must have ", want, " tensors, not ", v.size());
+}
+
+// One float on the device, or None.
+at::Tensor device_value(PyObject* o, const char* name, c10::Device dev) {
+    const at::Tensor t = optional_of(o, name, Kind::kFloat, dev);
+    TORCH_CHECK_VALUE(!t.defined() || t.numel() == 1, name, " must hold one value");
+    return t;
+}
+
+// grad_norm(grads, scale, max_norm or None, stream): (norm, factor)
+PyObject* py_grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return entry(n, 4, [&]() -> PyObject* {
+        const std::vector<at::Tensor> grads = tensors_of(a[0], "grads");
+        TORCH_CHECK_VALUE(!grads.empty(), "grads must have at least one tensor");
+        const c10::Device dev = gpu_of(grads[0], "grads");
+        std::vector<gear_step_tensor> list(grads.size());
+        for (size_t i = 0; i < grads.size(); i++) {
+            need_device(grads[i], "grads", dev);
+            need_contiguous(grads[i], "grads");
+            list[i] = gear_step_tensor{};
+            list[i].dtype = float_code(grads[i], "grads");
+            list[i].n = grads[i].numel();
+            list[i].d_grad = grads[i].data_ptr();
+        }
+        const float scale = as_float(a[1]), max_norm = a[2] == Py_None ? INFINITY : as_float(a[2]);
+        void* s = as_ptr(a[3]);
+        const c10::DeviceGuard guard(dev);
+        int64_t bytes = 0;
+        int rc = f_step_sizes(&bytes, nullptr);
+        if (rc != GEAR_OK) return PyLong_FromLong(rc);
+        at::Tensor norm = make({}, at::kFloat, dev), factor = make({}, at::kFloat, dev);
+        const at::Tensor work = workspace(bytes, dev);
+        rc = without_gil([&] {
+            return f_grad_norm(list.data(), (int64_t)list.size(), scale, max_norm, data<float>(norm), data<float>(factor),
+                               data<void>(work), bytes, s);
+        });
+        if (rc != GEAR_OK) return PyLong_FromLong(rc);
+        Tuple t(2);
+        t.set(0, wrap(std::move(norm)));
+        t.set(1, wrap(std::move(factor)));
+        return t.release();
+    });
+}
+
+// adamw(params, grads, exp_avg, exp_avg_sq, step, scales or None, masters or None, lr, beta1, beta2, eps, weight_decay,
+//       factor or None, stream): None
+PyObject* py_adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return entry(n, 14, [&]() -> PyObject* {
+        const std::vector<at::Tensor> params = tensors_of(a[0], "params"), grads = tensors_of(a[1], "grads"),
+                                      m = tensors_of(a[2], "exp_avg"), v = tensors_of(a[3], "exp_avg_sq");
+        const size_t count = params.size();
+        need_count(grads, "grads", count);
+        need_count(m, "exp_avg", count);
+        need_count(v, "exp_avg_sq", count);
+        const at::Tensor& step = tensor_of(a[4], "step");
+        const c10::Device dev = gpu_of(step, "step");
+        TORCH_CHECK_VALUE(step.scalar_type() == at::kLong && step.numel() == 1, "step must be one int64");
+        gear_adamw_desc d{};
+        const bool eight = a[5] != Py_None;
+        d.state_bits = eight ? 8 : 32;
+        std::vector<at::Tensor> ms, vs, master;
+        if (eight) {
+            TORCH_CHECK_VALUE(PyTuple_Check(a[5]) && PyTuple_GET_SIZE(a[5]) == 2,
+                              "scales must be a pair of lists, of exp_avg and of exp_avg_sq");
+            ms = tensors_of(PyTuple_GET_ITEM(a[5], 0), "scales");
+            vs = tensors_of(PyTuple_GET_ITEM(a[5], 1), "scales");
+            need_count(ms, "scales", count);
+            need_count(vs, "scales", count);
+        }
+        if (a[6] != Py_None) {
+            master = tensors_of(a[6], "master", true);
+            need_count(master, "master", count);
+        }
+        at::Tensor lr;
+        if (THPVariable_Check(a[7])) lr = device_value(a[7], "lr", dev);
+        else d.lr = as_double(a[7]);
+        d.beta1 = as_double(a[8]);
+        d.beta2 = as_double(a[9]);
+        d.eps = as_double(a[10]);
+        d.weight_decay = as_double(a[11]);
+        const at::Tensor factor = device_value(a[12], "factor", dev);
+        d.d_lr = data<float>(lr);
+        d.d_factor = data<float>(factor);
+        void* s = as_ptr(a[13]);
+
+        typedef std::pair<const char*, const char*> Range;
+        std::vector<Range> written, read;
+        const auto range_of = [](const at::Tensor& t) {
+            return Range(data<char>(t), data<char>(t) + t.nbytes());
+        };
+        std::vector<gear_step_tensor> list(count);
+        const auto state = [&](const at::Tensor& t, const char* name, const at::Tensor& p, at::ScalarType type) {
+            need_device(t, name, dev);
+            TORCH_CHECK_VALUE(t.scalar_type() == type, name, " must be ", type, ", not ", t.scalar_type());
+            TORCH_CHECK_VALUE(t.numel() == p.numel(), name, " must have the parameter's ", p.numel(), " values, not ",
+                              t.numel());
+            need_contiguous(t, name);
+            if (t.numel()) written.push_back(range_of(t));
+        };
+        const at::ScalarType avg = eight ? at::kFloat8_e4m3fn : at::kFloat;
+        for (size_t i = 0; i < count; i++) {
+            const at::Tensor &p = params[i], &g = grads[i];
+            gear_step_tensor& t = list[i];
+            t = gear_step_tensor{};
+            t.dtype = float_code(p, "params");
+            t.n = p.numel();
+            state(p, "params", p, p.scalar_type());
+            need_device(g, "grads", dev);
+            TORCH_CHECK_VALUE(g.scalar_type() == p.scalar_type(), "a gradient must have its parameter's dtype");
+            need_sizes(g, "a gradient", p.sizes().vec());
+            need_contiguous(g, "grads");
+            if (t.n) read.push_back(range_of(g));
+            state(m[i], "exp_avg", p, avg);
+            state(v[i], "exp_avg_sq", p, avg);
+            if (eight) {
+                const int64_t blocks = (t.n + GEAR_STEP_BLOCK - 1) / GEAR_STEP_BLOCK;
+                for (const at::Tensor* sc : {&ms[i], &vs[i]}) {
+                    need_device(*sc, "scales", dev);
+                    TORCH_CHECK_VALUE(sc->scalar_type() == at::kFloat && sc->numel() == blocks,
+                                      "scales must be float32, one value for ", GEAR_STEP_BLOCK, " of the parameter's");
+                    need_contiguous(*sc, "scales");
+                    if (blocks) written.push_back(range_of(*sc));
+                }
+                t.d_exp_avg_scale = data<float>(ms[i]);
+                t.d_exp_avg_sq_scale = data<float>(vs[i]);
+            }
+            if (!master.empty() && master[i].defined()) {
+                TORCH_CHECK_VALUE(p.scalar_type() != at::kFloat, "a float32 parameter has no master");
+                state(master[i], "master", p, at::kFloat);
+                t.d_master = data<float>(master[i]);
+            }
+            t.d_grad = g.data_ptr();
+            t.d_param = p.data_ptr();
+            t.d_exp_avg = m[i].data_ptr();
+            t.d_exp_avg_sq = v[i].data_ptr();
+        }
+        written.push_back(range_of(step));
+        if (lr.defined()) read.push_back(range_of(lr));
+        if (factor.defined()) read.push_back(range_of(factor));
+        // What is written lies apart, and apart from what is read: workgroups run in no order.
+        std::sort(written.begin(), written.end());
+        for (size_t i = 1; i < written.size(); i++)
+            TORCH_CHECK_VALUE(written[i - 1].second <= written[i].first,
+                              "parameters, averages, masters, scales and step must not overlap");
+        for (const Range& r : read) {
+            const auto after = std::upper_bound(written.begin(), written.end(), Range(r.second - 1, nullptr),
+                                                [](const Range& x, const Range& y) { return x.first < y.first; });
+            TORCH_CHECK_VALUE(after == written.begin() || (after - 1)->second <= r.first,
+                              "a gradient, lr or factor must not overlap what is written");
+        }
+        const c10::DeviceGuard guard(dev);
+        int64_t bytes = 0;
+        int rc = f_step_sizes(nullptr, &bytes);
+        if (rc != GEAR_OK) return PyLong_FromLong(rc);
+        const at::Tensor work = workspace(bytes, dev);
+        const std::vector<at::Tensor>* const lists[] = {&params, &m, &v, &ms, &vs, &master};
+        for (const std::vector<at::Tensor>* each : lists)
+            for (const at::Tensor& t : *each)
+                if (t.defined()) overwrites(t);
+        overwrites(step);
+        rc = without_gil([&] { return f_adamw(&d, list.data(), (int64_t)count, data<int64_t>(step), data<void>(work), bytes, s); });
+        if (rc != GEAR_OK) return PyLong_FromLong(rc);
+        Py_RETURN_NONE;
+    });
+}
+
 #define GEAR_METHOD(name, doc) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(py_##name)), METH_FASTCALL, doc}
 PyMethodDef methods[] = {
     GEAR_METHOD(bind, "addresses of the library's entry points"),
@@ -915,6 +1394,12 @@ PyMethodDef methods[] = {
     GEAR_METHOD(advantages, "gear_advantages with allocated outputs"),
     GEAR_METHOD(policy_loss, "gear_policy_loss with allocated outputs"),
     GEAR_METHOD(action_logp, "gear_action_logp with allocated outputs"),
+    GEAR_METHOD(layer_norm, "gear_layer_norm with allocated outputs"),
+    GEAR_METHOD(layer_norm_backward, "gear_layer_norm_backward with allocated gradients"),
+    GEAR_METHOD(token_loss, "gear_token_loss with allocated outputs"),
+    GEAR_METHOD(token_loss_backward, "gear_token_loss_backward with allocated gradients"),
+    GEAR_METHOD(grad_norm, "gear_grad_norm of a list of tensors"),
+    GEAR_METHOD(adamw, "gear_adamw of lists of tensors"),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Per-step calls of the experience-replay library.", -1, methods,

@@ -1,0 +1,391 @@
+// The optimizer's step of many tensors at once, and the norm of their gradients
+// (include/gear.h).  A value is read, updated in 32 bits and written in one pass;
+// the averages are held in 32 bits, or in e4m3 with a scale per 256 values:
+//   m = q s,  v = (q' s')^2,  s = max |.| / 448 over the block.
+// The second average is held by its root: e4m3 reaches over 17 powers of two below a
+// block's largest, and the root needs half of what v itself would.
+//
+// Tensors travel in the kernel's arguments, 56 a launch, so a call needs no table
+// on the device and a captured call keeps its own.
+#include <math.h>
+
+#include "element.h"
+#include "gear_internal.h"
+
+namespace gear {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kValues = 8;                           // values a lane takes at a time
+constexpr int kChunk = kThreads * kValues * 4;       // values of a workgroup
+constexpr int kItems = 56;                           // tensors of one launch
+constexpr int kGroup = GEAR_STEP_BLOCK / kValues;    // lanes of an 8-bit block
+constexpr int kNormBlocks = 1024;
+constexpr float kTop = 448.0f, kLeast = 0.001953125f;  // e4m3: its largest value, and its least above 0
+constexpr float kNothing = 7.888609e-31f;              // 2^-100
+
+struct Item {
+    const void* grad;
+    void *param, *m, *v;
+    float *master, *ms, *vs;
+    int64_t n;
+};
+struct Items {
+    Item item[kItems];
+    uint32_t first[kItems + 1];  // chunks before each tensor
+    int32_t count;
+};
+
+// What a step multiplies by; made once on the device.
+struct Factors {
+    float grad, decay, rate, root;  // factor, 1 - lr weight_decay, lr / (1 - beta1^s), 1 / (1 - beta2^s)
+    int32_t skip;
+};
+
+// The tensor that a chunk belongs to.
+__device__ __forceinline__ int item_of(const Items& t, uint32_t chunk) {
+    int lo = 0, hi = t.count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (t.first[mid] <= chunk) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+template <int N, typename E>
+__device__ __forceinline__ void load(const E* p, int64_t left, float (&f)[N]) {
+    if (left >= N) {
+        Vec<E, N>::unpack(Vec<E, N>::load(p), f);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; j++) f[j] = j < left ? (float)p[j] : 0.0f;
+    }
+}
+template <int N, typename E>
+__device__ __forceinline__ void store(E* p, int64_t left, const float (&f)[N]) {
+    if (left >= N) {
+        Vec<E, N>::store(p, f);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; j++)
+            if (j < left) p[j] = (E)f[j];
+    }
+}
+
+typedef uint32_t Bytes __attribute__((ext_vector_type(2)));
+typedef Bytes LooseBytes __attribute__((aligned(1)));
+__device__ __forceinline__ void load8(const uint8_t* p, int64_t left, float scale, float (&f)[kValues]) {
+    Bytes b = {0, 0};
+    if (left >= kValues) {
+        b = *reinterpret_cast<const LooseBytes*>(p);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kValues; j++)
+            if (j < left) b[j / 4] |= (uint32_t)p[j] << (8 * (j % 4));
+    }
+#pragma unroll
+    for (int j = 0; j < kValues; j += 4) {
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)b[j / 4], false);
+        const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)b[j / 4], true);
+        f[j] = lo[0] * scale;
+        f[j + 1] = lo[1] * scale;
+        f[j + 2] = hi[0] * scale;
+        f[j + 3] = hi[1] * scale;
+    }
+}
+// A lane's values of a block, under the block's scale, which is returned.
+__device__ __forceinline__ float store8(uint8_t* p, int64_t left, const float (&f)[kValues]) {
+    float top = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kValues; j++) top = fmaxf(top, fabsf(f[j]));
+#pragma unroll
+    for (int off = 1; off < kGroup; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
+    const bool some = top >= kNothing;
+    const float inv = some ? kTop / top : 0.0f;
+    Bytes b;
+#pragma unroll
+    for (int j = 0; j < kValues; j += 4) {
+        float q[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const float x = f[j + k] * inv;
+            q[k] = x;
+            // Comparisons that a NaN passes through.
+            if (fabsf(x) > kTop) q[k] = copysignf(kTop, x);
+            if (fabsf(x) < kLeast) q[k] = f[j + k] != 0.0f && some ? copysignf(kLeast, x) : 0.0f;
+        }
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true);
+        b[j / 4] = (uint32_t)w;
+    }
+    if (left >= kValues) {
+        *reinterpret_cast<LooseBytes*>(p) = b;
+    } else {
+#pragma unroll
+        for (int j = 0; j < kValues; j++)
+            if (j < left) p[j] = (uint8_t)(b[j / 4] >> (8 * (j % 4)));
+    }
+    return some ? top / kTop : 0.0f;
+}
+
+// The step's factors, and the step counted; one lane.
+__global__ void factors_kernel(Factors* out, int64_t* step, const float* d_lr, const float* d_factor, double lr,
+                               double log1, double log2, double weight_decay) {
+    const float factor = d_factor ? *d_factor : 1.0f;
+    if (d_lr) lr = (double)*d_lr;
+    Factors f{};
+    f.skip = !(fabsf(factor) < INFINITY) || !(fabs(lr) < (double)INFINITY);
+    if (!f.skip) {
+        const double s = (double)(*step + 1);
+        *step += 1;
+        f.grad = factor;
+        f.decay = (float)(1.0 - lr * weight_decay);
+        f.rate = (float)(lr / -expm1(s * log1));
+        f.root = (float)(1.0 / -expm1(s * log2));
+    }
+    *out = f;
+}
+
+struct Betas {
+    float b1, c1, b2, c2, eps;  // c = 1 - b
+};
+
+template <typename E, bool MASTER, bool BITS8>
+__global__ __launch_bounds__(kThreads) void update_kernel(const Items t, const Betas b, const Factors* factors) {
+    const Factors f = *factors;
+    if (f.skip) return;
+    for (uint32_t chunk = blockIdx.x; chunk < t.first[t.count]; chunk += gridDim.x) {
+        const int k = item_of(t, chunk);
+        const Item& it = t.item[k];
+        const int64_t base = (int64_t)(chunk - t.first[k]) * kChunk;
+        const int64_t end = it.n - base < kChunk ? it.n : base + kChunk;
+        // Whole lanes of a block stay together: its scale is theirs together.
+        for (int64_t at = base; at < end; at += kThreads * kValues) {
+            const int64_t i = at + threadIdx.x * kValues, left = end - i;
+            float g[kValues], p[kValues], m[kValues], v[kValues];
+            load<kValues>(static_cast<const E*>(it.grad) + i, left, g);
+            if (MASTER) load<kValues>(it.master + i, left, p);
+            else load<kValues>(static_cast<const E*>(it.param) + i, left, p);
+            if (BITS8) {
+                const bool in = left > 0;
+                load8(static_cast<const uint8_t*>(it.m) + i, left, in ? it.ms[i / GEAR_STEP_BLOCK] : 0.0f, m);
+                load8(static_cast<const uint8_t*>(it.v) + i, left, in ? it.vs[i / GEAR_STEP_BLOCK] : 0.0f, v);
+#pragma unroll
+                for (int j = 0; j < kValues; j++) v[j] *= v[j];
+            } else {
+                load<kValues>(static_cast<const float*>(it.m) + i, left, m);
+                load<kValues>(static_cast<const float*>(it.v) + i, left, v);
+            }
+            float r[kValues];
+#pragma unroll
+            for (int j = 0; j < kValues; j++) {
+                const float x = g[j] * f.grad;
+                m[j] = b.b1 * m[j] + b.c1 * x;
+                v[j] = b.b2 * v[j] + b.c2 * (x * x);
+                if (BITS8) r[j] = sqrtf(v[j]);
+                p[j] = p[j] * f.decay - f.rate * m[j] / (sqrtf(v[j] * f.root) + b.eps);
+            }
+            if (MASTER) store<kValues>(it.master + i, left, p);
+            store<kValues>(static_cast<E*>(it.param) + i, left, p);
+            if (BITS8) {
+                const float sm = store8(static_cast<uint8_t*>(it.m) + i, left, m);
+                const float sv = store8(static_cast<uint8_t*>(it.v) + i, left, r);
+                if (left > 0 && (threadIdx.x & (kGroup - 1)) == 0) {
+                    it.ms[i / GEAR_STEP_BLOCK] = sm;
+                    it.vs[i / GEAR_STEP_BLOCK] = sv;
+                }
+            } else {
+                store<kValues>(static_cast<float*>(it.m) + i, left, m);
+                store<kValues>(static_cast<float*>(it.v) + i, left, v);
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ double block_add(double v, double* s) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0;
+#pragma unroll
+    for (int k = 0; k < kThreads / 64; k++) v += s[k];
+    return v;
+}
+
+// Squares of the gradients, a sum per workgroup; ADD to those of the launches before.
+template <typename E>
+__global__ __launch_bounds__(kThreads) void squares_kernel(const Items t, double* sums, int add) {
+    __shared__ double s[kThreads / 64];
+    double sum = 0.0;
+    for (uint32_t chunk = blockIdx.x; chunk < t.first[t.count]; chunk += gridDim.x) {
+        const int k = item_of(t, chunk);
+        const Item& it = t.item[k];
+        const int64_t base = (int64_t)(chunk - t.first[k]) * kChunk;
+        const int64_t end = it.n - base < kChunk ? it.n : base + kChunk;
+        for (int64_t at = base; at < end; at += kThreads * kValues) {
+            const int64_t i = at + threadIdx.x * kValues;
+            float g[kValues];
+            load<kValues>(static_cast<const E*>(it.grad) + i, end - i, g);
+#pragma unroll
+            for (int j = 0; j < kValues; j++) sum = fma((double)g[j], (double)g[j], sum);
+        }
+    }
+    sum = block_add(sum, s);
+    if (threadIdx.x == 0) sums[blockIdx.x] = sum + (add ? sums[blockIdx.x] : 0.0);
+}
+
+__global__ __launch_bounds__(kThreads) void norm_kernel(const double* sums, int blocks, float scale, float max_norm,
+                                                        float* norm, float* factor) {
+    __shared__ double s[kThreads / 64];
+    double sum = 0.0;
+    for (int k = threadIdx.x; k < blocks; k += kThreads) sum += sums[k];
+    sum = block_add(sum, s);
+    if (threadIdx.x == 0) {
+        const double x = sqrt(sum) * (double)scale;
+        *norm = (float)x;
+        const double limit = x > (double)max_norm ? (double)max_norm / x : 1.0;
+        *factor = fabsf((float)x) < INFINITY ? (float)((double)scale * limit) : NAN;
+    }
+}
+
+constexpr int64_t kMaxN = 1ll << 40;
+
+const char* flaw(const gear_step_tensor* t, int64_t count) {
+    if (count < 0 || (count > 0 && t == nullptr)) return "NULL or negative list of tensors";
+    for (int64_t i = 0; i < count; i++) {
+        if (float_bytes(t[i].dtype) == 0) return "dtype must be F16, BF16 or F32";
+        if (t[i].n < 0 || t[i].n > kMaxN) return "size out of range";
+        if (t[i].n > 0 && t[i].d_grad == nullptr) return "NULL gradient";
+    }
+    return nullptr;
+}
+const char* flaw(const gear_adamw_desc* d, const gear_step_tensor* t, int64_t count) {
+    if (d == nullptr) return "NULL descriptor";
+    if (d->state_bits != 32 && d->state_bits != 8) return "state_bits must be 32 or 8";
+    if (!(d->lr >= 0.0) || !(d->lr < 3e38) || !(d->weight_decay >= 0.0) || !(d->weight_decay < 3e38))
+        return "lr or weight_decay below 0 or not finite";
+    if (!(d->beta1 >= 0.0 && d->beta1 < 1.0) || !(d->beta2 >= 0.0 && d->beta2 < 1.0)) return "betas must lie in [0, 1)";
+    if (!((float)d->eps > 0.0f) || !(d->eps < 3e38)) return "eps must be above 0 in 32 bits, and finite";
+    for (int64_t i = 0; i < count; i++) {
+        if (t[i].n == 0) continue;
+        if (t[i].d_param == nullptr || t[i].d_exp_avg == nullptr || t[i].d_exp_avg_sq == nullptr)
+            return "NULL parameter or average";
+        if (d->state_bits == 8 && (t[i].d_exp_avg_scale == nullptr || t[i].d_exp_avg_sq_scale == nullptr))
+            return "8-bit averages need their scales";
+        if (t[i].d_master != nullptr && t[i].dtype == GEAR_DTYPE_F32) return "a 32-bit parameter has no master";
+    }
+    return nullptr;
+}
+
+// Fills `out` with tensors from `i` on that `want` accepts; true when there are any.
+template <typename F>
+bool gather(const gear_step_tensor* t, int64_t count, int64_t& i, Items& out, F want) {
+    out.count = 0;
+    out.first[0] = 0;
+    for (; i < count && out.count < kItems; i++) {
+        if (t[i].n == 0 || !want(t[i])) continue;
+        const uint64_t chunks = (uint64_t)((t[i].n + kChunk - 1) / kChunk);
+        if (out.first[out.count] + chunks > 0xFFFFFFFFull) break;  // the next launch's
+        out.item[out.count] = Item{t[i].d_grad, t[i].d_param, t[i].d_exp_avg, t[i].d_exp_avg_sq,
+                                   t[i].d_master, t[i].d_exp_avg_scale, t[i].d_exp_avg_sq_scale, t[i].n};
+        out.first[out.count + 1] = (uint32_t)(out.first[out.count] + chunks);
+        out.count++;
+    }
+    return out.count > 0;
+}
+
+typedef void (*Update)(const Items, const Betas, const Factors*);
+template <bool BITS8>
+Update update_of(int32_t dtype, bool master) {
+    if (dtype == GEAR_DTYPE_F32) return update_kernel<float, false, BITS8>;
+    if (dtype == GEAR_DTYPE_BF16) return master ? update_kernel<__bf16, true, BITS8> : update_kernel<__bf16, false, BITS8>;
+    return master ? update_kernel<_Float16, true, BITS8> : update_kernel<_Float16, false, BITS8>;
+}
+
+}  // namespace
+}  // namespace gear
+
+extern "C" int gear_step_sizes(int64_t* norm_bytes, int64_t* adamw_bytes) {
+    using namespace gear;
+    if (norm_bytes) *norm_bytes = 3 * (int64_t)(kNormBlocks * sizeof(double));
+    if (adamw_bytes) *adamw_bytes = (int64_t)sizeof(Factors);
+    return GEAR_OK;
+}
+
+extern "C" int gear_grad_norm(const gear_step_tensor* tensors, int64_t count, float scale, float max_norm,
+                              float* d_norm, float* d_factor, void* d_work, int64_t work_bytes, void* stream) {
+    using namespace gear;
+    if (const char* w = flaw(tensors, count)) return fail(GEAR_E_INVAL, std::string("gear_grad_norm: ") + w);
+    if (!(scale > 0.0f) || !(scale < 3e38f)) return fail(GEAR_E_INVAL, "gear_grad_norm: scale must be above 0 and finite");
+    if (!(max_norm > 0.0f)) return fail(GEAR_E_INVAL, "gear_grad_norm: max_norm must be above 0");
+    if (d_norm == nullptr || d_factor == nullptr) return fail(GEAR_E_INVAL, "gear_grad_norm: NULL norm or factor");
+    int64_t need = 0;
+    gear_step_sizes(&need, nullptr);
+    if (d_work == nullptr || work_bytes < need)
+        return fail(GEAR_E_INVAL, "gear_grad_norm: workspace smaller than gear_step_sizes states");
+    double* sums = static_cast<double*>(d_work);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    (void)hipGetLastError();  // an error pending from an earlier HIP call is not this call's
+    int blocks = 0;  // sums that the launches so far have left
+    Items items;
+    hipError_t e = hipSuccess;
+    const int32_t types[3] = {GEAR_DTYPE_F32, GEAR_DTYPE_BF16, GEAR_DTYPE_F16};
+    for (const int32_t type : types) {
+        // Each type has sums of its own.
+        int used = 0;
+        int64_t i = 0;
+        while (gather(tensors, count, i, items, [&](const gear_step_tensor& t) { return t.dtype == type; })) {
+            // Later launches add to all sums of the first, so they are as many workgroups.
+            const int grid = used ? used : kNormBlocks;
+            const auto kernel = type == GEAR_DTYPE_F32 ? squares_kernel<float>
+                                : type == GEAR_DTYPE_BF16 ? squares_kernel<__bf16> : squares_kernel<_Float16>;
+            hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, s, items, sums + blocks, used ? 1 : 0);
+            e = hipGetLastError();
+            if (e != hipSuccess) return hip_fail(e, "gear_grad_norm: launch");
+            used = grid;
+        }
+        blocks += used;
+    }
+    hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kThreads), 0, s, sums, blocks, scale, max_norm, d_norm, d_factor);
+    e = hipGetLastError();
+    return e == hipSuccess ? GEAR_OK : hip_fail(e, "gear_grad_norm: sum launch");
+}
+
+extern "C" int gear_adamw(const gear_adamw_desc* d, const gear_step_tensor* tensors, int64_t count, int64_t* d_step,
+                          void* d_work, int64_t work_bytes, void* stream) {
+    using namespace gear;
+    if (const char* w = flaw(tensors, count)) return fail(GEAR_E_INVAL, std::string("gear_adamw: ") + w);
+    if (const char* w = flaw(d, tensors, count)) return fail(GEAR_E_INVAL, std::string("gear_adamw: ") + w);
+    if (d_step == nullptr) return fail(GEAR_E_INVAL, "gear_adamw: NULL step");
+    if (d_work == nullptr || work_bytes < (int64_t)sizeof(Factors))
+        return fail(GEAR_E_INVAL, "gear_adamw: workspace smaller than gear_step_sizes states");
+    Factors* factors = static_cast<Factors*>(d_work);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    (void)hipGetLastError();  // an error pending from an earlier HIP call is not this call's
+    hipLaunchKernelGGL(factors_kernel, dim3(1), dim3(1), 0, s, factors, d_step, d->d_lr, d->d_factor, d->lr,
+                       log(d->beta1), log(d->beta2), d->weight_decay);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return hip_fail(e, "gear_adamw: factor launch");
+    const Betas b{(float)d->beta1, (float)(1.0 - d->beta1), (float)d->beta2, (float)(1.0 - d->beta2), (float)d->eps};
+    Items items;
+    const int32_t types[3] = {GEAR_DTYPE_F32, GEAR_DTYPE_BF16, GEAR_DTYPE_F16};
+    for (const int32_t type : types) {
+        for (int master = 0; master < 2; master++) {
+            int64_t i = 0;
+            while (gather(tensors, count, i, items, [&](const gear_step_tensor& t) {
+                return t.dtype == type && (t.d_master != nullptr) == (master != 0);
+            })) {
+                const Update kernel = d->state_bits == 8 ? update_of<true>(type, master != 0)
+                                                         : update_of<false>(type, master != 0);
+                const uint32_t chunks = items.first[items.count];
+                const uint32_t grid = chunks < (1u << 20) ? chunks : 1u << 20;
+                hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, s, items, b, factors);
+                e = hipGetLastError();
+                if (e != hipSuccess) return hip_fail(e, "gear_adamw: launch");
+            }
+        }
+    }
+    return GEAR_OK;
+}

@@ -10,7 +10,8 @@ device memory and to name the current stream.  Its calls of every step go
 through the native module ``_binding`` (built beside libgear.so), which
 allocates the outputs and makes the C call in one go; so do the learner's
 operators on collected windows (``recurrence``, ``advantages``,
-``policy_loss``, ``action_logp``), which take and return torch tensors.
+``policy_loss``, ``action_logp``, ``layer_norm``, ``token_loss``, ``grad_norm``,
+``adamw``), which take and return torch tensors.
 """
 import ctypes
 import os
@@ -50,6 +51,8 @@ GEAR_DTYPE_U32, GEAR_DTYPE_I32, GEAR_DTYPE_F32, GEAR_DTYPE_U64, GEAR_DTYPE_I64, 
 GEAR_MAX_NAME = 63
 GEAR_GATE_VALUE, GEAR_GATE_SIGMOID = 0, 1
 GEAR_RECURRENCE_STEPS = 16
+GEAR_TOKEN_MAX = 16777216
+GEAR_STEP_BLOCK = 256
 # torch dtype name of each GEAR_DTYPE_* (the library only moves bytes).
 DTYPE_NAMES = {GEAR_DTYPE_U8: "uint8", GEAR_DTYPE_I8: "int8", GEAR_DTYPE_U16: "uint16", GEAR_DTYPE_I16: "int16",
                GEAR_DTYPE_F16: "float16", GEAR_DTYPE_BF16: "bfloat16", GEAR_DTYPE_U32: "uint32",
@@ -89,6 +92,36 @@ class gear_policy_desc(ctypes.Structure):
                 + [(n, ctypes.c_float) for n in ("clip_low", "clip_high", "kl", "entropy", "denom", "grad_scale")])
 
 
+class gear_norm_desc(ctypes.Structure):
+    """Mirror of the C descriptor gear_norm_desc."""
+    _fields_ = ([("dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32)]
+                + [(n, ctypes.c_int64) for n in ("n", "D", "x_row", "residual_row", "dy_row", "dtotal_row")]
+                + [("eps", ctypes.c_float)])
+
+
+class gear_token_desc(ctypes.Structure):
+    """Mirror of the C descriptor gear_token_desc."""
+    _fields_ = ([("dtype", ctypes.c_int32), ("target_dtype", ctypes.c_int32)]
+                + [(n, ctypes.c_int64) for n in ("n", "D", "V", "hidden_row", "head_row")]
+                + [(n, ctypes.c_void_p) for n in ("d_target", "d_mask", "d_weight")]
+                + [(n, ctypes.c_int64) for n in ("mask_group", "weight_group")]
+                + [(n, ctypes.c_float) for n in ("denom", "grad_scale")])
+
+
+class gear_step_tensor(ctypes.Structure):
+    """Mirror of the C descriptor gear_step_tensor."""
+    _fields_ = ([("dtype", ctypes.c_int32), ("n", ctypes.c_int64)]
+                + [(n, ctypes.c_void_p) for n in ("d_grad", "d_param", "d_master", "d_exp_avg", "d_exp_avg_sq",
+                                                  "d_exp_avg_scale", "d_exp_avg_sq_scale")])
+
+
+class gear_adamw_desc(ctypes.Structure):
+    """Mirror of the C descriptor gear_adamw_desc."""
+    _fields_ = ([("state_bits", ctypes.c_int32)]
+                + [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")]
+                + [("d_lr", ctypes.c_void_p), ("d_factor", ctypes.c_void_p)])
+
+
 class GearError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__("%s (code %d)" % (msg, code))
@@ -114,7 +147,9 @@ def native():
                         (L.gear_select, L.gear_collect, L.gear_select_collect, L.gear_update_priorities,
                          L.gear_select_shard, L.gear_is_weights, L.gear_topk_merge, L.gear_recurrence_sizes,
                          L.gear_recurrence, L.gear_recurrence_backward, L.gear_advantages_sizes, L.gear_advantages,
-                         L.gear_policy_sizes, L.gear_policy_loss, L.gear_action_logp)])
+                         L.gear_policy_sizes, L.gear_policy_loss, L.gear_action_logp, L.gear_layer_norm_sizes,
+                         L.gear_layer_norm, L.gear_layer_norm_backward, L.gear_token_loss_sizes, L.gear_token_loss,
+                         L.gear_token_loss_backward, L.gear_step_sizes, L.gear_grad_norm, L.gear_adamw)])
         _native = _binding
     return _native
 
@@ -172,6 +207,17 @@ def lib():
         L.gear_policy_sizes.argtypes = [pol, pi64]
         L.gear_policy_loss.argtypes = [pol, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
         L.gear_action_logp.argtypes = [pol, vp, vp, vp, vp]
+        norm, tok, ten = (ctypes.POINTER(t) for t in (gear_norm_desc, gear_token_desc, gear_step_tensor))
+        f32 = ctypes.c_float
+        L.gear_layer_norm_sizes.argtypes = [norm, pi64]
+        L.gear_layer_norm.argtypes = [norm, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.gear_layer_norm_backward.argtypes = [norm, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.gear_token_loss_sizes.argtypes = [tok, pi64, pi64]
+        L.gear_token_loss.argtypes = [tok, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.gear_token_loss_backward.argtypes = [tok, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.gear_step_sizes.argtypes = [pi64, pi64]
+        L.gear_grad_norm.argtypes = [ten, i64, f32, f32, vp, vp, vp, i64, vp]
+        L.gear_adamw.argtypes = [ctypes.POINTER(gear_adamw_desc), ten, i64, vp, vp, i64, vp]
         for name in ["gear_table_create", "gear_table_destroy", "gear_insert", "gear_select", "gear_collect",
                      "gear_select_collect",
                      "gear_update_priorities", "gear_table_sync", "gear_table_info", "gear_table_column",
@@ -181,7 +227,9 @@ def lib():
                      "gear_select_prioritized_noalloc", "gear_table_create_columns", "gear_table_column_info",
                      "gear_table_find_column", "gear_recurrence_sizes", "gear_recurrence",
                      "gear_recurrence_backward", "gear_advantages_sizes", "gear_advantages", "gear_policy_sizes",
-                     "gear_policy_loss", "gear_action_logp"]:
+                     "gear_policy_loss", "gear_action_logp", "gear_layer_norm_sizes", "gear_layer_norm",
+                     "gear_layer_norm_backward", "gear_token_loss_sizes", "gear_token_loss",
+                     "gear_token_loss_backward", "gear_step_sizes", "gear_grad_norm", "gear_adamw"]:
             getattr(L, name).restype = ctypes.c_int
         L.gear_last_error.argtypes = []
         L.gear_last_error.restype = ctypes.c_char_p
@@ -444,6 +492,80 @@ def action_logp(logits, action, *, mask=None, stream=None):
     """Log-probabilities of the actions taken and entropies, float32 (gear_action_logp);
     arguments as for policy_loss."""
     return _on_stream(native().action_logp, logits, stream, logits, action, mask)
+
+
+def layer_norm(x, weight=None, bias=None, *, eps=1e-5, residual=None, save=False, stream=None):
+    """Layer norm of rows, with the residual sum before it (gear_layer_norm).
+
+    x [..., D] (float32, bfloat16 or float16), its rows at one stride; weight,
+    bias [D], float32 or of x's dtype (None: ones, zeros; a bias needs a
+    weight); residual like x.  Returns (y, total, saved): y and total
+    contiguous, total = x + residual in x's dtype, which is what is normalised,
+    or None without a residual; saved float32 [rows, 2], what
+    layer_norm_backward needs, or None without `save`.  No gradient is recorded:
+    see ``learn.layer_norm``.
+    """
+    return _on_stream(native().layer_norm, x, stream, x, weight, bias, eps, residual, save)
+
+
+def layer_norm_backward(dy, x, saved, weight=None, *, dtotal=None, stream=None):
+    """Gradients (dx, dweight, dbias) of a layer_norm call for the gradients dy of
+    its y and dtotal of its total: x is what was normalised (its total where there
+    was a residual, whose gradient dx is too), saved as that call returned it.
+    dweight and dbias are of weight's dtype, None without one."""
+    return _on_stream(native().layer_norm_backward, x, stream, dy, x, saved, weight, dtotal)
+
+
+def token_loss(hidden, head, target, *, weight=None, mask=None, denom=None, stream=None):
+    """Cross entropy of targets under a token head, without its logits (gear_token_loss).
+
+    hidden [..., D] and head [V, D] of one dtype (float32, bfloat16 or float16),
+    the rows of each at one stride; target uint8, int32 or int64 of hidden's
+    leading shape; weight (float32) and mask (uint8 or bool) of that shape or of
+    its first dimensions, each value then serving every row below it; denom: what
+    the weighted sum is divided by, the number of rows that take part if None.  A row
+    with mask 0 or a target outside [0, V) takes no part.  Returns float32
+    (loss, logp, lse): a scalar, and per row the target's log-probability and the
+    logarithm of the sum that token_loss_backward needs.  No gradient is recorded:
+    see ``learn.token_loss``.
+    """
+    return _on_stream(native().token_loss, hidden, stream, hidden, head, target, weight, mask, denom)
+
+
+def token_loss_backward(hidden, head, target, lse, *, weight=None, mask=None, denom=None, grad_scale=1.0, grad_loss=None,
+                        dhidden=True, dhead=True, stream=None):
+    """Gradients (dhidden, dhead) of grad_scale * grad_loss * the loss of a token_loss
+    call with the same arguments, lse as it returned it (gear_token_loss_backward);
+    grad_loss a float32 tensor of one value or None.  Either gradient may be left
+    out, and is None then."""
+    return _on_stream(native().token_loss_backward, hidden, stream, hidden, head, target, lse, weight, mask, denom,
+                      grad_scale, grad_loss, dhidden, dhead)
+
+
+def grad_norm(grads, *, max_norm=None, scale=1.0, stream=None):
+    """The 2-norm of a list of gradients together, and the factor that clips it
+    (gear_grad_norm): float32 scalars (norm, factor) on the device, norm that of
+    scale * grads (scale: 1 over a loss scale), factor = scale * min(1, max_norm / norm),
+    NaN where the norm is not finite.  ``adamw`` takes the factor."""
+    return _on_stream(native().grad_norm, grads[0] if len(grads) else None, stream, grads, scale, max_norm)
+
+
+def adamw(params, grads, exp_avg, exp_avg_sq, step, *, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, scales=None,
+          master=None, factor=None, stream=None):
+    """One AdamW step of lists of contiguous tensors, in place (gear_adamw).
+
+    params float32, bfloat16 or float16, grads of the same dtypes and shapes;
+    step int64, one value: the steps taken so far, counted up.  Averages are
+    float32 of the parameters' sizes, or with `scales`, a pair of lists, 8-bit: then
+    float8_e4m3fn, exp_avg times its scale (float32, one for GEAR_STEP_BLOCK values)
+    the first average, and (exp_avg_sq times its scale) squared the second.  master: a
+    list of float32 copies, None for parameters without one; it is then what steps, and the
+    parameter its rounded copy.  lr: a number, or a float32 tensor of one value, read
+    on the device.  factor: a float32 tensor of one value that multiplies the gradients;
+    where it or the lr tensor is not finite, nothing is changed.
+    """
+    _on_stream(native().adamw, step, stream, params, grads, exp_avg, exp_avg_sq, step, scales, master, lr, betas[0],
+               betas[1], eps, weight_decay, factor)
 
 
 class _DeviceBytes:

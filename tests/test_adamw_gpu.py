@@ -1,0 +1,336 @@
+"""AdamW over lists of tensors and the norm of their gradients against their formulas in 64 bits (GPU)."""
+import math
+
+import pytest
+import torch
+
+from paper_2310_05205_amd import gear, learn
+from tests.helpers import cuda, say
+from tests.network_reference import BLOCK, LEAST, STEP, TOP, U, U32, adamw, d64, decoded, near
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+KW = {"lr": 1e-2, "betas": (0.9, 0.99), "eps": 1e-8, "weight_decay": 0.1}
+SIZES = [1, 7, 8, 255, 256, 257, 2047, 2048, 2049, 8191, 8192, 8193, 20011, 0, 100000]
+
+
+def random(n, seed, scale=1.0):
+    return scale * torch.randn(n, generator=torch.Generator().manual_seed(seed))
+
+
+class Tensors:
+    """Parameters, gradients and averages of a run, on the GPU."""
+
+    def __init__(self, sizes, dtypes, bits, master, seed=1):
+        self.bits = bits
+        self.p = [random(n, seed + i).to(t).to(cuda()) for i, (n, t) in enumerate(zip(sizes, dtypes))]
+        self.g = [random(n, seed + 100 + i, 10.0 ** (-i % 4)).to(t).to(cuda()) for i, (n, t) in enumerate(zip(sizes, dtypes))]
+        self.master = [p.float() if master and p.dtype != torch.float32 else None for p in self.p]
+        self.step = torch.tensor([4], device=cuda())
+        m = [random(n, seed + 200 + i, 10.0 ** (-i % 4)) for i, n in enumerate(sizes)]
+        v = [random(n, seed + 300 + i, 10.0 ** (-i % 4)).square() for i, n in enumerate(sizes)]
+        if bits == 32:
+            self.m, self.v, self.scales = [x.to(cuda()) for x in m], [x.to(cuda()) for x in v], None
+        else:
+            pairs = [[encode(x) for x in m], [encode(x.sqrt()) for x in v]]
+            self.m, self.v = ([q.to(cuda()) for q, _ in pair] for pair in pairs)
+            self.scales = tuple([s.to(cuda()) for _, s in pair] for pair in pairs)
+
+    def run(self, factor=None, **kw):
+        gear.adamw(self.p, self.g, self.m, self.v, self.step, scales=self.scales,
+                   master=self.master if any(x is not None for x in self.master) else None, factor=factor, **dict(KW, **kw))
+
+    def averages(self, i):
+        if self.bits == 32:
+            return d64(self.m[i]), d64(self.v[i])
+        return decoded(self.m[i], self.scales[0][i]), decoded(self.v[i], self.scales[1][i]).square()
+
+    def copies(self):
+        return [t.clone() for part in (self.p, self.m, self.v, [x for x in self.master if x is not None], [self.step])
+                + (self.scales or ()) for t in part]
+
+
+def encode(x):
+    """e4m3 bytes and scales of a float32 vector."""
+    n = x.numel()
+    b = torch.nn.functional.pad(x, (0, -n % BLOCK)).view(-1, BLOCK)
+    s = b.abs().amax(1) / TOP if n else torch.zeros(0)
+    q = (b / torch.where(s > 0, s, 1.0)[:, None]).clamp(-TOP, TOP)
+    return q.to(torch.float8_e4m3fn).view(-1)[:n].contiguous(), s
+
+
+def expect(before, i, factor, kw):
+    p = d64(before.p[i] if before.master[i] is None else before.master[i])
+    m, v = before.averages(i)
+    g = d64(before.g[i]) * factor
+    t = int(before.step) + 1
+    return adamw(p, g, m, v, t, kw["lr"], kw["betas"], kw["eps"], kw["weight_decay"]) + (g,)
+
+
+def check(sizes, dtypes, bits, master, factor, what, **kw):
+    say("adamw " + what)
+    kw = dict(KW, **kw)
+    t, was = (Tensors(sizes, dtypes, bits, master) for _ in range(2))
+    f = None if factor is None else torch.tensor(factor, device=cuda())
+    t.run(f, **kw)
+    assert int(t.step) == int(was.step) + 1
+    for i, n in enumerate(sizes):
+        p, m, v, up, g = expect(was, i, 1.0 if factor is None else float(f), kw)
+        # A handful of 32-bit roundings of each term; the update's division and root a few more.
+        m0, v0 = was.averages(i)
+        m_off = 4 * U32 * (m0.abs() + g.abs()) + STEP[torch.float32]
+        v_off = 8 * U32 * v + STEP[torch.float32]
+        step = kw["lr"] / (1 - kw["betas"][0] ** int(t.step)) / (torch.sqrt(v / (1 - kw["betas"][1] ** int(t.step))) + kw["eps"])
+        off = 4 * U32 * p.abs() + 4 * U32 * (p + up).abs() + 16 * U32 * up + step * m_off
+        if t.master[i] is not None:
+            near(t.master[i], p, off, "master %d" % n)
+            assert torch.equal(t.p[i], t.master[i].to(t.p[i].dtype))
+        else:
+            near(t.p[i], p, off + U[t.p[i].dtype] * p.abs() * 1.01 + STEP[t.p[i].dtype], "param %d" % n)
+        if bits == 32:
+            near(t.m[i], m, m_off, "exp_avg %d" % n)
+            near(t.v[i], v, v_off, "exp_avg_sq %d" % n)
+        else:
+            for q, scale, x, x_off in ((t.m[i], t.scales[0][i], m, m_off), (t.v[i], t.scales[1][i], v.sqrt(), 8 * U32 * v.sqrt())):
+                tops = torch.nn.functional.pad(x.abs(), (0, -n % BLOCK)).view(-1, BLOCK).amax(1) if n else torch.zeros(0)
+                near(scale, tops.double() / TOP, 8 * U32 * tops / TOP + (m_off.max() if n and x is m else 0.0) / TOP, "scale")
+                s = scale.cpu().double().repeat_interleave(BLOCK)[:n]
+                # Half a step of 3 bits after the first, at least of the least value; what is not 0 may take a whole one.
+                near(decoded(q, scale), x, x.abs() * 2.0 ** -4 * 1.001 + s * LEAST + x_off, "values")
+                assert not (decoded(q, scale)[x != 0] == 0).any()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("master", [False, True])
+def test_sizes(bits, dtype, master):
+    check(SIZES, [dtype] * len(SIZES), bits, master, None, "%d bits %s master %s" % (bits, dtype, master))
+    check(SIZES, [dtype] * len(SIZES), bits, master, 0.37, "%d bits %s master %s, factor" % (bits, dtype, master))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_mixed_types_and_many_tensors(bits):
+    """More tensors than one launch takes, types in turn."""
+    sizes = [1 + 37 * k % 999 for k in range(400)]
+    check(sizes, [TYPES[k % 3] for k in range(400)], bits, True, 2.0, "400 tensors, %d bits" % bits)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_constants(bits):
+    for kw in ({"betas": (0.0, 0.0)}, {"lr": 0.0}, {"weight_decay": 0.0}, {"betas": (0.9, 0.999999)}, {"eps": 1.0}):
+        check([1000, 77], [torch.float32, torch.bfloat16], bits, True, None, str(kw), **kw)
+
+
+def test_tensors_that_begin_anywhere():
+    """Views at odd places of one buffer, neighbours of each other: what lies between stays."""
+    n, gap = 1001, 1
+    flat = {k: torch.zeros(8 * (n + gap), dtype=dt, device=cuda()) for k, dt in
+            (("p", torch.bfloat16), ("g", torch.bfloat16), ("m", torch.float32), ("v", torch.float32))}
+    part = {k: [f[1 + i * (n + gap):1 + i * (n + gap) + n] for i in range(7)] for k, f in flat.items()}
+    for k in ("p", "g"):
+        for i, x in enumerate(part[k]):
+            x.copy_(random(n, i + (50 if k == "g" else 0)))
+    say("adamw views")
+    apart = {k: [x.clone() for x in v] for k, v in part.items()}
+    step, step2 = torch.tensor([0], device=cuda()), torch.tensor([0], device=cuda())
+    gear.adamw(part["p"], part["g"], part["m"], part["v"], step, **KW)
+    gear.adamw(apart["p"], apart["g"], apart["m"], apart["v"], step2, **KW)
+    for k in part:
+        assert all(torch.equal(a, b) for a, b in zip(part[k], apart[k])), k
+        assert not flat[k][::n + gap].any()
+
+
+def test_many_steps_in_32_bits_follow_the_formula():
+    p = random(500, 1)
+    x, g = p.to(cuda()), torch.empty(500, device=cuda())
+    m, v, step = torch.zeros(500, device=cuda()), torch.zeros(500, device=cuda()), torch.zeros(1, dtype=torch.int64, device=cuda())
+    w, a, b = p.double(), torch.zeros(500, dtype=torch.float64), torch.zeros(500, dtype=torch.float64)
+    say("adamw 50 steps")
+    for t in range(1, 51):
+        grad = random(500, 1000 + t)
+        g.copy_(grad)
+        gear.adamw([x], [g], [m], [v], step, **KW)
+        w, a, b, _ = adamw(w, grad.double(), a, b, t, *(KW[k] for k in ("lr", "betas", "eps", "weight_decay")))
+    # Each step adds a few roundings of a parameter of up to 4 and an update of up to 0.1.
+    near(x, w, 50 * 32 * U32 * 4.0, "after 50 steps")
+
+
+def test_blocks_of_zeros_and_tiny_values():
+    """8-bit blocks of zeros stay zeros, without a division by their scale; small roots do not vanish beside large ones."""
+    p, g = torch.ones(1024, device=cuda()), torch.zeros(1024, device=cuda())
+    g[256] = 1e3
+    g[257:512] = 1e-4
+    g[512:768] = 1e-18
+    m, v = (torch.zeros(1024, dtype=torch.uint8, device=cuda()).view(torch.float8_e4m3fn) for _ in range(2))
+    scales = ([torch.zeros(4, device=cuda())], [torch.zeros(4, device=cuda())])
+    step = torch.zeros(1, dtype=torch.int64, device=cuda())
+    say("adamw tiny values in 8 bits")
+    for k in range(2):
+        gear.adamw([p], [g], [m], [v], step, scales=scales, **dict(KW, weight_decay=0.0, eps=1e-30))
+        x = p.cpu().double()
+        # An update is at most lr m / sqrt(v) with m and v of one gradient: lr, times the first steps' corrections.
+        assert torch.equal(x[:256], torch.ones(256, dtype=torch.float64)) and torch.equal(x[768:], torch.ones(256, dtype=torch.float64))
+        assert (1 - x[256:768] <= (k + 1) * KW["lr"] * 1.1).all() and (1 - x[257:512] >= 0).all()
+    assert (v[256:768].float() > 0).all()
+    assert not v[:256].float().any() and float(scales[1][0][0]) == 0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_factor_that_is_not_finite_changes_nothing(bits, bad):
+    t = Tensors([1000, 5], [torch.bfloat16, torch.float32], bits, True)
+    was = t.copies()
+    say("adamw factor %s" % bad)
+    t.run(torch.tensor(bad, device=cuda()))
+    t.run(lr=torch.tensor(bad, device=cuda()))
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(was, t.copies()))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_rate_on_the_device(bits):
+    a, b = (Tensors([3000], [torch.bfloat16], bits, True) for _ in range(2))
+    a.run(lr=0.25)  # exact in 32 bits
+    b.run(lr=torch.tensor(0.25, device=cuda()))
+    assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a.copies(), b.copies()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_norm(dtype):
+    g = [random(n, 7 + i, 10.0 ** (-i % 4)).to(dtype).to(cuda()) for i, n in enumerate(SIZES)]
+    want = math.sqrt(sum(float(d64(x).square().sum()) for x in g))
+    say("grad_norm %s" % dtype)
+    for limit, scale in ((None, 1.0), (want / 3, 1.0), (want * 3, 1.0), (1.0, 1 / 1024)):
+        norm, factor = gear.grad_norm(g, max_norm=limit, scale=scale)
+        f = scale * min(1.0, math.inf if limit is None else limit / (want * scale))
+        # Squares are added in 64 bits: one rounding, and that of the limit.
+        assert abs(float(norm) - want * scale) <= 2 * U32 * want * scale
+        assert abs(float(factor) - f) <= 4 * U32 * f
+
+
+def test_norm_of_everything():
+    """Types together, more tensors than a launch takes, values whose squares leave fp32, none, and NaN."""
+    g = [random(1 + k % 50, k).to(TYPES[k % 3]).to(cuda()) for k in range(700)]
+    want = math.sqrt(sum(float(d64(x).square().sum()) for x in g))
+    say("grad_norm of 700")
+    assert abs(float(gear.grad_norm(g)[0]) - want) <= 2 * U32 * want
+    for x, y in ((1e30, 2e30), (1e-30, 2e-30)):
+        norm, factor = gear.grad_norm([torch.full((4,), x, device=cuda())], max_norm=1.0)
+        assert abs(float(norm) - y) <= 4 * U32 * y and abs(float(factor) - min(1.0, 1 / y)) <= 4 * U32 * min(1.0, 1 / y)
+    norm, factor = gear.grad_norm([torch.empty(0, device=cuda())], max_norm=1.0)
+    assert float(norm) == 0 and float(factor) == 1
+    for bad in (float("nan"), float("inf")):
+        g[3][0] = bad
+        norm, factor = gear.grad_norm(g, max_norm=1.0)
+        assert not math.isfinite(float(norm)) and math.isnan(float(factor))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_captured_steps_replay(bits):
+    """Every replay is a step: the count lies on the device."""
+    a, b = (Tensors([5000, 300], [torch.bfloat16, torch.float32], bits, True) for _ in range(2))
+
+    def run(t):
+        norm, factor = gear.grad_norm(t.g, max_norm=1.0)
+        t.run(factor)
+        return norm
+    run(a), run(b)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(a)
+    for seed in range(4):
+        for t in (a, b):
+            for k, g in enumerate(t.g):
+                g.copy_(random(g.numel(), seed * 10 + k))
+        run(b)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a.copies(), b.copies())), seed
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_optimizer(bits):
+    """learn.AdamW: clips, leaves out what has no gradient, goes on from its state, bumps versions."""
+    def model():
+        g = torch.Generator().manual_seed(1)
+        return [torch.nn.Parameter(torch.randn(s, generator=g).to(t).to(cuda()))
+                for s, t in (((40, 30), torch.float32), ((30,), torch.bfloat16), ((7, 3), torch.float32))]
+    a, b = model(), model()
+    say("learn.AdamW %d" % bits)
+    one = learn.AdamW(a, lr=1e-2, bits=bits, max_norm=1.0)
+    for step in range(6):
+        two = learn.AdamW(b, lr=1e-2, bits=bits, max_norm=1.0)
+        if step:
+            two.load_state_dict(state)
+        for ps in (a, b):
+            for k, p in enumerate(ps[:2]):
+                p.grad = random(p.numel(), step * 10 + k).view(p.shape).to(p.dtype).to(cuda())
+        version = a[0]._version
+        n1, n2 = one.step(), two.step()
+        assert torch.equal(n1, n2) and a[0]._version > version
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+        state = two.state_dict()
+        one.zero_grad()
+        assert a[0].grad is None
+    fresh = model()
+    assert torch.equal(a[2], fresh[2]) and not torch.equal(a[0], fresh[0]) and int(one.count) == 6
+    other = learn.AdamW(a, bits=40 - bits)
+    with pytest.raises(ValueError):
+        other.load_state_dict(state)
+    with pytest.raises(ValueError):
+        learn.AdamW(a[:2], bits=bits).load_state_dict(state)
+    # Not finite: left out.
+    a[0].grad = torch.full_like(a[0], float("inf"))
+    was = a[0].detach().clone()
+    one.step(scale=0.5)
+    assert torch.equal(a[0], was) and int(one.count) == 6
+
+
+def test_optimizer_steps_as_torch_does():
+    g = torch.Generator().manual_seed(1)
+    w = torch.randn(50, 20, generator=g)
+    a, b = (torch.nn.Parameter(w.clone().to(cuda())) for _ in range(2))
+    mine, theirs = learn.AdamW([a], lr=1e-2, weight_decay=0.1), torch.optim.AdamW([b], lr=1e-2, weight_decay=0.1)
+    for _ in range(10):
+        grad = torch.randn(50, 20, generator=g).to(cuda())
+        a.grad, b.grad = grad.clone(), grad.clone()
+        mine.step(), theirs.step()
+    # Ten steps of a few 32-bit roundings each on both sides.
+    assert (a - b).abs().max().item() <= 10 * 2 * 32 * U32 * float(w.abs().max())
+
+
+def test_refusals():
+    p, g, m, v = (torch.ones(300, device=cuda()) for _ in range(4))
+    step = torch.zeros(1, dtype=torch.int64, device=cuda())
+    q = torch.zeros(300, dtype=torch.uint8, device=cuda()).view(torch.float8_e4m3fn)
+    q2 = q.clone()
+    s, s2 = torch.zeros(2, device=cuda()), torch.zeros(2, device=cuda())
+    bad = [(([p], [g], [m], []), {}), (([p], [g.half()], [m], [v]), {}), (([p], [g[:299]], [m], [v]), {}),
+           (([p], [g], [m[:299]], [v]), {}), (([p], [g], [m.half()], [v]), {}), (([p], [g], [m], [m]), {}),
+           (([p], [g], [p], [v]), {}), (([p], [p], [m], [v]), {}), (([p, p], [g, g], [m, v], [torch.ones_like(m), torch.ones_like(m)]), {}),
+           (([p], [g], [m], [v]), {"master": [m.clone()]}), (([p], [g], [q], [q2]), {}), (([p], [g], [q], [q2]), {"scales": [s, s2]}),
+           (([p], [g], [q], [q2]), {"scales": ([s], [s])}), (([p], [g], [q], [q2]), {"scales": ([s[:1]], [s2])}),
+           (([p.cpu()], [g], [m], [v]), {}), (([p], [g.expand(2, 300)[0:1].t()], [m], [v]), {}), ((p, [g], [m], [v]), {}),
+           (([p], [g], [m], [v]), {"factor": torch.ones(2, device=cuda())}), (([p], [g], [m], [v]), {"factor": p[:1]}),
+           (([p], [g], [m], [v]), {"lr": torch.ones(1)}), (([None], [g], [m], [v]), {})]
+    for args, kw in bad:
+        with pytest.raises((ValueError, TypeError)):
+            gear.adamw(*args, step, **dict(KW, **kw))
+    for kw in ({"lr": -1.0}, {"betas": (1.0, 0.9)}, {"betas": (0.9, -0.1)}, {"eps": 0.0}, {"eps": 1e-60}, {"weight_decay": float("inf")}):
+        with pytest.raises(gear.GearError):
+            gear.adamw([p], [g], [m], [v], step, **dict(KW, **kw))
+    for kw in ({"step": step.int()}, {"step": torch.zeros(2, dtype=torch.int64, device=cuda())}):
+        with pytest.raises(ValueError):
+            gear.adamw([p], [g], [m], [v], kw["step"], **KW)
+    assert int(step) == 0 and torch.equal(p, torch.ones_like(p))
+    with pytest.raises(ValueError):
+        gear.grad_norm([])
+    for kw in ({"max_norm": 0.0}, {"max_norm": float("nan")}, {"scale": 0.0}, {"scale": float("inf")}):
+        with pytest.raises(gear.GearError):
+            gear.grad_norm([g], **kw)
+    with pytest.raises(ValueError):
+        gear.grad_norm([g, g.view(30, 10).t()])
+    for build in (lambda: learn.AdamW([]), lambda: learn.AdamW([p], bits=16), lambda: learn.AdamW([p.view(30, 10).t()])):
+        with pytest.raises(ValueError):
+            build()

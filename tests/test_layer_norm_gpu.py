@@ -1,0 +1,217 @@
+"""Layer norm with the residual sum before it against its formulas in 64 bits (GPU)."""
+import pytest
+import torch
+
+from paper_2310_05205_amd import gear, learn
+from tests.helpers import cuda, say
+from tests.network_reference import Norm, near
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def rows(n, D, dtype, seed, offset=0.5):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(n, D, generator=g) * (0.5 + torch.rand(n, 1, generator=g)) + offset * torch.randn(n, 1, generator=g)
+    return x.to(dtype)
+
+
+def check(x, weight, bias, eps, residual, dy, dtotal, what):
+    """x and the others as GPU tensors of any layout."""
+    say("layer_norm " + what)
+    y, total, saved = gear.layer_norm(x, weight, bias, eps=eps, residual=residual, save=True)
+    flat = lambda t: None if t is None else t.detach().cpu().reshape(-1, x.shape[-1])  # noqa: E731
+    on_cpu = lambda t: None if t is None else t.detach().cpu()  # noqa: E731
+    want = Norm(flat(x), on_cpu(weight), on_cpu(bias), eps, flat(residual))
+    near(y.reshape(want.y.shape), want.y, want.y_bound, "y")
+    if residual is None:
+        assert total is None
+    else:
+        assert torch.equal(flat(total).double(), want.t)
+    alone = gear.layer_norm(x, weight, bias, eps=eps, residual=residual)
+    assert torch.equal(alone[0], y) and alone[2] is None
+    dx, dw, db = gear.layer_norm_backward(dy, x if total is None else total, saved, weight, dtotal=dtotal)
+    want.backward(flat(dy), flat(dtotal), x.dtype if weight is None else weight.dtype)
+    near(dx.reshape(want.dx.shape), want.dx, want.dx_bound, "dx")
+    if weight is None:
+        assert dw is None and db is None
+    else:
+        assert dw.dtype == db.dtype == weight.dtype
+        near(dw, want.dw, want.dw_bound, "dweight")
+        near(db, want.db, want.db_bound, "dbias")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,D", [(1, 1), (5, 2), (3, 3), (7, 8), (1, 31), (70, 32), (33, 33), (64, 64), (65, 65),
+                                 (9, 127), (300, 128), (31, 200), (1000, 256), (5, 257), (19, 511), (40, 512),
+                                 (3, 513), (77, 1003), (2, 1024), (9, 2047), (33, 2048), (4, 2049), (6, 4096),
+                                 (3, 5001), (2, 8192), (3, 8193), (2, 12289), (3, 16384), (2, 20000), (2, 32768),
+                                 (1, 33001), (2, 70000)])
+def test_sizes(dtype, n, D):
+    x, res, dy, dt = (rows(n, D, dtype, s).to(cuda()) for s in (1, 2, 3, 4))
+    w, b = (1 + 0.2 * rows(2, D, torch.float32, 5)).to(cuda())
+    check(x, w, b, 1e-5, res, dy, dt, "%d x %d %s, residual" % (n, D, dtype))
+    check(x, w.to(dtype), b.to(dtype), 1e-5, None, dy, None, "%d x %d %s" % (n, D, dtype))
+    check(x, None, None, 1e-3, None, dy, None, "%d x %d %s, no parameters" % (n, D, dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_rows(dtype):
+    """More rows than workgroups, so that each goes through several."""
+    for n, D in ((70001, 24), (40003, 130), (9001, 1003)):
+        x, dy = rows(n, D, dtype, 1).to(cuda()), rows(n, D, dtype, 2).to(cuda())
+        w, b = (1 + 0.2 * rows(2, D, torch.float32, 5)).to(cuda())
+        check(x, w, b, 1e-5, dy, dy, x, "%d x %d %s" % (n, D, dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [24, 65, 1003, 9001])
+def test_layouts(dtype, D):
+    """Halves of a projection, rows that begin anywhere, one row for all, leading dimensions."""
+    wide = rows(6, 2 * D + 3, dtype, 1).to(cuda())
+    w, b = (1 + 0.2 * rows(2, D, torch.float32, 5)).to(cuda())
+    x, dy = wide[:, 1:D + 1], wide[:, D + 2:2 * D + 2]
+    check(x, w, b, 1e-5, dy, dy, x, "slices of %d %s" % (D, dtype))
+    one = wide[:1, :D].expand(6, D)
+    check(x, w, b, 1e-5, one, one, one, "one row for all, %d %s" % (D, dtype))
+    lead = wide[:, :D].reshape(2, 3, D)
+    check(lead, w, b, 1e-5, lead, lead, lead, "two leading dimensions, %d %s" % (D, dtype))
+    check(wide[0, :D], w, b, 1e-5, None, wide[1, :D], None, "one row of one dimension, %d %s" % (D, dtype))
+
+
+def test_values_out_of_the_ordinary():
+    """Constant rows, offsets far beyond the deviation, large and tiny values, eps of 0."""
+    for D in (8, 100, 1003, 9000):
+        x = rows(6, D, torch.float32, 1)
+        x[1] = 3.0
+        x[2] = 1e4 + x[2]
+        x[3] *= 1e15
+        x[4] *= 1e-15
+        x[5] = 0.0
+        w, b = (1 + 0.2 * rows(2, D, torch.float32, 5)).to(cuda())
+        dy = rows(6, D, torch.float32, 2).to(cuda())
+        check(x.to(cuda()), w, b, 1e-5, None, dy, None, "odd values, %d" % D)
+        check(x[[0, 2]].to(cuda()), w, b, 0.0, None, dy[:2], None, "eps of 0, %d" % D)
+
+
+@pytest.mark.parametrize("D", [24, 1003, 20000])
+def test_nan_and_infinity_stay_in_their_row(D):
+    x, dy = rows(5, D, torch.float32, 1), rows(5, D, torch.float32, 2)
+    x[1, D // 2], x[3, D - 1] = float("nan"), float("inf")
+    w, b = (1 + 0.2 * rows(2, D, torch.float32, 5)).to(cuda())
+    say("layer_norm NaN rows, %d" % D)
+    y, _, saved = gear.layer_norm(x.to(cuda()), w, b, save=True)
+    dx, dw, db = gear.layer_norm_backward(dy.to(cuda()), x.to(cuda()), saved, w)
+    assert torch.isnan(y[[1, 3]]).all() and torch.isnan(dx[[1, 3]]).all() and torch.isnan(dw).all()
+    keep = [0, 2, 4]
+    y2, _, saved2 = gear.layer_norm(x[keep].to(cuda()), w, b, save=True)
+    assert torch.equal(y[keep], y2)
+    assert torch.equal(dx[keep], gear.layer_norm_backward(dy[keep].to(cuda()), x[keep].to(cuda()), saved2, w)[0])
+    assert torch.isfinite(db).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_no_rows(dtype):
+    x = torch.empty(0, 7, dtype=dtype, device=cuda())
+    w = torch.ones(7, device=cuda())
+    y, total, saved = gear.layer_norm(x, w, w, residual=x, save=True)
+    assert y.shape == total.shape == (0, 7) and saved.shape == (0, 2)
+    dx, dw, db = gear.layer_norm_backward(x, x, saved, w)
+    assert dx.shape == (0, 7) and not dw.any() and not db.any()
+
+
+def test_results_repeat():
+    for D in (24, 512, 1003, 20000):
+        x, dy = rows(999, D, torch.bfloat16, 1).to(cuda()), rows(999, D, torch.bfloat16, 2).to(cuda())
+        w = torch.ones(D, device=cuda())
+        y, _, saved = gear.layer_norm(x, w, save=True)
+        first = gear.layer_norm_backward(dy, x, saved, w)
+        for _ in range(3):
+            assert all(torch.equal(a, b) for a, b in zip(first, gear.layer_norm_backward(dy, x, saved, w)))
+
+
+def test_gradients_by_differences():
+    """The derivative along random directions against differences of the 64-bit definition, and autograd's paths."""
+    g = torch.Generator().manual_seed(3)
+    n, D = 6, 37
+    x, r, w, b, cy, ct = (torch.randn(s, generator=g, dtype=torch.float64)
+                          for s in ((n, D), (n, D), (D,), (D,), (n, D), (n, D)))
+
+    def f(x, r, w, b):
+        t = x + r
+        c = t - t.mean(1, keepdim=True)
+        y = c / torch.sqrt(c.square().mean(1, keepdim=True) + 1e-5) * w + b
+        return (y * cy).sum() + (t * ct).sum()
+    ins = [t.float().to(cuda()).requires_grad_() for t in (x, r, w, b)]
+    say("learn.layer_norm")
+    y, total = learn.layer_norm(ins[0], ins[2], ins[3], residual=ins[1])
+    ((y * cy.float().to(cuda())).sum() + (total * ct.float().to(cuda())).sum()).backward()
+    base = [t.detach().cpu().double() for t in ins]
+    for k in range(4):
+        way = torch.randn(base[k].shape, generator=g, dtype=torch.float64)
+        h = 1e-5
+        up, down = list(base), list(base)
+        up[k], down[k] = base[k] + h * way, base[k] - h * way
+        slope = (f(*up) - f(*down)) / (2 * h)
+        got = (ins[k].grad.cpu().double() * way).sum()
+        # Differences of a 64-bit function: h^2 and 2^-52 / h of its size; gradients in 32 bits.
+        size = float((ins[k].grad.cpu().double().abs() * way.abs()).sum())
+        assert abs(slope - got) < 1e-4 * abs(slope) + 1e-5 * size
+    # The sum alone, and y alone through a broadcast gradient.
+    for pick, want in ((1, None), (0, None)):
+        for t in ins:
+            t.grad = None
+        learn.layer_norm(ins[0], ins[2], ins[3], residual=ins[1])[pick].sum().backward()
+        assert torch.equal(ins[0].grad, ins[1].grad)
+        if pick == 1:
+            assert torch.equal(ins[0].grad, torch.ones_like(ins[0])) and ins[2].grad is None
+
+
+def test_captured_calls_replay():
+    x, dy = rows(300, 200, torch.bfloat16, 1).to(cuda()), rows(300, 200, torch.bfloat16, 2).to(cuda())
+    w, b = (1 + 0.2 * rows(2, 200, torch.float32, 5)).to(cuda())
+
+    def run():
+        y, total, saved = gear.layer_norm(x, w, b, residual=dy, save=True)
+        return (y, total) + gear.layer_norm_backward(dy, total, saved, w)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for seed in (11, 12, 13):
+        x.copy_(rows(300, 200, torch.bfloat16, seed))
+        want = run()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(got, want)), seed
+
+
+def test_another_stream():
+    s = torch.cuda.Stream()
+    x = rows(500, 700, torch.float32, 1).to(cuda())
+    w = torch.ones(700, device=cuda())
+    want = gear.layer_norm(x, w)[0]
+    torch.cuda.synchronize()
+    got = gear.layer_norm(x, w, stream=s)[0]
+    s.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_refusals():
+    x = torch.randn(4, 6, device=cuda())
+    w = torch.ones(6, device=cuda())
+    bad = [((x, w.half()), {}), ((x, w[:5]), {}), ((x.t(), None), {}), ((x, None, w), {}), ((x, w, w.cpu()), {}),
+           ((x.double(), None), {}), ((x, w), {"residual": x[:3]}), ((x, w), {"residual": x.half()}),
+           ((x.reshape(2, 2, 6).transpose(0, 1), w), {}), ((x[:, :0], None), {}), ((x.cpu(), None), {})]
+    for args, kw in bad:
+        with pytest.raises((ValueError, TypeError)):
+            gear.layer_norm(*args, **kw)
+    with pytest.raises(gear.GearError):
+        gear.layer_norm(x, w, eps=-1.0)
+    y, _, saved = gear.layer_norm(x, w, save=True)
+    for args, kw in [((y[:3], x, saved, w), {}), ((y, x, saved[:3], w), {}), ((y, x, None, w), {}),
+                     ((y.half(), x, saved, w), {}), ((None, x, saved, w), {}), ((y, x, saved, w), {"dtotal": y.half()})]:
+        with pytest.raises((ValueError, TypeError)):
+            gear.layer_norm_backward(*args, **kw)
