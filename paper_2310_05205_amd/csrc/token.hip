@@ -26,10 +26,11 @@ namespace gear {
 namespace {
 
 constexpr int kStep = 64;                 // k of one step: 128 bytes a row
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;             // of the kernels that are not products
 constexpr int64_t kPieceValues = 1 << 27;  // values of e formed at a time, at most
 constexpr int64_t kPieceTokens = 1 << 16;
 constexpr int kParts = 512;               // workgroups that look at the rows
+constexpr int64_t kSoloRows = 8192;       // one looks at so many
 
 typedef __bf16 B8 __attribute__((ext_vector_type(8)));
 typedef _Float16 H8 __attribute__((ext_vector_type(8)));
@@ -94,45 +95,51 @@ struct Args {
     double* sums;      // [kParts]
     int64_t* counts;   // [kParts]
     float* tops;       // [kParts]
-    float* part_max;   // [tiles of tokens][n]
-    float* part_sum;
+    float2* part;      // [n][tiles]: maximum and sum of a tile of tokens
     float* at_target;  // [n]: the target's logit
     int64_t n, D, V, mask_group, weight_group;
-    int32_t target_dtype, tiles, parts;
+    int32_t target_dtype, tiles, row_parts, lse_parts;
     float denom, grad_scale;
 };
 
 // --- rows ---------------------------------------------------------------------
 
 template <typename T>
-__device__ __forceinline__ T wave_add(T v) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+__device__ __forceinline__ T lanes_add(T v, int lanes) {
+    for (int off = lanes / 2; off > 0; off >>= 1) v += __shfl_xor(v, off);
     return v;
 }
-// Targets and weights of the rows, how many take part, and their largest weight.
-__global__ __launch_bounds__(kThreads) void rows_kernel(const Args a) {
+// The larger magnitude; a NaN or an infinity stays, as it makes every gradient of the head one.
+__device__ __forceinline__ float larger(float top, float w) { return fabsf(w) <= top ? top : fabsf(w); }
+
+__device__ __forceinline__ Row row_of(const Args& a, int64_t r) {
+    const int64_t y = a.target_dtype == GEAR_DTYPE_I32   ? (int64_t)static_cast<const int32_t*>(a.target)[r]
+                      : a.target_dtype == GEAR_DTYPE_I64 ? static_cast<const int64_t*>(a.target)[r]
+                                                         : (int64_t)static_cast<const uint8_t*>(a.target)[r];
+    const bool on = y >= 0 && y < a.V && (a.mask == nullptr || a.mask[r / a.mask_group] != 0);
+    const float w = !on ? 0.0f : a.weight ? a.weight[r / a.weight_group] : 1.0f;
+    return Row{on ? (int32_t)y : -1, w};
+}
+__device__ __forceinline__ Totals totals_of(const Args& a, int64_t count, float top) {
+    return Totals{1.0f / (a.denom > 0.0f ? a.denom : count > 0 ? (float)count : 1.0f), top};
+}
+
+// Targets and weights of the rows, how many take part, and their largest weight;
+// workgroup `block` of a.row_parts.
+__device__ __forceinline__ void look_at_rows(const Args& a, int block) {
     __shared__ int64_t s_count[kThreads / 64];
     __shared__ float s_top[kThreads / 64];
     int64_t count = 0;
     float top = 0.0f;
-    for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < a.n; r += (int64_t)gridDim.x * kThreads) {
-        const int64_t y = a.target_dtype == GEAR_DTYPE_I32   ? (int64_t)static_cast<const int32_t*>(a.target)[r]
-                          : a.target_dtype == GEAR_DTYPE_I64 ? static_cast<const int64_t*>(a.target)[r]
-                                                             : (int64_t)static_cast<const uint8_t*>(a.target)[r];
-        const bool on = y >= 0 && y < a.V && (a.mask == nullptr || a.mask[r / a.mask_group] != 0);
-        const float w = !on ? 0.0f : a.weight ? a.weight[r / a.weight_group] : 1.0f;
-        a.rows[r] = Row{on ? (int32_t)y : -1, w};
-        count += on ? 1 : 0;
-        // A NaN or an infinity has to stay: it makes every gradient of the head one.
-        if (on && !(fabsf(w) <= top)) top = fabsf(w);
+#pragma unroll 4
+    for (int64_t r = (int64_t)block * kThreads + threadIdx.x; r < a.n; r += (int64_t)a.row_parts * kThreads) {
+        const Row row = row_of(a, r);
+        a.rows[r] = row;
+        count += row.target >= 0 ? 1 : 0;
+        if (row.target >= 0) top = larger(top, row.weight);
     }
-    count = wave_add(count);
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        const float o = __shfl_xor(top, off);
-        if (!(o <= top)) top = o;
-    }
+    count = lanes_add(count, 64);
+    for (int off = 32; off > 0; off >>= 1) top = larger(top, __shfl_xor(top, off));
     if ((threadIdx.x & 63) == 0) {
         s_count[threadIdx.x >> 6] = count;
         s_top[threadIdx.x >> 6] = top;
@@ -141,62 +148,72 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const Args a) {
     if (threadIdx.x == 0) {
         for (int k = 1; k < kThreads / 64; k++) {
             count += s_count[k];
-            if (!(s_top[k] <= top)) top = s_top[k];
+            top = larger(top, s_top[k]);
         }
-        a.counts[blockIdx.x] = count;
-        a.tops[blockIdx.x] = top;
+        if (a.row_parts == 1) {
+            *a.totals = totals_of(a, count, top);
+        } else {
+            a.counts[block] = count;
+            a.tops[block] = top;
+        }
     }
 }
 __global__ __launch_bounds__(64) void totals_kernel(const Args a) {
     int64_t count = 0;
     float top = 0.0f;
-    for (int k = threadIdx.x; k < a.parts; k += 64) {
+    for (int k = threadIdx.x; k < a.row_parts; k += 64) {
         count += a.counts[k];
-        if (!(a.tops[k] <= top)) top = a.tops[k];
+        top = larger(top, a.tops[k]);
     }
-    count = wave_add(count);
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        const float o = __shfl_xor(top, off);
-        if (!(o <= top)) top = o;
-    }
-    if (threadIdx.x == 0) {
-        a.totals->share = 1.0f / (a.denom > 0.0f ? a.denom : count > 0 ? (float)count : 1.0f);
-        a.totals->weight = top;
-    }
+    count = lanes_add(count, 64);
+    for (int off = 32; off > 0; off >>= 1) top = larger(top, __shfl_xor(top, off));
+    if (threadIdx.x == 0) *a.totals = totals_of(a, count, top);
 }
 
-// Joins the tiles' maxima and sums: lse, logp, and a sum of the losses per workgroup.
+// Joins the tiles' maxima and sums, LANES lanes a row: lse, logp, and a sum of the
+// losses per workgroup; of all where there is but one.
+template <int LANES>
 __global__ __launch_bounds__(kThreads) void lse_kernel(const Args a) {
     __shared__ double s[kThreads / 64];
+    const int lane = threadIdx.x % LANES;
     double sum = 0.0;
-    for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < a.n; r += (int64_t)gridDim.x * kThreads) {
-        float m = -INFINITY;
-        for (int t = 0; t < a.tiles; t++) m = fmaxf(m, a.part_max[t * a.n + r]);
-        const float from = m == -INFINITY ? 0.0f : m;
-        float S = 0.0f;
-        for (int t = 0; t < a.tiles; t++) S += a.part_sum[t * a.n + r] * fast_exp(a.part_max[t * a.n + r] - from);
-        const float lse = from + __builtin_amdgcn_logf(S) * kLn2;
+    for (int64_t r = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / LANES; r < a.n;
+         r += (int64_t)gridDim.x * kThreads / LANES) {
+        float m = -INFINITY, S = 0.0f;
+        for (int t = lane; t < a.tiles; t += LANES) {
+            const float2 p = a.part[r * a.tiles + t];
+            const float top = fmaxf(m, p.x), from = top == -INFINITY ? 0.0f : top;
+            S = S * fast_exp(m - from) + p.y * fast_exp(p.x - from);
+            m = top;
+        }
+        float top = m;
+#pragma unroll
+        for (int off = LANES / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+        const float from = top == -INFINITY ? 0.0f : top;
+        S = lanes_add(S * fast_exp(m - from), LANES);
+        if (lane != 0) continue;
+        const float log_S = __builtin_amdgcn_logf(S) * kLn2;
         const Row row = a.rows[r];
         const bool on = row.target >= 0;
-        const float lp = on ? (a.at_target[r] - from) - __builtin_amdgcn_logf(S) * kLn2 : 0.0f;
+        const float lp = on ? (a.at_target[r] - from) - log_S : 0.0f;
         if (a.logp) a.logp[r] = lp;
-        if (a.lse) a.lse[r] = on ? lse : 0.0f;
+        if (a.lse) a.lse[r] = on ? from + log_S : 0.0f;
         // A weight of 0 leaves 0 of an infinite term.
         if (on && !(row.weight == 0.0f && lp == -INFINITY)) sum -= (double)row.weight * (double)lp;
     }
-    sum = wave_add(sum);
+    sum = lanes_add(sum, 64);
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int k = 1; k < kThreads / 64; k++) sum += s[k];
-        a.sums[blockIdx.x] = sum;
+        if (gridDim.x == 1) *a.loss = (float)(sum * (double)a.totals->share);
+        else a.sums[blockIdx.x] = sum;
     }
 }
 __global__ __launch_bounds__(64) void loss_kernel(const Args a) {
     double sum = 0.0;
-    for (int k = threadIdx.x; k < a.parts; k += 64) sum += a.sums[k];
-    sum = wave_add(sum);
+    for (int k = threadIdx.x; k < a.lse_parts; k += 64) sum += a.sums[k];
+    sum = lanes_add(sum, 64);
     if (threadIdx.x == 0) *a.loss = (float)(sum * (double)a.totals->share);
 }
 
@@ -217,59 +234,88 @@ __device__ __forceinline__ void cut(float v, T (&part)[N]) {
         v = fabsf(v) < INFINITY ? v - (float)h : 0.0f;
     }
 }
-
-// Rows copied to rows of whole steps, zeros behind their end.
+// The parts of 8 values in a row, to `to` and, `part` values apart, behind it.
+template <typename T, int N>
+__device__ __forceinline__ void put8(const float (&f)[8], T* to, int64_t part) {
+    typename Matrix<T>::V8 out[N];
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        T p[N];
+        cut<T, N>(f[j], p);
+#pragma unroll
+        for (int k = 0; k < N; k++) out[k][j] = p[k];
+    }
+#pragma unroll
+    for (int k = 0; k < N; k++) *reinterpret_cast<typename Matrix<T>::V8*>(to + k * part) = out[k];
+}
+// 8 values of a row of `left`, zeros behind its end.
 template <typename E>
-__global__ __launch_bounds__(kThreads) void copy_kernel(const E* src, int64_t rows, int64_t cols, int64_t ld_src,
-                                                        typename Parts<E>::T* dst, int64_t ld, int64_t part) {
-    typedef typename Parts<E>::T T;
-    constexpr int N = Parts<E>::kCount;
-    const int64_t per_row = ld / 8;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < rows * per_row; i += (int64_t)gridDim.x * kThreads) {
-        const int64_t r = i / per_row, c = i % per_row * 8;
-        typename Matrix<T>::V8 out[N];
+__device__ __forceinline__ void get8(const E* p, int64_t left, float (&f)[8]) {
+    if (left >= 8) {
+        Vec<E, 8>::unpack(Vec<E, 8>::load(p), f);
+    } else {
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-            T p[N];
-            cut<T, N>(c + j < cols ? (float)src[r * ld_src + c + j] : 0.0f, p);
-#pragma unroll
-            for (int k = 0; k < N; k++) out[k][j] = p[k];
-        }
-#pragma unroll
-        for (int k = 0; k < N; k++) *reinterpret_cast<typename Matrix<T>::V8*>(dst + k * part + r * ld + c) = out[k];
+        for (int j = 0; j < 8; j++) f[j] = j < left ? (float)p[j] : 0.0f;
     }
 }
 
-// The transpose: dst[c][r], zeros behind the last row, and in place of rows that take no part.
+// A copy of rows as rows of whole steps (ld), or turned: dst[column][row], zeros
+// behind the last row.  `on`: rows that take no part become zeros.
+struct Job {
+    const void* src;
+    void* dst;
+    int64_t rows, cols, ld_src, ld, part;
+    int32_t first;  // workgroup
+    int32_t on;
+};
+struct Jobs {
+    Job copy[2], turn[2];
+    int32_t row_blocks, blocks;  // workgroups that look at the rows, the first ones; of all
+};
 template <typename E>
-__global__ __launch_bounds__(kThreads) void turn_kernel(const E* src, int64_t rows, int64_t cols, int64_t ld_src,
-                                                        typename Parts<E>::T* dst, int64_t ld, int64_t part,
-                                                        const Row* only) {
+__device__ __forceinline__ void run_copy(const Job& j, int block, int blocks) {
     typedef typename Parts<E>::T T;
-    constexpr int N = Parts<E>::kCount;
-    __shared__ float tile[64][65];
-    const int64_t down = ld / 64, across = (cols + 63) / 64;
-    for (int64_t t = blockIdx.x; t < down * across; t += gridDim.x) {
-        const int64_t r0 = t % down * 64, c0 = t / down * 64;
+    const int64_t per_row = j.ld / 8;
+    for (int64_t i = (int64_t)block * kThreads + threadIdx.x; i < j.rows * per_row; i += (int64_t)blocks * kThreads) {
+        const int64_t r = i / per_row, c = i % per_row * 8;
+        float f[8];
+        get8(static_cast<const E*>(j.src) + r * j.ld_src + c, j.cols - c, f);
+        put8<T, Parts<E>::kCount>(f, static_cast<T*>(j.dst) + r * j.ld + c, j.part);
+    }
+}
+template <typename E>
+__device__ __forceinline__ void run_turn(const Args& a, const Job& j, int block, int blocks, float (*tile)[65]) {
+    typedef typename Parts<E>::T T;
+    static_assert(kThreads == 512, "a lane takes 8 values of the tile");
+    const int64_t down = j.ld / 64, across = (j.cols + 63) / 64;
+    const int at = threadIdx.x >> 3, k = (threadIdx.x & 7) * 8;
+    for (int64_t t = block; t < down * across; t += blocks) {
+        // Neighbouring workgroups go along the rows, so that lines are read whole.
+        const int64_t c0 = t % across * 64, r0 = t / across * 64;
+        float f[8];
+        const bool in = r0 + at < j.rows && (!j.on || row_of(a, r0 + at).target >= 0);
+        get8(static_cast<const E*>(j.src) + (r0 + at) * j.ld_src + c0 + k, in ? j.cols - c0 - k : 0, f);
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 16; k++) {
-            const int i = k * 4 + threadIdx.x / 64, j = threadIdx.x % 64;
-            const bool in = r0 + i < rows && c0 + j < cols && (only == nullptr || only[r0 + i].target >= 0);
-            tile[i][j] = in ? (float)src[(r0 + i) * ld_src + c0 + j] : 0.0f;
-        }
+        for (int q = 0; q < 8; q++) tile[at][k + q] = f[q];
         __syncthreads();
+        if (c0 + at < j.cols) {
 #pragma unroll
-        for (int k = 0; k < 16; k++) {
-            const int i = threadIdx.x % 64, j = k * 4 + threadIdx.x / 64;
-            if (c0 + j < cols) {
-                T p[N];
-                cut<T, N>(tile[i][j], p);
-#pragma unroll
-                for (int q = 0; q < N; q++) dst[q * part + (c0 + j) * ld + r0 + i] = p[q];
-            }
+            for (int q = 0; q < 8; q++) f[q] = tile[k + q][at];
+            put8<T, Parts<E>::kCount>(f, static_cast<T*>(j.dst) + (c0 + at) * j.ld + r0 + k, j.part);
         }
     }
+}
+// What has to be done before a product, in one launch: workgroups for each job.
+template <typename E>
+__global__ __launch_bounds__(kThreads) void prepare_kernel(const Args a, const Jobs jobs) {
+    __shared__ float tile[64][65];
+    const int b = blockIdx.x;
+    if (b < jobs.row_blocks) return look_at_rows(a, b);
+    if (b < jobs.copy[1].first) return run_copy<E>(jobs.copy[0], b - jobs.copy[0].first, jobs.copy[1].first - jobs.copy[0].first);
+    if (b < jobs.turn[0].first) return run_copy<E>(jobs.copy[1], b - jobs.copy[1].first, jobs.turn[0].first - jobs.copy[1].first);
+    if (b < jobs.turn[1].first) return run_turn<E>(a, jobs.turn[0], b - jobs.turn[0].first, jobs.turn[1].first - jobs.turn[0].first, tile);
+    run_turn<E>(a, jobs.turn[1], b - jobs.turn[1].first, jobs.blocks - jobs.turn[1].first, tile);
 }
 
 // --- the tile loop --------------------------------------------------------------
@@ -279,14 +325,33 @@ __device__ __forceinline__ void load_lds(const void* from, void* to) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                      (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
+// All waves here, all LDS reads of before done, and all but the last LOADS loads.
+template <int LOADS>
+__device__ __forceinline__ void meet() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+}
 
 // A tile of BM x BN of the product by WM x WN waves, each with MI x NJ squares of 16.
 // An operand's tile lies in LDS as rows of 128 bytes; the 16-byte pieces of a row are
 // exchanged by the row's number, so that lanes reading a column of pieces meet all banks.
-template <typename T, int BM, int BN, int WM, int WN, int PAIRS>
-struct Tile {
-    static constexpr int kWaves = WM * WN, MI = BM / WM / 16, NJ = BN / WN / 16;
+// STAGES steps of k are on their way or in use.
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
+struct Shape {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
+    static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves, MI = BM / WM / 16, NJ = BN / WN / 16;
     static constexpr int kBytes = (BM + BN) * kStep * 2;  // of one step
+    static constexpr int kLds = STAGES * kBytes > BM * BN * 2 ? STAGES * kBytes : BM * BN * 2;
+    static constexpr int kWavesPerSimd = kLds > 80 * 1024 ? kWaves / 4 : kWaves / 2;
+    static constexpr int kLoads = (BM + BN) / 8 / kWaves;  // of a wave for one step
+    static_assert(BM / 8 % kWaves == 0 && BN / 8 % kWaves == 0, "waves fetch alike");
+};
+typedef Shape<256, 256, 2, 4, 2> Big;
+typedef Shape<128, 128, 2, 2, 2> Middle;
+typedef Shape<64, 64, 2, 2, 4> Small;
+
+template <typename T, typename S, int PAIRS>
+struct Tile {
+    static constexpr int MI = S::MI, NJ = S::NJ;
     typedef typename Matrix<T>::V8 V8;
 
     template <int ROWS>
@@ -295,8 +360,8 @@ struct Tile {
         const int r = lane >> 3, piece = (lane & 7) ^ r;
         const T* p = static_cast<const T*>(o.p) + part * o.part + k + piece * 8;
 #pragma unroll
-        for (int i = 0; i < ROWS / 8 / kWaves; i++) {
-            const int block = i * kWaves + wave;
+        for (int i = 0; i < ROWS / 8 / S::kWaves; i++) {
+            const int block = i * S::kWaves + wave;
             int64_t row = row0 + block * 8 + r;
             row = row < o.rows ? row : o.rows - 1;  // rows past the end: any, their products are not used
             load_lds(p + row * o.ld, lds + block * 1024);
@@ -310,102 +375,155 @@ struct Tile {
     static __device__ __forceinline__ void run(const Operand& x, const Operand& y, int64_t x0, int64_t y0, int64_t k0,
                                                int steps, char* lds, F4 (&acc)[MI][NJ]) {
         const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-        const int m = wave / WN * MI * 16 + (lane & 15), n = wave % WN * NJ * 16 + (lane & 15);
+        const int m = wave / S::WN * MI * 16 + (lane & 15), n = wave % S::WN * NJ * 16 + (lane & 15);
 #pragma unroll
         for (int i = 0; i < MI; i++)
 #pragma unroll
             for (int j = 0; j < NJ; j++) acc[i][j] = F4{0.0f, 0.0f, 0.0f, 0.0f};
-        int pair = 0, at = 0;  // of the step that is fetched next
-        const auto fetch_next = [&](char* to) {
+        int pair = 0, at = 0, next = 0;  // of the step that is fetched next, and its place
+        const auto fetch_next = [&]() {
             const int px = PAIRS == 1 ? 0 : kPairs[pair][0], py = PAIRS == 1 ? 0 : kPairs[pair][1];
-            fetch<BM>(x, px, x0, k0 + (int64_t)at * kStep, to);
-            fetch<BN>(y, py, y0, k0 + (int64_t)at * kStep, to + BM * 128);
+            char* to = lds + next * S::kBytes;
+            fetch<S::BM>(x, px, x0, k0 + (int64_t)at * kStep, to);
+            fetch<S::BN>(y, py, y0, k0 + (int64_t)at * kStep, to + S::BM * 128);
             if (++at == steps) {
                 at = 0;
                 pair++;
             }
+            next = next + 1 == S::STAGES ? 0 : next + 1;
         };
         const int total = steps * PAIRS;
-        if (total > 0) fetch_next(lds);
+        int here = 0;
+        meet<0>();  // the last tile's reads
+        for (int t = 0; t < S::STAGES - 1 && t < total; t++) fetch_next();
         for (int t = 0; t < total; t++) {
-            __syncthreads();  // step t is there, and step t - 1 read
-            if (t + 1 < total) fetch_next(lds + ((t + 1) & 1) * kBytes);
-            const char* xs = lds + (t & 1) * kBytes;
-            const char* ys = xs + BM * 128;
+            // Step t is there, and step t - 1 read, whose place step t + STAGES - 1 takes.
+            if (t + S::STAGES - 2 < total) meet<(S::STAGES - 2) * S::kLoads>();
+            else meet<0>();
+            if (t + S::STAGES - 1 < total) fetch_next();
+            const char* xs = lds + here * S::kBytes;
+            const char* ys = xs + S::BM * 128;
+            here = here + 1 == S::STAGES ? 0 : here + 1;
 #pragma unroll
             for (int k = 0; k < kStep / 32; k++) {
                 V8 fx[MI], fy[NJ];
 #pragma unroll
-                for (int i = 0; i < MI; i++) fx[i] = piece_at(xs, m + i * 16, k * 4 + (lane >> 4));
-#pragma unroll
                 for (int j = 0; j < NJ; j++) fy[j] = piece_at(ys, n + j * 16, k * 4 + (lane >> 4));
+#pragma unroll
+                for (int i = 0; i < MI; i++) fx[i] = piece_at(xs, m + i * 16, k * 4 + (lane >> 4));
 #pragma unroll
                 for (int i = 0; i < MI; i++)
 #pragma unroll
                     for (int j = 0; j < NJ; j++) acc[i][j] = Matrix<T>::mfma(fx[i], fy[j], acc[i][j]);
             }
         }
-        __syncthreads();
+        meet<0>();
     }
 };
 
-constexpr int kBM = 128, kBN = 128, kWM = 2, kWN = 2;
+// Which tile of tm x tn workgroup `b` takes.  Workgroups go round the 8 XCDs; each XCD
+// takes neighbouring tiles, 8 down before the next column, so that its L2 serves their rows.
+struct Place {
+    int m, n;
+};
+__device__ __forceinline__ Place place_of(int b, int tm, int tn) {
+    const int total = tm * tn, xcd = b & 7, per = total >> 3, rest = total & 7;
+    const int id = xcd * per + (xcd < rest ? xcd : rest) + (b >> 3);
+    const int width = 8 * tn, group = id / width, first = group * 8, in = id - group * width;
+    const int high = tm - first < 8 ? tm - first : 8;
+    return Place{first + in % high, in / high};
+}
 
 // Maximum and sum of exponentials of a tile's logits, per row, and the targets' logits;
 // `first` is the token of the head's first row.
-template <typename T, int PAIRS>
-__global__ __launch_bounds__(kThreads) void logits_kernel(const Args a, const Operand head, const Operand hidden,
-                                                          int steps, int64_t first, int32_t tiles) {
-    typedef Tile<T, kBM, kBN, kWM, kWN, PAIRS> Tl;
-    __shared__ __attribute__((aligned(16))) char lds[2 * Tl::kBytes];
-    const int64_t v0 = (int64_t)(blockIdx.x % tiles) * kBM, r0 = (int64_t)(blockIdx.x / tiles) * kBN;
+template <typename T, typename S, int PAIRS>
+__global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void logits_kernel(const Args a, const Operand head,
+                                                                               const Operand hidden, int steps,
+                                                                               int64_t first, int tm, int tn) {
+    typedef Tile<T, S, PAIRS> Tl;
+    __shared__ __attribute__((aligned(16))) char lds[S::STAGES * S::kBytes];
+    const Place at = place_of(blockIdx.x, tm, tn);
+    const int64_t v0 = (int64_t)at.m * S::BM, r0 = (int64_t)at.n * S::BN;
     F4 acc[Tl::MI][Tl::NJ];
     Tl::run(head, hidden, v0, r0, 0, steps, lds, acc);
-    const int64_t tile = (first + v0) / kBM;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / kWN, wn = wave % kWN;
-    float* s_max = reinterpret_cast<float*>(lds);  // [kWM][kBN]
-    float* s_sum = s_max + kWM * kBN;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / S::WN, wn = wave % S::WN;
+    float* s_max = reinterpret_cast<float*>(lds);  // [WM][BN]
+    float* s_sum = s_max + S::WM * S::BN;
     const int64_t v = first + v0 + wm * Tl::MI * 16 + (lane >> 4) * 4;
+    if (first + v0 + S::BM > a.V) {
+#pragma unroll
+        for (int i = 0; i < Tl::MI; i++)
+#pragma unroll
+            for (int j = 0; j < Tl::NJ; j++)
+#pragma unroll
+                for (int q = 0; q < 4; q++)
+                    if (v + i * 16 + q >= a.V) acc[i][j][q] = -INFINITY;
+    }
 #pragma unroll
     for (int j = 0; j < Tl::NJ; j++) {
         const int in = wn * Tl::NJ * 16 + j * 16 + (lane & 15);
         const int64_t r = r0 + in;
-        const int32_t y = r < a.n ? a.rows[r].target : -1;
+        const int64_t y = (r < a.n ? a.rows[r].target : -1) - v;
         float m = -INFINITY;
 #pragma unroll
         for (int i = 0; i < Tl::MI; i++)
 #pragma unroll
-            for (int q = 0; q < 4; q++) {
-                if (v + i * 16 + q >= a.V) acc[i][j][q] = -INFINITY;
-                else if (v + i * 16 + q == y) a.at_target[r] = acc[i][j][q];
-                m = fmaxf(m, acc[i][j][q]);
-            }
+            for (int q = 0; q < 4; q++) m = fmaxf(m, acc[i][j][q]);
+        if (y >= 0 && y < Tl::MI * 16 && (y & 15) < 4) {
+#pragma unroll
+            for (int i = 0; i < Tl::MI; i++)
+#pragma unroll
+                for (int q = 0; q < 4; q++)
+                    if (y == i * 16 + q) a.at_target[r] = acc[i][j][q];
+        }
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
         const float from = m == -INFINITY ? 0.0f : m;
-        float S = 0.0f;
+        float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < Tl::MI; i++)
 #pragma unroll
-            for (int q = 0; q < 4; q++) S += fast_exp(acc[i][j][q] - from);
-        S += __shfl_xor(S, 16);
-        S += __shfl_xor(S, 32);
+            for (int q = 0; q < 4; q++) sum += fast_exp(acc[i][j][q] - from);
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
         if (lane < 16) {
-            s_max[wm * kBN + in] = m;
-            s_sum[wm * kBN + in] = S;
+            s_max[wm * S::BN + in] = m;
+            s_sum[wm * S::BN + in] = sum;
         }
     }
     __syncthreads();
-    for (int in = threadIdx.x; in < kBN; in += kThreads) {
+    for (int in = threadIdx.x; in < S::BN; in += S::kThreads) {
         if (r0 + in >= a.n) continue;
         float m = -INFINITY;
-        for (int k = 0; k < kWM; k++) m = fmaxf(m, s_max[k * kBN + in]);
+#pragma unroll
+        for (int k = 0; k < S::WM; k++) m = fmaxf(m, s_max[k * S::BN + in]);
         const float from = m == -INFINITY ? 0.0f : m;
-        float S = 0.0f;
-        for (int k = 0; k < kWM; k++) S += s_sum[k * kBN + in] * fast_exp(s_max[k * kBN + in] - from);
-        a.part_max[tile * a.n + r0 + in] = m;
-        a.part_sum[tile * a.n + r0 + in] = S;
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < S::WM; k++) sum += s_sum[k * S::BN + in] * fast_exp(s_max[k * S::BN + in] - from);
+        a.part[(r0 + in) * a.tiles + (first + v0) / S::BM] = float2{m, sum};
     }
+}
+
+// A tile of 16-bit values goes through LDS, so that memory is written in whole rows of
+// the tile.  It has `ROWS` rows of COLS values; pieces of 8 bytes are exchanged by the
+// row's number.
+template <int COLS>
+__device__ __forceinline__ char* spot(char* lds, int row, int col) {
+    static_assert(COLS >= 64, "16 pieces a row");
+    return lds + row * COLS * 2 + ((col / 4 ^ ((row & 15) << 2) % (COLS / 4)) << 3);
+}
+
+// Four lanes' four 16-bit values each, turned: lane k of four gets value k of all four.
+__device__ __forceinline__ uint2 turned(uint2 x) {
+    const int lane = threadIdx.x & 3;
+    const auto other = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, false); };
+    const auto across = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, false); };
+    // Even lanes take the low halves of their own and the next lane's words, odd ones the high halves.
+    const uint32_t pick = lane & 1 ? 0x03020706u : 0x05040100u;
+    const uint32_t A = __builtin_amdgcn_perm(other(x.x), x.x, pick), B = __builtin_amdgcn_perm(other(x.y), x.y, pick);
+    const uint32_t got = across(lane & 2 ? A : B);
+    return lane & 2 ? uint2{got, B} : uint2{A, got};
 }
 
 // e of a piece of the vocabulary: e[n][ld], and with the rows' weights over their
@@ -414,118 +532,174 @@ struct Errors {
     void *e, *we;      // either may be NULL
     int64_t ld, part, ld_turned, part_turned;
     int64_t first;     // token of the piece
-    int32_t tiles;     // tiles of tokens in the piece
 };
-template <typename T, int PAIRS>
-__global__ __launch_bounds__(kThreads) void errors_kernel(const Args a, const Operand head, const Operand hidden,
-                                                          int steps, const Errors o) {
-    typedef Tile<T, kBM, kBN, kWM, kWN, PAIRS> Tl;
+template <typename T, typename S, int PAIRS>
+__global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void errors_kernel(const Args a, const Operand head,
+                                                                               const Operand hidden, int steps,
+                                                                               const Errors o, int tm, int tn) {
+    typedef Tile<T, S, PAIRS> Tl;
     constexpr int N = PAIRS == 1 ? 1 : 3;
-    __shared__ __attribute__((aligned(16))) char lds[2 * Tl::kBytes];
-    const int64_t v0 = (int64_t)(blockIdx.x % o.tiles) * kBM, r0 = (int64_t)(blockIdx.x / o.tiles) * kBN;
+    __shared__ __attribute__((aligned(16))) char lds[S::kLds];
+    const Place at = place_of(blockIdx.x, tm, tn);
+    const int64_t v0 = (int64_t)at.m * S::BM, r0 = (int64_t)at.n * S::BN;
     F4 acc[Tl::MI][Tl::NJ];
     Tl::run(head, hidden, v0, r0, 0, steps, lds, acc);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / kWN, wn = wave % kWN;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / S::WN, wn = wave % S::WN;
+    const int vt = wm * Tl::MI * 16 + (lane >> 4) * 4, rt = wn * Tl::NJ * 16 + (lane & 15);  // in the tile
     const float top = a.totals->weight;
+    float w[Tl::NJ];
 #pragma unroll
     for (int j = 0; j < Tl::NJ; j++) {
-        const int64_t r = r0 + wn * Tl::NJ * 16 + j * 16 + (lane & 15);
+        const int64_t r = r0 + rt + j * 16;
         const Row row = r < a.n ? a.rows[r] : Row{-1, 0.0f};
         const bool on = row.target >= 0;
         const float lse = on ? a.lse_in[r] : 0.0f;
-        const float w = on && top != 0.0f ? row.weight / top : 0.0f;
+        w[j] = on && top != 0.0f ? row.weight / top : 0.0f;
+        const int64_t left = a.V - o.first - v0 - vt, y = row.target - (o.first + v0 + vt);
 #pragma unroll
-        for (int i = 0; i < Tl::MI; i++) {
-            const int64_t v = v0 + wm * Tl::MI * 16 + i * 16 + (lane >> 4) * 4;
-            typedef T T4 __attribute__((ext_vector_type(4)));
-            T4 e[N];
-            T we[N][4];
+        for (int i = 0; i < Tl::MI; i++)
 #pragma unroll
             for (int q = 0; q < 4; q++) {
-                float x = 0.0f;
-                if (on && o.first + v + q < a.V) {
-                    x = fast_exp(acc[i][j][q] - lse);
-                    if (o.first + v + q == row.target) x -= 1.0f;
+                float x = fast_exp(acc[i][j][q] - lse);
+                if (y == i * 16 + q) x -= 1.0f;
+                acc[i][j][q] = on && i * 16 + q < left ? x * Matrix<T>::kScale : 0.0f;
+            }
+    }
+    // The parts of both orders in turn; a part is taken off what remains.
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    typedef uint32_t Line __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int order = 0; order < 2; order++) {
+        void* out = order == 0 ? o.e : o.we;
+        if (out == nullptr) continue;
+#pragma unroll
+        for (int part = 0; part < N; part++) {
+            if (order + part > 0) __syncthreads();
+#pragma unroll
+            for (int j = 0; j < Tl::NJ; j++)
+#pragma unroll
+                for (int i = 0; i < Tl::MI; i++) {
+                    T4 e;
+#pragma unroll
+                    for (int q = 0; q < 4; q++) {
+                        T p[N];
+                        cut<T, N>(order == 0 ? acc[i][j][q] : acc[i][j][q] * w[j], p);
+                        e[q] = p[part];
+                    }
+                    uint2 bits = __builtin_bit_cast(uint2, e);
+                    if (order == 0) {
+                        *reinterpret_cast<uint2*>(spot<S::BM>(lds, rt + j * 16, vt + i * 16)) = bits;
+                    } else {
+                        // Lane k of four has token vt + k, and the four lanes' rows.
+                        bits = turned(bits);
+                        *reinterpret_cast<uint2*>(spot<S::BN>(lds, vt + i * 16 + (lane & 3), (rt + j * 16) & ~3)) = bits;
+                    }
                 }
-                x *= Matrix<T>::kScale;
-                T p[N];
-                cut<T, N>(x, p);
-#pragma unroll
-                for (int k = 0; k < N; k++) e[k][q] = p[k];
-                cut<T, N>(on ? x * w : 0.0f, p);
-#pragma unroll
-                for (int k = 0; k < N; k++) we[k][q] = p[k];
-            }
-            if (o.e && r < a.n && v < o.ld) {
-#pragma unroll
-                for (int k = 0; k < N; k++) *reinterpret_cast<T4*>(static_cast<T*>(o.e) + k * o.part + r * o.ld + v) = e[k];
-            }
-            if (o.we && r < o.ld_turned) {
-#pragma unroll
-                for (int q = 0; q < 4; q++)
-#pragma unroll
-                    for (int k = 0; k < N; k++)
-                        if (v + q < o.ld) static_cast<T*>(o.we)[k * o.part_turned + (v + q) * o.ld_turned + r] = we[k][q];
+            __syncthreads();
+            // 16 bytes a lane, rows of the tile after each other.
+            constexpr int COLS[2] = {S::BM, S::BN}, ROWS[2] = {S::BN, S::BM};
+            const int64_t row0 = order == 0 ? r0 : v0, col0 = order == 0 ? v0 : r0;
+            const int64_t rows = order == 0 ? a.n : o.ld, ld = order == 0 ? o.ld : o.ld_turned;
+            T* to = static_cast<T*>(out) + part * (order == 0 ? o.part : o.part_turned);
+#pragma unroll 4
+            for (int k = threadIdx.x; k < ROWS[order] * (COLS[order] / 8); k += S::kThreads) {
+                const int row = k / (COLS[order] / 8), col = k % (COLS[order] / 8) * 8;
+                const char* from = order == 0 ? spot<S::BM>(lds, row, col) : spot<S::BN>(lds, row, col);
+                if (row0 + row < rows && col0 + col < ld)
+                    *reinterpret_cast<Line*>(to + (row0 + row) * ld + col0 + col) = *reinterpret_cast<const Line*>(from);
             }
         }
     }
 }
 
-// dW of a piece: out[token][D], times what the errors were held by.
-template <typename E, typename T, int PAIRS>
-__global__ __launch_bounds__(kThreads) void dhead_kernel(const Args a, const Operand x, const Operand y, int steps, E* out) {
-    typedef Tile<T, kBM, kBN, kWM, kWN, PAIRS> Tl;
-    __shared__ __attribute__((aligned(16))) char lds[2 * Tl::kBytes];
-    const int across = (int)((a.D + kBM - 1) / kBM);
-    const int64_t d0 = (int64_t)(blockIdx.x % across) * kBM, v0 = (int64_t)(blockIdx.x / across) * kBN;
+// Both gradients of a piece in one launch, the workgroups of dh first: their k is longer.
+struct Gradients {
+    Operand wt, er;         // of dh: W^T, e
+    Operand ht, we;         // of dW: h^T, (c e)^T
+    float* slab;            // [splits][n][ld]: dh so far; a split of the piece's tokens each
+    void* dhead;            // the piece's first row
+    int64_t ld;
+    int32_t steps_v, steps_n, splits, add;
+    int32_t dh_blocks, tm, tn_rows, tn_tokens;  // tiles across D, down the rows and the tokens
+};
+template <typename E, typename T, typename S, int PAIRS>
+__global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gradients_kernel(const Args a, const Gradients g) {
+    typedef Tile<T, S, PAIRS> Tl;
+    __shared__ __attribute__((aligned(16))) char lds[S::kLds];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / S::WN, wn = wave % S::WN;
+    const int dt = wm * Tl::MI * 16 + (lane >> 4) * 4, nt = wn * Tl::NJ * 16 + (lane & 15);  // in the tile
     F4 acc[Tl::MI][Tl::NJ];
-    Tl::run(x, y, d0, v0, 0, steps, lds, acc);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / kWN, wn = wave % kWN;
+    if ((int)blockIdx.x < g.dh_blocks) {
+        const int split = blockIdx.x % g.splits;
+        const Place at = place_of(blockIdx.x / g.splits, g.tm, g.tn_rows);
+        const int64_t d0 = (int64_t)at.m * S::BM, r0 = (int64_t)at.n * S::BN;
+        const int from = (int)((int64_t)g.steps_v * split / g.splits), to = (int)((int64_t)g.steps_v * (split + 1) / g.splits);
+        Tl::run(g.wt, g.er, d0, r0, (int64_t)from * kStep, to - from, lds, acc);
+#pragma unroll
+        for (int j = 0; j < Tl::NJ; j++) {
+            const int64_t r = r0 + nt + j * 16;
+            if (r >= a.n) continue;
+#pragma unroll
+            for (int i = 0; i < Tl::MI; i++) {
+                const int64_t d = d0 + dt + i * 16;
+                if (d >= g.ld) continue;
+                F4* to = reinterpret_cast<F4*>(g.slab + (split * a.n + r) * g.ld + d);
+                *to = g.add ? *to + acc[i][j] : acc[i][j];
+            }
+        }
+        return;
+    }
+    const Place at = place_of(blockIdx.x - g.dh_blocks, g.tm, g.tn_tokens);
+    const int64_t d0 = (int64_t)at.m * S::BM, v0 = (int64_t)at.n * S::BN;
+    Tl::run(g.ht, g.we, d0, v0, 0, g.steps_n, lds, acc);
     const float by = a.totals->weight * a.totals->share * a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / Matrix<T>::kScale;
+    E* out = static_cast<E*>(g.dhead);
+    if constexpr (sizeof(E) == 4) {
+        // 16 bytes a lane as they are.
 #pragma unroll
-    for (int j = 0; j < Tl::NJ; j++) {
-        const int64_t v = v0 + wn * Tl::NJ * 16 + j * 16 + (lane & 15);
-        if (v >= y.rows) continue;
+        for (int j = 0; j < Tl::NJ; j++) {
+            const int64_t v = v0 + nt + j * 16;
+            if (v >= g.we.rows) continue;
 #pragma unroll
-        for (int i = 0; i < Tl::MI; i++) {
-            const int64_t d = d0 + wm * Tl::MI * 16 + i * 16 + (lane >> 4) * 4;
-            float f[4];
+            for (int i = 0; i < Tl::MI; i++) {
+                const int64_t d = d0 + dt + i * 16;
+                float f[4];
 #pragma unroll
-            for (int q = 0; q < 4; q++) f[q] = acc[i][j][q] * by;
-            if (d + 4 <= a.D) {
-                Vec<E, 4>::store(out + v * a.D + d, f);
-            } else {
+                for (int q = 0; q < 4; q++) f[q] = acc[i][j][q] * by;
+                if (d + 4 <= a.D) {
+                    Vec<E, 4>::store(out + v * a.D + d, f);
+                } else {
 #pragma unroll
-                for (int q = 0; q < 4; q++)
-                    if (d + q < a.D) out[v * a.D + d + q] = (E)f[q];
+                    for (int q = 0; q < 4; q++)
+                        if (d + q < a.D) out[v * a.D + d + q] = (E)f[q];
+                }
             }
         }
-    }
-}
-
-// dh of a piece, added to what the pieces before left: slab[split][n][ld], a split of the piece's tokens each.
-template <typename T, int PAIRS>
-__global__ __launch_bounds__(kThreads) void dhidden_kernel(const Args a, const Operand x, const Operand y, int steps,
-                                                           int splits, float* slab, int64_t ld, int add) {
-    typedef Tile<T, kBM, kBN, kWM, kWN, PAIRS> Tl;
-    __shared__ __attribute__((aligned(16))) char lds[2 * Tl::kBytes];
-    const int across = (int)((a.D + kBM - 1) / kBM);
-    const int split = blockIdx.x % splits, tile = blockIdx.x / splits;
-    const int64_t d0 = (int64_t)(tile % across) * kBM, r0 = (int64_t)(tile / across) * kBN;
-    const int from = (int)((int64_t)steps * split / splits), to = (int)((int64_t)steps * (split + 1) / splits);
-    F4 acc[Tl::MI][Tl::NJ];
-    Tl::run(x, y, d0, r0, (int64_t)from * kStep, to - from, lds, acc);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / kWN, wn = wave % kWN;
+    } else {
+        typedef E E4 __attribute__((ext_vector_type(4)));
+        typedef uint32_t Line __attribute__((ext_vector_type(4)));
+        typedef Line LooseLine __attribute__((aligned(2)));
 #pragma unroll
-    for (int j = 0; j < Tl::NJ; j++) {
-        const int64_t r = r0 + wn * Tl::NJ * 16 + j * 16 + (lane & 15);
-        if (r >= a.n) continue;
+        for (int j = 0; j < Tl::NJ; j++)
 #pragma unroll
-        for (int i = 0; i < Tl::MI; i++) {
-            const int64_t d = d0 + wm * Tl::MI * 16 + i * 16 + (lane >> 4) * 4;
-            if (d >= ld) continue;
-            F4* at = reinterpret_cast<F4*>(slab + (split * a.n + r) * ld + d);
-            *at = add ? *at + acc[i][j] : acc[i][j];
+            for (int i = 0; i < Tl::MI; i++) {
+                E4 f;
+#pragma unroll
+                for (int q = 0; q < 4; q++) f[q] = (E)(acc[i][j][q] * by);
+                *reinterpret_cast<uint2*>(spot<S::BM>(lds, nt + j * 16, dt + i * 16)) = __builtin_bit_cast(uint2, f);
+            }
+        __syncthreads();
+#pragma unroll 4
+        for (int k = threadIdx.x; k < S::BN * (S::BM / 8); k += S::kThreads) {
+            const int row = k / (S::BM / 8), col = k % (S::BM / 8) * 8;
+            if (v0 + row >= g.we.rows || d0 + col >= a.D) continue;
+            E* to = out + (v0 + row) * a.D + d0 + col;
+            const char* from = spot<S::BM>(lds, row, col);
+            if (d0 + col + 8 <= a.D) {
+                *reinterpret_cast<LooseLine*>(to) = *reinterpret_cast<const Line*>(from);
+            } else {
+                for (int q = 0; q < 8 && d0 + col + q < a.D; q++) to[q] = reinterpret_cast<const E*>(from)[q];
+            }
         }
     }
 }
@@ -535,30 +709,49 @@ template <typename E>
 __global__ __launch_bounds__(kThreads) void rows_out_kernel(const Args a, const float* slab, int64_t ld, int splits,
                                                             float held, E* out) {
     const float by = a.totals->share * a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / held;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < a.n * a.D; i += (int64_t)gridDim.x * kThreads) {
-        const int64_t r = i / a.D, d = i % a.D;
+    const int64_t per_row = (a.D + 3) / 4;
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < a.n * per_row; i += (int64_t)gridDim.x * kThreads) {
+        const int64_t r = i / per_row, d = i % per_row * 4;
         const Row row = a.rows[r];
-        float v = 0.0f;
+        F4 v = {0.0f, 0.0f, 0.0f, 0.0f};
         if (row.target >= 0) {
-            for (int k = 0; k < splits; k++) v += slab[(k * a.n + r) * ld + d];
+            for (int k = 0; k < splits; k++) v += *reinterpret_cast<const F4*>(slab + (k * a.n + r) * ld + d);
             v *= row.weight * by;
         }
-        out[i] = (E)v;
+        const float f[4] = {v[0], v[1], v[2], v[3]};
+        if (d + 4 <= a.D) {
+            Vec<E, 4>::store(out + r * a.D + d, f);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; q++)
+                if (d + q < a.D) out[r * a.D + d + q] = (E)f[q];
+        }
     }
 }
 
 // --- the plan -------------------------------------------------------------------
 
 inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+inline int64_t tiles(int64_t x, int64_t m) { return (x + m - 1) / m; }
+
+// Sizes of tiles.  Few rows leave the products to memory, and small tiles keep many
+// steps on their way; otherwise big ones where they fill the GPU.
+enum Size { kSmall, kMiddle, kBig };
+Size size_of(int64_t m, int64_t n, int64_t rows) {
+    if (rows <= 64) return kSmall;
+    return tiles(m, 256) * tiles(n, 256) >= 192 ? kBig : kMiddle;
+}
+int edge(Size s) { return s == kBig ? 256 : s == kMiddle ? 128 : 64; }
 
 // Where everything lies in the workspace.
 struct Plan {
     int parts = 0;                       // of a value
     int64_t ldk = 0, ldn = 0, ldv = 0;   // padded D, n and tokens of a piece
     int64_t piece = 0, loss_piece = 0;   // tokens of a piece, backward and forward
-    int tiles = 0;                       // tiles of tokens
+    Size logits = kMiddle, errors = kMiddle, gradients = kMiddle;
+    int tiles = 0;                       // tiles of tokens, forward
     int splits = 0;
-    int64_t rows = 0, totals = 0, sums = 0, counts = 0, tops = 0, at_target = 0, part_max = 0, part_sum = 0;
+    int64_t rows = 0, totals = 0, sums = 0, counts = 0, tops = 0, at_target = 0, part = 0;
     int64_t hidden = 0, head = 0, head_piece = 0, hidden_t = 0, head_t = 0, e = 0, we = 0, slab = 0;
     int64_t bytes_loss = 0, bytes_backward = 0;
 };
@@ -573,16 +766,20 @@ Plan plan_of(const gear_token_desc& d) {
     p.parts = d.dtype == GEAR_DTYPE_F32 ? 3 : 1;
     p.ldk = up(d.D, kStep);
     p.ldn = up(d.n, kStep);
-    p.tiles = (int)((d.V + kBM - 1) / kBM);
-    int64_t piece = kPieceValues / (d.n > 0 ? d.n : 1) / p.parts / kBM * kBM;
-    piece = piece < kBM ? kBM : piece > kPieceTokens ? kPieceTokens : piece;
+    int64_t piece = kPieceValues / (d.n > 0 ? d.n : 1) / p.parts / 256 * 256;
+    piece = piece < 256 ? 256 : piece > kPieceTokens ? kPieceTokens : piece;
     p.piece = piece < d.V ? piece : d.V;
     p.loss_piece = kPieceTokens < d.V ? kPieceTokens : d.V;
     p.ldv = up(p.piece, kStep);
+    p.logits = size_of(p.loss_piece, d.n, d.n);
+    p.errors = size_of(p.piece, d.n, d.n);
+    if (p.parts > 1 && p.errors == kBig) p.errors = kMiddle;  // three parts of a big tile's values leave the registers
+    p.gradients = d.n <= 64 ? kSmall : d.D < 192 ? kMiddle : size_of(d.D, p.piece + d.n, d.n);
+    p.tiles = (int)tiles(d.V, edge(p.logits));
     // Few tiles of dh share the GPU's 256 units by splitting the tokens.
-    const int64_t tiles = (d.D + kBM - 1) / kBM * ((d.n + kBN - 1) / kBN), steps = p.ldv / kStep;
+    const int64_t dh = tiles(d.D, edge(p.gradients)) * tiles(d.n, edge(p.gradients)), steps = p.ldv / kStep;
     p.splits = 1;
-    while (tiles * p.splits < 512 && p.splits * 8 <= steps && p.splits < 16) p.splits *= 2;
+    while (dh * p.splits < 256 && p.splits * 8 <= steps && p.splits < 16) p.splits *= 2;
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
         const int64_t here = at;
@@ -597,8 +794,7 @@ Plan plan_of(const gear_token_desc& d) {
     p.hidden = take(d.n * p.ldk * p.parts * 2);
     const int64_t common = at;
     p.at_target = take(d.n * 4);
-    p.part_max = take(d.n * (int64_t)p.tiles * 4);
-    p.part_sum = take(d.n * (int64_t)p.tiles * 4);
+    p.part = take(d.n * (int64_t)p.tiles * (int64_t)sizeof(float2));
     p.head = take(p.loss_piece * p.ldk * p.parts * 2);
     p.bytes_loss = at;
     at = common;
@@ -649,7 +845,7 @@ Args args_of(const gear_token_desc& d, const Plan& p, char* work) {
     a.weight_group = d.weight_group;
     a.target_dtype = d.target_dtype;
     a.tiles = p.tiles;
-    a.parts = (int32_t)some_blocks(d.n, kParts);
+    a.row_parts = d.n <= kSoloRows ? 1 : (int32_t)some_blocks(d.n, kParts);
     a.denom = d.denom;
     a.grad_scale = d.grad_scale;
     return a;
@@ -664,69 +860,104 @@ struct Call {
     char* work;
     hipStream_t s;
 
-    hipError_t copy(const void* src, int64_t rows, int64_t ld_src, int64_t to) const {
-        hipLaunchKernelGGL(copy_kernel<E>, dim3(some_blocks(rows * (p.ldk / 8), 8192)), dim3(kThreads), 0, s,
-                           static_cast<const E*>(src), rows, d.D, ld_src, reinterpret_cast<T*>(work + to), p.ldk,
-                           rows * p.ldk);
-        return hipGetLastError();
+    // An operand of rows as they lie, or of a copy that `job` makes.
+    Operand operand(const void* src, int64_t rows, int64_t ld_src, int64_t to, Job& job) const {
+        if (plain_rows(d.dtype, src, ld_src, d.D)) return Operand{src, rows, ld_src, 0};
+        job = Job{src, work + to, rows, d.D, ld_src, p.ldk, rows * p.ldk, 0, 0};
+        return Operand{work + to, rows, p.ldk, rows * p.ldk};
     }
-    hipError_t turn(const void* src, int64_t rows, int64_t ld_src, int64_t ld, int64_t to, const Row* only) const {
-        const int64_t tiles = ld / 64 * ((d.D + 63) / 64);
-        hipLaunchKernelGGL(turn_kernel<E>, dim3((unsigned)(tiles < 16384 ? tiles : 16384)), dim3(kThreads), 0, s,
-                           static_cast<const E*>(src), rows, d.D, ld_src, reinterpret_cast<T*>(work + to), ld, d.D * ld, only);
-        return hipGetLastError();
+    // A turned copy: d.D rows of ld values.
+    Operand turned_operand(const void* src, int64_t rows, int64_t ld_src, int64_t ld, int64_t to, bool on, Job& job) const {
+        job = Job{src, work + to, rows, d.D, ld_src, ld, d.D * ld, 0, on ? 1 : 0};
+        return Operand{work + to, d.D, ld, d.D * ld};
     }
-    // The operand of rows as they lie, or of a copy.
-    hipError_t operand(const void* src, int64_t rows, int64_t ld_src, int64_t to, Operand& o) const {
-        if (plain_rows(d.dtype, src, ld_src, d.D)) {
-            o = Operand{src, rows, ld_src, 0};
-            return hipSuccess;
+    // Nothing to do costs no launch.
+    hipError_t prepare(const Args& a, Jobs& j, bool rows) const {
+        int32_t at = j.row_blocks = rows ? a.row_parts : 0;
+        for (Job& c : j.copy) {
+            c.first = at;
+            if (c.src) at += (int32_t)some_blocks(c.rows * (c.ld / 8), 4096);
         }
-        o = Operand{work + to, rows, p.ldk, rows * p.ldk};
-        return copy(src, rows, ld_src, to);
-    }
-    hipError_t rows(const Args& a) const {
-        hipLaunchKernelGGL(rows_kernel, dim3(a.parts), dim3(kThreads), 0, s, a);
-        hipLaunchKernelGGL(totals_kernel, dim3(1), dim3(64), 0, s, a);
+        for (Job& c : j.turn) {
+            c.first = at;
+            if (c.src) at += (int32_t)(tiles(c.ld, 64) * tiles(c.cols, 64) < 8192 ? tiles(c.ld, 64) * tiles(c.cols, 64) : 8192);
+        }
+        j.blocks = at;
+        if (at == 0) return hipSuccess;
+        hipLaunchKernelGGL(prepare_kernel<E>, dim3((unsigned)at), dim3(kThreads), 0, s, a, j);
+        if (rows && a.row_parts > 1) hipLaunchKernelGGL(totals_kernel, dim3(1), dim3(64), 0, s, a);
         return hipGetLastError();
     }
 
+    template <typename S>
+    hipError_t logits(const Args& a, const Operand& x, const Operand& y, int64_t first) const {
+        const int tm = (int)tiles(x.rows, S::BM), tn = (int)tiles(a.n, S::BN);
+        hipLaunchKernelGGL((logits_kernel<T, S, PAIRS>), dim3((unsigned)(tm * tn)), dim3(S::kThreads), 0, s, a, x, y,
+                           (int)(p.ldk / kStep), first, tm, tn);
+        return hipGetLastError();
+    }
+    template <int LANES>
+    hipError_t join(Args a) const {
+        // One workgroup where it has few rounds, and a launch less.
+        const int64_t want = tiles(a.n * LANES, kThreads);
+        a.lse_parts = (int32_t)(want <= 4 ? 1 : want < kParts ? want : kParts);
+        hipLaunchKernelGGL(lse_kernel<LANES>, dim3(a.lse_parts), dim3(kThreads), 0, s, a);
+        if (a.lse_parts > 1) hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(64), 0, s, a);
+        return hipGetLastError();
+    }
     hipError_t loss(Args a, const void* hidden, const void* head) const {
         a.at_target = reinterpret_cast<float*>(work + p.at_target);
-        a.part_max = reinterpret_cast<float*>(work + p.part_max);
-        a.part_sum = reinterpret_cast<float*>(work + p.part_sum);
-        hipError_t e = rows(a);
-        if (e != hipSuccess) return e;
-        if (a.n > 0) {
-            Operand x, y;
-            if ((e = operand(hidden, a.n, d.hidden_row, p.hidden, y)) != hipSuccess) return e;
-            for (int64_t first = 0; first < a.V; first += p.loss_piece) {
-                const int64_t tokens = a.V - first < p.loss_piece ? a.V - first : p.loss_piece;
-                const int tiles = (int)((tokens + kBM - 1) / kBM);
-                const E* from = static_cast<const E*>(head) + first * d.head_row;
-                if ((e = operand(from, tokens, d.head_row, p.head, x)) != hipSuccess) return e;
-                hipLaunchKernelGGL((logits_kernel<T, PAIRS>), dim3((unsigned)(tiles * ((a.n + kBN - 1) / kBN))),
-                                   dim3(kThreads), 0, s, a, x, y, (int)(p.ldk / kStep), first, tiles);
-                if ((e = hipGetLastError()) != hipSuccess) return e;
-            }
+        a.part = reinterpret_cast<float2*>(work + p.part);
+        hipError_t e = hipSuccess;
+        if (a.n == 0) {
+            Jobs j{};
+            if ((e = prepare(a, j, true)) != hipSuccess) return e;
         }
-        hipLaunchKernelGGL(lse_kernel, dim3(a.parts), dim3(kThreads), 0, s, a);
-        hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(64), 0, s, a);
-        return hipGetLastError();
+        for (int64_t first = 0; first < a.V && a.n > 0; first += p.loss_piece) {
+            const int64_t tokens = a.V - first < p.loss_piece ? a.V - first : p.loss_piece;
+            Jobs j{};
+            const Operand x = operand(static_cast<const E*>(head) + first * d.head_row, tokens, d.head_row, p.head, j.copy[0]);
+            Operand y = operand(hidden, a.n, d.hidden_row, p.hidden, j.copy[1]);
+            if (first > 0) j.copy[1] = Job{};
+            if ((e = prepare(a, j, first == 0)) != hipSuccess) return e;
+            e = p.logits == kBig ? logits<Big>(a, x, y, first) : p.logits == kMiddle ? logits<Middle>(a, x, y, first)
+                                                                                      : logits<Small>(a, x, y, first);
+            if (e != hipSuccess) return e;
+        }
+        return p.tiles <= 4 ? join<1>(a) : p.tiles <= 32 ? join<8>(a) : join<64>(a);
     }
 
+    template <typename S>
+    hipError_t errors(const Args& a, const Operand& x, const Operand& y, const Errors& o) const {
+        const int tm = (int)tiles(o.ld, S::BM), tn = (int)tiles(p.ldn, S::BN);
+        hipLaunchKernelGGL((errors_kernel<T, S, PAIRS>), dim3((unsigned)(tm * tn)), dim3(S::kThreads), 0, s, a, x, y,
+                           (int)(p.ldk / kStep), o, tm, tn);
+        return hipGetLastError();
+    }
+    template <typename S>
+    hipError_t gradients(const Args& a, Gradients g, bool dhidden, bool dhead, int64_t tokens) const {
+        g.tm = (int)tiles(a.D, S::BM);
+        g.tn_rows = (int)tiles(a.n, S::BN);
+        g.tn_tokens = (int)tiles(tokens, S::BN);
+        g.dh_blocks = dhidden ? g.splits * g.tm * g.tn_rows : 0;
+        const int blocks = g.dh_blocks + (dhead ? g.tm * g.tn_tokens : 0);
+        hipLaunchKernelGGL((gradients_kernel<E, T, S, PAIRS>), dim3((unsigned)blocks), dim3(S::kThreads), 0, s, a, g);
+        return hipGetLastError();
+    }
     hipError_t backward(const Args& a, const void* hidden, const void* head, void* dhidden, void* dhead) const {
-        hipError_t e = rows(a);
-        if (e != hipSuccess) return e;
-        Operand x, y;
-        if ((e = operand(hidden, a.n, d.hidden_row, p.hidden, y)) != hipSuccess) return e;
-        if (dhead && (e = turn(hidden, a.n, d.hidden_row, p.ldn, p.hidden_t, a.rows)) != hipSuccess) return e;
-        const int across = (int)((a.D + kBM - 1) / kBM);
+        hipError_t e = hipSuccess;
         float* slab = reinterpret_cast<float*>(work + p.slab);
         for (int64_t first = 0; first < a.V; first += p.piece) {
             const int64_t tokens = a.V - first < p.piece ? a.V - first : p.piece, ldv = up(tokens, kStep);
             const E* from = static_cast<const E*>(head) + first * d.head_row;
-            if ((e = operand(from, tokens, d.head_row, p.head_piece, x)) != hipSuccess) return e;
+            Jobs j{};
+            Gradients g{};
+            const Operand x = operand(from, tokens, d.head_row, p.head_piece, j.copy[0]);
+            const Operand y = operand(hidden, a.n, d.hidden_row, p.hidden, j.copy[1]);
+            if (dhead) g.ht = turned_operand(hidden, a.n, d.hidden_row, p.ldn, p.hidden_t, true, j.turn[0]);
+            if (dhidden) g.wt = turned_operand(from, tokens, d.head_row, ldv, p.head_t, false, j.turn[1]);
+            if (first > 0) j.copy[1] = j.turn[0] = Job{};  // made for the first piece
+            if ((e = prepare(a, j, first == 0)) != hipSuccess) return e;
             Errors o{};
             o.e = dhidden ? work + p.e : nullptr;
             o.we = dhead ? work + p.we : nullptr;
@@ -735,30 +966,29 @@ struct Call {
             o.ld_turned = p.ldn;
             o.part_turned = ldv * p.ldn;
             o.first = first;
-            o.tiles = (int32_t)((ldv + kBM - 1) / kBM);
-            hipLaunchKernelGGL((errors_kernel<T, PAIRS>), dim3((unsigned)(o.tiles * ((p.ldn + kBN - 1) / kBN))),
-                               dim3(kThreads), 0, s, a, x, y, (int)(p.ldk / kStep), o);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
-            if (dhead) {
-                const Operand ht{work + p.hidden_t, a.D, p.ldn, a.D * p.ldn};
-                const Operand we{work + p.we, tokens, p.ldn, ldv * p.ldn};
-                hipLaunchKernelGGL((dhead_kernel<E, T, PAIRS>), dim3((unsigned)(across * ((tokens + kBN - 1) / kBN))),
-                                   dim3(kThreads), 0, s, a, ht, we, (int)(p.ldn / kStep), static_cast<E*>(dhead) + first * a.D);
-                if ((e = hipGetLastError()) != hipSuccess) return e;
+            if constexpr (N == 1) {
+                if (p.errors == kBig) e = errors<Big>(a, x, y, o);
             }
-            if (dhidden) {
-                if ((e = turn(from, tokens, d.head_row, ldv, p.head_t, nullptr)) != hipSuccess) return e;
-                const Operand wt{work + p.head_t, a.D, ldv, a.D * ldv};
-                const Operand er{work + p.e, a.n, ldv, a.n * ldv};
-                hipLaunchKernelGGL((dhidden_kernel<T, PAIRS>),
-                                   dim3((unsigned)(p.splits * across * ((a.n + kBN - 1) / kBN))), dim3(kThreads), 0, s, a,
-                                   wt, er, (int)(ldv / kStep), p.splits, slab, p.ldk, first > 0 ? 1 : 0);
-                if ((e = hipGetLastError()) != hipSuccess) return e;
-            }
+            if (p.errors == kMiddle) e = errors<Middle>(a, x, y, o);
+            if (p.errors == kSmall) e = errors<Small>(a, x, y, o);
+            if (e != hipSuccess) return e;
+            g.er = Operand{work + p.e, a.n, ldv, a.n * ldv};
+            g.we = Operand{work + p.we, tokens, p.ldn, ldv * p.ldn};
+            g.slab = slab;
+            g.dhead = dhead ? static_cast<E*>(dhead) + first * a.D : nullptr;
+            g.ld = p.ldk;
+            g.steps_v = (int32_t)(ldv / kStep);
+            g.steps_n = (int32_t)(p.ldn / kStep);
+            g.splits = p.splits;
+            g.add = first > 0 ? 1 : 0;
+            e = p.gradients == kBig      ? gradients<Big>(a, g, dhidden != nullptr, dhead != nullptr, tokens)
+                : p.gradients == kMiddle ? gradients<Middle>(a, g, dhidden != nullptr, dhead != nullptr, tokens)
+                                         : gradients<Small>(a, g, dhidden != nullptr, dhead != nullptr, tokens);
+            if (e != hipSuccess) return e;
         }
         if (dhidden) {
-            hipLaunchKernelGGL(rows_out_kernel<E>, dim3(some_blocks(a.n * a.D, 8192)), dim3(kThreads), 0, s, a, slab, p.ldk,
-                               p.splits, Matrix<T>::kScale, static_cast<E*>(dhidden));
+            hipLaunchKernelGGL(rows_out_kernel<E>, dim3(some_blocks(a.n * ((a.D + 3) / 4), 8192)), dim3(kThreads), 0, s, a,
+                               slab, p.ldk, p.splits, Matrix<T>::kScale, static_cast<E*>(dhidden));
             e = hipGetLastError();
         }
         return e;
