@@ -65,8 +65,8 @@ struct Parts<float> {
     typedef __bf16 T;
     static constexpr int kCount = 3;
 };
-// The products of parts (first, second) that a step of k goes through.
-constexpr int kPairs[6][2] = {{0, 0}, {0, 1}, {1, 0}, {1, 1}, {0, 2}, {2, 0}};
+// The products of parts (first, second), small ones first.
+constexpr int kPairs[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
 
 // An operand: `rows` rows of `k` values at stride ld; 32-bit operands have their parts `part` apart.
 struct Operand {
@@ -171,50 +171,68 @@ __global__ __launch_bounds__(64) void totals_kernel(const Args a) {
 }
 
 // Joins the tiles' maxima and sums, LANES lanes a row: lse, logp, and a sum of the
-// losses per workgroup; of all where there is but one.
+// losses and a count of the rows that take part per workgroup; the loss where there is but one.
 template <int LANES>
 __global__ __launch_bounds__(kThreads) void lse_kernel(const Args a) {
     __shared__ double s[kThreads / 64];
+    __shared__ int64_t s_count[kThreads / 64];
     const int lane = threadIdx.x % LANES;
     double sum = 0.0;
+    int64_t count = 0;
     for (int64_t r = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / LANES; r < a.n;
          r += (int64_t)gridDim.x * kThreads / LANES) {
-        float m = -INFINITY, S = 0.0f;
-        for (int t = lane; t < a.tiles; t += LANES) {
-            const float2 p = a.part[r * a.tiles + t];
-            const float top = fmaxf(m, p.x), from = top == -INFINITY ? 0.0f : top;
-            S = S * fast_exp(m - from) + p.y * fast_exp(p.x - from);
-            m = top;
-        }
-        float top = m;
+        const float2* part = a.part + r * a.tiles;
+        const Row row = row_of(a, r);
+        const bool on = row.target >= 0;
+        const float z = on ? a.at_target[r] : 0.0f;
+        float top = -INFINITY, S = 0.0f;
+#pragma unroll 8
+        for (int t = lane; t < a.tiles; t += LANES) top = fmaxf(top, part[t].x);
 #pragma unroll
         for (int off = LANES / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
         const float from = top == -INFINITY ? 0.0f : top;
-        S = lanes_add(S * fast_exp(m - from), LANES);
+#pragma unroll 8
+        for (int t = lane; t < a.tiles; t += LANES) S = fmaf(part[t].y, fast_exp(part[t].x - from), S);
+        S = lanes_add(S, LANES);
         if (lane != 0) continue;
         const float log_S = __builtin_amdgcn_logf(S) * kLn2;
-        const Row row = a.rows[r];
-        const bool on = row.target >= 0;
-        const float lp = on ? (a.at_target[r] - from) - log_S : 0.0f;
+        const float lp = on ? (z - from) - log_S : 0.0f;
         if (a.logp) a.logp[r] = lp;
         if (a.lse) a.lse[r] = on ? from + log_S : 0.0f;
+        count += on ? 1 : 0;
         // A weight of 0 leaves 0 of an infinite term.
         if (on && !(row.weight == 0.0f && lp == -INFINITY)) sum -= (double)row.weight * (double)lp;
     }
     sum = lanes_add(sum, 64);
-    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = sum;
+    count = lanes_add(count, 64);
+    if ((threadIdx.x & 63) == 0) {
+        s[threadIdx.x >> 6] = sum;
+        s_count[threadIdx.x >> 6] = count;
+    }
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int k = 1; k < kThreads / 64; k++) sum += s[k];
-        if (gridDim.x == 1) *a.loss = (float)(sum * (double)a.totals->share);
-        else a.sums[blockIdx.x] = sum;
+        for (int k = 1; k < kThreads / 64; k++) {
+            sum += s[k];
+            count += s_count[k];
+        }
+        if (gridDim.x == 1) {
+            *a.loss = (float)(sum * (double)totals_of(a, count, 0.0f).share);
+        } else {
+            a.sums[blockIdx.x] = sum;
+            a.counts[blockIdx.x] = count;
+        }
     }
 }
 __global__ __launch_bounds__(64) void loss_kernel(const Args a) {
     double sum = 0.0;
-    for (int k = threadIdx.x; k < a.lse_parts; k += 64) sum += a.sums[k];
+    int64_t count = 0;
+    for (int k = threadIdx.x; k < a.lse_parts; k += 64) {
+        sum += a.sums[k];
+        count += a.counts[k];
+    }
     sum = lanes_add(sum, 64);
-    if (threadIdx.x == 0) *a.loss = (float)(sum * (double)a.totals->share);
+    count = lanes_add(count, 64);
+    if (threadIdx.x == 0) *a.loss = (float)(sum * (double)totals_of(a, count, 0.0f).share);
 }
 
 // --- operands -----------------------------------------------------------------
@@ -332,46 +350,63 @@ __device__ __forceinline__ void meet() {
 }
 
 // A tile of BM x BN of the product by WM x WN waves, each with MI x NJ squares of 16.
-// An operand's tile lies in LDS as rows of 128 bytes; the 16-byte pieces of a row are
-// exchanged by the row's number, so that lanes reading a column of pieces meet all banks.
-// STAGES steps of k are on their way or in use.
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
+// Of a step, an operand's tile lies in LDS as rows of ROW bytes, a tile for each of its N parts; the
+// 16-byte pieces of a row are exchanged by the row's number, so that lanes reading a column of
+// pieces meet all banks.  STAGES steps are on their way or in use.
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int N_ = 1>
 struct Shape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, N = N_;
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves, MI = BM / WM / 16, NJ = BN / WN / 16;
-    static constexpr int kBytes = (BM + BN) * kStep * 2;  // of one step
+    static constexpr int ROW = N == 1 ? 128 : 64, K = ROW / 2;  // bytes and values of a row in a step
+    static constexpr int kBytes = (BM + BN) * ROW * N;          // of a step
     static constexpr int kLds = STAGES * kBytes > BM * BN * 2 ? STAGES * kBytes : BM * BN * 2;
     static constexpr int kWavesPerSimd = kLds > 80 * 1024 ? kWaves / 4 : kWaves / 2;
-    static constexpr int kLoads = (BM + BN) / 8 / kWaves;  // of a wave for one step
-    static_assert(BM / 8 % kWaves == 0 && BN / 8 % kWaves == 0, "waves fetch alike");
+    static constexpr int kRows = 1024 / ROW;                    // of a wave's load
+    static constexpr int kLoads = (BM + BN) / kRows / kWaves * N;  // of a wave for one step
+    static_assert(BM / kRows % kWaves == 0 && BN / kRows % kWaves == 0, "waves fetch alike");
 };
-typedef Shape<256, 256, 2, 4, 2> Big;
-typedef Shape<128, 128, 2, 2, 2> Middle;
-typedef Shape<64, 64, 2, 2, 4> Small;
+// For N parts.  Three parts of 256 x 256 do not fit.
+template <int N>
+struct Shapes {
+    typedef Shape<256, 256, 2, 4, 2> Big;
+    typedef Shape<128, 128, 2, 2, 2> Middle;
+    typedef Shape<64, 64, 2, 2, 4> Small;
+};
+template <>
+struct Shapes<3> {
+    typedef Shape<128, 128, 2, 4, 3, 3> Big, Middle;
+    typedef Shape<64, 64, 2, 2, 3, 3> Small;
+};
 
-template <typename T, typename S, int PAIRS>
+template <typename T, typename S>
 struct Tile {
-    static constexpr int MI = S::MI, NJ = S::NJ;
+    static constexpr int MI = S::MI, NJ = S::NJ, N = S::N;
     typedef typename Matrix<T>::V8 V8;
 
+    static __device__ __forceinline__ int exchanged(int row, int piece) {
+        return S::ROW == 128 ? piece ^ (row & 7) : piece ^ ((row >> 1) & 3);
+    }
     template <int ROWS>
-    static __device__ __forceinline__ void fetch(const Operand& o, int part, int64_t row0, int64_t k, char* lds) {
+    static __device__ __forceinline__ void fetch(const Operand& o, int64_t row0, int64_t k, char* lds) {
         const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-        const int r = lane >> 3, piece = (lane & 7) ^ r;
-        const T* p = static_cast<const T*>(o.p) + part * o.part + k + piece * 8;
+        const int r = lane / (S::ROW / 16), piece = exchanged(r, lane % (S::ROW / 16));
 #pragma unroll
-        for (int i = 0; i < ROWS / 8 / S::kWaves; i++) {
-            const int block = i * S::kWaves + wave;
-            int64_t row = row0 + block * 8 + r;
-            row = row < o.rows ? row : o.rows - 1;  // rows past the end: any, their products are not used
-            load_lds(p + row * o.ld, lds + block * 1024);
+        for (int part = 0; part < N; part++) {
+            const T* p = static_cast<const T*>(o.p) + part * o.part + k + piece * 8;
+#pragma unroll
+            for (int i = 0; i < ROWS / S::kRows / S::kWaves; i++) {
+                const int block = i * S::kWaves + wave;
+                int64_t row = row0 + block * S::kRows + r;
+                row = row < o.rows ? row : o.rows - 1;  // rows past the end: any, their products are not used
+                load_lds(p + row * o.ld, lds + part * ROWS * S::ROW + block * 1024);
+            }
         }
     }
     static __device__ __forceinline__ V8 piece_at(const char* lds, int row, int piece) {
-        return *reinterpret_cast<const V8*>(lds + row * 128 + ((piece ^ (row & 7)) << 4));
+        return *reinterpret_cast<const V8*>(lds + row * S::ROW + (exchanged(row, piece) << 4));
     }
 
-    // acc[i][j][q]: row wave_m + 16 i + 4 (lane / 16) + q of X, row wave_n + 16 j + lane % 16 of Y.
+    // acc[i][j][q]: row wave_m + 16 i + 4 (lane / 16) + q of X, row wave_n + 16 j + lane % 16 of Y; `steps` of kStep.
     static __device__ __forceinline__ void run(const Operand& x, const Operand& y, int64_t x0, int64_t y0, int64_t k0,
                                                int steps, char* lds, F4 (&acc)[MI][NJ]) {
         const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -380,19 +415,15 @@ struct Tile {
         for (int i = 0; i < MI; i++)
 #pragma unroll
             for (int j = 0; j < NJ; j++) acc[i][j] = F4{0.0f, 0.0f, 0.0f, 0.0f};
-        int pair = 0, at = 0, next = 0;  // of the step that is fetched next, and its place
+        int at = 0, next = 0;  // the step that is fetched next, and its place
         const auto fetch_next = [&]() {
-            const int px = PAIRS == 1 ? 0 : kPairs[pair][0], py = PAIRS == 1 ? 0 : kPairs[pair][1];
             char* to = lds + next * S::kBytes;
-            fetch<S::BM>(x, px, x0, k0 + (int64_t)at * kStep, to);
-            fetch<S::BN>(y, py, y0, k0 + (int64_t)at * kStep, to + S::BM * 128);
-            if (++at == steps) {
-                at = 0;
-                pair++;
-            }
+            fetch<S::BM>(x, x0, k0 + (int64_t)at * S::K, to);
+            fetch<S::BN>(y, y0, k0 + (int64_t)at * S::K, to + S::BM * S::ROW * N);
+            at++;
             next = next + 1 == S::STAGES ? 0 : next + 1;
         };
-        const int total = steps * PAIRS;
+        const int total = steps * (kStep / S::K);
         int here = 0;
         meet<0>();  // the last tile's reads
         for (int t = 0; t < S::STAGES - 1 && t < total; t++) fetch_next();
@@ -402,19 +433,26 @@ struct Tile {
             else meet<0>();
             if (t + S::STAGES - 1 < total) fetch_next();
             const char* xs = lds + here * S::kBytes;
-            const char* ys = xs + S::BM * 128;
+            const char* ys = xs + S::BM * S::ROW * N;
             here = here + 1 == S::STAGES ? 0 : here + 1;
 #pragma unroll
-            for (int k = 0; k < kStep / 32; k++) {
-                V8 fx[MI], fy[NJ];
+            for (int k = 0; k < S::K / 32; k++) {
+                V8 fx[N][MI], fy[N][NJ];
 #pragma unroll
-                for (int j = 0; j < NJ; j++) fy[j] = piece_at(ys, n + j * 16, k * 4 + (lane >> 4));
+                for (int part = 0; part < N; part++) {
 #pragma unroll
-                for (int i = 0; i < MI; i++) fx[i] = piece_at(xs, m + i * 16, k * 4 + (lane >> 4));
+                    for (int j = 0; j < NJ; j++) fy[part][j] = piece_at(ys + part * S::BN * S::ROW, n + j * 16, k * 4 + (lane >> 4));
 #pragma unroll
-                for (int i = 0; i < MI; i++)
+                    for (int i = 0; i < MI; i++) fx[part][i] = piece_at(xs + part * S::BM * S::ROW, m + i * 16, k * 4 + (lane >> 4));
+                }
+                constexpr int PAIRS = N == 1 ? 1 : 6;
 #pragma unroll
-                    for (int j = 0; j < NJ; j++) acc[i][j] = Matrix<T>::mfma(fx[i], fy[j], acc[i][j]);
+                for (int pair = 0; pair < PAIRS; pair++)
+#pragma unroll
+                    for (int i = 0; i < MI; i++)
+#pragma unroll
+                        for (int j = 0; j < NJ; j++)
+                            acc[i][j] = Matrix<T>::mfma(fx[N == 1 ? 0 : kPairs[pair][0]][i], fy[N == 1 ? 0 : kPairs[pair][1]][j], acc[i][j]);
             }
         }
         meet<0>();
@@ -436,11 +474,11 @@ __device__ __forceinline__ Place place_of(int b, int tm, int tn) {
 
 // Maximum and sum of exponentials of a tile's logits, per row, and the targets' logits;
 // `first` is the token of the head's first row.
-template <typename T, typename S, int PAIRS>
+template <typename T, typename S>
 __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void logits_kernel(const Args a, const Operand head,
                                                                                const Operand hidden, int steps,
                                                                                int64_t first, int tm, int tn) {
-    typedef Tile<T, S, PAIRS> Tl;
+    typedef Tile<T, S> Tl;
     __shared__ __attribute__((aligned(16))) char lds[S::STAGES * S::kBytes];
     const Place at = place_of(blockIdx.x, tm, tn);
     const int64_t v0 = (int64_t)at.m * S::BM, r0 = (int64_t)at.n * S::BN;
@@ -463,7 +501,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void logits_kernel(c
     for (int j = 0; j < Tl::NJ; j++) {
         const int in = wn * Tl::NJ * 16 + j * 16 + (lane & 15);
         const int64_t r = r0 + in;
-        const int64_t y = (r < a.n ? a.rows[r].target : -1) - v;
+        const int64_t y = (r < a.n ? row_of(a, r).target : -1) - v;
         float m = -INFINITY;
 #pragma unroll
         for (int i = 0; i < Tl::MI; i++)
@@ -533,12 +571,12 @@ struct Errors {
     int64_t ld, part, ld_turned, part_turned;
     int64_t first;     // token of the piece
 };
-template <typename T, typename S, int PAIRS>
+template <typename T, typename S>
 __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void errors_kernel(const Args a, const Operand head,
                                                                                const Operand hidden, int steps,
                                                                                const Errors o, int tm, int tn) {
-    typedef Tile<T, S, PAIRS> Tl;
-    constexpr int N = PAIRS == 1 ? 1 : 3;
+    typedef Tile<T, S> Tl;
+    constexpr int N = S::N;
     __shared__ __attribute__((aligned(16))) char lds[S::kLds];
     const Place at = place_of(blockIdx.x, tm, tn);
     const int64_t v0 = (int64_t)at.m * S::BM, r0 = (int64_t)at.n * S::BN;
@@ -622,9 +660,9 @@ struct Gradients {
     int32_t steps_v, steps_n, splits, add;
     int32_t dh_blocks, tm, tn_rows, tn_tokens;  // tiles across D, down the rows and the tokens
 };
-template <typename E, typename T, typename S, int PAIRS>
+template <typename E, typename T, typename S>
 __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gradients_kernel(const Args a, const Gradients g) {
-    typedef Tile<T, S, PAIRS> Tl;
+    typedef Tile<T, S> Tl;
     __shared__ __attribute__((aligned(16))) char lds[S::kLds];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / S::WN, wn = wave % S::WN;
     const int dt = wm * Tl::MI * 16 + (lane >> 4) * 4, nt = wn * Tl::NJ * 16 + (lane & 15);  // in the tile
@@ -737,8 +775,9 @@ inline int64_t tiles(int64_t x, int64_t m) { return (x + m - 1) / m; }
 // Sizes of tiles.  Few rows leave the products to memory, and small tiles keep many
 // steps on their way; otherwise big ones where they fill the GPU.
 enum Size { kSmall, kMiddle, kBig };
-Size size_of(int64_t m, int64_t n, int64_t rows) {
+Size size_of(int64_t m, int64_t n, int64_t rows, int parts) {
     if (rows <= 64) return kSmall;
+    if (parts > 1) return kMiddle;
     return tiles(m, 256) * tiles(n, 256) >= 192 ? kBig : kMiddle;
 }
 int edge(Size s) { return s == kBig ? 256 : s == kMiddle ? 128 : 64; }
@@ -771,10 +810,9 @@ Plan plan_of(const gear_token_desc& d) {
     p.piece = piece < d.V ? piece : d.V;
     p.loss_piece = kPieceTokens < d.V ? kPieceTokens : d.V;
     p.ldv = up(p.piece, kStep);
-    p.logits = size_of(p.loss_piece, d.n, d.n);
-    p.errors = size_of(p.piece, d.n, d.n);
-    if (p.parts > 1 && p.errors == kBig) p.errors = kMiddle;  // three parts of a big tile's values leave the registers
-    p.gradients = d.n <= 64 ? kSmall : d.D < 192 ? kMiddle : size_of(d.D, p.piece + d.n, d.n);
+    p.logits = size_of(p.loss_piece, d.n, d.n, p.parts);
+    p.errors = size_of(p.piece, d.n, d.n, p.parts);
+    p.gradients = d.n <= 64 ? kSmall : d.D < 192 ? kMiddle : size_of(d.D, p.piece + d.n, d.n, p.parts);
     p.tiles = (int)tiles(d.V, edge(p.logits));
     // Few tiles of dh share the GPU's 256 units by splitting the tokens.
     const int64_t dh = tiles(d.D, edge(p.gradients)) * tiles(d.n, edge(p.gradients)), steps = p.ldv / kStep;
@@ -854,7 +892,10 @@ Args args_of(const gear_token_desc& d, const Plan& p, char* work) {
 template <typename E>
 struct Call {
     typedef typename Parts<E>::T T;
-    static constexpr int N = Parts<E>::kCount, PAIRS = N == 1 ? 1 : 6;
+    static constexpr int N = Parts<E>::kCount;
+    typedef typename Shapes<N>::Big Big;
+    typedef typename Shapes<N>::Middle Middle;
+    typedef typename Shapes<N>::Small Small;
     const gear_token_desc& d;
     const Plan p;
     char* work;
@@ -892,7 +933,7 @@ struct Call {
     template <typename S>
     hipError_t logits(const Args& a, const Operand& x, const Operand& y, int64_t first) const {
         const int tm = (int)tiles(x.rows, S::BM), tn = (int)tiles(a.n, S::BN);
-        hipLaunchKernelGGL((logits_kernel<T, S, PAIRS>), dim3((unsigned)(tm * tn)), dim3(S::kThreads), 0, s, a, x, y,
+        hipLaunchKernelGGL((logits_kernel<T, S>), dim3((unsigned)(tm * tn)), dim3(S::kThreads), 0, s, a, x, y,
                            (int)(p.ldk / kStep), first, tm, tn);
         return hipGetLastError();
     }
@@ -909,17 +950,13 @@ struct Call {
         a.at_target = reinterpret_cast<float*>(work + p.at_target);
         a.part = reinterpret_cast<float2*>(work + p.part);
         hipError_t e = hipSuccess;
-        if (a.n == 0) {
-            Jobs j{};
-            if ((e = prepare(a, j, true)) != hipSuccess) return e;
-        }
         for (int64_t first = 0; first < a.V && a.n > 0; first += p.loss_piece) {
             const int64_t tokens = a.V - first < p.loss_piece ? a.V - first : p.loss_piece;
             Jobs j{};
             const Operand x = operand(static_cast<const E*>(head) + first * d.head_row, tokens, d.head_row, p.head, j.copy[0]);
             Operand y = operand(hidden, a.n, d.hidden_row, p.hidden, j.copy[1]);
             if (first > 0) j.copy[1] = Job{};
-            if ((e = prepare(a, j, first == 0)) != hipSuccess) return e;
+            if ((e = prepare(a, j, false)) != hipSuccess) return e;
             e = p.logits == kBig ? logits<Big>(a, x, y, first) : p.logits == kMiddle ? logits<Middle>(a, x, y, first)
                                                                                       : logits<Small>(a, x, y, first);
             if (e != hipSuccess) return e;
@@ -930,7 +967,7 @@ struct Call {
     template <typename S>
     hipError_t errors(const Args& a, const Operand& x, const Operand& y, const Errors& o) const {
         const int tm = (int)tiles(o.ld, S::BM), tn = (int)tiles(p.ldn, S::BN);
-        hipLaunchKernelGGL((errors_kernel<T, S, PAIRS>), dim3((unsigned)(tm * tn)), dim3(S::kThreads), 0, s, a, x, y,
+        hipLaunchKernelGGL((errors_kernel<T, S>), dim3((unsigned)(tm * tn)), dim3(S::kThreads), 0, s, a, x, y,
                            (int)(p.ldk / kStep), o, tm, tn);
         return hipGetLastError();
     }
@@ -941,7 +978,7 @@ struct Call {
         g.tn_tokens = (int)tiles(tokens, S::BN);
         g.dh_blocks = dhidden ? g.splits * g.tm * g.tn_rows : 0;
         const int blocks = g.dh_blocks + (dhead ? g.tm * g.tn_tokens : 0);
-        hipLaunchKernelGGL((gradients_kernel<E, T, S, PAIRS>), dim3((unsigned)blocks), dim3(S::kThreads), 0, s, a, g);
+        hipLaunchKernelGGL((gradients_kernel<E, T, S>), dim3((unsigned)blocks), dim3(S::kThreads), 0, s, a, g);
         return hipGetLastError();
     }
     hipError_t backward(const Args& a, const void* hidden, const void* head, void* dhidden, void* dhead) const {
@@ -966,11 +1003,8 @@ struct Call {
             o.ld_turned = p.ldn;
             o.part_turned = ldv * p.ldn;
             o.first = first;
-            if constexpr (N == 1) {
-                if (p.errors == kBig) e = errors<Big>(a, x, y, o);
-            }
-            if (p.errors == kMiddle) e = errors<Middle>(a, x, y, o);
-            if (p.errors == kSmall) e = errors<Small>(a, x, y, o);
+            e = p.errors == kBig ? errors<Big>(a, x, y, o) : p.errors == kMiddle ? errors<Middle>(a, x, y, o)
+                                                                                  : errors<Small>(a, x, y, o);
             if (e != hipSuccess) return e;
             g.er = Operand{work + p.e, a.n, ldv, a.n * ldv};
             g.we = Operand{work + p.we, tokens, p.ldn, ldv * p.ldn};
