@@ -472,6 +472,13 @@ __device__ __forceinline__ Place place_of(int b, int tm, int tn) {
     return Place{first + in % high, in / high};
 }
 
+// exp(z - top).  Beside 16-bit products one operation less: from = top log2 e, rounded, costs
+// up to |top| 2^-24 of the result.
+template <int N>
+__device__ __forceinline__ float exp_from(float z, float top, float from) {
+    return N == 1 ? __builtin_amdgcn_exp2f(fmaf(z, kLog2e, -from)) : fast_exp(z - top);
+}
+
 // Maximum and sum of exponentials of a tile's logits, per row, and the targets' logits;
 // `first` is the token of the head's first row.
 template <typename T, typename S>
@@ -516,12 +523,12 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void logits_kernel(c
         }
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
-        const float from = m == -INFINITY ? 0.0f : m;
+        const float top = m == -INFINITY ? 0.0f : m, from = top * kLog2e;
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < Tl::MI; i++)
 #pragma unroll
-            for (int q = 0; q < 4; q++) sum += fast_exp(acc[i][j][q] - from);
+            for (int q = 0; q < 4; q++) sum += exp_from<S::N>(acc[i][j][q], top, from);
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (lane < 16) {
@@ -593,15 +600,32 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void errors_kernel(c
         const bool on = row.target >= 0;
         const float lse = on ? a.lse_in[r] : 0.0f;
         w[j] = on && top != 0.0f ? row.weight / top : 0.0f;
-        const int64_t left = a.V - o.first - v0 - vt, y = row.target - (o.first + v0 + vt);
+        const float from = lse * kLog2e;
 #pragma unroll
         for (int i = 0; i < Tl::MI; i++)
 #pragma unroll
             for (int q = 0; q < 4; q++) {
-                float x = fast_exp(acc[i][j][q] - lse);
-                if (y == i * 16 + q) x -= 1.0f;
-                acc[i][j][q] = on && i * 16 + q < left ? x * Matrix<T>::kScale : 0.0f;
+                const float x = exp_from<N>(acc[i][j][q], lse, from);
+                acc[i][j][q] = on ? Matrix<T>::kScale * x : 0.0f;
             }
+        const int64_t y = row.target - (o.first + v0 + vt);
+        if (on && y >= 0 && y < Tl::MI * 16 && (y & 15) < 4) {
+#pragma unroll
+            for (int i = 0; i < Tl::MI; i++)
+#pragma unroll
+                for (int q = 0; q < 4; q++)
+                    if (y == i * 16 + q) acc[i][j][q] -= Matrix<T>::kScale;
+        }
+    }
+    if (o.first + v0 + S::BM > a.V) {
+        const int64_t left = a.V - o.first - v0 - vt;
+#pragma unroll
+        for (int i = 0; i < Tl::MI; i++)
+#pragma unroll
+            for (int j = 0; j < Tl::NJ; j++)
+#pragma unroll
+                for (int q = 0; q < 4; q++)
+                    if (i * 16 + q >= left) acc[i][j][q] = 0.0f;
     }
     // The parts of both orders in turn; a part is taken off what remains.
     typedef T T4 __attribute__((ext_vector_type(4)));
@@ -617,12 +641,17 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void errors_kernel(c
             for (int j = 0; j < Tl::NJ; j++)
 #pragma unroll
                 for (int i = 0; i < Tl::MI; i++) {
+                    const F4 x = order == 0 ? acc[i][j] : acc[i][j] * w[j];
                     T4 e;
+                    if constexpr (N == 1) {
+                        e = __builtin_convertvector(x, T4);
+                    } else {
 #pragma unroll
-                    for (int q = 0; q < 4; q++) {
-                        T p[N];
-                        cut<T, N>(order == 0 ? acc[i][j][q] : acc[i][j][q] * w[j], p);
-                        e[q] = p[part];
+                        for (int q = 0; q < 4; q++) {
+                            T p[N];
+                            cut<T, N>(x[q], p);
+                            e[q] = p[part];
+                        }
                     }
                     uint2 bits = __builtin_bit_cast(uint2, e);
                     if (order == 0) {
