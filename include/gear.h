@@ -908,7 +908,7 @@ int gear_grad_norm(const gear_step_tensor *tensors, int64_t count, float scale, 
 /* Constants of gear_adamw. */
 typedef struct gear_adamw_desc {
     int32_t state_bits;     /* 32 or 8, of the averages */
-    double lr, beta1, beta2, eps, weight_decay;  /* lr, weight_decay 0 or more, betas in [0, 1), eps above 0 (in 32 bits) */
+    double lr, beta1, beta2, eps, weight_decay;  /* lr, weight_decay 0 or more, betas in [0, 1), eps 2^-126 or more */
     const float *d_lr;      /* one float that takes lr's place, read on the device, or NULL */
     const float *d_factor;  /* one float that multiplies the gradients, read on the device, or NULL for 1 */
 } gear_adamw_desc;

@@ -7,6 +7,9 @@
 //
 // Tensors travel in the kernel's arguments, 56 a launch, so a call needs no table
 // on the device and a captured call keeps its own.
+//
+// The bytes bound it: 218 M bf16 values with masters and 32-bit averages, their norm
+// among it, take 1120 to 1280 us (boxes differ), 5.1 to 5.9 TB/s; a plain copy reaches 5.1.
 #include <math.h>
 
 #include "element.h"
@@ -17,8 +20,13 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kValues = 8;                           // values a lane takes at a time
-constexpr int kChunk = kThreads * kValues * 4;       // values of a workgroup
+constexpr int kRound = kThreads * kValues;           // values of a workgroup at a time
+// Values of a workgroup: four rounds, or one where the whole step has few (26000 values in 13
+// tensors: the update takes 8.6 us with four, 5 with one).
+constexpr int kChunk = 4 * kRound;
+constexpr int64_t kFewValues = 1 << 21;
 constexpr int kItems = 56;                           // tensors of one launch
+constexpr int kGrads = 160;                          // gradients of one launch of the norm
 constexpr int kGroup = GEAR_STEP_BLOCK / kValues;    // lanes of an 8-bit block
 constexpr int kNormBlocks = 1024;
 constexpr float kTop = 448.0f, kLeast = 0.001953125f;  // e4m3: its largest value, and its least above 0
@@ -30,20 +38,28 @@ struct Item {
     float *master, *ms, *vs;
     int64_t n;
 };
-struct Items {
-    Item item[kItems];
-    uint32_t first[kItems + 1];  // chunks before each tensor
-    int32_t count;
+struct Grad {
+    const void* grad;
+    int64_t n;
 };
+template <typename I, int N>
+struct List {
+    I item[N];
+    uint32_t first[N + 1];  // chunks before each tensor
+    int32_t count, chunk;   // values of a chunk
+};
+typedef List<Item, kItems> Items;
+typedef List<Grad, kGrads> Grads;
 
 // What a step multiplies by; made once on the device.
 struct Factors {
-    float grad, decay, rate, root;  // factor, 1 - lr weight_decay, lr / (1 - beta1^s), 1 / (1 - beta2^s)
+    float grad, decay, rate, root;  // factor, 1 - lr weight_decay, lr / (1 - beta1^s), (1 - beta2^s)^-1/2
     int32_t skip;
 };
 
 // The tensor that a chunk belongs to.
-__device__ __forceinline__ int item_of(const Items& t, uint32_t chunk) {
+template <typename L>
+__device__ __forceinline__ int item_of(const L& t, uint32_t chunk) {
     int lo = 0, hi = t.count;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -53,19 +69,19 @@ __device__ __forceinline__ int item_of(const Items& t, uint32_t chunk) {
     return lo;
 }
 
-template <int N, typename E>
+template <int N, bool STREAM, typename E>
 __device__ __forceinline__ void load(const E* p, int64_t left, float (&f)[N]) {
     if (left >= N) {
-        Vec<E, N>::unpack(Vec<E, N>::load(p), f);
+        Vec<E, N>::unpack(Vec<E, N>::template load<STREAM>(p), f);
     } else {
 #pragma unroll
         for (int j = 0; j < N; j++) f[j] = j < left ? (float)p[j] : 0.0f;
     }
 }
-template <int N, typename E>
+template <int N, bool STREAM, typename E>
 __device__ __forceinline__ void store(E* p, int64_t left, const float (&f)[N]) {
     if (left >= N) {
-        Vec<E, N>::store(p, f);
+        Vec<E, N>::template store<STREAM>(p, f);
     } else {
 #pragma unroll
         for (int j = 0; j < N; j++)
@@ -75,10 +91,18 @@ __device__ __forceinline__ void store(E* p, int64_t left, const float (&f)[N]) {
 
 typedef uint32_t Bytes __attribute__((ext_vector_type(2)));
 typedef Bytes LooseBytes __attribute__((aligned(1)));
+// The root by the hardware's instruction, which is within one unit, of normal numbers alone: what is smaller is scaled.
+__device__ __forceinline__ float root_of(float v) {
+    const bool small = v < 1.2621774e-29f;  // 2^-96
+    const float r = __builtin_amdgcn_sqrtf(small ? v * 1.8446744e19f : v);
+    return small ? r * 2.3283064e-10f : r;
+}
+template <bool STREAM>
 __device__ __forceinline__ void load8(const uint8_t* p, int64_t left, float scale, float (&f)[kValues]) {
     Bytes b = {0, 0};
     if (left >= kValues) {
-        b = *reinterpret_cast<const LooseBytes*>(p);
+        const LooseBytes* at = reinterpret_cast<const LooseBytes*>(p);
+        b = STREAM ? __builtin_nontemporal_load(at) : *at;
     } else {
 #pragma unroll
         for (int j = 0; j < kValues; j++)
@@ -95,6 +119,7 @@ __device__ __forceinline__ void load8(const uint8_t* p, int64_t left, float scal
     }
 }
 // A lane's values of a block, under the block's scale, which is returned.
+template <bool STREAM>
 __device__ __forceinline__ float store8(uint8_t* p, int64_t left, const float (&f)[kValues]) {
     float top = 0.0f;
 #pragma unroll
@@ -102,7 +127,7 @@ __device__ __forceinline__ float store8(uint8_t* p, int64_t left, const float (&
 #pragma unroll
     for (int off = 1; off < kGroup; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
     const bool some = top >= kNothing;
-    const float inv = some ? kTop / top : 0.0f;
+    const float inv = some ? kTop * __builtin_amdgcn_rcpf(top) : 0.0f;
     Bytes b;
 #pragma unroll
     for (int j = 0; j < kValues; j += 4) {
@@ -120,13 +145,15 @@ __device__ __forceinline__ float store8(uint8_t* p, int64_t left, const float (&
         b[j / 4] = (uint32_t)w;
     }
     if (left >= kValues) {
-        *reinterpret_cast<LooseBytes*>(p) = b;
+        LooseBytes* at = reinterpret_cast<LooseBytes*>(p);
+        if (STREAM) __builtin_nontemporal_store(b, at);
+        else *at = b;
     } else {
 #pragma unroll
         for (int j = 0; j < kValues; j++)
             if (j < left) p[j] = (uint8_t)(b[j / 4] >> (8 * (j % 4)));
     }
-    return some ? top / kTop : 0.0f;
+    return some ? top * (1.0f / kTop) : 0.0f;
 }
 
 // The step's factors, and the step counted; one lane.
@@ -142,7 +169,7 @@ __global__ void factors_kernel(Factors* out, int64_t* step, const float* d_lr, c
         f.grad = factor;
         f.decay = (float)(1.0 - lr * weight_decay);
         f.rate = (float)(lr / -expm1(s * log1));
-        f.root = (float)(1.0 / -expm1(s * log2));
+        f.root = (float)sqrt(1.0 / -expm1(s * log2));
     }
     *out = f;
 }
@@ -151,31 +178,31 @@ struct Betas {
     float b1, c1, b2, c2, eps;  // c = 1 - b
 };
 
-template <typename E, bool MASTER, bool BITS8>
+template <typename E, bool MASTER, bool BITS8, bool STREAM>
 __global__ __launch_bounds__(kThreads) void update_kernel(const Items t, const Betas b, const Factors* factors) {
     const Factors f = *factors;
     if (f.skip) return;
     for (uint32_t chunk = blockIdx.x; chunk < t.first[t.count]; chunk += gridDim.x) {
         const int k = item_of(t, chunk);
         const Item& it = t.item[k];
-        const int64_t base = (int64_t)(chunk - t.first[k]) * kChunk;
-        const int64_t end = it.n - base < kChunk ? it.n : base + kChunk;
+        const int64_t base = (int64_t)(chunk - t.first[k]) * t.chunk;
+        const int64_t end = it.n - base < t.chunk ? it.n : base + t.chunk;
         // Whole lanes of a block stay together: its scale is theirs together.
-        for (int64_t at = base; at < end; at += kThreads * kValues) {
+        for (int64_t at = base; at < end; at += kRound) {
             const int64_t i = at + threadIdx.x * kValues, left = end - i;
             float g[kValues], p[kValues], m[kValues], v[kValues];
-            load<kValues>(static_cast<const E*>(it.grad) + i, left, g);
-            if (MASTER) load<kValues>(it.master + i, left, p);
-            else load<kValues>(static_cast<const E*>(it.param) + i, left, p);
+            load<kValues, STREAM>(static_cast<const E*>(it.grad) + i, left, g);
+            if (MASTER) load<kValues, STREAM>(it.master + i, left, p);
+            else load<kValues, STREAM>(static_cast<const E*>(it.param) + i, left, p);
             if (BITS8) {
                 const bool in = left > 0;
-                load8(static_cast<const uint8_t*>(it.m) + i, left, in ? it.ms[i / GEAR_STEP_BLOCK] : 0.0f, m);
-                load8(static_cast<const uint8_t*>(it.v) + i, left, in ? it.vs[i / GEAR_STEP_BLOCK] : 0.0f, v);
+                load8<STREAM>(static_cast<const uint8_t*>(it.m) + i, left, in ? it.ms[i / GEAR_STEP_BLOCK] : 0.0f, m);
+                load8<STREAM>(static_cast<const uint8_t*>(it.v) + i, left, in ? it.vs[i / GEAR_STEP_BLOCK] : 0.0f, v);
 #pragma unroll
                 for (int j = 0; j < kValues; j++) v[j] *= v[j];
             } else {
-                load<kValues>(static_cast<const float*>(it.m) + i, left, m);
-                load<kValues>(static_cast<const float*>(it.v) + i, left, v);
+                load<kValues, STREAM>(static_cast<const float*>(it.m) + i, left, m);
+                load<kValues, STREAM>(static_cast<const float*>(it.v) + i, left, v);
             }
             float r[kValues];
 #pragma unroll
@@ -183,21 +210,22 @@ __global__ __launch_bounds__(kThreads) void update_kernel(const Items t, const B
                 const float x = g[j] * f.grad;
                 m[j] = b.b1 * m[j] + b.c1 * x;
                 v[j] = b.b2 * v[j] + b.c2 * (x * x);
-                if (BITS8) r[j] = sqrtf(v[j]);
-                p[j] = p[j] * f.decay - f.rate * m[j] / (sqrtf(v[j] * f.root) + b.eps);
+                r[j] = root_of(v[j]);
+                // eps is a normal number, and so its reciprocal is finite.
+                p[j] = p[j] * f.decay - f.rate * m[j] * __builtin_amdgcn_rcpf(r[j] * f.root + b.eps);
             }
-            if (MASTER) store<kValues>(it.master + i, left, p);
-            store<kValues>(static_cast<E*>(it.param) + i, left, p);
+            if (MASTER) store<kValues, STREAM>(it.master + i, left, p);
+            store<kValues, STREAM>(static_cast<E*>(it.param) + i, left, p);
             if (BITS8) {
-                const float sm = store8(static_cast<uint8_t*>(it.m) + i, left, m);
-                const float sv = store8(static_cast<uint8_t*>(it.v) + i, left, r);
+                const float sm = store8<STREAM>(static_cast<uint8_t*>(it.m) + i, left, m);
+                const float sv = store8<STREAM>(static_cast<uint8_t*>(it.v) + i, left, r);
                 if (left > 0 && (threadIdx.x & (kGroup - 1)) == 0) {
                     it.ms[i / GEAR_STEP_BLOCK] = sm;
                     it.vs[i / GEAR_STEP_BLOCK] = sv;
                 }
             } else {
-                store<kValues>(static_cast<float*>(it.m) + i, left, m);
-                store<kValues>(static_cast<float*>(it.v) + i, left, v);
+                store<kValues, STREAM>(static_cast<float*>(it.m) + i, left, m);
+                store<kValues, STREAM>(static_cast<float*>(it.v) + i, left, v);
             }
         }
     }
@@ -216,18 +244,18 @@ __device__ __forceinline__ double block_add(double v, double* s) {
 
 // Squares of the gradients, a sum per workgroup; ADD to those of the launches before.
 template <typename E>
-__global__ __launch_bounds__(kThreads) void squares_kernel(const Items t, double* sums, int add) {
+__global__ __launch_bounds__(kThreads) void squares_kernel(const Grads t, double* sums, int add) {
     __shared__ double s[kThreads / 64];
     double sum = 0.0;
     for (uint32_t chunk = blockIdx.x; chunk < t.first[t.count]; chunk += gridDim.x) {
         const int k = item_of(t, chunk);
-        const Item& it = t.item[k];
-        const int64_t base = (int64_t)(chunk - t.first[k]) * kChunk;
-        const int64_t end = it.n - base < kChunk ? it.n : base + kChunk;
-        for (int64_t at = base; at < end; at += kThreads * kValues) {
+        const Grad& it = t.item[k];
+        const int64_t base = (int64_t)(chunk - t.first[k]) * t.chunk;
+        const int64_t end = it.n - base < t.chunk ? it.n : base + t.chunk;
+        for (int64_t at = base; at < end; at += kRound) {
             const int64_t i = at + threadIdx.x * kValues;
             float g[kValues];
-            load<kValues>(static_cast<const E*>(it.grad) + i, end - i, g);
+            load<kValues, false>(static_cast<const E*>(it.grad) + i, end - i, g);
 #pragma unroll
             for (int j = 0; j < kValues; j++) sum = fma((double)g[j], (double)g[j], sum);
         }
@@ -267,7 +295,7 @@ const char* flaw(const gear_adamw_desc* d, const gear_step_tensor* t, int64_t co
     if (!(d->lr >= 0.0) || !(d->lr < 3e38) || !(d->weight_decay >= 0.0) || !(d->weight_decay < 3e38))
         return "lr or weight_decay below 0 or not finite";
     if (!(d->beta1 >= 0.0 && d->beta1 < 1.0) || !(d->beta2 >= 0.0 && d->beta2 < 1.0)) return "betas must lie in [0, 1)";
-    if (!((float)d->eps > 0.0f) || !(d->eps < 3e38)) return "eps must be above 0 in 32 bits, and finite";
+    if (!((float)d->eps >= 1.17549435e-38f) || !(d->eps < 3e38)) return "eps must be 2^-126 or more, and finite";
     for (int64_t i = 0; i < count; i++) {
         if (t[i].n == 0) continue;
         if (t[i].d_param == nullptr || t[i].d_exp_avg == nullptr || t[i].d_exp_avg_sq == nullptr)
@@ -279,30 +307,43 @@ const char* flaw(const gear_adamw_desc* d, const gear_step_tensor* t, int64_t co
     return nullptr;
 }
 
+void set(Item& to, const gear_step_tensor& t) {
+    to = Item{t.d_grad, t.d_param, t.d_exp_avg, t.d_exp_avg_sq, t.d_master, t.d_exp_avg_scale, t.d_exp_avg_sq_scale, t.n};
+}
+void set(Grad& to, const gear_step_tensor& t) { to = Grad{t.d_grad, t.n}; }
+
 // Fills `out` with tensors from `i` on that `want` accepts; true when there are any.
-template <typename F>
-bool gather(const gear_step_tensor* t, int64_t count, int64_t& i, Items& out, F want) {
+template <typename I, int N, typename F>
+bool gather(const gear_step_tensor* t, int64_t count, int64_t& i, List<I, N>& out, F want) {
     out.count = 0;
     out.first[0] = 0;
-    for (; i < count && out.count < kItems; i++) {
+    for (; i < count && out.count < N; i++) {
         if (t[i].n == 0 || !want(t[i])) continue;
-        const uint64_t chunks = (uint64_t)((t[i].n + kChunk - 1) / kChunk);
+        const uint64_t chunks = (uint64_t)((t[i].n + out.chunk - 1) / out.chunk);
         if (out.first[out.count] + chunks > 0xFFFFFFFFull) break;  // the next launch's
-        out.item[out.count] = Item{t[i].d_grad, t[i].d_param, t[i].d_exp_avg, t[i].d_exp_avg_sq,
-                                   t[i].d_master, t[i].d_exp_avg_scale, t[i].d_exp_avg_sq_scale, t[i].n};
+        set(out.item[out.count], t[i]);
         out.first[out.count + 1] = (uint32_t)(out.first[out.count] + chunks);
         out.count++;
     }
     return out.count > 0;
 }
+int64_t values_of(const gear_step_tensor* t, int64_t count) {
+    int64_t n = 0;
+    for (int64_t i = 0; i < count; i++) n += t[i].n;
+    return n;
+}
 
 typedef void (*Update)(const Items, const Betas, const Factors*);
-template <bool BITS8>
+template <bool BITS8, bool STREAM = false>
 Update update_of(int32_t dtype, bool master) {
-    if (dtype == GEAR_DTYPE_F32) return update_kernel<float, false, BITS8>;
-    if (dtype == GEAR_DTYPE_BF16) return master ? update_kernel<__bf16, true, BITS8> : update_kernel<__bf16, false, BITS8>;
-    return master ? update_kernel<_Float16, true, BITS8> : update_kernel<_Float16, false, BITS8>;
+    if (dtype == GEAR_DTYPE_F32) return update_kernel<float, false, BITS8, STREAM>;
+    if (dtype == GEAR_DTYPE_BF16) return master ? update_kernel<__bf16, true, BITS8, STREAM> : update_kernel<__bf16, false, BITS8, STREAM>;
+    return master ? update_kernel<_Float16, true, BITS8, STREAM> : update_kernel<_Float16, false, BITS8, STREAM>;
 }
+// With 8-bit averages, what no cache holds until the next step passes by it: 123 M values
+// with masters, a step with its norm, 428 us, and 461 through the caches.  With 32-bit averages
+// that gains nothing (218 M values: 1306 and 1278).
+constexpr int64_t kStreamValues = 16 << 20;
 
 }  // namespace
 }  // namespace gear
@@ -329,7 +370,9 @@ extern "C" int gear_grad_norm(const gear_step_tensor* tensors, int64_t count, fl
     hipStream_t s = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();  // an error pending from an earlier HIP call is not this call's
     int blocks = 0;  // sums that the launches so far have left
-    Items items;
+    Grads items;
+    const int64_t values = values_of(tensors, count);
+    items.chunk = values < kFewValues ? kRound : kChunk;
     hipError_t e = hipSuccess;
     const int32_t types[3] = {GEAR_DTYPE_F32, GEAR_DTYPE_BF16, GEAR_DTYPE_F16};
     for (const int32_t type : types) {
@@ -338,7 +381,8 @@ extern "C" int gear_grad_norm(const gear_step_tensor* tensors, int64_t count, fl
         int64_t i = 0;
         while (gather(tensors, count, i, items, [&](const gear_step_tensor& t) { return t.dtype == type; })) {
             // Later launches add to all sums of the first, so they are as many workgroups.
-            const int grid = used ? used : kNormBlocks;
+            const int64_t most = values / items.chunk + count;
+            const int grid = (int)(most < kNormBlocks ? most : kNormBlocks);
             const auto kernel = type == GEAR_DTYPE_F32 ? squares_kernel<float>
                                 : type == GEAR_DTYPE_BF16 ? squares_kernel<__bf16> : squares_kernel<_Float16>;
             hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, s, items, sums + blocks, used ? 1 : 0);
@@ -370,6 +414,9 @@ extern "C" int gear_adamw(const gear_adamw_desc* d, const gear_step_tensor* tens
     if (e != hipSuccess) return hip_fail(e, "gear_adamw: factor launch");
     const Betas b{(float)d->beta1, (float)(1.0 - d->beta1), (float)d->beta2, (float)(1.0 - d->beta2), (float)d->eps};
     Items items;
+    const int64_t values = values_of(tensors, count);
+    items.chunk = values < kFewValues ? kRound : kChunk;
+    const bool past = d->state_bits == 8 && values >= kStreamValues;
     const int32_t types[3] = {GEAR_DTYPE_F32, GEAR_DTYPE_BF16, GEAR_DTYPE_F16};
     for (const int32_t type : types) {
         for (int master = 0; master < 2; master++) {
@@ -377,8 +424,8 @@ extern "C" int gear_adamw(const gear_adamw_desc* d, const gear_step_tensor* tens
             while (gather(tensors, count, i, items, [&](const gear_step_tensor& t) {
                 return t.dtype == type && (t.d_master != nullptr) == (master != 0);
             })) {
-                const Update kernel = d->state_bits == 8 ? update_of<true>(type, master != 0)
-                                                         : update_of<false>(type, master != 0);
+                const Update kernel = d->state_bits == 32 ? update_of<false>(type, master != 0)
+                                      : past ? update_of<true, true>(type, master != 0) : update_of<true>(type, master != 0);
                 const uint32_t chunks = items.first[items.count];
                 const uint32_t grid = chunks < (1u << 20) ? chunks : 1u << 20;
                 hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, s, items, b, factors);
