@@ -282,7 +282,7 @@ __device__ __forceinline__ void get8(const E* p, int64_t left, float (&f)[8]) {
 struct Job {
     const void* src;
     void* dst;
-    int64_t rows, cols, ld_src, ld, part;
+    int64_t rows, cols, ld_src, len, ld, part;  // len: of a row of dst, in whole steps
     int32_t first;  // workgroup
     int32_t on;
 };
@@ -293,7 +293,7 @@ struct Jobs {
 template <typename E>
 __device__ __forceinline__ void run_copy(const Job& j, int block, int blocks) {
     typedef typename Parts<E>::T T;
-    const int64_t per_row = j.ld / 8;
+    const int64_t per_row = j.len / 8;
     for (int64_t i = (int64_t)block * kThreads + threadIdx.x; i < j.rows * per_row; i += (int64_t)blocks * kThreads) {
         const int64_t r = i / per_row, c = i % per_row * 8;
         float f[8];
@@ -305,7 +305,7 @@ template <typename E>
 __device__ __forceinline__ void run_turn(const Args& a, const Job& j, int block, int blocks, float (*tile)[65]) {
     typedef typename Parts<E>::T T;
     static_assert(kThreads == 512, "a lane takes 8 values of the tile");
-    const int64_t down = j.ld / 64, across = (j.cols + 63) / 64;
+    const int64_t down = j.len / 64, across = (j.cols + 63) / 64;
     const int at = threadIdx.x >> 3, k = (threadIdx.x & 7) * 8;
     for (int64_t t = block; t < down * across; t += blocks) {
         // Neighbouring workgroups go along the rows, so that lines are read whole.
@@ -575,6 +575,7 @@ __device__ __forceinline__ uint2 turned(uint2 x) {
 // largest, turned, we[tokens][ld_turned].
 struct Errors {
     void *e, *we;      // either may be NULL
+    int64_t tokens, rows;  // of the piece and of all, in whole steps
     int64_t ld, part, ld_turned, part_turned;
     int64_t first;     // token of the piece
 };
@@ -666,13 +667,14 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void errors_kernel(c
             // 16 bytes a lane, rows of the tile after each other.
             constexpr int COLS[2] = {S::BM, S::BN}, ROWS[2] = {S::BN, S::BM};
             const int64_t row0 = order == 0 ? r0 : v0, col0 = order == 0 ? v0 : r0;
-            const int64_t rows = order == 0 ? a.n : o.ld, ld = order == 0 ? o.ld : o.ld_turned;
+            const int64_t rows = order == 0 ? a.n : o.tokens, cols = order == 0 ? o.tokens : o.rows;
+            const int64_t ld = order == 0 ? o.ld : o.ld_turned;
             T* to = static_cast<T*>(out) + part * (order == 0 ? o.part : o.part_turned);
 #pragma unroll 4
             for (int k = threadIdx.x; k < ROWS[order] * (COLS[order] / 8); k += S::kThreads) {
                 const int row = k / (COLS[order] / 8), col = k % (COLS[order] / 8) * 8;
                 const char* from = order == 0 ? spot<S::BM>(lds, row, col) : spot<S::BN>(lds, row, col);
-                if (row0 + row < rows && col0 + col < ld)
+                if (row0 + row < rows && col0 + col < cols)
                     *reinterpret_cast<Line*>(to + (row0 + row) * ld + col0 + col) = *reinterpret_cast<const Line*>(from);
             }
         }
@@ -799,6 +801,8 @@ __global__ __launch_bounds__(kThreads) void rows_out_kernel(const Args a, const 
 // --- the plan -------------------------------------------------------------------
 
 inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+// Rows that begin whole kilobytes apart would meet in few channels of the L2.
+inline int64_t pitch(int64_t len) { return len % 512 == 0 ? len + 64 : len; }
 inline int64_t tiles(int64_t x, int64_t m) { return (x + m - 1) / m; }
 
 // Sizes of tiles.  Few rows leave the products to memory, and small tiles keep many
@@ -858,18 +862,18 @@ Plan plan_of(const gear_token_desc& d) {
     p.sums = take(kParts * sizeof(double));
     p.counts = take(kParts * sizeof(int64_t));
     p.tops = take(kParts * sizeof(float));
-    p.hidden = take(d.n * p.ldk * p.parts * 2);
+    p.hidden = take(d.n * pitch(p.ldk) * p.parts * 2);
     const int64_t common = at;
     p.at_target = take(d.n * 4);
     p.part = take(d.n * (int64_t)p.tiles * (int64_t)sizeof(float2));
-    p.head = take(p.loss_piece * p.ldk * p.parts * 2);
+    p.head = take(p.loss_piece * pitch(p.ldk) * p.parts * 2);
     p.bytes_loss = at;
     at = common;
-    p.head_piece = take(p.piece * p.ldk * p.parts * 2);
-    p.hidden_t = take(d.D * p.ldn * p.parts * 2);
-    p.head_t = take(d.D * p.ldv * p.parts * 2);
-    p.e = take(d.n * p.ldv * p.parts * 2);
-    p.we = take(p.ldv * p.ldn * p.parts * 2);
+    p.head_piece = take(p.piece * pitch(p.ldk) * p.parts * 2);
+    p.hidden_t = take(d.D * pitch(p.ldn) * p.parts * 2);
+    p.head_t = take(d.D * (p.ldv + 64) * p.parts * 2);
+    p.e = take(d.n * (p.ldv + 64) * p.parts * 2);
+    p.we = take(p.ldv * pitch(p.ldn) * p.parts * 2);
     p.slab = take(p.splits * d.n * p.ldk * 4);
     p.bytes_backward = at;
     return p;
@@ -933,12 +937,13 @@ struct Call {
     // An operand of rows as they lie, or of a copy that `job` makes.
     Operand operand(const void* src, int64_t rows, int64_t ld_src, int64_t to, Job& job) const {
         if (plain_rows(d.dtype, src, ld_src, d.D)) return Operand{src, rows, ld_src, 0};
-        job = Job{src, work + to, rows, d.D, ld_src, p.ldk, rows * p.ldk, 0, 0};
-        return Operand{work + to, rows, p.ldk, rows * p.ldk};
+        job = Job{src, work + to, rows, d.D, ld_src, p.ldk, pitch(p.ldk), rows * pitch(p.ldk), 0, 0};
+        return Operand{work + to, rows, pitch(p.ldk), rows * pitch(p.ldk)};
     }
     // A turned copy: d.D rows of ld values.
-    Operand turned_operand(const void* src, int64_t rows, int64_t ld_src, int64_t ld, int64_t to, bool on, Job& job) const {
-        job = Job{src, work + to, rows, d.D, ld_src, ld, d.D * ld, 0, on ? 1 : 0};
+    Operand turned_operand(const void* src, int64_t rows, int64_t ld_src, int64_t len, int64_t to, bool on, Job& job) const {
+        const int64_t ld = pitch(len);
+        job = Job{src, work + to, rows, d.D, ld_src, len, ld, d.D * ld, 0, on ? 1 : 0};
         return Operand{work + to, d.D, ld, d.D * ld};
     }
     // Nothing to do costs no launch.
@@ -946,11 +951,11 @@ struct Call {
         int32_t at = j.row_blocks = rows ? a.row_parts : 0;
         for (Job& c : j.copy) {
             c.first = at;
-            if (c.src) at += (int32_t)some_blocks(c.rows * (c.ld / 8), 4096);
+            if (c.src) at += (int32_t)some_blocks(c.rows * (c.len / 8), 4096);
         }
         for (Job& c : j.turn) {
             c.first = at;
-            if (c.src) at += (int32_t)(tiles(c.ld, 64) * tiles(c.cols, 64) < 8192 ? tiles(c.ld, 64) * tiles(c.cols, 64) : 8192);
+            if (c.src) at += (int32_t)(tiles(c.len, 64) * tiles(c.cols, 64) < 8192 ? tiles(c.len, 64) * tiles(c.cols, 64) : 8192);
         }
         j.blocks = at;
         if (at == 0) return hipSuccess;
@@ -995,7 +1000,7 @@ struct Call {
 
     template <typename S>
     hipError_t errors(const Args& a, const Operand& x, const Operand& y, const Errors& o) const {
-        const int tm = (int)tiles(o.ld, S::BM), tn = (int)tiles(p.ldn, S::BN);
+        const int tm = (int)tiles(o.tokens, S::BM), tn = (int)tiles(p.ldn, S::BN);
         hipLaunchKernelGGL((errors_kernel<T, S>), dim3((unsigned)(tm * tn)), dim3(S::kThreads), 0, s, a, x, y,
                            (int)(p.ldk / kStep), o, tm, tn);
         return hipGetLastError();
@@ -1027,16 +1032,18 @@ struct Call {
             Errors o{};
             o.e = dhidden ? work + p.e : nullptr;
             o.we = dhead ? work + p.we : nullptr;
-            o.ld = ldv;
-            o.part = a.n * ldv;
-            o.ld_turned = p.ldn;
-            o.part_turned = ldv * p.ldn;
+            o.tokens = ldv;
+            o.rows = p.ldn;
+            o.ld = pitch(ldv);
+            o.part = a.n * o.ld;
+            o.ld_turned = pitch(p.ldn);
+            o.part_turned = ldv * o.ld_turned;
             o.first = first;
             e = p.errors == kBig ? errors<Big>(a, x, y, o) : p.errors == kMiddle ? errors<Middle>(a, x, y, o)
                                                                                   : errors<Small>(a, x, y, o);
             if (e != hipSuccess) return e;
-            g.er = Operand{work + p.e, a.n, ldv, a.n * ldv};
-            g.we = Operand{work + p.we, tokens, p.ldn, ldv * p.ldn};
+            g.er = Operand{work + p.e, a.n, o.ld, o.part};
+            g.we = Operand{work + p.we, tokens, o.ld_turned, o.part_turned};
             g.slab = slab;
             g.dhead = dhead ? static_cast<E*>(dhead) + first * a.D : nullptr;
             g.ld = p.ldk;
