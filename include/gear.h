@@ -840,10 +840,11 @@ int gear_token_loss_sizes(const gear_token_desc *d, int64_t *loss_bytes, int64_t
  *   d_logp, d_lse     float[n] or NULL; 0 for rows that take no part
  *   d_work            workspace; its contents do not matter
  *
- * Products of 16-bit values are exact and added in 32 bits; 32-bit values enter
- * the products in three 16-bit parts, their six largest products: as exact as
- * products in 32 bits, but an infinity among 32-bit values counts as NaN.  A NaN in a
- * row that takes part, or in the head, shows in the loss.
+ * Products of 16-bit values are exact and added in 32 bits.  32-bit values enter as
+ * two fp16 parts under a power of two that the largest finite value of the tensor
+ * sets (of hidden, of the rows that take part): off by 2^-22 of the value, or 2^-39 of the
+ * largest where that is more.  An infinity among them counts as NaN.  A NaN in a row
+ * that takes part, or in the head, shows in the loss.
  * Results repeat bit for bit.
  * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
  */
@@ -863,7 +864,7 @@ int gear_token_loss(const gear_token_desc *d, const void *d_hidden, const void *
  *   d_dhead      [V][D], contiguous, or NULL: not written
  *
  * The logits are formed again, a piece of the vocabulary at a time, and e is
- * rounded once to the products' type (three parts for 32-bit values).
+ * rounded once to the products' type (two fp16 parts for 32-bit values), fp16 times 2^14.
  * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
  */
 int gear_token_loss_backward(const gear_token_desc *d, const void *d_hidden, const void *d_head, const float *d_lse,

@@ -12,9 +12,12 @@
 // orders, a piece of the vocabulary at a time.  The copies pad k to whole steps with
 // zeros, so odd sizes and alignments end there.
 //
-// 32-bit values are cut into three bf16 parts a = a1 + a2 + a3 (8 bits each); the six
-// products a1 b1, a1 b2, a2 b1, a2 b2, a1 b3, a3 b1 leave an error of 2^-25 of |a b|,
-// and matrix instructions of 16-bit types are 16 times as fast as those of 32.
+// 32-bit values are cut into two fp16 parts, a 2^s = a1 + a2 (11 bits each), s making the
+// tensor's largest finite value 2^14 to 2^15; a part is off by 2^-22 of the value, or by 2^-40
+// of the largest where the value is far below it.  The products a1 b1, a1 b2 and a2 b1 leave out
+// 2^-22 of |a b| at most.  Matrix instructions of 16-bit types are 16 times as fast as those of 32
+// bits, so three of them take a fifth of the time.  (Three bf16 parts need no scale and leave
+// 2^-25, but six products: 1000 x 512 x 8192, forward and backward, took 245 us with them and takes 175.)
 #include <math.h>
 
 #include <type_traits>
@@ -62,11 +65,11 @@ struct Parts {
 };
 template <>
 struct Parts<float> {
-    typedef __bf16 T;
-    static constexpr int kCount = 3;
+    typedef _Float16 T;
+    static constexpr int kCount = 2;
 };
 // The products of parts (first, second), small ones first.
-constexpr int kPairs[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
+constexpr int kPairs[3][2] = {{1, 0}, {0, 1}, {0, 0}};
 
 // An operand: `rows` rows of `k` values at stride ld; 32-bit operands have their parts `part` apart.
 struct Operand {
@@ -84,6 +87,10 @@ struct Totals {
     float share;     // 1 / denom
     float weight;    // largest |weight| of a row that takes part
 };
+// Powers of two that 32-bit hidden values and the head are multiplied by before they are cut.
+struct Scales {
+    int32_t hidden, head;
+};
 
 struct Args {
     const void* target;
@@ -92,13 +99,15 @@ struct Args {
     float *loss, *logp, *lse;
     Row* rows;
     Totals* totals;
+    Scales* scales;    // of 32-bit values
+    uint32_t* largest; // [2][kParts]: largest finite magnitudes of hidden and head, a workgroup each
     double* sums;      // [kParts]
     int64_t* counts;   // [kParts]
     float* tops;       // [kParts]
     float2* part;      // [n][tiles]: maximum and sum of a tile of tokens
     float* at_target;  // [n]: the target's logit
     int64_t n, D, V, mask_group, weight_group;
-    int32_t target_dtype, tiles, row_parts, lse_parts;
+    int32_t target_dtype, tiles, row_parts, lse_parts, max_parts;
     float denom, grad_scale;
 };
 
@@ -237,21 +246,75 @@ __global__ __launch_bounds__(64) void loss_kernel(const Args a) {
 
 // --- operands -----------------------------------------------------------------
 
-// A value's parts.  Each is the rest so far, rounded; one that rounds to an infinity is cut instead.
+// A value's parts: each is the rest so far, rounded.  An infinity or a NaN is one in both.
 template <typename T, int N>
 __device__ __forceinline__ void cut(float v, T (&part)[N]) {
-    if (N == 1) {
-        part[0] = (T)v;
-        return;
-    }
 #pragma unroll
     for (int k = 0; k < N; k++) {
-        T h = (T)v;
-        if (!(fabsf((float)h) < INFINITY) && fabsf(v) < INFINITY) h = __builtin_bit_cast(T, (uint16_t)(__builtin_bit_cast(uint32_t, v) >> 16));
-        part[k] = h;
-        v = fabsf(v) < INFINITY ? v - (float)h : 0.0f;
+        part[k] = (T)v;
+        v -= (float)part[k];
     }
 }
+
+// The power of two that takes `top`, a finite magnitude, to 2^14 .. 2^15; none for 0.
+__device__ __forceinline__ int32_t scale_for(uint32_t top) {
+    return top == 0 ? 0 : 15 - __builtin_amdgcn_frexp_expf(__builtin_bit_cast(float, top));
+}
+// Largest finite magnitudes of 32-bit hidden rows that take part and of the head: a.max_parts workgroups each.
+__global__ __launch_bounds__(kThreads) void largest_kernel(const Args a, const float* hidden, int64_t hidden_row,
+                                                           const float* head, int64_t head_row) {
+    __shared__ uint32_t s[kThreads / 64];
+    const bool first = (int)blockIdx.x < a.max_parts;
+    const int64_t rows = first ? a.n : a.V, ld = first ? hidden_row : head_row;
+    const float* p = first ? hidden : head;
+    const int64_t pieces = (a.D + 3) / 4;
+    uint32_t top = 0;
+    for (int64_t i = (int64_t)(blockIdx.x % a.max_parts) * kThreads + threadIdx.x; i < rows * pieces;
+         i += (int64_t)a.max_parts * kThreads) {
+        const int64_t r = i / pieces, c = i % pieces * 4;
+        if (first && row_of(a, r).target < 0) continue;
+        float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (c + 4 <= a.D) {
+            Vec<float, 4>::unpack(Vec<float, 4>::load(p + r * ld + c), f);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; q++)
+                if (c + q < a.D) f[q] = p[r * ld + c + q];
+        }
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const uint32_t m = __builtin_bit_cast(uint32_t, f[q]) & 0x7FFFFFFFu;  // in the magnitudes' order
+            if (m < 0x7F800000u && m > top) top = m;
+        }
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off));
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int k = 1; k < kThreads / 64; k++) top = max(top, s[k]);
+        a.largest[(first ? 0 : kParts) + blockIdx.x % a.max_parts] = top;
+    }
+}
+// The scales, in every thread of a workgroup.
+__device__ __forceinline__ Scales find_scales(const Args& a) {
+    __shared__ uint32_t s[2][kThreads / 64];
+    static_assert(kThreads >= kParts, "a lane for each workgroup's");
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        uint32_t top = (int)threadIdx.x < a.max_parts ? a.largest[q * kParts + threadIdx.x] : 0;
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off));
+        if ((threadIdx.x & 63) == 0) s[q][threadIdx.x >> 6] = top;
+    }
+    __syncthreads();
+    uint32_t top[2] = {0, 0};
+#pragma unroll
+    for (int q = 0; q < 2; q++)
+        for (int k = 0; k < kThreads / 64; k++) top[q] = max(top[q], s[q][k]);
+    return Scales{scale_for(top[0]), scale_for(top[1])};
+}
+
 // The parts of 8 values in a row, to `to` and, `part` values apart, behind it.
 template <typename T, int N>
 __device__ __forceinline__ void put8(const float (&f)[8], T* to, int64_t part) {
@@ -291,18 +354,22 @@ struct Jobs {
     int32_t row_blocks, blocks;  // workgroups that look at the rows, the first ones; of all
 };
 template <typename E>
-__device__ __forceinline__ void run_copy(const Job& j, int block, int blocks) {
+__device__ __forceinline__ void run_copy(const Job& j, int32_t by, int block, int blocks) {
     typedef typename Parts<E>::T T;
     const int64_t per_row = j.len / 8;
     for (int64_t i = (int64_t)block * kThreads + threadIdx.x; i < j.rows * per_row; i += (int64_t)blocks * kThreads) {
         const int64_t r = i / per_row, c = i % per_row * 8;
         float f[8];
         get8(static_cast<const E*>(j.src) + r * j.ld_src + c, j.cols - c, f);
+        if (Parts<E>::kCount > 1) {
+#pragma unroll
+            for (int q = 0; q < 8; q++) f[q] = ldexpf(f[q], by);
+        }
         put8<T, Parts<E>::kCount>(f, static_cast<T*>(j.dst) + r * j.ld + c, j.part);
     }
 }
 template <typename E>
-__device__ __forceinline__ void run_turn(const Args& a, const Job& j, int block, int blocks, float (*tile)[65]) {
+__device__ __forceinline__ void run_turn(const Args& a, const Job& j, int32_t by, int block, int blocks, float (*tile)[65]) {
     typedef typename Parts<E>::T T;
     static_assert(kThreads == 512, "a lane takes 8 values of the tile");
     const int64_t down = j.len / 64, across = (j.cols + 63) / 64;
@@ -315,7 +382,7 @@ __device__ __forceinline__ void run_turn(const Args& a, const Job& j, int block,
         get8(static_cast<const E*>(j.src) + (r0 + at) * j.ld_src + c0 + k, in ? j.cols - c0 - k : 0, f);
         __syncthreads();
 #pragma unroll
-        for (int q = 0; q < 8; q++) tile[at][k + q] = f[q];
+        for (int q = 0; q < 8; q++) tile[at][k + q] = Parts<E>::kCount > 1 ? ldexpf(f[q], by) : f[q];
         __syncthreads();
         if (c0 + at < j.cols) {
 #pragma unroll
@@ -324,16 +391,23 @@ __device__ __forceinline__ void run_turn(const Args& a, const Job& j, int block,
         }
     }
 }
-// What has to be done before a product, in one launch: workgroups for each job.
+// What has to be done before a product, in one launch: workgroups for each job; copies of
+// the head and of hidden rows, then hidden rows and the head turned.
 template <typename E>
 __global__ __launch_bounds__(kThreads) void prepare_kernel(const Args a, const Jobs jobs) {
     __shared__ float tile[64][65];
+    Scales by{0, 0};
+    if constexpr (Parts<E>::kCount > 1) {
+        by = find_scales(a);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.scales = by;
+    }
     const int b = blockIdx.x;
     if (b < jobs.row_blocks) return look_at_rows(a, b);
-    if (b < jobs.copy[1].first) return run_copy<E>(jobs.copy[0], b - jobs.copy[0].first, jobs.copy[1].first - jobs.copy[0].first);
-    if (b < jobs.turn[0].first) return run_copy<E>(jobs.copy[1], b - jobs.copy[1].first, jobs.turn[0].first - jobs.copy[1].first);
-    if (b < jobs.turn[1].first) return run_turn<E>(a, jobs.turn[0], b - jobs.turn[0].first, jobs.turn[1].first - jobs.turn[0].first, tile);
-    run_turn<E>(a, jobs.turn[1], b - jobs.turn[1].first, jobs.blocks - jobs.turn[1].first, tile);
+    const int copy1 = jobs.copy[1].first, turn0 = jobs.turn[0].first, turn1 = jobs.turn[1].first;
+    if (b < copy1) return run_copy<E>(jobs.copy[0], by.head, b - jobs.copy[0].first, copy1 - jobs.copy[0].first);
+    if (b < turn0) return run_copy<E>(jobs.copy[1], by.hidden, b - copy1, turn0 - copy1);
+    if (b < turn1) return run_turn<E>(a, jobs.turn[0], by.hidden, b - turn0, turn1 - turn0, tile);
+    run_turn<E>(a, jobs.turn[1], by.head, b - turn1, jobs.blocks - turn1, tile);
 }
 
 // --- the tile loop --------------------------------------------------------------
@@ -365,7 +439,7 @@ struct Shape {
     static constexpr int kLoads = (BM + BN) / kRows / kWaves * N;  // of a wave for one step
     static_assert(BM / kRows % kWaves == 0 && BN / kRows % kWaves == 0, "waves fetch alike");
 };
-// For N parts.  Three parts of 256 x 256 do not fit.
+// For N parts.
 template <int N>
 struct Shapes {
     typedef Shape<256, 256, 2, 4, 2> Big;
@@ -373,9 +447,10 @@ struct Shapes {
     typedef Shape<64, 64, 2, 2, 4> Small;
 };
 template <>
-struct Shapes<3> {
-    typedef Shape<128, 128, 2, 4, 3, 3> Big, Middle;
-    typedef Shape<64, 64, 2, 2, 3, 3> Small;
+struct Shapes<2> {
+    typedef Shape<256, 256, 2, 4, 2, 2> Big;
+    typedef Shape<128, 128, 2, 2, 2, 2> Middle;
+    typedef Shape<64, 64, 2, 2, 4, 2> Small;
 };
 
 template <typename T, typename S>
@@ -445,7 +520,7 @@ struct Tile {
 #pragma unroll
                     for (int i = 0; i < MI; i++) fx[part][i] = piece_at(xs + part * S::BM * S::ROW, m + i * 16, k * 4 + (lane >> 4));
                 }
-                constexpr int PAIRS = N == 1 ? 1 : 6;
+                constexpr int PAIRS = N == 1 ? 1 : 3;
 #pragma unroll
                 for (int pair = 0; pair < PAIRS; pair++)
 #pragma unroll
@@ -472,6 +547,18 @@ __device__ __forceinline__ Place place_of(int b, int tm, int tn) {
     return Place{first + in % high, in / high};
 }
 
+// Products of scaled values.
+template <typename S>
+__device__ __forceinline__ void unscale(F4 (&acc)[S::MI][S::NJ], const Scales& by) {
+    const int32_t e = -by.hidden - by.head;
+#pragma unroll
+    for (int i = 0; i < S::MI; i++)
+#pragma unroll
+        for (int j = 0; j < S::NJ; j++)
+#pragma unroll
+            for (int q = 0; q < 4; q++) acc[i][j][q] = ldexpf(acc[i][j][q], e);
+}
+
 // exp(z - top).  Beside 16-bit products one operation less: from = top log2 e, rounded, costs
 // up to |top| 2^-24 of the result.
 template <int N>
@@ -495,6 +582,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void logits_kernel(c
     float* s_max = reinterpret_cast<float*>(lds);  // [WM][BN]
     float* s_sum = s_max + S::WM * S::BN;
     const int64_t v = first + v0 + wm * Tl::MI * 16 + (lane >> 4) * 4;
+    if (S::N > 1) unscale<S>(acc, *a.scales);
     if (first + v0 + S::BM > a.V) {
 #pragma unroll
         for (int i = 0; i < Tl::MI; i++)
@@ -592,6 +680,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void errors_kernel(c
     Tl::run(head, hidden, v0, r0, 0, steps, lds, acc);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / S::WN, wn = wave % S::WN;
     const int vt = wm * Tl::MI * 16 + (lane >> 4) * 4, rt = wn * Tl::NJ * 16 + (lane & 15);  // in the tile
+    if (S::N > 1) unscale<S>(acc, *a.scales);
     const float top = a.totals->weight;
     float w[Tl::NJ];
 #pragma unroll
@@ -642,7 +731,10 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void errors_kernel(c
             for (int j = 0; j < Tl::NJ; j++)
 #pragma unroll
                 for (int i = 0; i < Tl::MI; i++) {
-                    const F4 x = order == 0 ? acc[i][j] : acc[i][j] * w[j];
+                    F4 x = order == 0 ? acc[i][j] : acc[i][j] * w[j];
+                    // A product rounded to 32 bits: folded into the cut it would be rounded otherwise for one part
+                    // than for the other.  And it is cut anew: parts kept from the last time would fill the registers.
+                    if (N > 1) asm volatile("" : "+v"(x));
                     T4 e;
                     if constexpr (N == 1) {
                         e = __builtin_convertvector(x, T4);
@@ -681,16 +773,30 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void errors_kernel(c
     }
 }
 
+// Times f 2^e, which together may lie in range where neither alone does.
+struct Factor {
+    float m;
+    int32_t e;
+    __device__ __forceinline__ Factor(float f, int32_t exponent)
+        : m(__builtin_amdgcn_frexp_mantf(f)), e(__builtin_amdgcn_frexp_expf(f) + exponent) {}
+    __device__ __forceinline__ float operator()(float x) const { return ldexpf(x * m, e); }
+};
+
 // Both gradients of a piece in one launch, the workgroups of dh first: their k is longer.
 struct Gradients {
     Operand wt, er;         // of dh: W^T, e
     Operand ht, we;         // of dW: h^T, (c e)^T
     float* slab;            // [splits][n][ld]: dh so far; a split of the piece's tokens each
+    float* slab_head;       // [splits_n][tokens][ld]: dW where the rows are split
     void* dhead;            // the piece's first row
     int64_t ld;
-    int32_t steps_v, steps_n, splits, add;
+    int32_t steps_v, steps_n, splits, splits_n, add;
     int32_t dh_blocks, tm, tn_rows, tn_tokens;  // tiles across D, down the rows and the tokens
 };
+template <typename T>
+__device__ __forceinline__ float head_factor(const Args& a) {
+    return a.totals->weight * a.totals->share * a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / Matrix<T>::kScale;
+}
 template <typename E, typename T, typename S>
 __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gradients_kernel(const Args a, const Gradients g) {
     typedef Tile<T, S> Tl;
@@ -718,12 +824,28 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gradients_kerne
         }
         return;
     }
-    const Place at = place_of(blockIdx.x - g.dh_blocks, g.tm, g.tn_tokens);
+    const int split = (blockIdx.x - g.dh_blocks) % g.splits_n;
+    const Place at = place_of((blockIdx.x - g.dh_blocks) / g.splits_n, g.tm, g.tn_tokens);
     const int64_t d0 = (int64_t)at.m * S::BM, v0 = (int64_t)at.n * S::BN;
-    Tl::run(g.ht, g.we, d0, v0, 0, g.steps_n, lds, acc);
-    const float by = a.totals->weight * a.totals->share * a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / Matrix<T>::kScale;
+    const int from = (int)((int64_t)g.steps_n * split / g.splits_n), to = (int)((int64_t)g.steps_n * (split + 1) / g.splits_n);
+    Tl::run(g.ht, g.we, d0, v0, (int64_t)from * kStep, to - from, lds, acc);
+    if (g.splits_n > 1) {
+#pragma unroll
+        for (int j = 0; j < Tl::NJ; j++) {
+            const int64_t v = v0 + nt + j * 16;
+            if (v >= g.we.rows) continue;
+#pragma unroll
+            for (int i = 0; i < Tl::MI; i++) {
+                const int64_t d = d0 + dt + i * 16;
+                if (d < g.ld) *reinterpret_cast<F4*>(g.slab_head + (split * g.we.rows + v) * g.ld + d) = acc[i][j];
+            }
+        }
+        return;
+    }
+    const float by = head_factor<T>(a);
     E* out = static_cast<E*>(g.dhead);
     if constexpr (sizeof(E) == 4) {
+        const Factor times(by, -a.scales->hidden);
         // 16 bytes a lane as they are.
 #pragma unroll
         for (int j = 0; j < Tl::NJ; j++) {
@@ -734,7 +856,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gradients_kerne
                 const int64_t d = d0 + dt + i * 16;
                 float f[4];
 #pragma unroll
-                for (int q = 0; q < 4; q++) f[q] = acc[i][j][q] * by;
+                for (int q = 0; q < 4; q++) f[q] = times(acc[i][j][q]);
                 if (d + 4 <= a.D) {
                     Vec<E, 4>::store(out + v * a.D + d, f);
                 } else {
@@ -773,27 +895,41 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gradients_kerne
     }
 }
 
-// The splits' sums, times the row's share.
-template <typename E>
-__global__ __launch_bounds__(kThreads) void rows_out_kernel(const Args a, const float* slab, int64_t ld, int splits,
-                                                            float held, E* out) {
-    const float by = a.totals->share * a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / held;
-    const int64_t per_row = (a.D + 3) / 4;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < a.n * per_row; i += (int64_t)gridDim.x * kThreads) {
+// Sums over the splits of dW of a piece, and of dh after the last piece, times what
+// each is to be multiplied by: dh of a.n rows, or none, then `tokens` rows of dW, or none.
+template <typename E, typename T>
+__global__ __launch_bounds__(kThreads) void splits_kernel(const Args a, const Gradients g, int64_t tokens, E* dhidden) {
+    const int64_t per_row = (a.D + 3) / 4, rows = dhidden ? a.n : 0;
+    const float by = a.totals->share * a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / Matrix<T>::kScale;
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < (rows + tokens) * per_row;
+         i += (int64_t)gridDim.x * kThreads) {
         const int64_t r = i / per_row, d = i % per_row * 4;
-        const Row row = a.rows[r];
+        const bool head = r >= rows;
+        const float* slab = head ? g.slab_head + (r - rows) * g.ld + d : g.slab + r * g.ld + d;
+        const int64_t next = (head ? tokens : a.n) * g.ld;
+        const int splits = head ? g.splits_n : g.splits;
+        E* out = head ? static_cast<E*>(g.dhead) + (r - rows) * a.D + d : dhidden + r * a.D + d;
+        const Row row = head ? Row{0, 0.0f} : a.rows[r];
         F4 v = {0.0f, 0.0f, 0.0f, 0.0f};
         if (row.target >= 0) {
-            for (int k = 0; k < splits; k++) v += *reinterpret_cast<const F4*>(slab + (k * a.n + r) * ld + d);
-            v *= row.weight * by;
+#pragma unroll 4
+            for (int k = 0; k < splits; k++) v += *reinterpret_cast<const F4*>(slab + k * next);
+            const float f = head ? head_factor<T>(a) : row.weight * by;
+            if constexpr (sizeof(E) == 4) {
+                const Factor times(f, head ? -a.scales->hidden : -a.scales->head);
+#pragma unroll
+                for (int q = 0; q < 4; q++) v[q] = times(v[q]);
+            } else {
+                v *= f;
+            }
         }
         const float f[4] = {v[0], v[1], v[2], v[3]};
         if (d + 4 <= a.D) {
-            Vec<E, 4>::store(out + r * a.D + d, f);
+            Vec<E, 4>::store(out, f);
         } else {
 #pragma unroll
             for (int q = 0; q < 4; q++)
-                if (d + q < a.D) out[r * a.D + d + q] = (E)f[q];
+                if (d + q < a.D) out[q] = (E)f[q];
         }
     }
 }
@@ -806,11 +942,13 @@ inline int64_t pitch(int64_t len) { return len % 512 == 0 ? len + 64 : len; }
 inline int64_t tiles(int64_t x, int64_t m) { return (x + m - 1) / m; }
 
 // Sizes of tiles.  Few rows leave the products to memory, and small tiles keep many
-// steps on their way; otherwise big ones where they fill the GPU.
+// steps on their way; few tiles leave units idle, and small ones are more (300 rows of 2048, 1000
+// tokens, bf16: 58 us, and 84 with middle ones; 8192 x 512 x 1000, 512 middle tiles: 99 with small
+// ones and 88); otherwise big ones where they fill the GPU.
 enum Size { kSmall, kMiddle, kBig };
-Size size_of(int64_t m, int64_t n, int64_t rows, int parts) {
+Size size_of(int64_t m, int64_t n, int64_t rows) {
     if (rows <= 64) return kSmall;
-    if (parts > 1) return kMiddle;
+    if (tiles(m, 128) * tiles(n, 128) < 256) return kSmall;
     return tiles(m, 256) * tiles(n, 256) >= 192 ? kBig : kMiddle;
 }
 int edge(Size s) { return s == kBig ? 256 : s == kMiddle ? 128 : 64; }
@@ -822,9 +960,9 @@ struct Plan {
     int64_t piece = 0, loss_piece = 0;   // tokens of a piece, backward and forward
     Size logits = kMiddle, errors = kMiddle, gradients = kMiddle;
     int tiles = 0;                       // tiles of tokens, forward
-    int splits = 0;
-    int64_t rows = 0, totals = 0, sums = 0, counts = 0, tops = 0, at_target = 0, part = 0;
-    int64_t hidden = 0, head = 0, head_piece = 0, hidden_t = 0, head_t = 0, e = 0, we = 0, slab = 0;
+    int splits = 0, splits_n = 0;        // of the tokens for dh, of the rows for dW
+    int64_t rows = 0, totals = 0, scales = 0, largest = 0, sums = 0, counts = 0, tops = 0, at_target = 0, part = 0;
+    int64_t hidden = 0, head = 0, head_piece = 0, hidden_t = 0, head_t = 0, e = 0, we = 0, slab = 0, slab_head = 0;
     int64_t bytes_loss = 0, bytes_backward = 0;
 };
 
@@ -835,7 +973,7 @@ bool plain_rows(int32_t dtype, const void* p, int64_t row, int64_t D) {
 // The workspace holds what any alignment of the operands needs.
 Plan plan_of(const gear_token_desc& d) {
     Plan p;
-    p.parts = d.dtype == GEAR_DTYPE_F32 ? 3 : 1;
+    p.parts = d.dtype == GEAR_DTYPE_F32 ? Parts<float>::kCount : 1;
     p.ldk = up(d.D, kStep);
     p.ldn = up(d.n, kStep);
     int64_t piece = kPieceValues / (d.n > 0 ? d.n : 1) / p.parts / 256 * 256;
@@ -843,14 +981,19 @@ Plan plan_of(const gear_token_desc& d) {
     p.piece = piece < d.V ? piece : d.V;
     p.loss_piece = kPieceTokens < d.V ? kPieceTokens : d.V;
     p.ldv = up(p.piece, kStep);
-    p.logits = size_of(p.loss_piece, d.n, d.n, p.parts);
-    p.errors = size_of(p.piece, d.n, d.n, p.parts);
-    p.gradients = d.n <= 64 ? kSmall : d.D < 192 ? kMiddle : size_of(d.D, p.piece + d.n, d.n, p.parts);
+    p.logits = size_of(p.loss_piece, d.n, d.n);
+    p.errors = size_of(p.piece, d.n, d.n);
+    p.gradients = d.n <= 64 ? kSmall : size_of(d.D, p.piece + d.n, d.n);
     p.tiles = (int)tiles(d.V, edge(p.logits));
     // Few tiles of dh share the GPU's 256 units by splitting the tokens.
     const int64_t dh = tiles(d.D, edge(p.gradients)) * tiles(d.n, edge(p.gradients)), steps = p.ldv / kStep;
     p.splits = 1;
     while (dh * p.splits < 256 && p.splits * 8 <= steps && p.splits < 16) p.splits *= 2;
+    // So do few tiles of dW, splitting the rows: 65536 rows of 64, a head of 18, bf16, forward and backward take 93 us so
+    // and 1490 with the rows in one piece.
+    const int64_t dw = tiles(d.D, edge(p.gradients)) * tiles(p.piece, edge(p.gradients));
+    p.splits_n = 1;
+    while (dw * p.splits_n < 256 && p.splits_n * 8 <= p.ldn / kStep && p.splits_n < 64) p.splits_n *= 2;
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
         const int64_t here = at;
@@ -859,6 +1002,8 @@ Plan plan_of(const gear_token_desc& d) {
     };
     p.rows = take(d.n * (int64_t)sizeof(Row));
     p.totals = take(sizeof(Totals));
+    p.scales = take(sizeof(Scales));
+    p.largest = take(2 * kParts * sizeof(uint32_t));
     p.sums = take(kParts * sizeof(double));
     p.counts = take(kParts * sizeof(int64_t));
     p.tops = take(kParts * sizeof(float));
@@ -875,6 +1020,7 @@ Plan plan_of(const gear_token_desc& d) {
     p.e = take(d.n * (p.ldv + 64) * p.parts * 2);
     p.we = take(p.ldv * pitch(p.ldn) * p.parts * 2);
     p.slab = take(p.splits * d.n * p.ldk * 4);
+    if (p.splits_n > 1) p.slab_head = take(p.splits_n * p.piece * p.ldk * 4);
     p.bytes_backward = at;
     return p;
 }
@@ -906,6 +1052,8 @@ Args args_of(const gear_token_desc& d, const Plan& p, char* work) {
     a.weight = d.d_weight;
     a.rows = reinterpret_cast<Row*>(work + p.rows);
     a.totals = reinterpret_cast<Totals*>(work + p.totals);
+    a.scales = reinterpret_cast<Scales*>(work + p.scales);
+    a.largest = reinterpret_cast<uint32_t*>(work + p.largest);
     a.sums = reinterpret_cast<double*>(work + p.sums);
     a.counts = reinterpret_cast<int64_t*>(work + p.counts);
     a.tops = reinterpret_cast<float*>(work + p.tops);
@@ -917,6 +1065,7 @@ Args args_of(const gear_token_desc& d, const Plan& p, char* work) {
     a.target_dtype = d.target_dtype;
     a.tiles = p.tiles;
     a.row_parts = d.n <= kSoloRows ? 1 : (int32_t)some_blocks(d.n, kParts);
+    a.max_parts = (int32_t)some_blocks((d.n > d.V ? d.n : d.V) * ((d.D + 3) / 4), kParts);
     a.denom = d.denom;
     a.grad_scale = d.grad_scale;
     return a;
@@ -945,6 +1094,15 @@ struct Call {
         const int64_t ld = pitch(len);
         job = Job{src, work + to, rows, d.D, ld_src, len, ld, d.D * ld, 0, on ? 1 : 0};
         return Operand{work + to, d.D, ld, d.D * ld};
+    }
+    // The scales of 32-bit values: before anything is copied.
+    hipError_t look(const Args& a, const void* hidden, const void* head) const {
+        if constexpr (N > 1) {
+            hipLaunchKernelGGL(largest_kernel, dim3(2 * a.max_parts), dim3(kThreads), 0, s, a, static_cast<const float*>(hidden),
+                               d.hidden_row, static_cast<const float*>(head), d.head_row);
+            return hipGetLastError();
+        }
+        return hipSuccess;
     }
     // Nothing to do costs no launch.
     hipError_t prepare(const Args& a, Jobs& j, bool rows) const {
@@ -983,7 +1141,8 @@ struct Call {
     hipError_t loss(Args a, const void* hidden, const void* head) const {
         a.at_target = reinterpret_cast<float*>(work + p.at_target);
         a.part = reinterpret_cast<float2*>(work + p.part);
-        hipError_t e = hipSuccess;
+        hipError_t e = a.n > 0 ? look(a, hidden, head) : hipSuccess;
+        if (e != hipSuccess) return e;
         for (int64_t first = 0; first < a.V && a.n > 0; first += p.loss_piece) {
             const int64_t tokens = a.V - first < p.loss_piece ? a.V - first : p.loss_piece;
             Jobs j{};
@@ -1011,12 +1170,13 @@ struct Call {
         g.tn_rows = (int)tiles(a.n, S::BN);
         g.tn_tokens = (int)tiles(tokens, S::BN);
         g.dh_blocks = dhidden ? g.splits * g.tm * g.tn_rows : 0;
-        const int blocks = g.dh_blocks + (dhead ? g.tm * g.tn_tokens : 0);
+        const int blocks = g.dh_blocks + (dhead ? g.splits_n * g.tm * g.tn_tokens : 0);
         hipLaunchKernelGGL((gradients_kernel<E, T, S>), dim3((unsigned)blocks), dim3(S::kThreads), 0, s, a, g);
         return hipGetLastError();
     }
     hipError_t backward(const Args& a, const void* hidden, const void* head, void* dhidden, void* dhead) const {
-        hipError_t e = hipSuccess;
+        hipError_t e = look(a, hidden, head);
+        if (e != hipSuccess) return e;
         float* slab = reinterpret_cast<float*>(work + p.slab);
         for (int64_t first = 0; first < a.V; first += p.piece) {
             const int64_t tokens = a.V - first < p.piece ? a.V - first : p.piece, ldv = up(tokens, kStep);
@@ -1045,21 +1205,25 @@ struct Call {
             g.er = Operand{work + p.e, a.n, o.ld, o.part};
             g.we = Operand{work + p.we, tokens, o.ld_turned, o.part_turned};
             g.slab = slab;
+            g.slab_head = reinterpret_cast<float*>(work + p.slab_head);
             g.dhead = dhead ? static_cast<E*>(dhead) + first * a.D : nullptr;
             g.ld = p.ldk;
             g.steps_v = (int32_t)(ldv / kStep);
             g.steps_n = (int32_t)(p.ldn / kStep);
             g.splits = p.splits;
+            g.splits_n = p.splits_n;
             g.add = first > 0 ? 1 : 0;
             e = p.gradients == kBig      ? gradients<Big>(a, g, dhidden != nullptr, dhead != nullptr, tokens)
                 : p.gradients == kMiddle ? gradients<Middle>(a, g, dhidden != nullptr, dhead != nullptr, tokens)
                                          : gradients<Small>(a, g, dhidden != nullptr, dhead != nullptr, tokens);
             if (e != hipSuccess) return e;
-        }
-        if (dhidden) {
-            hipLaunchKernelGGL(rows_out_kernel<E>, dim3(some_blocks(a.n * ((a.D + 3) / 4), 8192)), dim3(kThreads), 0, s, a,
-                               slab, p.ldk, p.splits, Matrix<T>::kScale, static_cast<E*>(dhidden));
-            e = hipGetLastError();
+            // What is left in splits: dW of this piece, dh after the last.
+            const bool last = first + p.piece >= a.V;
+            const int64_t heads = dhead && p.splits_n > 1 ? tokens : 0, rows = dhidden && last ? a.n : 0;
+            if (heads + rows == 0) continue;
+            hipLaunchKernelGGL((splits_kernel<E, T>), dim3(some_blocks((heads + rows) * ((a.D + 3) / 4), 8192)), dim3(kThreads), 0,
+                               s, a, g, heads, rows ? static_cast<E*>(dhidden) : nullptr);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
         }
         return e;
     }

@@ -97,9 +97,17 @@ class Token:
         self.lse = torch.logsumexp(z, 1)
         lp = z.gather(1, self.t[:, None])[:, 0] - self.lse
         D = self.h.shape[1]
-        # A logit: products exact (parts of 32-bit values: 2^-25 of them), added 32 at a time in 32 bits.
+        # A logit: products added 32 at a time in 32 bits.  Those of 16-bit values are exact.  32-bit values enter as two
+        # fp16 parts: the first is off by 2^-11 of the value at most, the second by 2^-11 of that, 2^-22 in all, or by
+        # 2^-25 of the unit that the tensor's largest value has 2^14 of, 2^-39 of that value; the product of the second
+        # parts, left out, is 2^-22 at most.  Three times 2^-22 are 12 units of 2^-24.
         size = self.h.abs() @ self.W.abs().t()
         self.z_off = (U32 * (8 + D / 16) * size).amax(1)
+        self.parts_off = 0.0
+        if self.dtype == torch.float32 and n:
+            self.parts_off = 12 * U32
+            low = 2.0 ** -39 * (self.h.abs().max() * self.W.abs().sum(1).max() + self.W.abs().max() * self.h.abs().sum(1).max())
+            self.z_off = self.z_off + (12 * U32 * size).amax(1) + low
         # Exponentials of rounded products of up to |z|, a logarithm, and sums over the vocabulary, all positive.
         self.lse_off = 2 * self.z_off + U32 * (16 + 2 * z.abs().amax(1)) + U32 * self.lse.abs()
         self.logp = torch.where(self.on, lp, 0.0)
@@ -117,15 +125,20 @@ class Token:
         # e: the exponential's own error, the subtraction's, the rounding to the products' type (its floor: 2^-39), and
         # the rounding of e times the weight.
         e_off = self.p * (self.z_off + self.lse_off + 8 * U32)[:, None] + (held * 1.01 + 8 * U32) * e.abs() + 2.0 ** -38
+        # The products of parts once more, and hidden values and head where they are far below the largest.
+        e_off = e_off + self.parts_off * e.abs()
+        low = 2.0 ** -39 if dt == torch.float32 else 0.0
+        low_W, low_h = (low * t.abs().max() if t.numel() else 0.0 for t in (self.W, self.h))
         n, V = e.shape
         self.dh = c * (e @ self.W)
-        off = c.abs() * (e_off @ self.W.abs() + U32 * (64 + V / 16) * (e.abs() @ self.W.abs()))
+        off = c.abs() * (e_off @ self.W.abs() + U32 * (64 + V / 16) * (e.abs() @ self.W.abs()) + low_W * e.abs().sum(1, keepdim=True))
         self.dh_bound = U[dt] * self.dh.abs() + 1.01 * off + STEP[dt]
         ce = c * e
         self.dW = ce.t() @ self.h
         # The floor is one of the largest weight.
         floor = 2.0 ** -38 * c.abs().max() if n else 0.0
         off = (c.abs() * e_off + floor).t() @ self.h.abs() + U32 * (64 + n / 16) * (ce.abs().t() @ self.h.abs())
+        off = off + low_h * ce.abs().sum(0)[:, None]
         self.dW_bound = U[dt] * self.dW.abs() + 1.01 * off + STEP[dt]
 
 

@@ -146,6 +146,24 @@ def test_large_logits():
     assert float(loss) == 0 and not logp.any()
 
 
+@pytest.mark.parametrize("hidden,head", [(1e30, 1e-30), (1e-30, 1e30), (1e-36, 1e34), (3e38, 1e-38), (0.0, 1.0), (1.0, 0.0), (1e-42, 1.0)])
+def test_32_bit_values_of_any_size(hidden, head):
+    """Ends of the range, zeros, subnormal values; rows that take no part are far larger."""
+    h, W, t, w = inputs(150, 64, 200, torch.float32)
+    h, W = h / h.abs().max() * hidden, W / W.abs().max() * head
+    on = torch.rand(150, generator=torch.Generator().manual_seed(2)) < 0.7
+    h[~on] = 1e38 if hidden < 1e37 else float("inf")
+    check(h.to(cuda()), W.to(cuda()), t.to(cuda()), on.to(cuda()), w.to(cuda()), what="values of %g and %g" % (hidden, head))
+
+
+def test_32_bit_rows_of_different_sizes():
+    """Rows and columns that differ by a thousand, the head's the other way round: every logit counts."""
+    h, W, t, w = inputs(150, 64, 200, torch.float32)
+    by = 10.0 ** torch.linspace(-3, 3, 64)
+    check((h * by).to(cuda()), (W / by).to(cuda()), t.to(cuda()), None, w.to(cuda()), what="columns of different sizes")
+    check((h * 10.0 ** torch.linspace(-6, 0, 150)[:, None]).to(cuda()), W.to(cuda()), t.to(cuda()), None, w.to(cuda()), what="rows of different sizes")
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_nan_and_infinity_show(dtype):
     h, W, t, w = inputs(40, 64, 130, dtype)
