@@ -231,6 +231,7 @@ __global__ __launch_bounds__(kThreads) void update_kernel(const Items t, const B
     }
 }
 
+template <int THREADS>
 __device__ __forceinline__ double block_add(double v, double* s) {
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
@@ -238,44 +239,66 @@ __device__ __forceinline__ double block_add(double v, double* s) {
     __syncthreads();
     v = 0.0;
 #pragma unroll
-    for (int k = 0; k < kThreads / 64; k++) v += s[k];
+    for (int k = 0; k < THREADS / 64; k++) v += s[k];
     return v;
 }
 
-// Squares of the gradients, a sum per workgroup; ADD to those of the launches before.
+// What a group of kThreads adds to the sum of squares: every `stride`-th chunk from `first` on.
 template <typename E>
-__global__ __launch_bounds__(kThreads) void squares_kernel(const Grads t, double* sums, int add) {
-    __shared__ double s[kThreads / 64];
+__device__ __forceinline__ double squares(const Grads& t, uint32_t first, uint32_t stride, int lane) {
     double sum = 0.0;
-    for (uint32_t chunk = blockIdx.x; chunk < t.first[t.count]; chunk += gridDim.x) {
+    for (uint32_t chunk = first; chunk < t.first[t.count]; chunk += stride) {
         const int k = item_of(t, chunk);
         const Grad& it = t.item[k];
         const int64_t base = (int64_t)(chunk - t.first[k]) * t.chunk;
         const int64_t end = it.n - base < t.chunk ? it.n : base + t.chunk;
         for (int64_t at = base; at < end; at += kRound) {
-            const int64_t i = at + threadIdx.x * kValues;
+            const int64_t i = at + lane * kValues;
             float g[kValues];
             load<kValues, false>(static_cast<const E*>(it.grad) + i, end - i, g);
 #pragma unroll
             for (int j = 0; j < kValues; j++) sum = fma((double)g[j], (double)g[j], sum);
         }
     }
-    sum = block_add(sum, s);
+    return sum;
+}
+
+// A sum per workgroup; `add` to those of the launches before.
+template <typename E>
+__global__ __launch_bounds__(kThreads) void squares_kernel(const Grads t, double* sums, int add) {
+    __shared__ double s[kThreads / 64];
+    const double sum = block_add<kThreads>(squares<E>(t, blockIdx.x, gridDim.x, threadIdx.x), s);
     if (threadIdx.x == 0) sums[blockIdx.x] = sum + (add ? sums[blockIdx.x] : 0.0);
 }
 
-__global__ __launch_bounds__(kThreads) void norm_kernel(const double* sums, int blocks, float scale, float max_norm,
-                                                        float* norm, float* factor) {
+struct Limit {
+    float scale, max_norm;
+    float *norm, *factor;
+
+    __device__ __forceinline__ void put(double sum) const {
+        const double x = sqrt(sum) * (double)scale;
+        *norm = (float)x;
+        const double by = x > (double)max_norm ? (double)max_norm / x : 1.0;
+        *factor = fabsf((float)x) < INFINITY ? (float)((double)scale * by) : NAN;
+    }
+};
+__global__ __launch_bounds__(kThreads) void norm_kernel(const double* sums, int blocks, const Limit limit) {
     __shared__ double s[kThreads / 64];
     double sum = 0.0;
     for (int k = threadIdx.x; k < blocks; k += kThreads) sum += sums[k];
-    sum = block_add(sum, s);
-    if (threadIdx.x == 0) {
-        const double x = sqrt(sum) * (double)scale;
-        *norm = (float)x;
-        const double limit = x > (double)max_norm ? (double)max_norm / x : 1.0;
-        *factor = fabsf((float)x) < INFINITY ? (float)((double)scale * limit) : NAN;
-    }
+    sum = block_add<kThreads>(sum, s);
+    if (threadIdx.x == 0) limit.put(sum);
+}
+
+// Few gradients of one type: one workgroup and no second launch.
+constexpr int kSoloThreads = 1024;
+constexpr uint32_t kSoloChunks = 32;
+template <typename E>
+__global__ __launch_bounds__(kSoloThreads) void solo_kernel(const Grads t, const Limit limit) {
+    __shared__ double s[kSoloThreads / 64];
+    const int groups = kSoloThreads / kThreads, group = threadIdx.x / kThreads;
+    const double sum = block_add<kSoloThreads>(squares<E>(t, group, groups, threadIdx.x % kThreads), s);
+    if (threadIdx.x == 0) limit.put(sum);
 }
 
 constexpr int64_t kMaxN = 1ll << 40;
@@ -369,12 +392,26 @@ extern "C" int gear_grad_norm(const gear_step_tensor* tensors, int64_t count, fl
     double* sums = static_cast<double*>(d_work);
     hipStream_t s = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();  // an error pending from an earlier HIP call is not this call's
+    const Limit limit{scale, max_norm, d_norm, d_factor};
     int blocks = 0;  // sums that the launches so far have left
     Grads items;
     const int64_t values = values_of(tensors, count);
     items.chunk = values < kFewValues ? kRound : kChunk;
     hipError_t e = hipSuccess;
     const int32_t types[3] = {GEAR_DTYPE_F32, GEAR_DTYPE_BF16, GEAR_DTYPE_F16};
+    for (const int32_t type : types) {
+        int64_t i = 0;
+        if (!gather(tensors, count, i, items, [&](const gear_step_tensor& t) { return t.dtype == type; })) continue;
+        if (items.first[items.count] > kSoloChunks || i < count) break;
+        bool others = false;
+        for (int64_t k = 0; k < count; k++) others |= tensors[k].n > 0 && tensors[k].dtype != type;
+        if (others) break;
+        const auto kernel = type == GEAR_DTYPE_F32 ? solo_kernel<float>
+                            : type == GEAR_DTYPE_BF16 ? solo_kernel<__bf16> : solo_kernel<_Float16>;
+        hipLaunchKernelGGL(kernel, dim3(1), dim3(kSoloThreads), 0, s, items, limit);
+        e = hipGetLastError();
+        return e == hipSuccess ? GEAR_OK : hip_fail(e, "gear_grad_norm: launch");
+    }
     for (const int32_t type : types) {
         // Each type has sums of its own.
         int used = 0;
@@ -392,7 +429,7 @@ extern "C" int gear_grad_norm(const gear_step_tensor* tensors, int64_t count, fl
         }
         blocks += used;
     }
-    hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kThreads), 0, s, sums, blocks, scale, max_norm, d_norm, d_factor);
+    hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kThreads), 0, s, sums, blocks, limit);
     e = hipGetLastError();
     return e == hipSuccess ? GEAR_OK : hip_fail(e, "gear_grad_norm: sum launch");
 }

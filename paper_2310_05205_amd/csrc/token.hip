@@ -506,7 +506,6 @@ struct Tile {
             // Step t is there, and step t - 1 read, whose place step t + STAGES - 1 takes.
             if (t + S::STAGES - 2 < total) meet<(S::STAGES - 2) * S::kLoads>();
             else meet<0>();
-            if (t + S::STAGES - 1 < total) fetch_next();
             const char* xs = lds + here * S::kBytes;
             const char* ys = xs + S::BM * S::ROW * N;
             here = here + 1 == S::STAGES ? 0 : here + 1;
@@ -520,6 +519,14 @@ struct Tile {
 #pragma unroll
                     for (int i = 0; i < MI; i++) fx[part][i] = piece_at(xs + part * S::BM * S::ROW, m + i * 16, k * 4 + (lane >> 4));
                 }
+                if (k == 0) {
+                    // Behind the first reads, which the matrix instructions wait for: 1250 TFLOP/s of logits at k of 4096,
+                    // and 1200 before them.
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (t + S::STAGES - 1 < total) fetch_next();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                __builtin_amdgcn_s_setprio(1);
                 constexpr int PAIRS = N == 1 ? 1 : 3;
 #pragma unroll
                 for (int pair = 0; pair < PAIRS; pair++)
@@ -528,6 +535,7 @@ struct Tile {
 #pragma unroll
                         for (int j = 0; j < NJ; j++)
                             acc[i][j] = Matrix<T>::mfma(fx[N == 1 ? 0 : kPairs[pair][0]][i], fy[N == 1 ? 0 : kPairs[pair][1]][j], acc[i][j]);
+                __builtin_amdgcn_s_setprio(0);
             }
         }
         meet<0>();

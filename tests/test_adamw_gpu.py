@@ -195,10 +195,11 @@ def test_rate_on_the_device(bits):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-def test_norm(dtype):
-    g = [random(n, 7 + i, 10.0 ** (-i % 4)).to(dtype).to(cuda()) for i, n in enumerate(SIZES)]
+@pytest.mark.parametrize("sizes", [SIZES, SIZES[:8], [5], [2048] * 32, [2048] * 33, [65536], [65537]])
+def test_norm(dtype, sizes):
+    g = [random(n, 7 + i, 10.0 ** (-i % 4)).to(dtype).to(cuda()) for i, n in enumerate(sizes)]
     want = math.sqrt(sum(float(d64(x).square().sum()) for x in g))
-    say("grad_norm %s" % dtype)
+    say("grad_norm %s %s" % (dtype, sizes))
     for limit, scale in ((None, 1.0), (want / 3, 1.0), (want * 3, 1.0), (1.0, 1 / 1024)):
         norm, factor = gear.grad_norm(g, max_norm=limit, scale=scale)
         f = scale * min(1.0, math.inf if limit is None else limit / (want * scale))
