@@ -252,6 +252,20 @@ __device__ __forceinline__ double squares(const Grads& t, uint32_t first, uint32
         const Grad& it = t.item[k];
         const int64_t base = (int64_t)(chunk - t.first[k]) * t.chunk;
         const int64_t end = it.n - base < t.chunk ? it.n : base + t.chunk;
+        if (end - base == kChunk) {
+            // Four rounds' loads on their way together.
+            typename Vec<E, kValues>::raw raw[4];
+#pragma unroll
+            for (int q = 0; q < 4; q++) raw[q] = Vec<E, kValues>::load(static_cast<const E*>(it.grad) + base + q * kRound + lane * kValues);
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                float g[kValues];
+                Vec<E, kValues>::unpack(raw[q], g);
+#pragma unroll
+                for (int j = 0; j < kValues; j++) sum = fma((double)g[j], (double)g[j], sum);
+            }
+            continue;
+        }
         for (int64_t at = base; at < end; at += kRound) {
             const int64_t i = at + lane * kValues;
             float g[kValues];
