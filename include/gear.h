@@ -755,7 +755,9 @@ int gear_action_logp(const gear_policy_desc *d, const void *d_logits, float *d_l
  *   t = x + r (rounded to the rows' type; t = x without a residual)
  *   u = (t - mean t) / sqrt(var t + eps),  y = u weight + bias
  *
- * var is the mean of (t - mean t)^2.  All sums are in 32 bits.
+ * var is the mean of (t - mean t)^2.  All sums are in 32 bits; deviations beyond 1e19 leave
+ * their range.  With eps 0 a row without deviation is NaN.  NaN and infinities stay in their row,
+ * and in dweight and dbias.
  */
 typedef struct gear_norm_desc {
     int32_t dtype;        /* of x, residual, y, total, dy, dtotal, dx: GEAR_DTYPE_F16, _BF16 or _F32 */

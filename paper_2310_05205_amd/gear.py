@@ -560,8 +560,8 @@ def adamw(params, grads, exp_avg, exp_avg_sq, step, *, lr, betas=(0.9, 0.999), e
     float8_e4m3fn, exp_avg times its scale (float32, one for GEAR_STEP_BLOCK values)
     the first average, and (exp_avg_sq times its scale) squared the second.  master: a
     list of float32 copies, None for parameters without one; it is then what steps, and the
-    parameter its rounded copy.  lr: a number, or a float32 tensor of one value, read
-    on the device.  factor: a float32 tensor of one value that multiplies the gradients;
+    parameter its rounded copy; a 16-bit parameter without one keeps what its own bits hold.
+    lr: a number, or a float32 tensor of one value, read on the device.  eps: 2^-126 or more.  factor: a float32 tensor of one value that multiplies the gradients;
     where it or the lr tensor is not finite, nothing is changed.
     """
     _on_stream(native().adamw, step, stream, params, grads, exp_avg, exp_avg_sq, step, scales, master, lr, betas[0],

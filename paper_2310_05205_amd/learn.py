@@ -4,6 +4,10 @@
 what their namesakes in ``gear`` take and record a gradient; every step, forward
 and backward, runs in the HIP library.  ``advantages`` and ``action_logp`` need
 no gradient: see ``gear``.  ``AdamW`` steps a model's parameters by ``gear.adamw``.
+
+A backward pass that is captured into a HIP graph must not meet leaves that an eager
+autograd graph still holds (torch's rule: it ends the process); the calls in ``gear``
+are captured without one.
 """
 import torch
 

@@ -140,6 +140,42 @@ def test_tensors_that_begin_anywhere():
         assert not flat[k][::n + gap].any()
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_steps_past_the_caches(bits):
+    """A step of 18 M values against the same tensors in steps of fewer."""
+    sizes = [9000001, 5000000, 4000007]
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rnd = lambda n, t: torch.randn(n, generator=g, device=cuda()).to(t)  # noqa: E731
+    p, grads, master = ([rnd(n, t) for n in sizes] for t in (torch.bfloat16, torch.bfloat16, torch.float32))
+    kind = torch.float32 if bits == 32 else torch.uint8
+    avg = [[torch.zeros(n, dtype=kind, device=cuda()) for n in sizes] for _ in range(2)]
+    scales = [[torch.zeros((n + 255) // 256, device=cuda()) for n in sizes] for _ in range(2)]
+    say("adamw 18 M values, %d bits" % bits)
+    sides = []
+    for pieces in ([range(3)], [[0], [1], [2]]):
+        own = [[x.clone() for x in v] for v in (p, master, avg[0], avg[1], scales[0], scales[1])]
+        for step in range(2):
+            for piece in pieces:
+                count = torch.tensor([step], device=cuda())
+                pick = lambda v: [v[i].view(torch.float8_e4m3fn) if v[i].dtype == torch.uint8 else v[i] for i in piece]  # noqa: E731
+                gear.adamw(pick(own[0]), pick(grads), pick(own[2]), pick(own[3]), count, master=pick(own[1]),
+                           scales=(pick(own[4]), pick(own[5])) if bits == 8 else None, **KW)
+        sides.append([x for v in own for x in v])
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(*sides))
+
+
+def test_another_stream():
+    a, b = (Tensors([70000, 9], [torch.bfloat16, torch.float32], 8, True) for _ in range(2))
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    norm, factor = gear.grad_norm(a.g, max_norm=1.0, stream=s)
+    a.run(factor, stream=s)
+    s.synchronize()
+    norm2, factor2 = gear.grad_norm(b.g, max_norm=1.0)
+    b.run(factor2)
+    assert torch.equal(norm, norm2) and all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a.copies(), b.copies()))
+
+
 def test_many_steps_in_32_bits_follow_the_formula():
     p = random(500, 1)
     x, g = p.to(cuda()), torch.empty(500, device=cuda())

@@ -64,6 +64,32 @@ def test_many_rows(dtype):
         check(x, w, b, 1e-5, dy, dy, x, "%d x %d %s" % (n, D, dtype))
 
 
+@pytest.mark.parametrize("dtype,n,D", [(torch.bfloat16, 140000, 512), (torch.float16, 70001, 1024), (torch.float32, 9001, 4096),
+                                       (torch.float32, 150000, 256)])
+def test_rows_past_the_caches(dtype, n, D):
+    """Calls too large for the caches, against the same rows in calls that are not."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, r, dy = (torch.randn(n, D, generator=g, device=cuda()).to(dtype) for _ in range(3))
+    w, b = (1 + 0.2 * rows(2, D, torch.float32, 5)).to(cuda())
+    say("layer_norm %d x %d %s" % (n, D, dtype))
+    y, total, saved = gear.layer_norm(x, w, b, residual=r, save=True)
+    dx, dw, db = gear.layer_norm_backward(dy, total, saved, w, dtotal=r)
+    sums = torch.zeros(2, D, dtype=torch.float64, device=cuda())
+    size = torch.zeros(2, D, dtype=torch.float64, device=cuda())
+    for part in torch.arange(n, device=cuda()).split(n // 5 + 1):
+        a, e = int(part[0]), int(part[-1]) + 1
+        y2, total2, saved2 = gear.layer_norm(x[a:e], w, b, residual=r[a:e], save=True)
+        dx2, _, _ = gear.layer_norm_backward(dy[a:e], total2, saved2, w, dtotal=r[a:e])
+        assert torch.equal(y[a:e], y2) and torch.equal(total[a:e], total2) and torch.equal(saved[a:e], saved2) and torch.equal(dx[a:e], dx2)
+        u = (total2.double() - saved2[:, :1].double()) * saved2[:, 1:].double()
+        d = dy[a:e].double()
+        sums += torch.stack([(d * u).sum(0), d.sum(0)])
+        size += torch.stack([(d * u).abs().sum(0), d.abs().sum(0)])
+    # Sums over rows in turn and then over workgroups: up to n / 1024 + 64 roundings of their terms, u's own two among them.
+    for got, k in ((dw, 0), (db, 1)):
+        assert ((got.double() - sums[k]).abs() <= 2.0 ** -24 * (n / 1024 + 64) * size[k]).all()
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("D", [24, 65, 1003, 9001])
 def test_layouts(dtype, D):
@@ -165,6 +191,14 @@ def test_gradients_by_differences():
         assert torch.equal(ins[0].grad, ins[1].grad)
         if pick == 1:
             assert torch.equal(ins[0].grad, torch.ones_like(ins[0])) and ins[2].grad is None
+
+
+def test_plain_rows_without_eps():
+    """eps of 0 divides by the deviation alone: a constant row has none, and is NaN by itself."""
+    x = rows(3, 40, torch.float32, 1)
+    x[1] = 2.0
+    y, _, _ = gear.layer_norm(x.to(cuda()), eps=0.0)
+    assert torch.isnan(y[1]).all() and torch.isfinite(y[[0, 2]]).all()
 
 
 def test_captured_calls_replay():

@@ -56,6 +56,15 @@ def test_sizes(dtype, n, D, V):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,D,V", [(300, 72, 11000), (520, 520, 30001), (5000, 70, 40), (9000, 200, 3), (3000, 300, 700)])
+def test_sizes_of_other_tiles(dtype, n, D, V):
+    """Middle and big tiles in each product, rows split for small heads."""
+    h, W, t, w = (x.to(cuda()) for x in inputs(n, D, V, dtype))
+    on = (torch.rand(n, generator=torch.Generator().manual_seed(7)) < 0.8).to(cuda())
+    check(h, W, t, on, w, scale=16.0 * n, what="%d x %d x %d %s" % (n, D, V, dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_several_pieces_of_the_vocabulary(dtype):
     """Tokens beyond one piece, forward and backward."""
     h, W, t, w = (x.to(cuda()) for x in inputs(40, 24, 140001, dtype))
