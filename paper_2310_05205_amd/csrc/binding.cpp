@@ -20,6 +20,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstddef>
 #include <cstdint>
 #include <exception>
 #include <utility>
@@ -1196,22 +1197,75 @@ PyObject* py_token_loss_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// The tensors of a list or tuple; undefined ones for None where `holes`.
-std::vector<at::Tensor> tensors_of(PyObject* o, const char* name, bool holes = false) {
-    TORCH_CHECK_TYPE(PyList_Check(o) || PyTuple_Check(o), name, " must be a list or tuple of tensors");
-    const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
-    std::vector<at::Tensor> out;
-    out.reserve((size_t)n);
-    for (Py_ssize_t i = 0; i < n; i++) {
-        PyObject* item = PySequence_Fast_GET_ITEM(o, i);
-        if (holes && item == Py_None) out.emplace_back();
-        else out.push_back(tensor_of(item, name));
+// The tensors of a list or tuple, held while this lives; NULL for None where `holes`.
+class Tensors {
+  public:
+    Tensors() = default;
+    Tensors(PyObject* o, const char* name, bool holes = false) {
+        TORCH_CHECK_TYPE(PyList_Check(o) || PyTuple_Check(o), name, " must be a list or tuple of tensors");
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+        at_.reserve((size_t)n);
+        for (Py_ssize_t i = 0; i < n; i++) {
+            PyObject* item = PySequence_Fast_GET_ITEM(o, i);
+            if (!(holes && item == Py_None)) TORCH_CHECK_TYPE(THPVariable_Check(item), name, " must hold torch tensors");
+            at_.push_back(item);
+        }
+        for (PyObject* item : at_) Py_INCREF(item);  // after the checks: no destructor follows a throw from here
     }
-    return out;
-}
-void need_count(const std::vector<at::Tensor>& v, const char* name, size_t want) {
+    Tensors(Tensors&& o) noexcept : at_(std::move(o.at_)) { o.at_.clear(); }
+    Tensors& operator=(Tensors&& o) noexcept {
+        std::swap(at_, o.at_);
+        return *this;
+    }
+    Tensors(const Tensors&) = delete;
+    ~Tensors() {
+        for (PyObject* o : at_) Py_DECREF(o);
+    }
+    size_t size() const { return at_.size(); }
+    bool empty() const { return at_.empty(); }
+    const at::Tensor* get(size_t i) const { return at_[i] == Py_None ? nullptr : &THPVariable_Unpack(at_[i]); }
+    const at::Tensor& operator[](size_t i) const { return THPVariable_Unpack(at_[i]); }
+
+  private:
+    std::vector<PyObject*> at_;
+};
+void need_count(const Tensors& v, const char* name, size_t want) {
     TORCH_CHECK_VALUE(v.size() == want, name, " must have ", want, " tensors, not ", v.size());
 }
+
+// Memory that a call writes or reads, as it is added tensor after tensor in lists.
+typedef std::pair<const char*, const char*> Range;
+class Ranges {
+  public:
+    void add(const void* p, size_t bytes) {
+        if (bytes) all_.emplace_back(static_cast<const char*>(p), static_cast<const char*>(p) + bytes);
+    }
+    // Ends a list.  Most are in order, and joining those takes a fraction of sorting all.
+    void end_list() {
+        const auto mid = all_.begin() + (std::ptrdiff_t)sorted_;
+        if (!std::is_sorted(mid, all_.end())) std::sort(mid, all_.end());
+        std::inplace_merge(all_.begin(), mid, all_.end());
+        sorted_ = all_.size();
+    }
+    bool apart() const {
+        for (size_t i = 1; i < all_.size(); i++)
+            if (all_[i - 1].second > all_[i].first) return false;
+        return true;
+    }
+    // Whether any of `o`, in order as these are, meets one of these, which lie apart.
+    bool meet(const Ranges& o) const {
+        size_t k = 0;
+        for (const Range& r : o.all_) {
+            while (k < all_.size() && all_[k].second <= r.first) k++;
+            if (k < all_.size() && all_[k].first < r.second) return true;
+        }
+        return false;
+    }
+
+  private:
+    std::vector<Range> all_;
+    size_t sorted_ = 0;
+};
 
 // One float on the device, or None.
 at::Tensor device_value(PyObject* o, const char* name, c10::Device dev) {
@@ -1223,7 +1277,7 @@ at::Tensor device_value(PyObject* o, const char* name, c10::Device dev) {
 // grad_norm(grads, scale, max_norm or None, stream): (norm, factor)
 PyObject* py_grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return entry(n, 4, [&]() -> PyObject* {
-        const std::vector<at::Tensor> grads = tensors_of(a[0], "grads");
+        const Tensors grads(a[0], "grads");
         TORCH_CHECK_VALUE(!grads.empty(), "grads must have at least one tensor");
         const c10::Device dev = gpu_of(grads[0], "grads");
         std::vector<gear_step_tensor> list(grads.size());
@@ -1259,8 +1313,7 @@ PyObject* py_grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
 //       factor or None, stream): None
 PyObject* py_adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return entry(n, 14, [&]() -> PyObject* {
-        const std::vector<at::Tensor> params = tensors_of(a[0], "params"), grads = tensors_of(a[1], "grads"),
-                                      m = tensors_of(a[2], "exp_avg"), v = tensors_of(a[3], "exp_avg_sq");
+        const Tensors params(a[0], "params"), grads(a[1], "grads"), m(a[2], "exp_avg"), v(a[3], "exp_avg_sq");
         const size_t count = params.size();
         need_count(grads, "grads", count);
         need_count(m, "exp_avg", count);
@@ -1271,17 +1324,17 @@ PyObject* py_adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
         gear_adamw_desc d{};
         const bool eight = a[5] != Py_None;
         d.state_bits = eight ? 8 : 32;
-        std::vector<at::Tensor> ms, vs, master;
+        Tensors ms, vs, master;
         if (eight) {
             TORCH_CHECK_VALUE(PyTuple_Check(a[5]) && PyTuple_GET_SIZE(a[5]) == 2,
                               "scales must be a pair of lists, of exp_avg and of exp_avg_sq");
-            ms = tensors_of(PyTuple_GET_ITEM(a[5], 0), "scales");
-            vs = tensors_of(PyTuple_GET_ITEM(a[5], 1), "scales");
+            ms = Tensors(PyTuple_GET_ITEM(a[5], 0), "scales");
+            vs = Tensors(PyTuple_GET_ITEM(a[5], 1), "scales");
             need_count(ms, "scales", count);
             need_count(vs, "scales", count);
         }
         if (a[6] != Py_None) {
-            master = tensors_of(a[6], "master", true);
+            master = Tensors(a[6], "master", true);
             need_count(master, "master", count);
         }
         at::Tensor lr;
@@ -1296,80 +1349,75 @@ PyObject* py_adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
         d.d_factor = data<float>(factor);
         void* s = as_ptr(a[13]);
 
-        typedef std::pair<const char*, const char*> Range;
-        std::vector<Range> written, read;
-        const auto range_of = [](const at::Tensor& t) {
-            return Range(data<char>(t), data<char>(t) + t.nbytes());
-        };
+        // What is written lies apart, and apart from what is read: workgroups run in no order.
+        Ranges written, read;
         std::vector<gear_step_tensor> list(count);
-        const auto state = [&](const at::Tensor& t, const char* name, const at::Tensor& p, at::ScalarType type) {
+        const auto state = [&](const at::Tensor& t, const char* name, const gear_step_tensor& p, at::ScalarType type) {
             need_device(t, name, dev);
             TORCH_CHECK_VALUE(t.scalar_type() == type, name, " must be ", type, ", not ", t.scalar_type());
-            TORCH_CHECK_VALUE(t.numel() == p.numel(), name, " must have the parameter's ", p.numel(), " values, not ",
-                              t.numel());
+            TORCH_CHECK_VALUE(t.numel() == p.n, name, " must have the parameter's ", p.n, " values, not ", t.numel());
             need_contiguous(t, name);
-            if (t.numel()) written.push_back(range_of(t));
+            void* at = t.data_ptr();
+            written.add(at, t.nbytes());
+            return at;
         };
-        const at::ScalarType avg = eight ? at::kFloat8_e4m3fn : at::kFloat;
         for (size_t i = 0; i < count; i++) {
             const at::Tensor &p = params[i], &g = grads[i];
             gear_step_tensor& t = list[i];
             t = gear_step_tensor{};
             t.dtype = float_code(p, "params");
             t.n = p.numel();
-            state(p, "params", p, p.scalar_type());
+            t.d_param = state(p, "params", t, p.scalar_type());
             need_device(g, "grads", dev);
             TORCH_CHECK_VALUE(g.scalar_type() == p.scalar_type(), "a gradient must have its parameter's dtype");
-            need_sizes(g, "a gradient", p.sizes().vec());
+            TORCH_CHECK_VALUE(g.sizes() == p.sizes(), "a gradient must have its parameter's shape ", p.sizes(), ", not ", g.sizes());
             need_contiguous(g, "grads");
-            if (t.n) read.push_back(range_of(g));
-            state(m[i], "exp_avg", p, avg);
-            state(v[i], "exp_avg_sq", p, avg);
-            if (eight) {
-                const int64_t blocks = (t.n + GEAR_STEP_BLOCK - 1) / GEAR_STEP_BLOCK;
-                for (const at::Tensor* sc : {&ms[i], &vs[i]}) {
-                    need_device(*sc, "scales", dev);
-                    TORCH_CHECK_VALUE(sc->scalar_type() == at::kFloat && sc->numel() == blocks,
-                                      "scales must be float32, one value for ", GEAR_STEP_BLOCK, " of the parameter's");
-                    need_contiguous(*sc, "scales");
-                    if (blocks) written.push_back(range_of(*sc));
-                }
-                t.d_exp_avg_scale = data<float>(ms[i]);
-                t.d_exp_avg_sq_scale = data<float>(vs[i]);
-            }
-            if (!master.empty() && master[i].defined()) {
-                TORCH_CHECK_VALUE(p.scalar_type() != at::kFloat, "a float32 parameter has no master");
-                state(master[i], "master", p, at::kFloat);
-                t.d_master = data<float>(master[i]);
-            }
             t.d_grad = g.data_ptr();
-            t.d_param = p.data_ptr();
-            t.d_exp_avg = m[i].data_ptr();
-            t.d_exp_avg_sq = v[i].data_ptr();
+            read.add(t.d_grad, g.nbytes());
         }
-        written.push_back(range_of(step));
-        if (lr.defined()) read.push_back(range_of(lr));
-        if (factor.defined()) read.push_back(range_of(factor));
-        // What is written lies apart, and apart from what is read: workgroups run in no order.
-        std::sort(written.begin(), written.end());
-        for (size_t i = 1; i < written.size(); i++)
-            TORCH_CHECK_VALUE(written[i - 1].second <= written[i].first,
-                              "parameters, averages, masters, scales and step must not overlap");
-        for (const Range& r : read) {
-            const auto after = std::upper_bound(written.begin(), written.end(), Range(r.second - 1, nullptr),
-                                                [](const Range& x, const Range& y) { return x.first < y.first; });
-            TORCH_CHECK_VALUE(after == written.begin() || (after - 1)->second <= r.first,
-                              "a gradient, lr or factor must not overlap what is written");
+        written.end_list();
+        read.end_list();
+        const at::ScalarType avg = eight ? at::kFloat8_e4m3fn : at::kFloat;
+        for (size_t i = 0; i < count; i++) list[i].d_exp_avg = state(m[i], "exp_avg", list[i], avg);
+        written.end_list();
+        for (size_t i = 0; i < count; i++) list[i].d_exp_avg_sq = state(v[i], "exp_avg_sq", list[i], avg);
+        written.end_list();
+        if (eight) {
+            const auto scale = [&](const at::Tensor& t, int64_t values) {
+                need_device(t, "scales", dev);
+                TORCH_CHECK_VALUE(t.scalar_type() == at::kFloat && t.numel() == (values + GEAR_STEP_BLOCK - 1) / GEAR_STEP_BLOCK,
+                                  "scales must be float32, one value for ", GEAR_STEP_BLOCK, " of the parameter's");
+                need_contiguous(t, "scales");
+                written.add(t.data_ptr(), t.nbytes());
+                return data<float>(t);
+            };
+            for (size_t i = 0; i < count; i++) list[i].d_exp_avg_scale = scale(ms[i], list[i].n);
+            written.end_list();
+            for (size_t i = 0; i < count; i++) list[i].d_exp_avg_sq_scale = scale(vs[i], list[i].n);
+            written.end_list();
         }
+        for (size_t i = 0; i < master.size(); i++) {
+            const at::Tensor* t = master.get(i);
+            if (t == nullptr) continue;
+            TORCH_CHECK_VALUE(list[i].dtype != GEAR_DTYPE_F32, "a float32 parameter has no master");
+            list[i].d_master = static_cast<float*>(state(*t, "master", list[i], at::kFloat));
+        }
+        written.add(step.data_ptr(), step.nbytes());
+        written.end_list();
+        if (lr.defined()) read.add(lr.data_ptr(), lr.nbytes());
+        if (factor.defined()) read.add(factor.data_ptr(), factor.nbytes());
+        read.end_list();
+        TORCH_CHECK_VALUE(written.apart(), "parameters, averages, masters, scales and step must not overlap");
+        TORCH_CHECK_VALUE(!written.meet(read), "a gradient, lr or factor must not overlap what is written");
         const c10::DeviceGuard guard(dev);
         int64_t bytes = 0;
         int rc = f_step_sizes(nullptr, &bytes);
         if (rc != GEAR_OK) return PyLong_FromLong(rc);
         const at::Tensor work = workspace(bytes, dev);
-        const std::vector<at::Tensor>* const lists[] = {&params, &m, &v, &ms, &vs, &master};
-        for (const std::vector<at::Tensor>* each : lists)
-            for (const at::Tensor& t : *each)
-                if (t.defined()) overwrites(t);
+        const Tensors* const lists[] = {&params, &m, &v, &ms, &vs, &master};
+        for (const Tensors* each : lists)
+            for (size_t i = 0; i < each->size(); i++)
+                if (const at::Tensor* t = each->get(i)) overwrites(*t);
         overwrites(step);
         rc = without_gil([&] { return f_adamw(&d, list.data(), (int64_t)count, data<int64_t>(step), data<void>(work), bytes, s); });
         if (rc != GEAR_OK) return PyLong_FromLong(rc);

@@ -1,5 +1,6 @@
 """AdamW over lists of tensors and the norm of their gradients against their formulas in 64 bits (GPU)."""
 import math
+import sys
 
 import pytest
 import torch
@@ -371,3 +372,53 @@ def test_refusals():
     for build in (lambda: learn.AdamW([]), lambda: learn.AdamW([p], bits=16), lambda: learn.AdamW([p.view(30, 10).t()])):
         with pytest.raises(ValueError):
             build()
+
+
+@pytest.mark.parametrize("order", [(0, 1, 2, 3), (3, 2, 1, 0), (2, 0, 3, 1)])
+def test_lists_of_one_buffer_in_any_order(order):
+    # Four parameters, gradients and averages are neighbours in one buffer: they touch, and
+    # a list that takes one value of a neighbour overlaps it.
+    n = 512
+    flat = torch.zeros(4, 4, n, device=cuda())
+    flat[0] = 1.0
+    flat[1] = torch.linspace(-1, 1, 4 * n, device=cuda()).view(4, n)
+    want = flat.clone()
+    step, step2 = (torch.zeros(1, dtype=torch.int64, device=cuda()) for _ in range(2))
+    at = [[flat[k][i] for i in order] for k in range(4)]
+    gear.adamw(*at, step, **KW)
+    for i in range(4):
+        step2.zero_()
+        gear.adamw(*([want[k][i]] for k in range(4)), step2, **KW)
+    assert torch.equal(flat, want)
+    one = flat.view(-1)
+    for k in range(4):
+        for i in range(4):
+            begin = (k * 4 + order[i]) * n
+            for shift in (-1, 1):
+                # A gradient may share values with another gradient only.
+                met = (begin if shift < 0 else begin + n) + (-1 if shift < 0 else 0)
+                if not 0 <= met < one.numel() or (k == 1 and met // (4 * n) == 1):
+                    continue
+                bad = [list(v) for v in at]
+                bad[k][i] = one[begin + shift:begin + shift + n]
+                with pytest.raises(ValueError, match="overlap"):
+                    gear.adamw(*bad, step, **KW)
+    for clash in ({"lr": flat[2][3][:1]}, {"factor": flat[0][1][n - 1:]}):
+        with pytest.raises(ValueError, match="overlap"):
+            gear.adamw(*at, step, **dict(KW, **clash))
+    assert torch.equal(flat, want) and int(step) == 1
+
+
+def test_lists_are_let_go():
+    p, g, m, v = (torch.ones(64, device=cuda()) for _ in range(4))
+    step = torch.zeros(1, dtype=torch.int64, device=cuda())
+    before = [sys.getrefcount(x) for x in (p, g, m, v, None)]
+    for _ in range(100):
+        gear.adamw([p], [g], [m], [v], step, **KW)
+        gear.grad_norm([g, g])
+        for bad in (([p], [g], [m], [None]), ([p, p], [g, g], [m, m], [v, 1]), ([p], [g], [m], []), ([p, p], [g, g], [m, m], [v, v])):
+            with pytest.raises((ValueError, TypeError)):
+                gear.adamw(*bad, step, **KW)
+    del bad  # it holds the last lists itself
+    after = [sys.getrefcount(x) for x in (p, g, m, v, None)]
+    assert after[:4] == before[:4] and after[4] - before[4] < 50
