@@ -843,9 +843,8 @@ int gear_token_loss_sizes(const gear_token_desc *d, int64_t *loss_bytes, int64_t
  *   d_work            workspace; its contents do not matter
  *
  * Products of 16-bit values are exact and added in 32 bits.  32-bit values enter as
- * two fp16 parts under a power of two that the largest finite value of the tensor
- * sets (of hidden, of the rows that take part): off by 2^-22 of the value, or 2^-39 of the
- * largest where that is more.  An infinity among them counts as NaN.  A NaN in a row
+ * two fp16 parts under a power of two that the largest finite value of their row sets:
+ * off by 2^-22 of the value, or 2^-39 of the row's largest where that is more.  An infinity among them counts as NaN.  A NaN in a row
  * that takes part, or in the head, shows in the loss.
  * Results repeat bit for bit.
  * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
@@ -867,6 +866,8 @@ int gear_token_loss(const gear_token_desc *d, const void *d_hidden, const void *
  *
  * The logits are formed again, a piece of the vocabulary at a time, and e is
  * rounded once to the products' type (two fp16 parts for 32-bit values), fp16 times 2^14.
+ * In the sums of the gradients 32-bit hidden values and the head are off by 2^-22 of the value, or
+ * by 2^-39 of the tensor's largest finite one (of hidden, of the rows that take part).
  * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
  */
 int gear_token_loss_backward(const gear_token_desc *d, const void *d_hidden, const void *d_head, const float *d_lse,

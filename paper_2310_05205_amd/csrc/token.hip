@@ -12,9 +12,10 @@
 // orders, a piece of the vocabulary at a time.  The copies pad k to whole steps with
 // zeros, so odd sizes and alignments end there.
 //
-// 32-bit values are cut into two fp16 parts, a 2^s = a1 + a2 (11 bits each), s making the
-// tensor's largest finite value 2^14 to 2^15; a part is off by 2^-22 of the value, or by 2^-40
-// of the largest where the value is far below it.  The products a1 b1, a1 b2 and a2 b1 leave out
+// 32-bit values are cut into two fp16 parts, a 2^s = a1 + a2 (11 bits each), s making the largest
+// finite value 2^14 to 2^15, of a row for the logits, which so depend on their own row and token
+// alone, and of the tensor for the turned copies, whose k runs over the rows; a part is off by
+// 2^-22 of the value, or by 2^-40 of the largest where the value is far below it.  The products a1 b1, a1 b2 and a2 b1 leave out
 // 2^-22 of |a b| at most.  Matrix instructions of 16-bit types are 16 times as fast as those of 32
 // bits, so three of them take a fifth of the time.  (Three bf16 parts need no scale and leave
 // 2^-25, but six products: 1000 x 512 x 8192, forward and backward, took 245 us with them and takes 175.)
@@ -87,7 +88,7 @@ struct Totals {
     float share;     // 1 / denom
     float weight;    // largest |weight| of a row that takes part
 };
-// Powers of two that 32-bit hidden values and the head are multiplied by before they are cut.
+// Powers of two that 32-bit hidden values and the head are multiplied by before they are cut and turned.
 struct Scales {
     int32_t hidden, head;
 };
@@ -99,7 +100,8 @@ struct Args {
     float *loss, *logp, *lse;
     Row* rows;
     Totals* totals;
-    Scales* scales;    // of 32-bit values
+    Scales* scales;    // of 32-bit values, turned
+    int32_t *hidden_scale, *head_scale;  // of each row, and of each token of a piece
     uint32_t* largest; // [2][kParts]: largest finite magnitudes of hidden and head, a workgroup each
     double* sums;      // [kParts]
     int64_t* counts;   // [kParts]
@@ -260,6 +262,11 @@ __device__ __forceinline__ void cut(float v, T (&part)[N]) {
 __device__ __forceinline__ int32_t scale_for(uint32_t top) {
     return top == 0 ? 0 : 15 - __builtin_amdgcn_frexp_expf(__builtin_bit_cast(float, top));
 }
+// The larger of `top` and a magnitude, in the magnitudes' order, unless that is not finite.
+__device__ __forceinline__ uint32_t larger_finite(uint32_t top, float f) {
+    const uint32_t m = __builtin_bit_cast(uint32_t, f) & 0x7FFFFFFFu;
+    return m < 0x7F800000u && m > top ? m : top;
+}
 // Largest finite magnitudes of 32-bit hidden rows that take part and of the head: a.max_parts workgroups each.
 __global__ __launch_bounds__(kThreads) void largest_kernel(const Args a, const float* hidden, int64_t hidden_row,
                                                            const float* head, int64_t head_row) {
@@ -282,10 +289,7 @@ __global__ __launch_bounds__(kThreads) void largest_kernel(const Args a, const f
                 if (c + q < a.D) f[q] = p[r * ld + c + q];
         }
 #pragma unroll
-        for (int q = 0; q < 4; q++) {
-            const uint32_t m = __builtin_bit_cast(uint32_t, f[q]) & 0x7FFFFFFFu;  // in the magnitudes' order
-            if (m < 0x7F800000u && m > top) top = m;
-        }
+        for (int q = 0; q < 4; q++) top = larger_finite(top, f[q]);
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off));
@@ -340,11 +344,13 @@ __device__ __forceinline__ void get8(const E* p, int64_t left, float (&f)[8]) {
     }
 }
 
-// A copy of rows as rows of whole steps (ld), or turned: dst[column][row], zeros
-// behind the last row.  `on`: rows that take no part become zeros.
+// A copy of rows as rows of whole steps (ld), 32-bit ones each times the power of two that it
+// leaves in `scale`, or turned: dst[column][row], zeros behind the last row.  `on`: rows that take no
+// part become zeros.
 struct Job {
     const void* src;
     void* dst;
+    int32_t* scale;
     int64_t rows, cols, ld_src, len, ld, part;  // len: of a row of dst, in whole steps
     int32_t first;  // workgroup
     int32_t on;
@@ -353,19 +359,41 @@ struct Jobs {
     Job copy[2], turn[2];
     int32_t row_blocks, blocks;  // workgroups that look at the rows, the first ones; of all
 };
+// Lanes that copy a 32-bit row of so many pieces of 8 values.
+__host__ __device__ __forceinline__ int lanes_of(int64_t pieces) { return pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 32 ? 32 : 64; }
 template <typename E>
-__device__ __forceinline__ void run_copy(const Job& j, int32_t by, int block, int blocks) {
+__device__ __forceinline__ void run_copy(const Job& j, int block, int blocks) {
     typedef typename Parts<E>::T T;
     const int64_t per_row = j.len / 8;
-    for (int64_t i = (int64_t)block * kThreads + threadIdx.x; i < j.rows * per_row; i += (int64_t)blocks * kThreads) {
-        const int64_t r = i / per_row, c = i % per_row * 8;
-        float f[8];
-        get8(static_cast<const E*>(j.src) + r * j.ld_src + c, j.cols - c, f);
-        if (Parts<E>::kCount > 1) {
-#pragma unroll
-            for (int q = 0; q < 8; q++) f[q] = ldexpf(f[q], by);
+    if constexpr (Parts<E>::kCount == 1) {
+        for (int64_t i = (int64_t)block * kThreads + threadIdx.x; i < j.rows * per_row; i += (int64_t)blocks * kThreads) {
+            const int64_t r = i / per_row, c = i % per_row * 8;
+            float f[8];
+            get8(static_cast<const E*>(j.src) + r * j.ld_src + c, j.cols - c, f);
+            put8<T, 1>(f, static_cast<T*>(j.dst) + r * j.ld + c, j.part);
         }
-        put8<T, Parts<E>::kCount>(f, static_cast<T*>(j.dst) + r * j.ld + c, j.part);
+    } else {
+        // A row is read for its scale, then again, from the cache.
+        const int lanes = lanes_of(per_row), lane = threadIdx.x & (lanes - 1);
+        for (int64_t r = ((int64_t)block * kThreads + threadIdx.x) / lanes; r < j.rows; r += (int64_t)blocks * (kThreads / lanes)) {
+            const E* row = static_cast<const E*>(j.src) + r * j.ld_src;
+            float f[8];
+            uint32_t top = 0;
+            for (int64_t c = lane * 8; c < j.cols; c += lanes * 8) {
+                get8(row + c, j.cols - c, f);
+#pragma unroll
+                for (int q = 0; q < 8; q++) top = larger_finite(top, f[q]);
+            }
+            for (int off = lanes / 2; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off));
+            const int32_t by = scale_for(top);
+            if (lane == 0) j.scale[r] = by;
+            for (int64_t c = lane * 8; c < j.len; c += lanes * 8) {
+                get8(row + c, j.cols - c, f);
+#pragma unroll
+                for (int q = 0; q < 8; q++) f[q] = ldexpf(f[q], by);
+                put8<T, 2>(f, static_cast<T*>(j.dst) + r * j.ld + c, j.part);
+            }
+        }
     }
 }
 template <typename E>
@@ -396,16 +424,16 @@ __device__ __forceinline__ void run_turn(const Args& a, const Job& j, int32_t by
 template <typename E>
 __global__ __launch_bounds__(kThreads) void prepare_kernel(const Args a, const Jobs jobs) {
     __shared__ float tile[64][65];
-    Scales by{0, 0};
-    if constexpr (Parts<E>::kCount > 1) {
-        by = find_scales(a);
-        if (blockIdx.x == 0 && threadIdx.x == 0) *a.scales = by;
-    }
     const int b = blockIdx.x;
     if (b < jobs.row_blocks) return look_at_rows(a, b);
     const int copy1 = jobs.copy[1].first, turn0 = jobs.turn[0].first, turn1 = jobs.turn[1].first;
-    if (b < copy1) return run_copy<E>(jobs.copy[0], by.head, b - jobs.copy[0].first, copy1 - jobs.copy[0].first);
-    if (b < turn0) return run_copy<E>(jobs.copy[1], by.hidden, b - copy1, turn0 - copy1);
+    if (b < copy1) return run_copy<E>(jobs.copy[0], b - jobs.copy[0].first, copy1 - jobs.copy[0].first);
+    if (b < turn0) return run_copy<E>(jobs.copy[1], b - copy1, turn0 - copy1);
+    Scales by{0, 0};
+    if constexpr (Parts<E>::kCount > 1) {
+        by = find_scales(a);
+        if (b == turn0 && threadIdx.x == 0) *a.scales = by;
+    }
     if (b < turn1) return run_turn<E>(a, jobs.turn[0], by.hidden, b - turn0, turn1 - turn0, tile);
     run_turn<E>(a, jobs.turn[1], by.head, b - turn1, jobs.blocks - turn1, tile);
 }
@@ -555,23 +583,24 @@ __device__ __forceinline__ Place place_of(int b, int tm, int tn) {
     return Place{first + in % high, in / high};
 }
 
-// Products of scaled values.
+// Products of rows from `r` on, every 16th, of scaled values, and of tokens from `t` of the piece on.
 template <typename S>
-__device__ __forceinline__ void unscale(F4 (&acc)[S::MI][S::NJ], const Scales& by) {
-    const int32_t e = -by.hidden - by.head;
+__device__ __forceinline__ void unscale(const Args& a, F4 (&acc)[S::MI][S::NJ], int64_t t, int64_t r) {
+    int32_t row[S::NJ];
 #pragma unroll
-    for (int i = 0; i < S::MI; i++)
+    for (int j = 0; j < S::NJ; j++) row[j] = r + j * 16 < a.n ? a.hidden_scale[r + j * 16] : 0;
 #pragma unroll
-        for (int j = 0; j < S::NJ; j++)
+    for (int i = 0; i < S::MI; i++) {
+        // The tokens' scales go on to whole tiles; what lies behind the last one is not used.
+        const int4 token = *reinterpret_cast<const int4*>(a.head_scale + t + i * 16);
 #pragma unroll
-            for (int q = 0; q < 4; q++) acc[i][j][q] = ldexpf(acc[i][j][q], e);
-}
-
-// exp(z - top).  Beside 16-bit products one operation less: from = top log2 e, rounded, costs
-// up to |top| 2^-24 of the result.
-template <int N>
-__device__ __forceinline__ float exp_from(float z, float top, float from) {
-    return N == 1 ? __builtin_amdgcn_exp2f(fmaf(z, kLog2e, -from)) : fast_exp(z - top);
+        for (int j = 0; j < S::NJ; j++) {
+            acc[i][j][0] = ldexpf(acc[i][j][0], -token.x - row[j]);
+            acc[i][j][1] = ldexpf(acc[i][j][1], -token.y - row[j]);
+            acc[i][j][2] = ldexpf(acc[i][j][2], -token.z - row[j]);
+            acc[i][j][3] = ldexpf(acc[i][j][3], -token.w - row[j]);
+        }
+    }
 }
 
 // Maximum and sum of exponentials of a tile's logits, per row, and the targets' logits;
@@ -590,7 +619,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void logits_kernel(c
     float* s_max = reinterpret_cast<float*>(lds);  // [WM][BN]
     float* s_sum = s_max + S::WM * S::BN;
     const int64_t v = first + v0 + wm * Tl::MI * 16 + (lane >> 4) * 4;
-    if (S::N > 1) unscale<S>(acc, *a.scales);
+    if (S::N > 1) unscale<S>(a, acc, v - first, r0 + wn * Tl::NJ * 16 + (lane & 15));
     if (first + v0 + S::BM > a.V) {
 #pragma unroll
         for (int i = 0; i < Tl::MI; i++)
@@ -619,12 +648,12 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void logits_kernel(c
         }
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
-        const float top = m == -INFINITY ? 0.0f : m, from = top * kLog2e;
+        const float top = m == -INFINITY ? 0.0f : m;
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < Tl::MI; i++)
 #pragma unroll
-            for (int q = 0; q < 4; q++) sum += exp_from<S::N>(acc[i][j][q], top, from);
+            for (int q = 0; q < 4; q++) sum += fast_exp(acc[i][j][q] - top);
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (lane < 16) {
@@ -688,7 +717,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void errors_kernel(c
     Tl::run(head, hidden, v0, r0, 0, steps, lds, acc);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / S::WN, wn = wave % S::WN;
     const int vt = wm * Tl::MI * 16 + (lane >> 4) * 4, rt = wn * Tl::NJ * 16 + (lane & 15);  // in the tile
-    if (S::N > 1) unscale<S>(acc, *a.scales);
+    if (S::N > 1) unscale<S>(a, acc, v0 + vt, r0 + rt);
     const float top = a.totals->weight;
     float w[Tl::NJ];
 #pragma unroll
@@ -698,12 +727,11 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void errors_kernel(c
         const bool on = row.target >= 0;
         const float lse = on ? a.lse_in[r] : 0.0f;
         w[j] = on && top != 0.0f ? row.weight / top : 0.0f;
-        const float from = lse * kLog2e;
 #pragma unroll
         for (int i = 0; i < Tl::MI; i++)
 #pragma unroll
             for (int q = 0; q < 4; q++) {
-                const float x = exp_from<N>(acc[i][j][q], lse, from);
+                const float x = fast_exp(acc[i][j][q] - lse);
                 acc[i][j][q] = on ? Matrix<T>::kScale * x : 0.0f;
             }
         const int64_t y = row.target - (o.first + v0 + vt);
@@ -969,7 +997,7 @@ struct Plan {
     Size logits = kMiddle, errors = kMiddle, gradients = kMiddle;
     int tiles = 0;                       // tiles of tokens, forward
     int splits = 0, splits_n = 0;        // of the tokens for dh, of the rows for dW
-    int64_t rows = 0, totals = 0, scales = 0, largest = 0, sums = 0, counts = 0, tops = 0, at_target = 0, part = 0;
+    int64_t rows = 0, totals = 0, scales = 0, hidden_scale = 0, head_scale = 0, largest = 0, sums = 0, counts = 0, tops = 0, at_target = 0, part = 0;
     int64_t hidden = 0, head = 0, head_piece = 0, hidden_t = 0, head_t = 0, e = 0, we = 0, slab = 0, slab_head = 0;
     int64_t bytes_loss = 0, bytes_backward = 0;
 };
@@ -1011,6 +1039,9 @@ Plan plan_of(const gear_token_desc& d) {
     p.rows = take(d.n * (int64_t)sizeof(Row));
     p.totals = take(sizeof(Totals));
     p.scales = take(sizeof(Scales));
+    // Whole tiles of tokens.
+    p.hidden_scale = take(p.parts > 1 ? d.n * 4 : 0);
+    p.head_scale = take(p.parts > 1 ? up(p.piece > p.loss_piece ? p.piece : p.loss_piece, 256) * 4 : 0);
     p.largest = take(2 * kParts * sizeof(uint32_t));
     p.sums = take(kParts * sizeof(double));
     p.counts = take(kParts * sizeof(int64_t));
@@ -1061,6 +1092,8 @@ Args args_of(const gear_token_desc& d, const Plan& p, char* work) {
     a.rows = reinterpret_cast<Row*>(work + p.rows);
     a.totals = reinterpret_cast<Totals*>(work + p.totals);
     a.scales = reinterpret_cast<Scales*>(work + p.scales);
+    a.hidden_scale = reinterpret_cast<int32_t*>(work + p.hidden_scale);
+    a.head_scale = reinterpret_cast<int32_t*>(work + p.head_scale);
     a.largest = reinterpret_cast<uint32_t*>(work + p.largest);
     a.sums = reinterpret_cast<double*>(work + p.sums);
     a.counts = reinterpret_cast<int64_t*>(work + p.counts);
@@ -1092,18 +1125,18 @@ struct Call {
     hipStream_t s;
 
     // An operand of rows as they lie, or of a copy that `job` makes.
-    Operand operand(const void* src, int64_t rows, int64_t ld_src, int64_t to, Job& job) const {
+    Operand operand(const void* src, int64_t rows, int64_t ld_src, int64_t to, int32_t* scale, Job& job) const {
         if (plain_rows(d.dtype, src, ld_src, d.D)) return Operand{src, rows, ld_src, 0};
-        job = Job{src, work + to, rows, d.D, ld_src, p.ldk, pitch(p.ldk), rows * pitch(p.ldk), 0, 0};
+        job = Job{src, work + to, scale, rows, d.D, ld_src, p.ldk, pitch(p.ldk), rows * pitch(p.ldk), 0, 0};
         return Operand{work + to, rows, pitch(p.ldk), rows * pitch(p.ldk)};
     }
     // A turned copy: d.D rows of ld values.
     Operand turned_operand(const void* src, int64_t rows, int64_t ld_src, int64_t len, int64_t to, bool on, Job& job) const {
         const int64_t ld = pitch(len);
-        job = Job{src, work + to, rows, d.D, ld_src, len, ld, d.D * ld, 0, on ? 1 : 0};
+        job = Job{src, work + to, nullptr, rows, d.D, ld_src, len, ld, d.D * ld, 0, on ? 1 : 0};
         return Operand{work + to, d.D, ld, d.D * ld};
     }
-    // The scales of 32-bit values: before anything is copied.
+    // The scales of 32-bit values: before anything is turned.
     hipError_t look(const Args& a, const void* hidden, const void* head) const {
         if constexpr (N > 1) {
             hipLaunchKernelGGL(largest_kernel, dim3(2 * a.max_parts), dim3(kThreads), 0, s, a, static_cast<const float*>(hidden),
@@ -1117,7 +1150,7 @@ struct Call {
         int32_t at = j.row_blocks = rows ? a.row_parts : 0;
         for (Job& c : j.copy) {
             c.first = at;
-            if (c.src) at += (int32_t)some_blocks(c.rows * (c.len / 8), 4096);
+            if (c.src) at += (int32_t)some_blocks(c.rows * (N > 1 ? lanes_of(c.len / 8) : c.len / 8), 4096);
         }
         for (Job& c : j.turn) {
             c.first = at;
@@ -1149,13 +1182,12 @@ struct Call {
     hipError_t loss(Args a, const void* hidden, const void* head) const {
         a.at_target = reinterpret_cast<float*>(work + p.at_target);
         a.part = reinterpret_cast<float2*>(work + p.part);
-        hipError_t e = a.n > 0 ? look(a, hidden, head) : hipSuccess;
-        if (e != hipSuccess) return e;
+        hipError_t e = hipSuccess;
         for (int64_t first = 0; first < a.V && a.n > 0; first += p.loss_piece) {
             const int64_t tokens = a.V - first < p.loss_piece ? a.V - first : p.loss_piece;
             Jobs j{};
-            const Operand x = operand(static_cast<const E*>(head) + first * d.head_row, tokens, d.head_row, p.head, j.copy[0]);
-            Operand y = operand(hidden, a.n, d.hidden_row, p.hidden, j.copy[1]);
+            const Operand x = operand(static_cast<const E*>(head) + first * d.head_row, tokens, d.head_row, p.head, a.head_scale, j.copy[0]);
+            Operand y = operand(hidden, a.n, d.hidden_row, p.hidden, a.hidden_scale, j.copy[1]);
             if (first > 0) j.copy[1] = Job{};
             if ((e = prepare(a, j, false)) != hipSuccess) return e;
             e = p.logits == kBig ? logits<Big>(a, x, y, first) : p.logits == kMiddle ? logits<Middle>(a, x, y, first)
@@ -1191,8 +1223,8 @@ struct Call {
             const E* from = static_cast<const E*>(head) + first * d.head_row;
             Jobs j{};
             Gradients g{};
-            const Operand x = operand(from, tokens, d.head_row, p.head_piece, j.copy[0]);
-            const Operand y = operand(hidden, a.n, d.hidden_row, p.hidden, j.copy[1]);
+            const Operand x = operand(from, tokens, d.head_row, p.head_piece, a.head_scale, j.copy[0]);
+            const Operand y = operand(hidden, a.n, d.hidden_row, p.hidden, a.hidden_scale, j.copy[1]);
             if (dhead) g.ht = turned_operand(hidden, a.n, d.hidden_row, p.ldn, p.hidden_t, true, j.turn[0]);
             if (dhidden) g.wt = turned_operand(from, tokens, d.head_row, ldv, p.head_t, false, j.turn[1]);
             if (first > 0) j.copy[1] = j.turn[0] = Job{};  // made for the first piece

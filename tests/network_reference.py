@@ -99,15 +99,16 @@ class Token:
         D = self.h.shape[1]
         # A logit: products added 32 at a time in 32 bits.  Those of 16-bit values are exact.  32-bit values enter as two
         # fp16 parts: the first is off by 2^-11 of the value at most, the second by 2^-11 of that, 2^-22 in all, or by
-        # 2^-25 of the unit that the tensor's largest value has 2^14 of, 2^-39 of that value; the product of the second
+        # 2^-25 of the unit that the row's largest value has 2^14 of, 2^-39 of that value; the product of the second
         # parts, left out, is 2^-22 at most.  Three times 2^-22 are 12 units of 2^-24.
         size = self.h.abs() @ self.W.abs().t()
         self.z_off = (U32 * (8 + D / 16) * size).amax(1)
         self.parts_off = 0.0
         if self.dtype == torch.float32 and n:
             self.parts_off = 12 * U32
-            low = 2.0 ** -39 * (self.h.abs().max() * self.W.abs().sum(1).max() + self.W.abs().max() * self.h.abs().sum(1).max())
-            self.z_off = self.z_off + (12 * U32 * size).amax(1) + low
+            h, W = self.h.abs(), self.W.abs()
+            low = 2.0 ** -39 * (h.amax(1)[:, None] * W.sum(1) + W.amax(1) * h.sum(1)[:, None])
+            self.z_off = self.z_off + (12 * U32 * size + low).amax(1)
         # Exponentials of rounded products of up to |z|, a logarithm, and sums over the vocabulary, all positive.
         self.lse_off = 2 * self.z_off + U32 * (16 + 2 * z.abs().amax(1)) + U32 * self.lse.abs()
         self.logp = torch.where(self.on, lp, 0.0)
@@ -125,7 +126,7 @@ class Token:
         # e: the exponential's own error, the subtraction's, the rounding to the products' type (its floor: 2^-39), and
         # the rounding of e times the weight.
         e_off = self.p * (self.z_off + self.lse_off + 8 * U32)[:, None] + (held * 1.01 + 8 * U32) * e.abs() + 2.0 ** -38
-        # The products of parts once more, and hidden values and head where they are far below the largest.
+        # The products of parts once more, and hidden values and head where they are far below the tensor's largest.
         e_off = e_off + self.parts_off * e.abs()
         low = 2.0 ** -39 if dt == torch.float32 else 0.0
         low_W, low_h = (low * t.abs().max() if t.numel() else 0.0 for t in (self.W, self.h))

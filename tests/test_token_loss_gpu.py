@@ -155,6 +155,43 @@ def test_large_logits():
     assert float(loss) == 0 and not logp.any()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_logits_far_from_zero(dtype):
+    """All logits of a row are 2^21 + a small integer, exact in 32 bits: log-probabilities depend on the small part alone."""
+    n, V = 70, 300
+    g = torch.Generator().manual_seed(3)
+    h = torch.tensor([2048.0, 1.0]).expand(n, 2).contiguous()
+    W = torch.stack([torch.full((V,), 1024.0), torch.randint(-9, 10, (V,), generator=g).float()], 1)
+    t = torch.randint(0, V, (n,), generator=g)
+    say("token_loss logits of 2^21 %s" % dtype)
+    loss, logp, lse = gear.token_loss(h.to(dtype).to(cuda()), W.to(dtype).to(cuda()), t.to(cuda()))
+    want = W.double()[t, 1] - torch.logsumexp(W.double()[:, 1], 0)
+    # Distances are whole numbers up to 18.  An exponential takes one rounding of distance times log2 e, at most 26 * 2^-24 / 2
+    # in the power and ln 2 of that in the value, and two units of its own: 11 * 2^-24.  A sum of 300 positive terms in tiles adds at
+    # most 16 roundings in a row per level and three levels: 48 * 2^-24.  A logarithm below 8 adds 2 units of 2^-21 at most,
+    # 16 * 2^-24; the difference below 32 one of 2^-20, 16 * 2^-24.
+    near(logp, want, torch.full_like(want, 91 * 2.0 ** -24), "logp")
+    # lse's last digit is 2^-2.
+    near(lse, 2.0 ** 21 + torch.logsumexp(W.double()[:, 1], 0).expand(n), torch.full((n,), 2.0 ** -2, dtype=torch.float64), "lse")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_certain_rows_of_every_type(dtype):
+    """The largest logits of the type, up to 1.5 * 2^127, are certain: 0, and no other value."""
+    far = 2.0 ** 15 if dtype == torch.float16 else 2.0 ** 63
+    h, W = torch.zeros(40, 8), torch.zeros(90, 8)
+    h[:, 0] = 2.0 ** torch.linspace(0, 15 if dtype == torch.float16 else 64, 40).round()
+    W[33, 0] = 1.5 * far
+    say("token_loss certain rows %s" % dtype)
+    t = torch.full((40,), 33)
+    args = [x.to(cuda()) for x in (h.to(dtype), W.to(dtype), t)]
+    loss, logp, lse = gear.token_loss(*args)
+    assert float(loss) == 0 and not logp.any()
+    assert torch.equal(lse.cpu(), h[:, 0] * 1.5 * far)
+    dh, dW = gear.token_loss_backward(*args, lse)
+    assert not dh.any() and not dW.any()
+
+
 @pytest.mark.parametrize("hidden,head", [(1e30, 1e-30), (1e-30, 1e30), (1e-36, 1e34), (3e38, 1e-38), (0.0, 1.0), (1.0, 0.0), (1e-42, 1.0)])
 def test_32_bit_values_of_any_size(hidden, head):
     """Ends of the range, zeros, subnormal values; rows that take no part are far larger."""
@@ -163,6 +200,19 @@ def test_32_bit_values_of_any_size(hidden, head):
     on = torch.rand(150, generator=torch.Generator().manual_seed(2)) < 0.7
     h[~on] = 1e38 if hidden < 1e37 else float("inf")
     check(h.to(cuda()), W.to(cuda()), t.to(cuda()), on.to(cuda()), w.to(cuda()), what="values of %g and %g" % (hidden, head))
+
+
+def test_32_bit_rows_stand_for_themselves():
+    """A row far larger than the others, or of infinities, changes none of them."""
+    h, W, t, w = inputs(150, 100, 200, torch.float32)
+    args = [x.to(cuda()) for x in (W, t)]
+    say("token_loss rows of their own")
+    _, logp, lse = gear.token_loss(h.to(cuda()), *args)
+    for odd in (1e30, float("inf"), float("nan")):
+        h[7] = odd
+        _, other, other_lse = gear.token_loss(h.to(cuda()), *args)
+        keep = torch.arange(150) != 7
+        assert torch.equal(other.cpu()[keep], logp.cpu()[keep]) and torch.equal(other_lse.cpu()[keep], lse.cpu()[keep])
 
 
 def test_32_bit_rows_of_different_sizes():
