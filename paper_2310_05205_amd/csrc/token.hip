@@ -300,23 +300,17 @@ __global__ __launch_bounds__(kThreads) void largest_kernel(const Args a, const f
         a.largest[(first ? 0 : kParts) + blockIdx.x % a.max_parts] = top;
     }
 }
-// The scales, in every thread of a workgroup.
-__device__ __forceinline__ Scales find_scales(const Args& a) {
-    __shared__ uint32_t s[2][kThreads / 64];
+// The scale of hidden values (q = 0) or of the head from those, in every thread of a workgroup.
+__device__ __forceinline__ int32_t find_scale(const Args& a, int q) {
+    __shared__ uint32_t s[kThreads / 64];
     static_assert(kThreads >= kParts, "a lane for each workgroup's");
+    uint32_t top = (int)threadIdx.x < a.max_parts ? a.largest[q * kParts + threadIdx.x] : 0;
 #pragma unroll
-    for (int q = 0; q < 2; q++) {
-        uint32_t top = (int)threadIdx.x < a.max_parts ? a.largest[q * kParts + threadIdx.x] : 0;
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off));
-        if ((threadIdx.x & 63) == 0) s[q][threadIdx.x >> 6] = top;
-    }
+    for (int off = 32; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off));
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = top;
     __syncthreads();
-    uint32_t top[2] = {0, 0};
-#pragma unroll
-    for (int q = 0; q < 2; q++)
-        for (int k = 0; k < kThreads / 64; k++) top[q] = max(top[q], s[q][k]);
-    return Scales{scale_for(top[0]), scale_for(top[1])};
+    for (int k = 0; k < kThreads / 64; k++) top = max(top, s[k]);
+    return scale_for(top);
 }
 
 // The parts of 8 values in a row, to `to` and, `part` values apart, behind it.
@@ -429,13 +423,14 @@ __global__ __launch_bounds__(kThreads) void prepare_kernel(const Args a, const J
     const int copy1 = jobs.copy[1].first, turn0 = jobs.turn[0].first, turn1 = jobs.turn[1].first;
     if (b < copy1) return run_copy<E>(jobs.copy[0], b - jobs.copy[0].first, copy1 - jobs.copy[0].first);
     if (b < turn0) return run_copy<E>(jobs.copy[1], b - copy1, turn0 - copy1);
-    Scales by{0, 0};
+    const int q = b < turn1 ? 0 : 1, first = q == 0 ? turn0 : turn1;
+    const Job& turn = jobs.turn[q];
+    int32_t by = 0;
     if constexpr (Parts<E>::kCount > 1) {
-        by = find_scales(a);
-        if (b == turn0 && threadIdx.x == 0) *a.scales = by;
+        by = find_scale(a, q);
+        if (b == first && threadIdx.x == 0) (q == 0 ? a.scales->hidden : a.scales->head) = by;
     }
-    if (b < turn1) return run_turn<E>(a, jobs.turn[0], by.hidden, b - turn0, turn1 - turn0, tile);
-    run_turn<E>(a, jobs.turn[1], by.head, b - turn1, jobs.blocks - turn1, tile);
+    run_turn<E>(a, turn, by, b - first, (q == 0 ? turn1 : jobs.blocks) - first, tile);
 }
 
 // --- the tile loop --------------------------------------------------------------
@@ -825,13 +820,73 @@ struct Gradients {
     float* slab;            // [splits][n][ld]: dh so far; a split of the piece's tokens each
     float* slab_head;       // [splits_n][tokens][ld]: dW where the rows are split
     void* dhead;            // the piece's first row
+    void* dhidden;          // where dh is one sum, written here and not to the slab
     int64_t ld;
     int32_t steps_v, steps_n, splits, splits_n, add;
     int32_t dh_blocks, tm, tn_rows, tn_tokens;  // tiles across D, down the rows and the tokens
 };
+// What the sums of a row of dh, per weight, and of dW are multiplied by.
+template <typename T>
+__device__ __forceinline__ float rows_factor(const Args& a) {
+    return a.totals->share * a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / Matrix<T>::kScale;
+}
 template <typename T>
 __device__ __forceinline__ float head_factor(const Args& a) {
-    return a.totals->weight * a.totals->share * a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / Matrix<T>::kScale;
+    return a.totals->weight * rows_factor<T>(a);
+}
+// A tile of a gradient, columns from d0 and `rows` - row0 rows at most, each times by[j] 2^e, or 0 where it is not on.
+template <typename E, typename S>
+__device__ __forceinline__ void put_tile(const F4 (&acc)[S::MI][S::NJ], char* lds, E* out, int64_t rows, int64_t D, int64_t row0,
+                                         int64_t d0, int nt, int dt, const float (&by)[S::NJ], const bool (&on)[S::NJ], int32_t e) {
+    if constexpr (sizeof(E) == 4) {
+        // 16 bytes a lane as they are.
+#pragma unroll
+        for (int j = 0; j < S::NJ; j++) {
+            const int64_t r = row0 + nt + j * 16;
+            if (r >= rows) continue;
+            const Factor times(by[j], e);
+#pragma unroll
+            for (int i = 0; i < S::MI; i++) {
+                const int64_t d = d0 + dt + i * 16;
+                float f[4];
+#pragma unroll
+                for (int q = 0; q < 4; q++) f[q] = on[j] ? times(acc[i][j][q]) : 0.0f;
+                if (d + 4 <= D) {
+                    Vec<E, 4>::store(out + r * D + d, f);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; q++)
+                        if (d + q < D) out[r * D + d + q] = (E)f[q];
+                }
+            }
+        }
+    } else {
+        typedef E E4 __attribute__((ext_vector_type(4)));
+        typedef uint32_t Line __attribute__((ext_vector_type(4)));
+        typedef Line LooseLine __attribute__((aligned(2)));
+#pragma unroll
+        for (int j = 0; j < S::NJ; j++)
+#pragma unroll
+            for (int i = 0; i < S::MI; i++) {
+                E4 f;
+#pragma unroll
+                for (int q = 0; q < 4; q++) f[q] = on[j] ? (E)(acc[i][j][q] * by[j]) : (E)0.0f;
+                *reinterpret_cast<uint2*>(spot<S::BM>(lds, nt + j * 16, dt + i * 16)) = __builtin_bit_cast(uint2, f);
+            }
+        __syncthreads();
+#pragma unroll 4
+        for (int k = threadIdx.x; k < S::BN * (S::BM / 8); k += S::kThreads) {
+            const int row = k / (S::BM / 8), col = k % (S::BM / 8) * 8;
+            if (row0 + row >= rows || d0 + col >= D) continue;
+            E* to = out + (row0 + row) * D + d0 + col;
+            const char* from = spot<S::BM>(lds, row, col);
+            if (d0 + col + 8 <= D) {
+                *reinterpret_cast<LooseLine*>(to) = *reinterpret_cast<const Line*>(from);
+            } else {
+                for (int q = 0; q < 8 && d0 + col + q < D; q++) to[q] = reinterpret_cast<const E*>(from)[q];
+            }
+        }
+    }
 }
 template <typename E, typename T, typename S>
 __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gradients_kernel(const Args a, const Gradients g) {
@@ -840,12 +895,26 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gradients_kerne
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / S::WN, wn = wave % S::WN;
     const int dt = wm * Tl::MI * 16 + (lane >> 4) * 4, nt = wn * Tl::NJ * 16 + (lane & 15);  // in the tile
     F4 acc[Tl::MI][Tl::NJ];
+    float by[Tl::NJ];
+    bool on[Tl::NJ];
     if ((int)blockIdx.x < g.dh_blocks) {
         const int split = blockIdx.x % g.splits;
         const Place at = place_of(blockIdx.x / g.splits, g.tm, g.tn_rows);
         const int64_t d0 = (int64_t)at.m * S::BM, r0 = (int64_t)at.n * S::BN;
         const int from = (int)((int64_t)g.steps_v * split / g.splits), to = (int)((int64_t)g.steps_v * (split + 1) / g.splits);
         Tl::run(g.wt, g.er, d0, r0, (int64_t)from * kStep, to - from, lds, acc);
+        if (g.dhidden) {
+            const float all = rows_factor<T>(a);
+#pragma unroll
+            for (int j = 0; j < Tl::NJ; j++) {
+                const int64_t r = r0 + nt + j * 16;
+                const Row row = r < a.n ? a.rows[r] : Row{-1, 0.0f};
+                on[j] = row.target >= 0;
+                by[j] = row.weight * all;
+            }
+            put_tile<E, S>(acc, lds, static_cast<E*>(g.dhidden), a.n, a.D, r0, d0, nt, dt, by, on, sizeof(E) == 4 ? -a.scales->head : 0);
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < Tl::NJ; j++) {
             const int64_t r = r0 + nt + j * 16;
@@ -878,57 +947,13 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gradients_kerne
         }
         return;
     }
-    const float by = head_factor<T>(a);
-    E* out = static_cast<E*>(g.dhead);
-    if constexpr (sizeof(E) == 4) {
-        const Factor times(by, -a.scales->hidden);
-        // 16 bytes a lane as they are.
+    const float all = head_factor<T>(a);
 #pragma unroll
-        for (int j = 0; j < Tl::NJ; j++) {
-            const int64_t v = v0 + nt + j * 16;
-            if (v >= g.we.rows) continue;
-#pragma unroll
-            for (int i = 0; i < Tl::MI; i++) {
-                const int64_t d = d0 + dt + i * 16;
-                float f[4];
-#pragma unroll
-                for (int q = 0; q < 4; q++) f[q] = times(acc[i][j][q]);
-                if (d + 4 <= a.D) {
-                    Vec<E, 4>::store(out + v * a.D + d, f);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 4; q++)
-                        if (d + q < a.D) out[v * a.D + d + q] = (E)f[q];
-                }
-            }
-        }
-    } else {
-        typedef E E4 __attribute__((ext_vector_type(4)));
-        typedef uint32_t Line __attribute__((ext_vector_type(4)));
-        typedef Line LooseLine __attribute__((aligned(2)));
-#pragma unroll
-        for (int j = 0; j < Tl::NJ; j++)
-#pragma unroll
-            for (int i = 0; i < Tl::MI; i++) {
-                E4 f;
-#pragma unroll
-                for (int q = 0; q < 4; q++) f[q] = (E)(acc[i][j][q] * by);
-                *reinterpret_cast<uint2*>(spot<S::BM>(lds, nt + j * 16, dt + i * 16)) = __builtin_bit_cast(uint2, f);
-            }
-        __syncthreads();
-#pragma unroll 4
-        for (int k = threadIdx.x; k < S::BN * (S::BM / 8); k += S::kThreads) {
-            const int row = k / (S::BM / 8), col = k % (S::BM / 8) * 8;
-            if (v0 + row >= g.we.rows || d0 + col >= a.D) continue;
-            E* to = out + (v0 + row) * a.D + d0 + col;
-            const char* from = spot<S::BM>(lds, row, col);
-            if (d0 + col + 8 <= a.D) {
-                *reinterpret_cast<LooseLine*>(to) = *reinterpret_cast<const Line*>(from);
-            } else {
-                for (int q = 0; q < 8 && d0 + col + q < a.D; q++) to[q] = reinterpret_cast<const E*>(from)[q];
-            }
-        }
+    for (int j = 0; j < Tl::NJ; j++) {
+        on[j] = true;
+        by[j] = all;
     }
+    put_tile<E, S>(acc, lds, static_cast<E*>(g.dhead), g.we.rows, a.D, v0, d0, nt, dt, by, on, sizeof(E) == 4 ? -a.scales->hidden : 0);
 }
 
 // Sums over the splits of dW of a piece, and of dh after the last piece, times what
@@ -936,7 +961,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gradients_kerne
 template <typename E, typename T>
 __global__ __launch_bounds__(kThreads) void splits_kernel(const Args a, const Gradients g, int64_t tokens, E* dhidden) {
     const int64_t per_row = (a.D + 3) / 4, rows = dhidden ? a.n : 0;
-    const float by = a.totals->share * a.grad_scale * (a.grad_loss ? *a.grad_loss : 1.0f) / Matrix<T>::kScale;
+    const float by = rows_factor<T>(a);
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < (rows + tokens) * per_row;
          i += (int64_t)gridDim.x * kThreads) {
         const int64_t r = i / per_row, d = i % per_row * 4;
@@ -997,6 +1022,7 @@ struct Plan {
     Size logits = kMiddle, errors = kMiddle, gradients = kMiddle;
     int tiles = 0;                       // tiles of tokens, forward
     int splits = 0, splits_n = 0;        // of the tokens for dh, of the rows for dW
+    bool direct = false;                 // dh is one sum
     int64_t rows = 0, totals = 0, scales = 0, hidden_scale = 0, head_scale = 0, largest = 0, sums = 0, counts = 0, tops = 0, at_target = 0, part = 0;
     int64_t hidden = 0, head = 0, head_piece = 0, hidden_t = 0, head_t = 0, e = 0, we = 0, slab = 0, slab_head = 0;
     int64_t bytes_loss = 0, bytes_backward = 0;
@@ -1021,15 +1047,19 @@ Plan plan_of(const gear_token_desc& d) {
     p.errors = size_of(p.piece, d.n, d.n);
     p.gradients = d.n <= 64 ? kSmall : size_of(d.D, p.piece + d.n, d.n);
     p.tiles = (int)tiles(d.V, edge(p.logits));
-    // Few tiles of dh share the GPU's 256 units by splitting the tokens.
+    // Few tiles of dh share the GPU's 256 units by splitting the tokens, from 16 steps on: one sum is written as dh itself, and
+    // splits cost their slab and a launch (fp32, rows of 64, forward and backward: 500 rows and tokens 38.7 us whole and 41.2
+    // in two; 1000 rows and tokens 46.2 whole and 44.5 in four).
     const int64_t dh = tiles(d.D, edge(p.gradients)) * tiles(d.n, edge(p.gradients)), steps = p.ldv / kStep;
     p.splits = 1;
-    while (dh * p.splits < 256 && p.splits * 8 <= steps && p.splits < 16) p.splits *= 2;
+    while (dh * p.splits < 256 && steps >= 16 && p.splits * 8 <= steps && p.splits < 16) p.splits *= 2;
+    p.direct = p.splits == 1 && p.piece >= d.V;
     // So do few tiles of dW, splitting the rows: 65536 rows of 64, a head of 18, bf16, forward and backward take 93 us so
     // and 1490 with the rows in one piece.
     const int64_t dw = tiles(d.D, edge(p.gradients)) * tiles(p.piece, edge(p.gradients));
     p.splits_n = 1;
-    while (dw * p.splits_n < 256 && p.splits_n * 8 <= p.ldn / kStep && p.splits_n < 64) p.splits_n *= 2;
+    const int64_t steps_n = p.ldn / kStep;
+    while (dw * p.splits_n < 256 && steps_n >= 16 && p.splits_n * 8 <= steps_n && p.splits_n < 64) p.splits_n *= 2;
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
         const int64_t here = at;
@@ -1058,7 +1088,7 @@ Plan plan_of(const gear_token_desc& d) {
     p.head_t = take(d.D * (p.ldv + 64) * p.parts * 2);
     p.e = take(d.n * (p.ldv + 64) * p.parts * 2);
     p.we = take(p.ldv * pitch(p.ldn) * p.parts * 2);
-    p.slab = take(p.splits * d.n * p.ldk * 4);
+    if (!p.direct) p.slab = take(p.splits * d.n * p.ldk * 4);
     if (p.splits_n > 1) p.slab_head = take(p.splits_n * p.piece * p.ldk * 4);
     p.bytes_backward = at;
     return p;
@@ -1247,6 +1277,7 @@ struct Call {
             g.slab = slab;
             g.slab_head = reinterpret_cast<float*>(work + p.slab_head);
             g.dhead = dhead ? static_cast<E*>(dhead) + first * a.D : nullptr;
+            g.dhidden = p.direct ? dhidden : nullptr;
             g.ld = p.ldk;
             g.steps_v = (int32_t)(ldv / kStep);
             g.steps_n = (int32_t)(p.ldn / kStep);
@@ -1259,7 +1290,7 @@ struct Call {
             if (e != hipSuccess) return e;
             // What is left in splits: dW of this piece, dh after the last.
             const bool last = first + p.piece >= a.V;
-            const int64_t heads = dhead && p.splits_n > 1 ? tokens : 0, rows = dhidden && last ? a.n : 0;
+            const int64_t heads = dhead && p.splits_n > 1 ? tokens : 0, rows = dhidden && last && !p.direct ? a.n : 0;
             if (heads + rows == 0) continue;
             hipLaunchKernelGGL((splits_kernel<E, T>), dim3(some_blocks((heads + rows) * ((a.D + 3) / 4), 8192)), dim3(kThreads), 0,
                                s, a, g, heads, rows ? static_cast<E*>(dhidden) : nullptr);
