@@ -1012,6 +1012,8 @@ Size size_of(int64_t m, int64_t n, int64_t rows) {
     if (tiles(m, 128) * tiles(n, 128) < 256) return kSmall;
     return tiles(m, 256) * tiles(n, 256) >= 192 ? kBig : kMiddle;
 }
+// Workgroups of a product that the GPU's 256 units run at once: as many as LDS holds.
+int64_t slots_of(Size s, int parts) { return s == kBig || (s == kMiddle && parts > 1) ? 256 : 512; }
 int edge(Size s) { return s == kBig ? 256 : s == kMiddle ? 128 : 64; }
 
 // Where everything lies in the workspace.
@@ -1047,19 +1049,22 @@ Plan plan_of(const gear_token_desc& d) {
     p.errors = size_of(p.piece, d.n, d.n);
     p.gradients = d.n <= 64 ? kSmall : size_of(d.D, p.piece + d.n, d.n);
     p.tiles = (int)tiles(d.V, edge(p.logits));
-    // Few tiles of dh share the GPU's 256 units by splitting the tokens, from 16 steps on: one sum is written as dh itself, and
+    // Few tiles of dh share the GPU by splitting the tokens, while they then run all at once: 24 big tiles (1519 x 1003 x 50001
+    // fp16, backward) take 625 us in 8 splits and 657 in 16, of which the second half would follow the first and the slab be
+    // twice as large (1500 x 1024 x 20000 bf16: 218 and 255).  And from 16 steps on: one sum is written as dh itself, and
     // splits cost their slab and a launch (fp32, rows of 64, forward and backward: 500 rows and tokens 38.7 us whole and 41.2
     // in two; 1000 rows and tokens 46.2 whole and 44.5 in four).
+    const int64_t slots = slots_of(p.gradients, p.parts);
     const int64_t dh = tiles(d.D, edge(p.gradients)) * tiles(d.n, edge(p.gradients)), steps = p.ldv / kStep;
     p.splits = 1;
-    while (dh * p.splits < 256 && steps >= 16 && p.splits * 8 <= steps && p.splits < 16) p.splits *= 2;
+    while (dh * p.splits * 2 <= slots && steps >= 16 && p.splits * 8 <= steps && p.splits < 16) p.splits *= 2;
     p.direct = p.splits == 1 && p.piece >= d.V;
     // So do few tiles of dW, splitting the rows: 65536 rows of 64, a head of 18, bf16, forward and backward take 93 us so
     // and 1490 with the rows in one piece.
     const int64_t dw = tiles(d.D, edge(p.gradients)) * tiles(p.piece, edge(p.gradients));
     p.splits_n = 1;
     const int64_t steps_n = p.ldn / kStep;
-    while (dw * p.splits_n < 256 && steps_n >= 16 && p.splits_n * 8 <= steps_n && p.splits_n < 64) p.splits_n *= 2;
+    while (dw * p.splits_n * 2 <= slots && steps_n >= 16 && p.splits_n * 8 <= steps_n && p.splits_n < 64) p.splits_n *= 2;
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
         const int64_t here = at;
