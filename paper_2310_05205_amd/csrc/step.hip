@@ -156,7 +156,8 @@ __device__ __forceinline__ float store8(uint8_t* p, int64_t left, const float (&
     return some ? top * (1.0f / kTop) : 0.0f;
 }
 
-// The step's factors, and the step counted; one lane.
+// The step's factors, and the step counted; one lane, 2 to 5 us.  In its own launch, as all workgroups of the update read
+// what it writes.
 __global__ void factors_kernel(Factors* out, int64_t* step, const float* d_lr, const float* d_factor, double lr,
                                double log1, double log2, double weight_decay) {
     const float factor = d_factor ? *d_factor : 1.0f;
@@ -178,6 +179,8 @@ struct Betas {
     float b1, c1, b2, c2, eps;  // c = 1 - b
 };
 
+// One read and one write of everything a value has; memory bounds it: 147 M bf16 values with masters and 32-bit averages, 28
+// bytes each, 760 us, 5.4 TB/s; 54 M with 8-bit averages, 16 bytes each, 164 us, 5.3 TB/s.
 template <typename E, bool MASTER, bool BITS8, bool STREAM>
 __global__ __launch_bounds__(kThreads) void update_kernel(const Items t, const Betas b, const Factors* factors) {
     const Factors f = *factors;
@@ -277,7 +280,8 @@ __device__ __forceinline__ double squares(const Grads& t, uint32_t first, uint32
     return sum;
 }
 
-// A sum per workgroup; `add` to those of the launches before.
+// A sum per workgroup; `add` to those of the launches before.  Squares in 64 bits, which memory hides: 218 M bf16 values 99 to
+// 124 us, 3.5 to 4.4 TB/s, 61 M 41.
 template <typename E>
 __global__ __launch_bounds__(kThreads) void squares_kernel(const Grads t, double* sums, int add) {
     __shared__ double s[kThreads / 64];
@@ -304,7 +308,8 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const double* sums, int 
     if (threadIdx.x == 0) limit.put(sum);
 }
 
-// Few gradients of one type: one workgroup and no second launch.
+// Few gradients of one type: one workgroup and no second launch (26000 values in 13 tensors: 8 us; norm and step together
+// 20 us, and 23.4 with two launches for the norm).
 constexpr int kSoloThreads = 1024;
 constexpr uint32_t kSoloChunks = 32;
 template <typename E>
@@ -378,7 +383,7 @@ Update update_of(int32_t dtype, bool master) {
     return master ? update_kernel<_Float16, true, BITS8, STREAM> : update_kernel<_Float16, false, BITS8, STREAM>;
 }
 // With 8-bit averages, what no cache holds until the next step passes by it: 123 M values
-// with masters, a step with its norm, 428 us, and 461 through the caches.  With 32-bit averages
+// with masters, a step with its norm, 417 us, and 461 through the caches.  With 32-bit averages
 // that gains nothing (218 M values: 1306 and 1278).
 constexpr int64_t kStreamValues = 16 << 20;
 

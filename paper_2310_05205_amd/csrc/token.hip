@@ -18,7 +18,7 @@
 // 2^-22 of the value, or by 2^-40 of the largest where the value is far below it.  The products a1 b1, a1 b2 and a2 b1 leave out
 // 2^-22 of |a b| at most.  Matrix instructions of 16-bit types are 16 times as fast as those of 32
 // bits, so three of them take a fifth of the time.  (Three bf16 parts need no scale and leave
-// 2^-25, but six products: 1000 x 512 x 8192, forward and backward, took 245 us with them and takes 175.)
+// 2^-25, but six products: 1000 x 512 x 8192, forward and backward, took 245 us with them and takes 158.)
 #include <math.h>
 
 #include <type_traits>
@@ -183,6 +183,8 @@ __global__ __launch_bounds__(64) void totals_kernel(const Args a) {
 
 // Joins the tiles' maxima and sums, LANES lanes a row: lse, logp, and a sum of the
 // losses and a count of the rows that take part per workgroup; the loss where there is but one.
+// Two passes over a row's tiles, the second from the cache; latency bounds it: 4096 rows of 128
+// tiles 7 us, 16 rows of 512 tiles in one workgroup 6, 320 rows of one tile 3.
 template <int LANES>
 __global__ __launch_bounds__(kThreads) void lse_kernel(const Args a) {
     __shared__ double s[kThreads / 64];
@@ -267,7 +269,9 @@ __device__ __forceinline__ uint32_t larger_finite(uint32_t top, float f) {
     const uint32_t m = __builtin_bit_cast(uint32_t, f) & 0x7FFFFFFFu;
     return m < 0x7F800000u && m > top ? m : top;
 }
-// Largest finite magnitudes of 32-bit hidden rows that take part and of the head: a.max_parts workgroups each.
+// Largest finite magnitudes of 32-bit hidden rows that take part and of the head: a.max_parts workgroups each.  1000 and 8192
+// rows of 512: 5.5 us, latency.  A workgroup that turns rows could look at all of them itself and save this launch,
+// which gains 1.8 us at 4000 values and loses 2.5 at 24000.
 __global__ __launch_bounds__(kThreads) void largest_kernel(const Args a, const float* hidden, int64_t hidden_row,
                                                            const float* head, int64_t head_row) {
     __shared__ uint32_t s[kThreads / 64];
@@ -414,7 +418,9 @@ __device__ __forceinline__ void run_turn(const Args& a, const Job& j, int32_t by
     }
 }
 // What has to be done before a product, in one launch: workgroups for each job; copies of
-// the head and of hidden rows, then hidden rows and the head turned.
+// the head and of hidden rows, then hidden rows and the head turned.  Memory bounds it: 50001 fp16
+// rows of 1003 copied 50 us (205 MB), copied and turned 100; 32768 bf16 rows of 1024 turned 30 (151 MB,
+// the hidden rows' among them).
 template <typename E>
 __global__ __launch_bounds__(kThreads) void prepare_kernel(const Args a, const Jobs jobs) {
     __shared__ float tile[64][65];
@@ -446,7 +452,11 @@ __device__ __forceinline__ void meet() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
 }
 
-// A tile of BM x BN of the product by WM x WN waves, each with MI x NJ squares of 16.
+// A tile of BM x BN of the product by WM x WN waves, each with MI x NJ squares of 16.  A wave reads MI + NJ
+// fragments for MI NJ matrix instructions, so large tiles keep LDS behind them: at 256 x 256 a step of 32 needs 768 cycles
+// of LDS reads and 1024 of matrix instructions, at 128 x 128 with 4 waves as many as each other.  The rest is
+// waiting for the step's loads and for the slowest wave at the barrier: at k of 4096 1250 TFLOP/s, the instructions
+// and barriers alone 1614 (the clock falls to 1.9 GHz).  Tried and slower: steps of 32 in four or five stages, 256 x 128 tiles with two workgroups a unit (19 %), 4 waves of 128 x 128.
 // Of a step, an operand's tile lies in LDS as rows of ROW bytes, a tile for each of its N parts; the
 // 16-byte pieces of a row are exchanged by the row's number, so that lanes reading a column of
 // pieces meet all banks.  STAGES steps are on their way or in use.
@@ -599,7 +609,10 @@ __device__ __forceinline__ void unscale(const Args& a, F4 (&acc)[S::MI][S::NJ], 
 }
 
 // Maximum and sum of exponentials of a tile's logits, per row, and the targets' logits;
-// `first` is the token of the head's first row.
+// `first` is the token of the head's first row.  4096 x 1024 x 32768 bf16: 260 to 281 us, 980 to 1060 TFLOP/s (torch's
+// product, which writes the logits, 258); a tile's first loads and its 128 exponentials a lane are 7 of its 35 us, in
+// which the matrix instructions stand still.  Few rows are bound by the head's bytes: 16 rows of 2048 and 32768
+// tokens 23 us, 5.8 TB/s.
 template <typename T, typename S>
 __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void logits_kernel(const Args a, const Operand head,
                                                                                const Operand hidden, int steps,
@@ -692,7 +705,8 @@ __device__ __forceinline__ uint2 turned(uint2 x) {
 }
 
 // e of a piece of the vocabulary: e[n][ld], and with the rows' weights over their
-// largest, turned, we[tokens][ld_turned].
+// largest, turned, we[tokens][ld_turned].  Both orders, as matrix operands have their k in a row.  The logits' kernel
+// but for its end, which writes: 345 to 365 us where that one takes 258 to 281, 537 MB in 86 us.
 struct Errors {
     void *e, *we;      // either may be NULL
     int64_t tokens, rows;  // of the piece and of all, in whole steps
@@ -813,7 +827,9 @@ struct Factor {
     __device__ __forceinline__ float operator()(float x) const { return ldexpf(x * m, e); }
 };
 
-// Both gradients of a piece in one launch, the workgroups of dh first: their k is longer.
+// Both gradients of a piece in one launch, the workgroups of dh first: their k is longer.  4096 x 1024 x 32768 bf16:
+// 484 to 507 us, 1090 to 1140 TFLOP/s (torch's products one after the other 551); 1519 x 1003 x 50001 fp16: 340 to 360, 850 to
+// 900, 3.8 rounds of tiles and rows of dW off a line.
 struct Gradients {
     Operand wt, er;         // of dh: W^T, e
     Operand ht, we;         // of dW: h^T, (c e)^T
@@ -957,7 +973,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gradients_kerne
 }
 
 // Sums over the splits of dW of a piece, and of dh after the last piece, times what
-// each is to be multiplied by: dh of a.n rows, or none, then `tokens` rows of dW, or none.
+// each is to be multiplied by: dh of a.n rows, or none, then `tokens` rows of dW, or none.  4 splits of 4096 x 1024
+// in 32 bits: 18 us (76 MB, latency at this size).
 template <typename E, typename T>
 __global__ __launch_bounds__(kThreads) void splits_kernel(const Args a, const Gradients g, int64_t tokens, E* dhidden) {
     const int64_t per_row = (a.D + 3) / 4, rows = dhidden ? a.n : 0;
