@@ -383,7 +383,7 @@ Update update_of(int32_t dtype, bool master) {
     return master ? update_kernel<_Float16, true, BITS8, STREAM> : update_kernel<_Float16, false, BITS8, STREAM>;
 }
 // With 8-bit averages, what no cache holds until the next step passes by it: 123 M values
-// with masters, a step with its norm, 417 us, and 461 through the caches.  With 32-bit averages
+// with masters, a step with its norm, 418 us, and 464 through the caches.  With 32-bit averages
 // that gains nothing (218 M values: 1306 and 1278).
 constexpr int64_t kStreamValues = 16 << 20;
 
