@@ -937,7 +937,8 @@ typedef struct gear_adamw_desc {
  * bound), but for blocks wholly below 2^-100, which are stored as zeros.  Zeros are
  * zeros in both.
  * Where the factor, or the device's lr, is not finite, the call leaves everything as
- * it was, s too.
+ * it was, s too.  An average that is not finite (a gradient above 1.8e19 has an infinite square)
+ * stays so: a value's own in 32 bits, its block's in 8; other blocks do not notice.
  * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.
  */
 int gear_adamw(const gear_adamw_desc *d, const gear_step_tensor *tensors, int64_t count, int64_t *d_step, void *d_work,

@@ -422,3 +422,22 @@ def test_lists_are_let_go():
     del bad  # it holds the last lists itself
     after = [sys.getrefcount(x) for x in (p, g, m, v, None)]
     assert after[:4] == before[:4] and after[4] - before[4] < 50
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", [1e25, float("inf"), float("nan")])
+def test_infinite_averages_stay_where_they_are(bits, bad):
+    """A gradient whose square is infinite, or a NaN: its own value in 32 bits, its block in 8, and no other."""
+    t, clean = (Tensors([2000, 700], [torch.float32] * 2, bits, False) for _ in range(2))
+    t.g[0][1000] = bad
+    for _ in range(3):
+        t.run()
+        clean.run()
+    hit = torch.zeros(2000, dtype=torch.bool)
+    hit[1000] = True
+    if bits == 8:
+        hit[1000 // BLOCK * BLOCK:(1000 // BLOCK + 1) * BLOCK] = True
+    assert torch.equal(t.p[1], clean.p[1]) and torch.equal(t.p[0].cpu()[~hit], clean.p[0].cpu()[~hit])
+    for a, b in zip(t.averages(0) + t.averages(1), clean.averages(0) + clean.averages(1)):
+        keep = ~hit if a.numel() == 2000 else slice(None)
+        assert torch.equal(a[keep], b[keep])
