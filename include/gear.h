@@ -862,7 +862,8 @@ int gear_token_loss(const gear_token_desc *d, const void *d_hidden, const void *
  *   d_lse        as that call wrote it
  *   d_grad_loss  one float that multiplies the gradients, read on the device, or NULL for 1
  *   d_dhidden    [n][D], contiguous, or NULL: not written; 0 for rows that take no part
- *   d_dhead      [V][D], contiguous, or NULL: not written
+ *   d_dhead      [V][D], contiguous, or NULL: not written.  NaN throughout where a row
+ *                that takes part has a NaN weight
  *
  * The logits are formed again, a piece of the vocabulary at a time, and e is
  * rounded once to the products' type (two fp16 parts for 32-bit values), fp16 times 2^14.

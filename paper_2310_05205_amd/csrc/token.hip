@@ -86,7 +86,7 @@ struct Row {
 // Of all rows; made by one workgroup.
 struct Totals {
     float share;     // 1 / denom
-    float weight;    // largest |weight| of a row that takes part
+    float weight;    // largest |weight| of a row that takes part, NaN where one is
 };
 // Powers of two that 32-bit hidden values and the head are multiplied by before they are cut and turned.
 struct Scales {
@@ -120,8 +120,8 @@ __device__ __forceinline__ T lanes_add(T v, int lanes) {
     for (int off = lanes / 2; off > 0; off >>= 1) v += __shfl_xor(v, off);
     return v;
 }
-// The larger magnitude; a NaN or an infinity stays, as it makes every gradient of the head one.
-__device__ __forceinline__ float larger(float top, float w) { return fabsf(w) <= top ? top : fabsf(w); }
+// The larger magnitude, or NaN where either is one: of weights, it makes every gradient of the head NaN.
+__device__ __forceinline__ float larger(float top, float w) { return top != top || fabsf(w) <= top ? top : fabsf(w); }
 
 __device__ __forceinline__ Row row_of(const Args& a, int64_t r) {
     const int64_t y = a.target_dtype == GEAR_DTYPE_I32   ? (int64_t)static_cast<const int32_t*>(a.target)[r]

@@ -238,6 +238,31 @@ def test_nan_and_infinity_show(dtype):
     assert not torch.isfinite(logp[3]) and torch.isfinite(logp[:3]).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [20, 320, 2000, 20000])
+def test_nan_weights_show(dtype, n):
+    """One NaN weight on a row that takes part, among zeros and among others, and NaN weights alone: the formula's NaN in
+    the loss, in the row's dhidden and in all of dhead.  On a row that takes no part it reaches nothing."""
+    h, W, t, w = (x.to(cuda()) for x in inputs(n, 24, 30, dtype))
+    nan = float("nan")
+    for at in (0, n // 2, n - 1):
+        for rest in (0.0, -2.0, nan):
+            weight = torch.full((n,), rest, device=cuda())
+            weight[at] = nan
+            say("token_loss NaN weight at %d of %d beside %s, %s" % (at, n, rest, dtype))
+            loss, logp, lse = gear.token_loss(h, W, t, weight=weight)
+            dh, dW = gear.token_loss_backward(h, W, t, lse, weight=weight)
+            assert torch.isnan(loss) and torch.isfinite(logp).all()
+            assert torch.equal(torch.isnan(dh).all(1), torch.isnan(weight)) and torch.equal(torch.isnan(dh).any(1), torch.isnan(weight))
+            assert torch.isnan(dW).all()
+    on = torch.ones(n, dtype=torch.bool, device=cuda())
+    on[n // 2] = False
+    w[n // 2] = nan
+    loss, logp, lse = gear.token_loss(h, W, t, weight=w, mask=on)
+    dh, dW = gear.token_loss_backward(h, W, t, lse, weight=w, mask=on)
+    assert torch.isfinite(loss) and torch.isfinite(dh).all() and torch.isfinite(dW).all() and not dh[n // 2].any()
+
+
 def test_gradient_scales_and_repeats():
     h, W, t, w = (x.to(cuda()) for x in inputs(300, 100, 500, torch.bfloat16))
     say("token_loss repeats")
