@@ -936,7 +936,12 @@ typedef struct gear_adamw_desc {
  * magnitude over 448; they are rounded to nearest when stored, and what is not 0 is
  * stored as no less than the least e4m3 value (an update divided by 0 would have no
  * bound), but for blocks wholly below 2^-100, which are stored as zeros.  Zeros are
- * zeros in both.
+ * zeros in both.  The exception is m of a value whose gradient is 0 in this step: it is
+ * rounded towards 0 (within 2^-20) and not kept from 0, so that it falls by beta1 or more in every
+ * such step until it is 0, and the parameter comes to rest as with 32 bits.  Where the
+ * gradient is not 0, rounding to nearest leaves m as it is while (1 - beta1) |g - m| is
+ * below half a step of e4m3: 2^-4 of m at most, or 2^-10 of the block's scale.  So does sqrt(v), with
+ * v's own change.
  * Where the factor, or the device's lr, is not finite, the call leaves everything as
  * it was, s too.  An average that is not finite (a gradient above 1.8e19 has an infinite square)
  * stays so: a value's own in 32 bits, its block's in 8; other blocks do not notice.

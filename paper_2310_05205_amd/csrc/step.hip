@@ -3,7 +3,10 @@
 // the averages are held in 32 bits, or in e4m3 with a scale per 256 values:
 //   m = q s,  v = (q' s')^2,  s = max |.| / 448 over the block.
 // The second average is held by its root: e4m3 reaches over 17 powers of two below a
-// block's largest, and the root needs half of what v itself would.
+// block's largest, and the root needs half of what v itself would.  The first one of a
+// value without a gradient is rounded towards 0: to nearest, beta1 m is m again where
+// 1 - beta1 of it is less than half a step of e4m3 (multiples of 2^-9 up to 4 of them at
+// 0.9, values of any size at 0.95), and the parameter would go on moving.
 //
 // Tensors travel in the kernel's arguments, 56 a launch, so a call needs no table
 // on the device and a captured call keeps its own.
@@ -118,9 +121,16 @@ __device__ __forceinline__ void load8(const uint8_t* p, int64_t left, float scal
         f[j + 3] = hi[1] * scale;
     }
 }
-// A lane's values of a block, under the block's scale, which is returned.
+// The e4m3 value next to x, |x| <= kTop, towards 0.  2^-20 more than x: what was such a value before roundings stays one.
+__device__ __forceinline__ float towards_0(float x) {
+    const float a = fminf(fabsf(x) * (1.0f + 9.5367432e-07f), kTop);
+    const float normal = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, a) & 0xFFF00000u);  // 3 bits after the first
+    return copysignf(a < 8.0f * kLeast ? truncf(a * (1.0f / kLeast)) * kLeast : normal, x);
+}
+// A lane's values of a block, under the block's scale, which is returned: to nearest, what is not 0 to no less than kLeast;
+// those of the bits `fading` towards 0.
 template <bool STREAM>
-__device__ __forceinline__ float store8(uint8_t* p, int64_t left, const float (&f)[kValues]) {
+__device__ __forceinline__ float store8(uint8_t* p, int64_t left, const float (&f)[kValues], uint32_t fading) {
     float top = 0.0f;
 #pragma unroll
     for (int j = 0; j < kValues; j++) top = fmaxf(top, fabsf(f[j]));
@@ -139,6 +149,7 @@ __device__ __forceinline__ float store8(uint8_t* p, int64_t left, const float (&
             // Comparisons that a NaN passes through.
             if (fabsf(x) > kTop) q[k] = copysignf(kTop, x);
             if (fabsf(x) < kLeast) q[k] = f[j + k] != 0.0f && some ? copysignf(kLeast, x) : 0.0f;
+            if ((fading >> (j + k) & 1) != 0 && x == x) q[k] = towards_0(x);
         }
         int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
         w = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true);
@@ -208,9 +219,11 @@ __global__ __launch_bounds__(kThreads) void update_kernel(const Items t, const B
                 load<kValues, STREAM>(static_cast<const float*>(it.v) + i, left, v);
             }
             float r[kValues];
+            uint32_t fading = 0;  // values without a gradient
 #pragma unroll
             for (int j = 0; j < kValues; j++) {
                 const float x = g[j] * f.grad;
+                fading |= x == 0.0f ? 1u << j : 0u;
                 m[j] = b.b1 * m[j] + b.c1 * x;
                 v[j] = b.b2 * v[j] + b.c2 * (x * x);
                 r[j] = root_of(v[j]);
@@ -220,8 +233,8 @@ __global__ __launch_bounds__(kThreads) void update_kernel(const Items t, const B
             if (MASTER) store<kValues, STREAM>(it.master + i, left, p);
             store<kValues, STREAM>(static_cast<E*>(it.param) + i, left, p);
             if (BITS8) {
-                const float sm = store8<STREAM>(static_cast<uint8_t*>(it.m) + i, left, m);
-                const float sv = store8<STREAM>(static_cast<uint8_t*>(it.v) + i, left, r);
+                const float sm = store8<STREAM>(static_cast<uint8_t*>(it.m) + i, left, m, fading);
+                const float sv = store8<STREAM>(static_cast<uint8_t*>(it.v) + i, left, r, 0);
                 if (left > 0 && (threadIdx.x & (kGroup - 1)) == 0) {
                     it.ms[i / GEAR_STEP_BLOCK] = sm;
                     it.vs[i / GEAR_STEP_BLOCK] = sv;

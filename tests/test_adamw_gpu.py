@@ -441,3 +441,45 @@ def test_infinite_averages_stay_where_they_are(bits, bad):
     for a, b in zip(t.averages(0) + t.averages(1), clean.averages(0) + clean.averages(1)):
         keep = ~hit if a.numel() == 2000 else slice(None)
         assert torch.equal(a[keep], b[keep])
+
+
+@pytest.mark.parametrize("n,beta1,steps", [(512, 0.9, 300), (512, 0.95, 600), (512, 0.99, 3000), (512, 0.0, 3), (16 << 20, 0.9, 300)])
+def test_8_bit_averages_end_with_their_gradients(n, beta1, steps):
+    """Values whose gradient stops, among others that go on: the first average falls by beta1 or more in every step, is 0 in
+    the end, and the parameter stays where it is, as with 32 bits.  A block that stops whole keeps its values' ratios.
+    16 M values go by the caches."""
+    say("adamw 8 bits, gradients that stop, beta1 %s, %d values" % (beta1, n))
+    p = torch.zeros(n, device=cuda())
+    m, v = (torch.zeros(n, dtype=torch.uint8, device=cuda()).view(torch.float8_e4m3fn) for _ in range(2))
+    scales = ([torch.zeros(n // BLOCK, device=cuda())], [torch.zeros(n // BLOCK, device=cuda())])
+    step = torch.zeros(1, dtype=torch.int64, device=cuda())
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    stop = torch.zeros(n, dtype=torch.bool, device=cuda())
+    stop[3:23] = True
+    stop[BLOCK:2 * BLOCK] = True
+    kw = dict(KW, betas=(beta1, 0.999), weight_decay=0.0, lr=1e-3)
+
+    def average():
+        return m[:512].float() * scales[0][0][:2].repeat_interleave(BLOCK)
+    for t in range(steps):
+        g = torch.randn(n, generator=gen, device=cuda())
+        if t == 0:
+            # From the largest of the block down to 1e-4 of it.
+            g[3:23] = 10.0 ** torch.linspace(0, -4, 20, device=cuda()) * torch.tensor([1.0, -1.0], device=cuda()).repeat(10)
+        else:
+            g[stop] = 0.0
+        before = average()
+        gear.adamw([p], [g], [m], [v], step, scales=scales, **kw)
+        if 0 < t < 120:
+            # Rounded towards 0 within 2^-20, and the 32-bit roundings of the average, its scale and their product.
+            now, old = average()[stop[:512]], beta1 * before[stop[:512]]
+            assert (now.abs() <= old.abs() * (1 + 2.0 ** -20 + 8 * U32)).all() and (now * old >= 0).all()
+            whole, old = average()[BLOCK:], beta1 * before[BLOCK:]
+            if t < 40:
+                assert ((whole - old).abs() <= 8 * U32 * old.abs()).all()
+    # 0.9^300, 0.95^600 and 0.99^3000 are below 2^-43; a block's least average above 0 is 2^-18 of its largest.
+    assert not m[3:23].float().any()
+    assert m[23:BLOCK].float().any() and torch.isfinite(p).all()
+    was = p.clone()
+    gear.adamw([p], [torch.where(stop, 0.0, 1.0)], [m], [v], step, scales=scales, **kw)
+    assert torch.equal(p[3:23], was[3:23]) and not torch.equal(p[23:BLOCK], was[23:BLOCK])
