@@ -127,6 +127,14 @@ def token_loss(hidden, head, target, *, weight=None, mask=None, denom=None):
     return _TokenLoss.apply(hidden, head, target, weight, mask, denom)
 
 
+def _versions(params):
+    """What a write to a parameter counts up; tensors of inference mode have none."""
+    try:
+        return [p._version for p in params]
+    except RuntimeError:
+        return [None if p.is_inference() else p._version for p in params]
+
+
 class AdamW:
     """AdamW over a model's parameters, each step one call for all of them.
 
@@ -137,6 +145,13 @@ class AdamW:
     without a gradient stay as they are; the count of steps is one for all.  A step
     whose gradients are not finite is left out, on the device, where norm or scale
     are asked for.
+
+    A parameter that the program writes between steps (a model's state that is
+    loaded, a reset) is what the next step starts from: values that differ from their
+    rounded masters take the masters' place.  step() and state_dict() look for that by
+    the parameter's version and address.  A write through ``.data`` changes neither, and the
+    replay of a captured step looks for nothing: call refresh() after the one and
+    before the other.
     """
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, *, bits=32, master=True,
@@ -164,6 +179,26 @@ class AdamW:
             if bits == 8:
                 self._scale.append(list(torch.zeros(sum(blocks), device=device).split(blocks)))
         self._master = [p.detach().float() if master and p.dtype != torch.float32 else None for p in self.params]
+        # Parameters with masters, where they lie and their versions, as the masters were last in line with them.
+        self._held = [i for i, m in enumerate(self._master) if m is not None]
+        self._places, self._versions = [p.data_ptr() for p in self.params], _versions(self.params)
+
+    def refresh(self):
+        """Takes what was written to parameters since the last step into their masters."""
+        self._refresh(self._held)
+
+    def _refresh(self, at):
+        with torch.no_grad():
+            for i in at:
+                p, m = self.params[i], self._master[i]
+                m.copy_(torch.where(m.to(p.dtype) == p, m, p.float()))
+                self._places[i], self._versions[i] = p.data_ptr(), _versions([p])[0]
+
+    def _refresh_changed(self):
+        held = [self.params[i] for i in self._held]
+        places, versions = [p.data_ptr() for p in held], _versions(held)
+        self._refresh([i for i, place, version in zip(self._held, places, versions)
+                       if version != self._versions[i] or place != self._places[i]])
 
     def step(self, scale=1.0):
         """Steps every parameter that has a gradient, the gradients times `scale` (1
@@ -172,6 +207,7 @@ class AdamW:
         at = [i for i, p in enumerate(self.params) if p.grad is not None]
         if not at:
             return None
+        self._refresh_changed()
         params = [self.params[i].detach() for i in at]
         grads = [self.params[i].grad.contiguous() for i in at]
         norm = factor = None
@@ -182,6 +218,8 @@ class AdamW:
                    eps=self.eps, weight_decay=self.weight_decay,
                    scales=(pick(self._scale[0]), pick(self._scale[1])) if self.bits == 8 else None,
                    master=pick(self._master), factor=factor)
+        if self._held:
+            self._versions = _versions(self.params)  # which the step counted up
         return norm
 
     def zero_grad(self):
@@ -196,11 +234,14 @@ class AdamW:
 
     def state_dict(self):
         """Copies of the count of steps, averages, scales and masters; not lr and its like."""
+        self._refresh_changed()
         state = {k: [None if t is None else t.clone() for t in v] for k, v in self._state().items()}
         return dict(state, count=self.count.clone())
 
     def load_state_dict(self, state):
-        """Takes what state_dict() of an optimizer over like parameters gave."""
+        """Takes what state_dict() of an optimizer over like parameters gave.  The parameters
+        stay as they are, and count where they differ from their rounded masters: load
+        the model's state too, before or after."""
         mine = dict(self._state(), count=[self.count])
         state = dict(state, count=[state["count"]])
         if set(mine) != set(state):
@@ -216,3 +257,4 @@ class AdamW:
                 for a, b in zip(v, state[k]):
                     if a is not None:
                         a.copy_(b)
+        self._places = [None] * len(self.params)  # masters may differ from the parameters' last ones

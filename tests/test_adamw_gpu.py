@@ -483,3 +483,98 @@ def test_8_bit_averages_end_with_their_gradients(n, beta1, steps):
     was = p.clone()
     gear.adamw([p], [torch.where(stop, 0.0, 1.0)], [m], [v], step, scales=scales, **kw)
     assert torch.equal(p[3:23], was[3:23]) and not torch.equal(p[23:BLOCK], was[23:BLOCK])
+
+
+def masters(opt):
+    return opt.state_dict()["master"]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_parameters_written_between_steps(bits, dtype):
+    """What a program writes to a parameter is what the next step starts from; values it leaves keep their masters."""
+    def grads(ps, seed):
+        for k, p in enumerate(ps):
+            p.grad = random(p.numel(), seed + k).view(p.shape).to(p.dtype).to(cuda())
+
+    def whole(p):
+        with torch.no_grad():
+            p.copy_(random(p.numel(), 77).view(p.shape))
+
+    def rows(p):
+        with torch.no_grad():
+            p[3:5] = 0.5
+
+    def swap(p):
+        p.data = random(p.numel(), 78).view(p.shape).to(p.dtype).to(cuda())
+
+    def load(p):
+        box = torch.nn.ParameterList([p])
+        box.load_state_dict({"0": random(p.numel(), 79).view(p.shape).to(p.dtype)})
+
+    def clamp(p):
+        with torch.no_grad():
+            p.clamp_(-0.5, 0.5)
+    for write in (whole, rows, swap, load, clamp):
+        say("learn.AdamW, %s between steps, %d bits %s" % (write.__name__, bits, dtype))
+        ps = [torch.nn.Parameter(random(600, 5).view(20, 30).to(dtype).to(cuda())), torch.nn.Parameter(random(70, 6).to(cuda()))]
+        opt = learn.AdamW(ps, lr=1e-3, bits=bits)
+        for k in range(3):
+            grads(ps, 10 * k)
+            opt.step()
+        was, before, kept = masters(opt)[0], ps[0].detach().clone(), masters(opt)[0].to(dtype)
+        assert torch.equal(kept, before) and not torch.equal(was, before.float())
+        write(ps[0])
+        now = ps[0].detach().clone()
+        assert not torch.equal(now, before)
+        want = torch.where(now == kept, was, now.float())
+        # A copy of the state holds them too, and so does an optimizer that takes it, in either order of loading.
+        state = opt.state_dict()
+        assert torch.equal(state["master"][0], want)
+        twins = []
+        for first in (True, False):
+            q = [torch.nn.Parameter(torch.zeros_like(p)) for p in ps]
+            two = learn.AdamW(q, lr=1e-3, bits=bits)
+            if first:
+                two.load_state_dict(state)
+            with torch.no_grad():
+                for a, b in zip(q, ps):
+                    a.copy_(b)
+            if not first:
+                two.load_state_dict(state)
+            twins.append((q, two))
+        # The same step by hand.
+        p, m, v = want.to(dtype), state["exp_avg"][0].clone(), state["exp_avg_sq"][0].clone()
+        scales = ([state["exp_avg_scale"][0].clone()], [state["exp_avg_sq_scale"][0].clone()]) if bits == 8 else None
+        grads(ps, 50)
+        gear.adamw([p], [ps[0].grad], [m], [v], state["count"].clone(), lr=1e-3, scales=scales, master=[want])
+        opt.step()
+        assert torch.equal(ps[0].detach(), p) and torch.equal(masters(opt)[0], want)
+        for q, two in twins:
+            grads(q, 50)
+            two.step()
+            assert torch.equal(q[0], ps[0]) and torch.equal(q[1], ps[1]) and torch.equal(masters(two)[0], want)
+
+
+def test_parameters_written_past_their_version():
+    """refresh() takes what was written through .data, which no version tells; replays of a captured step need it too."""
+    p = torch.nn.Parameter(random(600, 5).to(torch.bfloat16).to(cuda()))
+    opt = learn.AdamW([p], lr=1e-3)
+    p.grad = random(600, 6).to(torch.bfloat16).to(cuda())
+    say("learn.AdamW.refresh")
+    opt.step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step()
+    for k in range(3):
+        p.data.copy_(random(600, 20 + k))
+        opt.refresh()
+        assert torch.equal(masters(opt)[0], p.detach().float())
+        state = opt.state_dict()
+        q, m, v, w = p.detach().clone(), state["exp_avg"][0], state["exp_avg_sq"][0], state["master"][0]
+        gear.adamw([q], [p.grad], [m], [v], state["count"], lr=1e-3, master=[w])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(p.detach(), q) and torch.equal(masters(opt)[0], w)
