@@ -156,6 +156,8 @@ class AdamW:
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, *, bits=32, master=True,
                  max_norm=None):
+        if isinstance(params, torch.Tensor):
+            raise TypeError("params must be a list of tensors, not one, whose rows have no gradients")
         self.params = list(params)
         if not self.params:
             raise ValueError("no parameters")

@@ -4,7 +4,7 @@ import ctypes
 import pytest
 import torch
 
-from paper_2310_05205_amd import gear
+from paper_2310_05205_amd import gear, learn
 
 FAKE = 4096  # never dereferenced: every call here is refused or has nothing to do
 
@@ -142,3 +142,9 @@ def test_tensors_have_to_be_on_the_gpu():
                  lambda: gear.adamw([x], [x], [x], [x], torch.zeros(1, dtype=torch.int64), lr=0.1)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_optimizers_take_lists():
+    """A tensor alone would be taken for its rows, which never have a gradient."""
+    with pytest.raises(TypeError):
+        learn.AdamW(torch.nn.Parameter(torch.ones(3, 4)))
