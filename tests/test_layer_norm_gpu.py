@@ -4,7 +4,7 @@ import torch
 
 from paper_2310_05205_amd import gear, learn
 from tests.helpers import cuda, say
-from tests.network_reference import Norm, near
+from tests.network_reference import U, Norm, near
 
 pytestmark = pytest.mark.gpu
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
@@ -62,6 +62,45 @@ def test_many_rows(dtype):
         x, dy = rows(n, D, dtype, 1).to(cuda()), rows(n, D, dtype, 2).to(cuda())
         w, b = (1 + 0.2 * rows(2, D, torch.float32, 5)).to(cuda())
         check(x, w, b, 1e-5, dy, dy, x, "%d x %d %s" % (n, D, dtype))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,D", [(600, 5001), (1100, 12289), (1100, 20000), (600, 30001), (4099, 33001)])
+def test_many_long_rows(n, D, dtype):
+    """Rows of a workgroup or more, several for each workgroup, and several slices of rows, against the definition
+    a part of the rows at a time."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, r, dy, dt = ((torch.randn(n, D, generator=g, device=cuda()) + 0.5 * torch.randn(n, 1, generator=g, device=cuda())).to(dtype)
+                    for _ in range(4))
+    w, b = (1 + 0.2 * rows(2, D, torch.float32, 5)).to(cuda())
+    say("layer_norm %d x %d %s" % (n, D, dtype))
+    y, total, saved = gear.layer_norm(x, w, b, residual=r, save=True)
+    plain = gear.layer_norm(total, w, b)[0]
+    dx, dw, db = gear.layer_norm_backward(dy, total, saved, w, dtotal=dt)
+    dx_alone, none, _ = gear.layer_norm_backward(dy, total, saved, dtotal=dt)
+    want_w, want_b, size_w, size_b, off_w = torch.zeros(5, D, dtype=torch.float64)
+    for a in range(0, n, 256):
+        part = slice(a, min(n, a + 256))
+        want = Norm(x[part].cpu(), w.cpu(), b.cpu(), 1e-5, r[part].cpu())
+        near(y[part], want.y, want.y_bound, "y of rows from %d" % a)
+        near(plain[part], want.y, want.y_bound, "y without a residual of rows from %d" % a)
+        assert torch.equal(total[part].cpu().double(), want.t)
+        want.backward(dy[part].cpu(), dt[part].cpu(), torch.float32)
+        near(dx[part], want.dx, want.dx_bound, "dx of rows from %d" % a)
+        d = dy[part].cpu().double()
+        want_w += want.dw
+        want_b += want.db
+        size_w += (d * want.u).abs().sum(0)
+        size_b += d.abs().sum(0)
+        off_w += (d.abs() * want.u_off).sum(0)
+        one = Norm(x[part].cpu(), None, None, 1e-5, r[part].cpu())
+        one.backward(dy[part].cpu(), dt[part].cpu(), torch.float32)
+        near(dx_alone[part], one.dx, one.dx_bound, "dx without parameters of rows from %d" % a)
+    # Sums over rows: at least 32 workgroups or slices, whose rows are added in turn, and their sums, of at most 1024, in
+    # turns of 16; products round once more.
+    units = 32 + n / 32 + 64
+    near(dw, want_w, U[torch.float32] * (want_w.abs() + units * size_w) + off_w, "dweight")
+    near(db, want_b, U[torch.float32] * (want_b.abs() + units * size_b), "dbias")
 
 
 @pytest.mark.parametrize("dtype,n,D", [(torch.bfloat16, 140000, 512), (torch.float16, 70001, 1024), (torch.float32, 9001, 4096),
