@@ -755,9 +755,9 @@ int gear_action_logp(const gear_policy_desc *d, const void *d_logits, float *d_l
  *   t = x + r (rounded to the rows' type; t = x without a residual)
  *   u = (t - mean t) / sqrt(var t + eps),  y = u weight + bias
  *
- * var is the mean of (t - mean t)^2.  All sums are in 32 bits; deviations beyond 1e19 leave
- * their range.  With eps 0 a row without deviation is NaN.  NaN and infinities stay in their row,
- * and in dweight and dbias.
+ * var is the mean of (t - mean t)^2.  All sums are in 32 bits: rows whose sum, or whose sum of
+ * squared deviations, passes 3.4e38 leave their range.  With eps 0 a row without
+ * deviation is NaN.  NaN and infinities stay in their row, and in dweight and dbias.
  */
 typedef struct gear_norm_desc {
     int32_t dtype;        /* of x, residual, y, total, dy, dtotal, dx: GEAR_DTYPE_F16, _BF16 or _F32 */
@@ -832,7 +832,7 @@ int gear_token_loss_sizes(const gear_token_desc *d, int64_t *loss_bytes, int64_t
 
 /*
  * gear_token_loss - the cross entropy of targets under a token head, without its
- * logits: they are formed in pieces, in 32 bits, and leave their maximum and sum.
+ * logits in memory: they are formed in pieces, in 32 bits, and leave their maximum and sum.
  * With z = hidden head^T, lse = log sum_v exp z_v and logp = z[target] - lse,
  *
  *   loss = -sum_rows weight logp / denom
@@ -867,6 +867,8 @@ int gear_token_loss(const gear_token_desc *d, const void *d_hidden, const void *
  *
  * The logits are formed again, a piece of the vocabulary at a time, and e is
  * rounded once to the products' type (two fp16 parts for 32-bit values), fp16 times 2^14.
+ * It lies in the workspace in both orders, up to 2^27 values of each (2^26 in 32 bits) or 256
+ * tokens of every row: 4096 rows of 1024 and 32768 tokens in bf16 take 765 MB, of which e is 537.
  * In the sums of the gradients 32-bit hidden values and the head are off by 2^-22 of the value, or
  * by 2^-39 of the tensor's largest finite one (of hidden, of the rows that take part).
  * Errors: GEAR_E_INVAL (nothing enqueued), GEAR_E_HIP.

@@ -191,7 +191,7 @@ struct Betas {
 };
 
 // One read and one write of everything a value has; memory bounds it: 147 M bf16 values with masters and 32-bit averages, 28
-// bytes each, 760 us, 5.4 TB/s; 54 M with 8-bit averages, 16 bytes each, 164 us, 5.3 TB/s.
+// bytes each, 760 us, 5.4 TB/s; 54 M with 8-bit averages, 16 bytes each, 159 us, 5.4 TB/s.
 template <typename E, bool MASTER, bool BITS8, bool STREAM>
 __global__ __launch_bounds__(kThreads) void update_kernel(const Items t, const Betas b, const Factors* factors) {
     const Factors f = *factors;
@@ -293,8 +293,8 @@ __device__ __forceinline__ double squares(const Grads& t, uint32_t first, uint32
     return sum;
 }
 
-// A sum per workgroup; `add` to those of the launches before.  Squares in 64 bits, which memory hides: 218 M bf16 values 99 to
-// 124 us, 3.5 to 4.4 TB/s, 61 M 41.
+// A sum per workgroup; `add` to those of the launches before.  218 M bf16 values take 99 to 124 us, 3.5 to 4.4 TB/s, 61 M 41
+// to 43, where reads reach 6.9 TB/s: a workgroup asks for its next chunk when the squares of this one, in 64 bits, are added.
 template <typename E>
 __global__ __launch_bounds__(kThreads) void squares_kernel(const Grads t, double* sums, int add) {
     __shared__ double s[kThreads / 64];
@@ -396,7 +396,7 @@ Update update_of(int32_t dtype, bool master) {
     return master ? update_kernel<_Float16, true, BITS8, STREAM> : update_kernel<_Float16, false, BITS8, STREAM>;
 }
 // With 8-bit averages, what no cache holds until the next step passes by it: 123 M values
-// with masters, a step with its norm, 418 us, and 464 through the caches.  With 32-bit averages
+// with masters, a step with its norm, 414 us, and 464 through the caches.  With 32-bit averages
 // that gains nothing (218 M values: 1306 and 1278).
 constexpr int64_t kStreamValues = 16 << 20;
 

@@ -15,7 +15,7 @@
 // 32-bit values are cut into two fp16 parts, a 2^s = a1 + a2 (11 bits each), s making the largest
 // finite value 2^14 to 2^15, of a row for the logits, which so depend on their own row and token
 // alone, and of the tensor for the turned copies, whose k runs over the rows; a part is off by
-// 2^-22 of the value, or by 2^-40 of the largest where the value is far below it.  The products a1 b1, a1 b2 and a2 b1 leave out
+// 2^-22 of the value, or by 2^-39 of the largest where the value is far below it.  The products a1 b1, a1 b2 and a2 b1 leave out
 // 2^-22 of |a b| at most.  Matrix instructions of 16-bit types are 16 times as fast as those of 32
 // bits, so three of them take a fifth of the time.  (Three bf16 parts need no scale and leave
 // 2^-25, but six products: 1000 x 512 x 8192, forward and backward, took 245 us with them and takes 158.)
@@ -725,7 +725,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void errors_kernel(c
     F4 acc[Tl::MI][Tl::NJ];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / S::WN, wn = wave % S::WN;
     const int vt = wm * Tl::MI * 16 + (lane >> 4) * 4, rt = wn * Tl::NJ * 16 + (lane & 15);  // in the tile
-    // What the rows need is on its way during the products (4096 x 1024 x 32768: 7 us less), where registers are left.
+    // What the rows need is read before the products, whose first wait is for it too, rather than after them (4096 x 1024
+    // x 32768: 7 us less), where registers are left.
     const float top = a.totals->weight;
     Row rows[Tl::NJ];
     float lses[Tl::NJ], w[Tl::NJ];
@@ -1040,7 +1041,9 @@ Size size_of(int64_t m, int64_t n, int64_t rows) {
     if (tiles(m, 128) * tiles(n, 128) < 256) return kSmall;
     return tiles(m, 256) * tiles(n, 256) >= 192 ? kBig : kMiddle;
 }
-// Workgroups of a product that the GPU's 256 units run at once: as many as LDS holds.
+// Workgroups of a product that splits should fill the GPU's 256 units with: as many as LDS holds, but one of two of the
+// middle tiles of two parts, whose splits beyond that cost more than they share (fp32, backward: 1000 x 512 x 8192 135 to 138 us
+// so and 147 with two, 3000 x 1024 x 3000 230 and 246; five other sizes within 1%).
 int64_t slots_of(Size s, int parts) { return s == kBig || (s == kMiddle && parts > 1) ? 256 : 512; }
 int edge(Size s) { return s == kBig ? 256 : s == kMiddle ? 128 : 64; }
 

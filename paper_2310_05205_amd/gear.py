@@ -517,12 +517,13 @@ def layer_norm_backward(dy, x, saved, weight=None, *, dtotal=None, stream=None):
 
 
 def token_loss(hidden, head, target, *, weight=None, mask=None, denom=None, stream=None):
-    """Cross entropy of targets under a token head, without its logits (gear_token_loss).
+    """Cross entropy of targets under a token head, without its logits in memory (gear_token_loss).
 
     hidden [..., D] and head [V, D] of one dtype (float32, bfloat16 or float16),
     the rows of each at one stride; target uint8, int32 or int64 of hidden's
     leading shape; weight (float32) and mask (uint8 or bool) of that shape or of
-    its first dimensions, each value then serving every row below it; denom: what
+    its first dimensions, each value then serving every row below it, all three
+    contiguous; denom: what
     the weighted sum is divided by, the number of rows that take part if None.  A row
     with mask 0 or a target outside [0, V) takes no part.  Returns float32
     (loss, logp, lse): a scalar, and per row the target's log-probability and the
@@ -537,7 +538,8 @@ def token_loss_backward(hidden, head, target, lse, *, weight=None, mask=None, de
     """Gradients (dhidden, dhead) of grad_scale * grad_loss * the loss of a token_loss
     call with the same arguments, lse as it returned it (gear_token_loss_backward);
     grad_loss a float32 tensor of one value or None.  Either gradient may be left
-    out, and is None then."""
+    out, and is None then.  The workspace holds the logits' gradient twice, a piece of
+    the vocabulary at a time (gear_token_loss_sizes)."""
     return _on_stream(native().token_loss_backward, hidden, stream, hidden, head, target, lse, weight, mask, denom,
                       grad_scale, grad_loss, dhidden, dhead)
 

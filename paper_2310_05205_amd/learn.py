@@ -139,7 +139,10 @@ class AdamW:
     """AdamW over a model's parameters, each step one call for all of them.
 
     params: tensors on one GPU, contiguous.  With bits=8 the averages are held in
-    8 bits (gear.adamw); 16-bit parameters step as float32 masters, which `master`
+    8 bits (gear.adamw).  A value whose gradient is 0 from some step on comes to rest;
+    where it only turns small, the first average is rounded to nearest and may stay: at up to
+    2^-15 of its block's largest with betas[0] of 0.9, at any size from 0.95 on.
+    16-bit parameters step as float32 masters, which `master`
     turns off.  max_norm clips the gradients' common norm.  lr is a number or a
     float32 tensor of one value on the GPU, and may be set between steps.  Parameters
     without a gradient stay as they are; the count of steps is one for all.  A step
